@@ -517,8 +517,7 @@ def run(state):
                                                  st["table"], weights_in=st["before"],
                                                  cu_seqlens_host=st["cu_host"], **lens)}
         kept, cu, left = fp2.cache_evict(st["p"], st["cache"], st["weights"], st["cu_k"], st["table"],
-                                         st["target"], budget=case["budget"], recent_tokens=case["recent"],
-                                         workspace=st["workspace"], **lens)
+                                         st["target"], budget=case["budget"], recent_tokens=case["recent"], **lens)
         return {"kept": kept, "cu_k": cu, "weights": left, **_pools(st)}
     if case["op"] == "append":
         _append_one(st, "k")
