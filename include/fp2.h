@@ -19,6 +19,15 @@
  *                  fp2_csr_capacity sizes it.
  *   fp2_calibrate = MFMA and exp rate loops (measurement helper).
  *
+ * Beside the sparse prefill, the operators of the paged cache that a server
+ * needs around it (see "Paged cache" below):
+ *   fp2_cache_append  = new tokens' keys and values into the cache's pages;
+ *   fp2_cache_attend  = attention of the newest tokens over the cache, single
+ *                  tokens to whole prompts, causal, with an optional window
+ *                  and first tokens that stay visible;
+ *   fp2_cache_weights = the attention weight that each cached token received;
+ *   fp2_cache_evict   = the heaviest tokens of each head moved to other pages.
+ *
  * Conventions shared by every entry point
  * ---------------------------------------
  * - All tensor pointers are DEVICE pointers (hipMalloc'd or torch CUDA
@@ -403,6 +412,146 @@ fp2_status_t fp2_prefill_noalloc(const fp2_params_t* params, const void* q,
                                  const int32_t* block_table, const float* q_scale,
                                  const float* k_scale, const float* v_scale, void* out,
                                  float* lse, uint8_t* block_mask, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Paged cache: append, attention, weights, eviction
+ * ---------------------------------------------------------------------------
+ * The cache is a pool of token slots [num_slots, num_kv_heads, 128] of keys
+ * and one of values; key j of sequence b is slot
+ * block_table[b][j / page_size] * page_size + j % page_size, as above. Three
+ * forms:
+ *   FP2_BF16                        bf16 rows;
+ *   FP2_FP8_E4M3, scale_tokens 0    e4m3 codes with one fp32 scale per head
+ *                                   (what fp2_prefill reads);
+ *   FP2_FP8_E4M3, scale_tokens n    e4m3 codes with one scale for each block
+ *                                   of n tokens and head: slot s of head h
+ *                                   stands for code * 2^(byte - 127), byte =
+ *                                   block_scale[s / n][h], 1 <= byte <= 245
+ *                                   (fp2_cache_append writes 27 to 245). n is
+ *                                   16, 32, 64 or 128 and divides page_size.
+ * Queries and new keys and values are bf16, outputs bf16, sums fp32.
+ *
+ * cu_seqlens counts the new tokens of the call, cu_seqlens_k the tokens in the
+ * cache, the new ones included: the new tokens of sequence b are its last
+ * ones, and their keys and values are in the cache before fp2_cache_attend
+ * reads it. A sequence without new tokens takes no part in append and
+ * attention. Lengths, tables and scales are read on the device, so a captured
+ * call may be replayed with others inside the bounds of params. The caller
+ * keeps cu_seqlens_k[b + 1] - cu_seqlens_k[b] >= the new tokens, table entries
+ * inside the pool, and page_size whole slots behind each.
+ *
+ * A query at position t sees key j <= t where window_tokens is 0; else where
+ * also t - j < window_tokens or j < sink_tokens. What lies in slots that no
+ * query sees never reaches an output. The conventions at the top of this file
+ * hold (streams, capture, errors).
+ */
+typedef struct {
+  int32_t batch;              /* number of sequences, 0 .. 65536 */
+  int32_t num_q_heads;        /* H_q, a multiple of num_kv_heads */
+  int32_t num_kv_heads;       /* 1 .. 1024; g = H_q / H_kv is 1, 2, 4 or 8 */
+  int32_t head_dim;           /* must be 128 */
+  int32_t page_size;          /* tokens per page, >= 1 */
+  int32_t max_pages_per_seq;  /* block_table row stride, >= ceil(max_kv_len / page_size) */
+  int32_t max_seq_len;        /* bound of the new tokens of a sequence, <= max_kv_len */
+  int32_t max_kv_len;         /* bound of the tokens of a sequence, <= 1048576 */
+  int32_t dtype;              /* of the cache: fp2_dtype_t */
+  int32_t scale_tokens;       /* FP2_FP8_E4M3: tokens per scale, 0 = a scale per head; else 0 */
+  int32_t sink_tokens;        /* first tokens that stay visible, and stay in an eviction; >= 0 */
+  int32_t window_tokens;      /* 0 = all earlier tokens are visible; >= 0 */
+  int32_t kv_splits;          /* 0 = keys cut into parts by the work of the call; n in 1..32:
+                                 at most n parts for every sequence and head */
+  float softmax_scale;        /* <= 0 selects 1/sqrt(head_dim) */
+} fp2_cache_params_t;
+
+/* One layer's cache (device pointers, owned by the caller; 16-byte aligned k and v). */
+typedef struct {
+  void* k;
+  void* v;
+  const float* k_head_scale;  /* [num_kv_heads], positive and finite; scale_tokens == 0 codes only */
+  const float* v_head_scale;
+  uint8_t* k_block_scale;     /* [num_slots / scale_tokens, num_kv_heads]; scale_tokens > 0 only */
+  uint8_t* v_block_scale;
+} fp2_kv_cache_t;
+
+/* Bytes of workspace (256-byte aligned) that fp2_cache_attend needs for
+ * `params`: the partial outputs of sequences whose keys are cut into parts,
+ * at most some 70 MB where kv_splits is 0. 0 where none is needed, and for an
+ * invalid params. */
+size_t fp2_cache_workspace_bytes(const fp2_cache_params_t* params);
+
+/* Writes the new tokens' keys and values, bf16 [cu_seqlens[batch],
+ * num_kv_heads, 128] each, into their slots. Codes are rounded to nearest,
+ * ties to even, and held within +-448; an infinity or NaN becomes the NaN
+ * code. With a scale per head they are e4m3(x / scale). With a scale per
+ * block it is 2^e, e = ceil(log2(a / 448)) for the largest finite magnitude a
+ * of the block's new tokens, held in [-100, 118]; where the block already
+ * holds tokens (its first one lies before the new ones) it is at least the
+ * scale that it has, and if it grows their codes are rounded again (exact but
+ * for what falls below 2^-6). The same slot must not be written twice in a
+ * call: pages with new tokens belong to one sequence. */
+fp2_status_t fp2_cache_append(const fp2_cache_params_t* params, const void* k_new,
+                              const void* v_new, const int32_t* cu_seqlens,
+                              const int32_t* cu_seqlens_host, const int32_t* cu_seqlens_k,
+                              const int32_t* cu_seqlens_k_host, const fp2_kv_cache_t* cache,
+                              const int32_t* block_table, void* stream);
+
+/* out = softmax(scale * q k^T) v over the keys that each query sees; q and
+ * out bf16 [cu_seqlens[batch], num_q_heads, 128], lse (nullable) fp32 [...,
+ * num_q_heads], the natural log of the sum. Probabilities are rounded to bf16
+ * for the value product. Rows past cu_seqlens[batch] are not touched. Where
+ * max_seq_len * g <= 64 the keys are read once for all rows of a sequence;
+ * results depend on kv_splits, and with 0 on the other sequences of a call,
+ * through rounding only. */
+fp2_status_t fp2_cache_attend(const fp2_cache_params_t* params, const void* q,
+                              const int32_t* cu_seqlens, const int32_t* cu_seqlens_host,
+                              const int32_t* cu_seqlens_k, const int32_t* cu_seqlens_k_host,
+                              const fp2_kv_cache_t* cache, const int32_t* block_table, void* out,
+                              float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* What the cached tokens received of the queries' probabilities: for j < the
+ * tokens of sequence b,
+ *   weights[b][h][j] = weights_in[b][h][j] + sum over the new tokens that see
+ *       j and the g query heads of h of exp(scale * q.k_j - lse)
+ * with q as in fp2_cache_attend and the lse that it returned. weights and
+ * weights_in (nullable = zeros; may be weights itself) are fp32 [batch,
+ * num_kv_heads, weights_stride], weights_stride >= max_kv_len; entries past a
+ * sequence are left alone. No values are read: cache->v may be null. The
+ * result does not depend on the order of anything (no atomics). */
+fp2_status_t fp2_cache_weights(const fp2_cache_params_t* params, const void* q, const float* lse,
+                               const int32_t* cu_seqlens, const int32_t* cu_seqlens_host,
+                               const int32_t* cu_seqlens_k, const int32_t* cu_seqlens_k_host,
+                               const fp2_kv_cache_t* cache, const int32_t* block_table,
+                               const float* weights_in, float* weights, int64_t weights_stride,
+                               void* stream);
+
+/* Cuts the sequences to at most `budget` tokens per KV head: the first
+ * sink_tokens, the last recent_tokens and, of the others, the heaviest by
+ * weights [batch][num_kv_heads][weights_stride] (fp32; equal ones by the
+ * lowest index, NaN last). sink_tokens + recent_tokens <= budget. A sequence
+ * of at most `budget` tokens keeps them all. Different heads keep different
+ * tokens.
+ *   kept       int32 [batch][num_kv_heads][budget]: the indexes that stay,
+ *              ascending, -1 behind them;
+ *   cu_seqlens_k_out  int32 [batch + 1]: the new lengths min(L, budget);
+ *   weights_out  fp32 [batch][num_kv_heads][weights_stride]: weights of the
+ *              tokens that stay, zeros behind them (every entry is written;
+ *              not weights itself).
+ * The rows that stay are written to slots target_table[b][i / page_size] *
+ * page_size + i % page_size of the same pool, i = 0, 1, ...; target_table
+ * int32 [batch][target_pages], target_pages >= ceil(min(budget, max_kv_len) /
+ * page_size). Its pages must not be pages of the call's sequences nor appear
+ * twice; the old pages are left as they are (they may be shared with others).
+ * With a scale per block the new blocks get scales as fp2_cache_append gives
+ * them, and the codes are rounded again (exact but for what falls below
+ * 2^-6). Positions count from the start of the new order from here on, for
+ * windows and first tokens too. max_seq_len, window_tokens and softmax_scale
+ * do not matter. */
+fp2_status_t fp2_cache_evict(const fp2_cache_params_t* params, const fp2_kv_cache_t* cache,
+                             const int32_t* cu_seqlens_k, const int32_t* cu_seqlens_k_host,
+                             const int32_t* block_table, const int32_t* target_table,
+                             int32_t target_pages, int32_t budget, int32_t recent_tokens,
+                             const float* weights, float* weights_out, int64_t weights_stride,
+                             int32_t* kept, int32_t* cu_seqlens_k_out, void* stream);
 
 /* Static description of a status code. */
 const char* fp2_status_str(fp2_status_t status);

@@ -49,7 +49,9 @@ class Params(ctypes.Structure):
 
 EXPORTS = ["fp2_workspace_bytes", "fp2_prefill", "fp2_estimate", "fp2_attend", "fp2_pool",
            "fp2_csr_capacity", "fp2_mask_to_csr", "fp2_means_cache_slots", "fp2_prefill_cached",
-           "fp2_calibrate", "fp2_time_kernels", "fp2_prefill_noalloc", "fp2_status_str",
+           "fp2_calibrate", "fp2_time_kernels", "fp2_prefill_noalloc", "fp2_cache_workspace_bytes",
+           "fp2_cache_append", "fp2_cache_attend", "fp2_cache_weights", "fp2_cache_evict",
+           "fp2_status_str",
            "fp2_last_error"]
 
 CALIB_KINDS = {"mfma_bf16": 0, "mfma_fp8": 1, "exp": 2}
@@ -95,6 +97,16 @@ def lib():
         L.fp2_time_kernels.argtypes = [vp] * 4
         L.fp2_prefill_noalloc.restype = ctypes.c_int
         L.fp2_prefill_noalloc.argtypes = [P] + [vp] * 15
+        L.fp2_cache_workspace_bytes.restype = ctypes.c_size_t
+        L.fp2_cache_workspace_bytes.argtypes = [vp]
+        L.fp2_cache_append.restype = ctypes.c_int
+        L.fp2_cache_append.argtypes = [vp] * 10
+        L.fp2_cache_attend.restype = ctypes.c_int
+        L.fp2_cache_attend.argtypes = [vp] * 11 + [ctypes.c_size_t, vp]
+        L.fp2_cache_weights.restype = ctypes.c_int
+        L.fp2_cache_weights.argtypes = [vp] * 11 + [ctypes.c_int64, vp]
+        L.fp2_cache_evict.restype = ctypes.c_int
+        L.fp2_cache_evict.argtypes = [vp] * 6 + [ctypes.c_int32] * 3 + [vp] * 2 + [ctypes.c_int64] + [vp] * 3
         L.fp2_status_str.restype = ctypes.c_char_p
         L.fp2_status_str.argtypes = [ctypes.c_int]
         L.fp2_last_error.restype = ctypes.c_char_p
@@ -480,3 +492,8 @@ def mask_to_csr(p: Params, block_mask, cu_seqlens, *, cu_seqlens_k=None, cu_seql
                                workspace.numel(), _stream(stream))
     _check("fp2_mask_to_csr", st)
     return offsets, indices
+
+
+# the paged cache's operators
+from .cache import (KVCache, alloc_cache, alloc_cache_workspace, cache_append, cache_attend,  # noqa: E402,F401
+                    cache_evict, cache_weights, cache_workspace_bytes, make_cache_params)

@@ -1,0 +1,620 @@
+// Attention of few query rows over a paged cache: single tokens, drafted
+// tokens, short tails. Causal, over the first `sink` tokens and the last
+// `window` ones.
+//
+// A unit is a (sequence, KV head): its rows are the new tokens times the g
+// query heads that share the head's keys, at most 64 (16 NT). The keys are
+// read once for all of them, so the call is bound by memory, 2 * 128 bytes a
+// key and head in 8 bits, twice that in bf16.
+//
+// * Work: the visible keys of a unit come in tiles of 32; units are cut into
+//   parts of about equal length, as many as fill the chip over all sequences
+//   (every workgroup works that out from the lengths, which are on the device
+//   only), and combine_kernel joins the parts. A workgroup takes one part, its
+//   four waves alternate tiles and join in LDS.
+// * A wave goes from global memory to the matrix cores without LDS.
+//   S^T = K Q^T on v_mfma_f32_16x16x32_bf16: A holds 16 keys, and which of the
+//   128 dimensions stands at which place of a product is free, so four lanes
+//   load 64 adjacent bytes of a row. A lane then holds query l % 16 and keys
+//   4 (l / 16) + i of two groups of 16: these eight are the B operand of
+//   O^T += V^T P^T if the values come in that order. A lane loads eight
+//   dimensions of those eight keys (16 lanes a row) and turns the 8 x 8 block
+//   by byte permutes; row r of A is then dimension 8 r + t of product t.
+// * Codes become bf16 exactly, with the block's power of two in the
+//   conversion; a scale per head multiplies the scores and the output.
+// * The running maximum m of a row moves only when a score passes it by more
+//   than 2^8, so most tiles have no exchange between lanes. Probabilities are
+//   rounded to bf16 for the product; sums, maxima and outputs are fp32.
+#include <algorithm>
+#include <type_traits>
+
+#include "cache.h"
+
+namespace fp2 {
+
+namespace {
+
+constexpr float kLn2f = 0.69314718055994530942f;
+constexpr int kTile = 32;        // keys per wave and step
+constexpr int kWaves = 4;
+constexpr int kParts = 1024;     // parts that a call's keys are cut for: four workgroups a compute unit
+constexpr int kMinTiles = 16;    // tiles of a part, at least
+constexpr float kTau = 8.0f;
+constexpr float kNoRef = -1e30f; // maximum of a row that saw no key
+
+// Tiles of a sequence that some row sees: `sinks` leading ones, then those
+// from `from` on.
+struct Tiles {
+  int sinks, from, n;
+};
+
+__device__ __forceinline__ Tiles tiles_of(const CacheProblem& p, int Lq, int L) {
+  Tiles t{0, 0, 0};
+  if (Lq <= 0 || L <= 0) return t;
+  const int lo = max(L - Lq - p.window + 1, 0);
+  t.sinks = (min(p.sink, L) + kTile - 1) / kTile;
+  t.from = max(lo / kTile, t.sinks);
+  t.n = t.sinks + max((L - 1) / kTile - t.from + 1, 0);
+  return t;
+}
+
+__device__ __forceinline__ int wave_scan(int v, int lane) {   // inclusive
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(v, o, 64);
+    if (lane >= o) v += u;
+  }
+  return v;
+}
+
+struct Unit {
+  int b, h, part, parts, slot;   // slot: first partial slot of the unit, if parts > 1
+};
+
+// The `item`-th (sequence, part, head) of the call, or, with by_unit, the
+// unit (sequence, head) of that number. Wave-uniform; false past the last.
+template <bool BY_UNIT>
+__device__ __forceinline__ bool find_item(const CacheProblem& p, int item, Unit& out) {
+  const int lane = threadIdx.x & 63;
+  auto tiles_at = [&](int b) {
+    return b < p.batch ? tiles_of(p, p.cu[b + 1] - p.cu[b], p.cuk[b + 1] - p.cuk[b]).n : 0;
+  };
+  int64_t total = 0;   // tiles of the call
+  int cut = 0;         // tiles of a part
+  const int n0 = tiles_at(lane);
+  if (p.splits == 0) {
+    for (int b0 = 0; b0 < p.batch; b0 += 64) {
+      int64_t s = b0 ? tiles_at(b0 + lane) : n0;
+      for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+      total += s;
+    }
+    total *= p.hkv;
+    cut = max((int)((total + kParts - 1) / kParts), kMinTiles);
+  }
+  int items = 0, slots = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += 64) {
+    const int n = b0 ? tiles_at(b0 + lane) : n0;
+    const int parts = p.splits ? min(p.splits, n) : (n + cut - 1) / cut;
+    const int mine = BY_UNIT ? (b0 + lane < p.batch ? p.hkv : 0) : parts * p.hkv;
+    const int own_slots = parts > 1 ? parts * p.hkv : 0;
+    const int incl = wave_scan(mine, lane), sincl = wave_scan(own_slots, lane);
+    const uint64_t hit = __ballot(items + incl > item);
+    if (hit) {
+      const int l = __ffsll((unsigned long long)hit) - 1;
+      const int local = item - items - __shfl(incl - mine, l, 64);
+      out.b = b0 + l;
+      out.parts = __shfl(parts, l, 64);
+      out.h = local % p.hkv;
+      out.part = local / p.hkv;
+      out.slot = slots + __shfl(sincl - own_slots, l, 64) + out.h * out.parts;
+      out.b = __builtin_amdgcn_readfirstlane(out.b);
+      out.h = __builtin_amdgcn_readfirstlane(out.h);
+      out.part = __builtin_amdgcn_readfirstlane(out.part);
+      out.parts = __builtin_amdgcn_readfirstlane(out.parts);
+      out.slot = __builtin_amdgcn_readfirstlane(out.slot);
+      return true;
+    }
+    items += __shfl(incl, 63, 64);
+    slots += __shfl(sincl, 63, 64);
+  }
+  return false;
+}
+
+// A tile as it comes from memory.
+template <int FORM>
+struct Raw {
+  static constexpr bool kBf16 = FORM == kCacheBf16;
+  uint4 k[2][kBf16 ? 4 : 2];                               // keys r and 16 + r, 16 bytes a chunk
+  std::conditional_t<kBf16, uint4, uint2> v[8];            // eight keys, eight dimensions
+  uint32_t ks[2], vs[2];                                   // kCacheBlock: scale bytes of the groups
+};
+
+__device__ __forceinline__ bf16x8_t codes_to_bf16(uint32_t a, uint32_t b, float s) {
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  const b2 x[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)a, s, false),
+                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)a, s, true),
+                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)b, s, false),
+                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)b, s, true)};
+  return __builtin_bit_cast(bf16x8_t, x);
+}
+
+// Whether a row's eight values hold an infinity or a NaN.
+__device__ __forceinline__ bool odd_values(uint4 v) {
+  bool bad = false;
+  const uint32_t d[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    bad |= (d[i] & 0x7f800000u) == 0x7f800000u || (d[i] & 0x7f80u) == 0x7f80u;
+  return bad;
+}
+__device__ __forceinline__ bool odd_values(uint2 v) {
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    bad |= ((v.x >> (8 * i)) & 0x7f) == 0x7f || ((v.y >> (8 * i)) & 0x7f) == 0x7f;
+  return bad;
+}
+// The same with those values set to zero.
+__device__ __forceinline__ uint4 even_values(uint4 v) {
+  uint32_t d[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((d[i] & 0x7f800000u) == 0x7f800000u) d[i] &= 0xffffu;
+    if ((d[i] & 0x7f80u) == 0x7f80u) d[i] &= 0xffff0000u;
+  }
+  return make_uint4(d[0], d[1], d[2], d[3]);
+}
+__device__ __forceinline__ uint2 even_values(uint2 v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (((v.x >> (8 * i)) & 0x7f) == 0x7f) v.x &= ~(0xffu << (8 * i));
+    if (((v.y >> (8 * i)) & 0x7f) == 0x7f) v.y &= ~(0xffu << (8 * i));
+  }
+  return v;
+}
+// Value e of the eight where it is an infinity or NaN, else zero.
+__device__ __forceinline__ float odd_value(uint4 v, int e) {
+  const uint32_t d = e < 2 ? v.x : e < 4 ? v.y : e < 6 ? v.z : v.w;
+  const uint32_t u = e & 1 ? d & 0xffff0000u : d << 16;
+  return (u & 0x7f800000u) == 0x7f800000u ? __uint_as_float(u) : 0.f;
+}
+__device__ __forceinline__ float odd_value(uint2 v, int e) {
+  const uint32_t c = ((e < 4 ? v.x : v.y) >> (8 * (e & 3))) & 0x7f;
+  return c == 0x7f ? __uint_as_float(0x7fc00000u) : 0.f;
+}
+
+// FORM: the cache's type. NT: 16-row tiles of query rows. GROUPED: pages hold
+// a multiple of 16 tokens, so the 16 keys of a group lie one after the other
+// and their address is uniform (scalar); otherwise every key has its own.
+template <int FORM, int NT, bool GROUPED>
+__global__ __launch_bounds__(64 * kWaves) void decode_kernel(CacheProblem p, CachePartials part,
+                                                             uint16_t* __restrict__ out,
+                                                             float* __restrict__ lse) {
+  constexpr bool kBf16 = FORM == kCacheBf16;
+  constexpr int ESZ = kBf16 ? 2 : 1;
+  constexpr int KC = kBf16 ? 4 : 2;            // 16-byte chunks of a key per lane
+  constexpr int LDR = kHeadDim + 4;            // LDS row, padded against bank conflicts
+  __shared__ float s_o[kWaves][16][LDR];
+  __shared__ float s_ml[kWaves][16][2];
+  Unit un;
+  if (!find_item<false>(p, blockIdx.x, un)) return;
+
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c16 = lane & 15, kg = lane >> 4;
+  const int q0 = ld_uniform(p.cu, un.b), Lq = ld_uniform(p.cu, un.b + 1) - q0;
+  const int64_t tok0 = ld_uniform(p.cuk, un.b);
+  const int L = ld_uniform(p.cuk, un.b + 1) - (int)tok0;
+  const int first = L - Lq, last = L - 1;      // positions of the first and the last row
+  const int rows = Lq * p.g;
+  const Tiles tl = tiles_of(p, Lq, L);
+  const int lo = (int)((int64_t)tl.n * un.part / un.parts);
+  const int hi = (int)((int64_t)tl.n * (un.part + 1) / un.parts);
+  auto tile_at = [&](int i) { return i < tl.sinks ? i : tl.from + i - tl.sinks; };
+
+  // queries: the B operand of score product s holds, for lane group kg, eight
+  // of the dimensions that the key operand holds there
+  bf16x8_t qb[NT][4];
+  int pos[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = 16 * nt + c16;
+    pos[nt] = first + r / p.g;
+    const uint16_t* qrow = p.q + ((int64_t)(q0 + min(r / p.g, Lq - 1)) * p.hq + un.h * p.g + r % p.g) *
+                                     kHeadDim;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int d = kBf16 ? 32 * s + 8 * kg : 64 * (s >> 1) + 16 * kg + 8 * (s & 1);
+      uint4 x = *(const uint4*)(qrow + d);
+      if (r >= rows) x = make_uint4(0, 0, 0, 0);
+      qb[nt][s] = __builtin_bit_cast(bf16x8_t, x);
+    }
+  }
+  f32x4_t o[NT][8];
+  float m[NT], l[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) o[nt][t] = f32x4_t{};
+    m[nt] = kNoRef;
+    l[nt] = 0.f;
+  }
+  float cs = p.scale_log2, vsc = 1.f;
+  if constexpr (FORM == kCacheHead) {
+    cs *= ld_uniform(p.k_head, un.h);
+    vsc = ld_uniform(p.v_head, un.h);
+  }
+
+  const int64_t rowb = (int64_t)p.hkv * kHeadDim * ESZ;
+  const int64_t hoff = (int64_t)un.h * kHeadDim * ESZ;
+  const uint8_t* K = p.k + hoff;
+  const uint8_t* V = p.v + hoff;
+  const uint32_t koff = (uint32_t)(c16 * rowb + 16 * kg);
+  const uint32_t voff = (uint32_t)(4 * kg * rowb + 8 * ESZ * c16);
+
+  // where the keys of a tile lie: the slots of its two groups' first keys, or
+  // that of key lane % 32. Keys past the sequence stand on valid ones.
+  struct Where {
+    int64_t s[2];
+  };
+  auto where = [&](int tile) {
+    Where a;
+    const int t0 = kTile * tile;
+    if constexpr (GROUPED) {
+      const int32_t* row = p.pm.table + (int64_t)un.b * p.pm.stride;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int t = u && t0 + 16 > last ? t0 : t0 + 16 * u;
+        const int pg = p.pm.shift >= 0 ? t >> p.pm.shift : t / p.pm.page;
+        a.s[u] = (int64_t)ld_uniform(row, pg) * p.pm.page + (t - pg * p.pm.page);
+      }
+    } else {
+      a.s[0] = slot_of(p.pm, un.b, tok0, min(t0 + (lane & 31), last));
+      a.s[1] = 0;
+    }
+    return a;
+  };
+  typedef std::conditional_t<kBf16, uint4, uint2> vrow_t;
+  auto load = [&](const Where& a, Raw<FORM>& x) {
+    if constexpr (GROUPED) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint8_t* kb = K + a.s[u] * rowb;
+#pragma unroll
+        for (int c = 0; c < KC; ++c) x.k[u][c] = *(const uint4*)(kb + (koff + 64u * c));
+        const uint8_t* vb = V + a.s[u] * rowb;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x.v[4 * u + e] = *(const vrow_t*)(vb + e * rowb + voff);
+        if constexpr (FORM == kCacheBlock) {
+          const int64_t at = (a.s[u] >> p.sb_shift) * p.hkv + un.h;
+          x.ks[u] = p.k_block[at];
+          x.vs[u] = p.v_block[at];
+        }
+      }
+    } else {
+      const int slot = (int)a.s[0];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint8_t* kb = K + (int64_t)__shfl(slot, 16 * u + c16, 64) * rowb + 16 * kg;
+#pragma unroll
+        for (int c = 0; c < KC; ++c) x.k[u][c] = *(const uint4*)(kb + 64 * c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          x.v[4 * u + e] = *(const vrow_t*)(V + (int64_t)__shfl(slot, 16 * u + 4 * kg + e, 64) * rowb +
+                                            8 * ESZ * c16);
+      }
+    }
+  };
+
+  auto step = [&](int tile, Raw<FORM>& x) {
+    const int t0 = kTile * tile;
+    // keys that some row does not see: behind the first row, or before the
+    // last row's window and not among the first tokens
+    const bool masked = t0 + kTile - 1 > first ||
+                        (t0 <= last - p.window && t0 + kTile > p.sink);
+    f32x4_t s[NT][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      bf16x8_t a[4];
+      if constexpr (kBf16) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) a[c] = __builtin_bit_cast(bf16x8_t, x.k[u][c]);
+      } else {
+        const float sc = FORM == kCacheBlock ? block_scale(x.ks[u]) : 1.f;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          a[2 * c] = codes_to_bf16(x.k[u][c].x, x.k[u][c].y, sc);
+          a[2 * c + 1] = codes_to_bf16(x.k[u][c].z, x.k[u][c].w, sc);
+        }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        s[nt][u] = f32x4_t{};
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          s[nt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[c], qb[nt][c], s[nt][u], 0, 0, 0);
+      }
+    }
+    if (masked) {
+      // element i of group u is key t0 + 16 u + 4 kg + i
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = t0 + 16 * u + 4 * kg + i;
+            const bool see = key <= pos[nt] && (key < p.sink || key > pos[nt] - p.window);
+            s[nt][u][i] = see ? s[nt][u][i] : -INFINITY;
+          }
+      // values that no row sees (the pool holds anything there) must not meet
+      // the zero probabilities; nor infinities and NaN that some row does not see
+      bool bad = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int key = t0 + 16 * (e >> 2) + 4 * kg + (e & 3);
+        const bool any = key <= last && (key < p.sink || key > first - p.window);
+        if (!any) x.v[e] = vrow_t{};
+        if (Lq > 1) bad |= odd_values(x.v[e]);
+      }
+      if (Lq > 1 && __any(bad)) {
+        // rare: such values are added to the rows that see them by hand
+#pragma unroll 1
+        for (int k = 0; k < kTile; ++k) {
+          const int key = t0 + k;
+          if (key > last || !(key < p.sink || key > first - p.window)) continue;
+          const uint8_t* row = V + slot_of(p.pm, un.b, tok0, key) * rowb;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const vrow_t v = *(const vrow_t*)(row + (32 * kg + 8 * i) * ESZ);
+            if (!odd_values(v)) continue;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              const bool see = key <= pos[nt] && (key < p.sink || key > pos[nt] - p.window);
+#pragma unroll
+              for (int t = 0; t < 8; ++t) o[nt][t][i] += see ? odd_value(v, t) : 0.f;
+            }
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x.v[e] = even_values(x.v[e]);
+      }
+    }
+    // values: pair (2p, 2p + 1) of keys, dimension 8 c16 + t -> word p of
+    // product t's A operand
+    uint32_t va[8][4];
+    if constexpr (kBf16) {
+#pragma unroll
+      for (int pr = 0; pr < 4; ++pr) {
+        const uint4 a = x.v[2 * pr], b = x.v[2 * pr + 1];
+        const uint32_t ad[4] = {a.x, a.y, a.z, a.w}, bd[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          va[2 * t][pr] = __builtin_amdgcn_perm(bd[t], ad[t], 0x05040100u);
+          va[2 * t + 1][pr] = __builtin_amdgcn_perm(bd[t], ad[t], 0x07060302u);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int pr = 0; pr < 4; ++pr) {
+        const float sc = FORM == kCacheBlock ? block_scale(x.vs[pr >> 1]) : 1.f;
+        const uint2 a = x.v[2 * pr], b = x.v[2 * pr + 1];
+        const uint32_t ad[2] = {a.x, a.y}, bd[2] = {b.x, b.y};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {   // bytes a0 b0 a1 b1 of two dimensions
+          const uint32_t y = __builtin_amdgcn_perm(bd[t >> 1], ad[t >> 1],
+                                                   t & 1 ? 0x07030602u : 0x05010400u);
+          typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+          const b2 y0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)y, sc, false);
+          const b2 y1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)y, sc, true);
+          va[2 * t][pr] = __builtin_bit_cast(uint32_t, y0);
+          va[2 * t + 1][pr] = __builtin_bit_cast(uint32_t, y1);
+        }
+      }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[nt][u][i]);
+      mx *= cs;
+      if (__any(mx > m[nt] + kTau)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float mn = mx > m[nt] + kTau ? mx : m[nt];
+        const float f = fast_exp2(m[nt] - mn);
+        m[nt] = mn;
+        l[nt] *= f;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) o[nt][t] *= f;
+      }
+      float e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = fast_exp2(fmaf(s[nt][i >> 2][i & 3], cs, -m[nt]));
+      l[nt] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+      const bf16x8_t pb = __builtin_bit_cast(
+          bf16x8_t, make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]),
+                               pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])));
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const bf16x8_t a = __builtin_bit_cast(bf16x8_t, make_uint4(va[t][0], va[t][1], va[t][2], va[t][3]));
+        o[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pb, o[nt][t], 0, 0, 0);
+      }
+    }
+  };
+
+  // the next tile's rows are on their way while a tile is computed
+  if (lo + w < hi) {
+    Raw<FORM> cur, nxt;
+    load(where(tile_at(lo + w)), cur);
+    Where ahead = where(tile_at(min(lo + w + kWaves, hi - 1)));
+#pragma unroll 1
+    for (int i = lo + w; i < hi; i += kWaves) {
+      if (i + kWaves < hi) load(ahead, nxt);
+      ahead = where(tile_at(min(i + 2 * kWaves, hi - 1)));
+      step(tile_at(i), cur);
+      cur = nxt;
+    }
+  }
+
+  // the four waves' parts, joined 16 rows at a time
+  const bool split = un.parts > 1;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    if (16 * nt >= rows) break;
+    l[nt] += __shfl_xor(l[nt], 16, 64);
+    l[nt] += __shfl_xor(l[nt], 32, 64);
+    if (nt) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float* d = &s_o[w][c16][32 * kg + 8 * i];
+      *(float4*)d = make_float4(o[nt][0][i], o[nt][1][i], o[nt][2][i], o[nt][3][i]);
+      *(float4*)(d + 4) = make_float4(o[nt][4][i], o[nt][5][i], o[nt][6][i], o[nt][7][i]);
+    }
+    if (kg == 0) {
+      s_ml[w][c16][0] = m[nt];
+      s_ml[w][c16][1] = l[nt];
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < 16 * 32; x += 64 * kWaves) {
+      const int r = x >> 5, d = 4 * (x & 31), pr = 16 * nt + r;
+      if (pr >= rows) continue;
+      float mm = s_ml[0][r][0];
+#pragma unroll
+      for (int v = 1; v < kWaves; ++v) mm = fmaxf(mm, s_ml[v][r][0]);
+      float ll = 0.f;
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) {
+        const float f = fast_exp2(s_ml[v][r][0] - mm);
+        const float4 y = *(const float4*)&s_o[v][r][d];
+        ll += f * s_ml[v][r][1];
+        a.x += f * y.x, a.y += f * y.y, a.z += f * y.z, a.w += f * y.w;
+      }
+      if (split) {
+        const int64_t at = (int64_t)(un.slot + un.part) * (16 * NT) + pr;
+        *(float4*)(part.o + at * kHeadDim + d) = a;
+        if (d == 0) *(float2*)(part.ml + 2 * at) = make_float2(mm, ll);
+      } else {
+        const float inv = vsc / ll;
+        const int64_t at = (int64_t)(q0 + pr / p.g) * p.hq + un.h * p.g + pr % p.g;
+        *(uint2*)(out + at * kHeadDim + d) =
+            make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
+        if (lse && d == 0) lse[at] = (mm + fast_log2(ll)) * kLn2f;
+      }
+    }
+  }
+}
+
+// Joins the parts of the units that were cut: a workgroup takes one packed
+// row, eight groups of 32 lanes every eighth part.
+__global__ __launch_bounds__(256) void combine_kernel(CacheProblem p, CachePartials part, int rows_cap,
+                                                      int max_rows, uint16_t* __restrict__ out,
+                                                      float* __restrict__ lse) {
+  __shared__ float s_m[8], s_l[8];
+  __shared__ float4 s_a[8][32];
+  Unit un;
+  if (!find_item<true>(p, blockIdx.x / max_rows, un) || un.parts <= 1) return;
+  const int pr = blockIdx.x % max_rows;
+  const int q0 = ld_uniform(p.cu, un.b), Lq = ld_uniform(p.cu, un.b + 1) - q0;
+  if (pr >= Lq * p.g) return;
+  const int grp = threadIdx.x >> 5, d = threadIdx.x & 31;
+  float m = kNoRef, l = 0.f;
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = grp; i < un.parts; i += 8) {
+    const int64_t at = (int64_t)(un.slot + i) * rows_cap + pr;
+    const float2 ml = *(const float2*)(part.ml + 2 * at);
+    const float4 y = *(const float4*)(part.o + at * kHeadDim + 4 * d);
+    const float mn = fmaxf(m, ml.x);
+    const float f = fast_exp2(m - mn), g = fast_exp2(ml.x - mn);
+    m = mn;
+    l = l * f + ml.y * g;
+    a.x = a.x * f + y.x * g, a.y = a.y * f + y.y * g;
+    a.z = a.z * f + y.z * g, a.w = a.w * f + y.w * g;
+  }
+  if (d == 0) s_m[grp] = m, s_l[grp] = l;
+  s_a[grp][d] = a;
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  float mm = s_m[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) mm = fmaxf(mm, s_m[i]);
+  float ll = 0.f;
+  a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float f = fast_exp2(s_m[i] - mm);
+    const float4 y = s_a[i][d];
+    ll += f * s_l[i];
+    a.x += f * y.x, a.y += f * y.y, a.z += f * y.z, a.w += f * y.w;
+  }
+  const float inv = (p.form == kCacheHead ? ld_uniform(p.v_head, un.h) : 1.f) / ll;
+  const int64_t at = (int64_t)(q0 + pr / p.g) * p.hq + un.h * p.g + pr % p.g;
+  *(uint2*)(out + at * kHeadDim + 4 * d) =
+      make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
+  if (lse && d == 0) lse[at] = (mm + fast_log2(ll)) * kLn2f;
+}
+
+// 16-row tiles of the bound of the rows.
+int row_tiles(const CacheProblem& p) {
+  const int rows = p.max_new * p.g;
+  return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+}
+
+// Parts of a unit, at most.
+int64_t max_parts(const CacheProblem& p) {
+  const int seen = (int)std::min((int64_t)p.max_kv, (int64_t)p.window + p.max_new + p.sink);
+  const int tiles = seen / kTile + 3;   // ends of the two ranges inside a tile
+  return p.splits ? std::min(p.splits, tiles) : (tiles + kMinTiles - 1) / kMinTiles;
+}
+
+template <int FORM, int NT, bool GROUPED>
+hipError_t launch(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse,
+                  hipStream_t s) {
+  const int64_t units = (int64_t)p.batch * p.hkv, mp = max_parts(p);
+  // a unit of n tiles is cut into ceil(n / cut) parts, cut >= all tiles / kParts
+  const int64_t grid = p.splits ? units * mp : std::min(units * mp, units + kParts);
+  const int max_rows = p.max_new * p.g;
+  if (grid > 0x7fffffff || units * max_rows > 0x7fffffff) return hipErrorInvalidValue;
+  decode_kernel<FORM, NT, GROUPED><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, part, out, lse);
+  if (mp > 1)
+    combine_kernel<<<(unsigned)(units * max_rows), 256, 0, s>>>(p, part, 16 * NT, max_rows, out, lse);
+  return hipGetLastError();
+}
+
+template <int FORM, int NT>
+hipError_t launch_pages(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse,
+                        hipStream_t s) {
+  // scales of blocks imply pages of a multiple of 16 tokens
+  if constexpr (FORM == kCacheBlock) return launch<FORM, NT, true>(p, part, out, lse, s);
+  else if (p.pm.page % 16 == 0) return launch<FORM, NT, true>(p, part, out, lse, s);
+  else return launch<FORM, NT, false>(p, part, out, lse, s);
+}
+
+template <int FORM>
+hipError_t launch_rows(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse,
+                       hipStream_t s) {
+  const int nt = row_tiles(p);
+  return nt == 1   ? launch_pages<FORM, 1>(p, part, out, lse, s)
+         : nt == 2 ? launch_pages<FORM, 2>(p, part, out, lse, s)
+                   : launch_pages<FORM, 4>(p, part, out, lse, s);
+}
+
+}  // namespace
+
+void cache_decode_partials(const CacheProblem& p, int64_t* slots, int* rows) {
+  const int64_t units = (int64_t)p.batch * p.hkv, mp = max_parts(p);
+  // parts of cut units only: ceil(n / cut) < 2 n / cut where n > cut
+  *slots = mp <= 1 ? 0 : p.splits ? units * mp : std::min(units * mp, (int64_t)2 * kParts);
+  *rows = 16 * row_tiles(p);
+}
+
+hipError_t launch_cache_decode(const CacheProblem& p, const CachePartials& part, uint16_t* out,
+                               float* lse, hipStream_t s) {
+  return p.form == kCacheBf16   ? launch_rows<kCacheBf16>(p, part, out, lse, s)
+         : p.form == kCacheHead ? launch_rows<kCacheHead>(p, part, out, lse, s)
+                                : launch_rows<kCacheBlock>(p, part, out, lse, s);
+}
+
+}  // namespace fp2
