@@ -473,10 +473,12 @@ typedef struct {
   uint8_t* v_block_scale;
 } fp2_kv_cache_t;
 
-/* Bytes of workspace (256-byte aligned) that fp2_cache_attend needs for
- * `params`: the partial outputs of sequences whose keys are cut into parts,
- * at most some 70 MB where kv_splits is 0. 0 where none is needed, and for an
- * invalid params. */
+/* Bytes of workspace (256-byte aligned) that fp2_cache_attend and
+ * fp2_cache_weights need for `params`: the partial results of sequences whose
+ * keys (or queries) are cut into parts, at most 70 MB where kv_splits is 0. 0
+ * where none is needed, and for an invalid params. One workspace serves calls
+ * in order on a stream; calls that overlap, and graphs that may, need their
+ * own. */
 size_t fp2_cache_workspace_bytes(const fp2_cache_params_t* params);
 
 /* Writes the new tokens' keys and values, bf16 [cu_seqlens[batch],
@@ -522,7 +524,7 @@ fp2_status_t fp2_cache_weights(const fp2_cache_params_t* params, const void* q, 
                                const int32_t* cu_seqlens_k, const int32_t* cu_seqlens_k_host,
                                const fp2_kv_cache_t* cache, const int32_t* block_table,
                                const float* weights_in, float* weights, int64_t weights_stride,
-                               void* stream);
+                               void* workspace, size_t workspace_bytes, void* stream);
 
 /* Cuts the sequences to at most `budget` tokens per KV head: the first
  * sink_tokens, the last recent_tokens and, of the others, the heaviest by

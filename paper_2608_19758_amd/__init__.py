@@ -104,7 +104,7 @@ def lib():
         L.fp2_cache_attend.restype = ctypes.c_int
         L.fp2_cache_attend.argtypes = [vp] * 11 + [ctypes.c_size_t, vp]
         L.fp2_cache_weights.restype = ctypes.c_int
-        L.fp2_cache_weights.argtypes = [vp] * 11 + [ctypes.c_int64, vp]
+        L.fp2_cache_weights.argtypes = [vp] * 11 + [ctypes.c_int64, vp, ctypes.c_size_t, vp]
         L.fp2_cache_evict.restype = ctypes.c_int
         L.fp2_cache_evict.argtypes = [vp] * 6 + [ctypes.c_int32] * 3 + [vp] * 2 + [ctypes.c_int64] + [vp] * 3
         L.fp2_status_str.restype = ctypes.c_char_p

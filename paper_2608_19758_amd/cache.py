@@ -228,8 +228,8 @@ def _weight_rows(p: CacheParams, name, w):
 
 
 def cache_weights(p: CacheParams, q, lse, cache: KVCache, cu_seqlens, cu_seqlens_k, block_table, *,
-                  weights=None, weights_in=None, cu_seqlens_host=None, cu_seqlens_k_host=None,
-                  stream=None):
+                  weights=None, weights_in=None, workspace=None, cu_seqlens_host=None,
+                  cu_seqlens_k_host=None, stream=None):
     """fp2_cache_weights: weights = weights_in (zeros if None) plus what each cached token
     received of these queries, fp32 [batch, num_kv_heads, max_kv_len or more]. To add in
     place give the same tensor as both. A result that is allocated here starts as a copy of
@@ -247,16 +247,20 @@ def cache_weights(p: CacheParams, q, lse, cache: KVCache, cu_seqlens, cu_seqlens
     _weight_rows(p, "weights", weights)
     if weights_in is not None and weights_in.shape[2] != weights.shape[2]:
         raise ValueError("weights and weights_in differ in their last size")
+    if workspace is None:
+        workspace = alloc_cache_workspace(p, q.device)
+    _need(workspace, "workspace", esz=1)
     dev = _same_device((("q", q), ("lse", lse), ("cache.k", cache.k), ("cache.k_scale", cache.k_scale),
                         ("cu_seqlens", cu_seqlens), ("cu_seqlens_k", cu_seqlens_k),
-                        ("block_table", block_table), ("weights", weights), ("weights_in", weights_in)))
+                        ("block_table", block_table), ("weights", weights), ("weights_in", weights_in),
+                        ("workspace", workspace)))
     c = _pointers(p, cache)
     guard, s = _on(dev, stream)
     with guard:
         _check("fp2_cache_weights", lib().fp2_cache_weights(
             ctypes.byref(p), _ptr(q), _ptr(lse), _ptr(cu_seqlens), _host_ptr(cu_seqlens_host),
             _ptr(cu_seqlens_k), _host_ptr(cu_seqlens_k_host), ctypes.byref(c), _ptr(block_table),
-            _ptr(weights_in), _ptr(weights), weights.shape[2], s))
+            _ptr(weights_in), _ptr(weights), weights.shape[2], _ptr(workspace), workspace.numel(), s))
     return weights
 
 

@@ -91,6 +91,9 @@ constexpr int kFewRows = 64;
 void cache_decode_partials(const CacheProblem& p, int64_t* slots, int* rows);
 void cache_extend_partials(const CacheProblem& p, int64_t* slots, int* rows);
 
+// Floats of the partial weights of a call.
+int64_t cache_weights_partials(const CacheProblem& p);
+
 hipError_t launch_cache_append(const CacheProblem& p, const uint16_t* k_new, const uint16_t* v_new,
                                hipStream_t s);
 hipError_t launch_cache_decode(const CacheProblem& p, const CachePartials& part, uint16_t* out,
@@ -98,7 +101,7 @@ hipError_t launch_cache_decode(const CacheProblem& p, const CachePartials& part,
 hipError_t launch_cache_extend(const CacheProblem& p, const CachePartials& part, uint16_t* out,
                                float* lse, hipStream_t s);
 hipError_t launch_cache_weights(const CacheProblem& p, const float* lse, const float* in, float* out,
-                                int64_t stride, hipStream_t s);
+                                int64_t stride, float* part, hipStream_t s);
 hipError_t launch_cache_evict(const CacheProblem& p, const PageMap& to, int budget, int recent,
                               const float* weights, int64_t stride, float* weights_out,
                               int64_t out_stride, int32_t* kept, int32_t* cu_out, hipStream_t s);

@@ -145,8 +145,11 @@ CacheProblem make_problem(const fp2_cache_params_t* p, const void* q, const int3
 
 bool few_rows(const CacheProblem& r) { return (int64_t)r.max_new * r.g <= fp2::kFewRows; }
 
-// Offset of the maxima behind the outputs, and all bytes.
-void workspace_of(const CacheProblem& r, size_t* ml, size_t* total) {
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Bytes that the attention needs, and the offset of the maxima behind the
+// partial outputs.
+size_t attend_bytes(const CacheProblem& r, size_t* ml) {
   int64_t slots = 0;
   int rows = 0;
   if (r.batch > 0 && r.max_new > 0) {
@@ -154,7 +157,19 @@ void workspace_of(const CacheProblem& r, size_t* ml, size_t* total) {
     else fp2::cache_extend_partials(r, &slots, &rows);
   }
   *ml = (size_t)slots * rows * fp2::kHeadDim * sizeof(float);   // a multiple of 256
-  *total = *ml + (((size_t)slots * rows * 2 * sizeof(float) + 255) & ~(size_t)255);
+  return *ml + align256((size_t)slots * rows * 2 * sizeof(float));
+}
+
+size_t weights_bytes(const CacheProblem& r) {
+  return r.batch > 0 ? align256((size_t)fp2::cache_weights_partials(r) * sizeof(float)) : 0;
+}
+
+fp2_status_t check_workspace(const void* ws, size_t bytes, size_t need) {
+  if (need == 0) return FP2_OK;
+  if (!ws) return fail(FP2_EWORKSPACE, "workspace is null (need %zu bytes)", need);
+  if (!aligned(ws, 256)) return fail(FP2_EWORKSPACE, "workspace is not 256-byte aligned");
+  if (bytes < need) return fail(FP2_EWORKSPACE, "workspace has %zu bytes, need %zu", bytes, need);
+  return FP2_OK;
 }
 
 fp2_status_t hip_status(hipError_t e, const char* what) {
@@ -169,9 +184,10 @@ extern "C" {
 
 size_t fp2_cache_workspace_bytes(const fp2_cache_params_t* params) {
   if (check_params(params) != FP2_OK) return 0;
-  size_t ml, total;
-  workspace_of(make_problem(params, nullptr, nullptr, nullptr, nullptr, nullptr), &ml, &total);
-  return total;
+  const CacheProblem r = make_problem(params, nullptr, nullptr, nullptr, nullptr, nullptr);
+  size_t ml;
+  const size_t a = attend_bytes(r, &ml), w = weights_bytes(r);
+  return a > w ? a : w;
 }
 
 fp2_status_t fp2_cache_append(const fp2_cache_params_t* params, const void* k_new,
@@ -208,14 +224,8 @@ fp2_status_t fp2_cache_attend(const fp2_cache_params_t* params, const void* q,
   if (!q || !out) return fail(FP2_EINVAL, "q or out is null");
   if (!aligned(q, 16) || !aligned(out, 16)) return fail(FP2_EINVAL, "q and out must be 16-byte aligned");
   const CacheProblem r = make_problem(params, q, cu_seqlens, cu_seqlens_k, cache, block_table);
-  size_t ml, need;
-  workspace_of(r, &ml, &need);
-  if (need) {
-    if (!workspace) return fail(FP2_EWORKSPACE, "workspace is null (need %zu bytes)", need);
-    if (!aligned(workspace, 256)) return fail(FP2_EWORKSPACE, "workspace is not 256-byte aligned");
-    if (workspace_bytes < need)
-      return fail(FP2_EWORKSPACE, "workspace has %zu bytes, need %zu", workspace_bytes, need);
-  }
+  size_t ml;
+  if ((st = check_workspace(workspace, workspace_bytes, attend_bytes(r, &ml)))) return st;
   const fp2::CachePartials part{(float*)workspace, (float*)((char*)workspace + ml)};
   const hipError_t e =
       few_rows(r) ? fp2::launch_cache_decode(r, part, (uint16_t*)out, lse, (hipStream_t)stream)
@@ -228,7 +238,7 @@ fp2_status_t fp2_cache_weights(const fp2_cache_params_t* params, const void* q, 
                                const int32_t* cu_seqlens_k, const int32_t* cu_seqlens_k_host,
                                const fp2_kv_cache_t* cache, const int32_t* block_table,
                                const float* weights_in, float* weights, int64_t weights_stride,
-                               void* stream) {
+                               void* workspace, size_t workspace_bytes, void* stream) {
   fp2_status_t st = check_params(params);
   if (st != FP2_OK) return st;
   if (params->batch == 0 || params->max_kv_len == 0) return ok();
@@ -241,8 +251,9 @@ fp2_status_t fp2_cache_weights(const fp2_cache_params_t* params, const void* q, 
     return fail(FP2_EINVAL, "weights_stride %lld < max_kv_len %d", (long long)weights_stride,
                 params->max_kv_len);
   const CacheProblem r = make_problem(params, q, cu_seqlens, cu_seqlens_k, cache, block_table);
+  if ((st = check_workspace(workspace, workspace_bytes, weights_bytes(r)))) return st;
   return hip_status(fp2::launch_cache_weights(r, lse, weights_in, weights, weights_stride,
-                                              (hipStream_t)stream),
+                                              (float*)workspace, (hipStream_t)stream),
                     "fp2_cache_weights launch");
 }
 

@@ -28,96 +28,16 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "cache.h"
+#include "cache_few.h"
 
 namespace fp2 {
 
 namespace {
 
 constexpr float kLn2f = 0.69314718055994530942f;
-constexpr int kTile = 32;        // keys per wave and step
 constexpr int kWaves = 4;
-constexpr int kParts = 1024;     // parts that a call's keys are cut for: four workgroups a compute unit
-constexpr int kMinTiles = 16;    // tiles of a part, at least
 constexpr float kTau = 8.0f;
 constexpr float kNoRef = -1e30f; // maximum of a row that saw no key
-
-// Tiles of a sequence that some row sees: `sinks` leading ones, then those
-// from `from` on.
-struct Tiles {
-  int sinks, from, n;
-};
-
-__device__ __forceinline__ Tiles tiles_of(const CacheProblem& p, int Lq, int L) {
-  Tiles t{0, 0, 0};
-  if (Lq <= 0 || L <= 0) return t;
-  const int lo = max(L - Lq - p.window + 1, 0);
-  t.sinks = (min(p.sink, L) + kTile - 1) / kTile;
-  t.from = max(lo / kTile, t.sinks);
-  t.n = t.sinks + max((L - 1) / kTile - t.from + 1, 0);
-  return t;
-}
-
-__device__ __forceinline__ int wave_scan(int v, int lane) {   // inclusive
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(v, o, 64);
-    if (lane >= o) v += u;
-  }
-  return v;
-}
-
-struct Unit {
-  int b, h, part, parts, slot;   // slot: first partial slot of the unit, if parts > 1
-};
-
-// The `item`-th (sequence, part, head) of the call, or, with by_unit, the
-// unit (sequence, head) of that number. Wave-uniform; false past the last.
-template <bool BY_UNIT>
-__device__ __forceinline__ bool find_item(const CacheProblem& p, int item, Unit& out) {
-  const int lane = threadIdx.x & 63;
-  auto tiles_at = [&](int b) {
-    return b < p.batch ? tiles_of(p, p.cu[b + 1] - p.cu[b], p.cuk[b + 1] - p.cuk[b]).n : 0;
-  };
-  int64_t total = 0;   // tiles of the call
-  int cut = 0;         // tiles of a part
-  const int n0 = tiles_at(lane);
-  if (p.splits == 0) {
-    for (int b0 = 0; b0 < p.batch; b0 += 64) {
-      int64_t s = b0 ? tiles_at(b0 + lane) : n0;
-      for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-      total += s;
-    }
-    total *= p.hkv;
-    cut = max((int)((total + kParts - 1) / kParts), kMinTiles);
-  }
-  int items = 0, slots = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += 64) {
-    const int n = b0 ? tiles_at(b0 + lane) : n0;
-    const int parts = p.splits ? min(p.splits, n) : (n + cut - 1) / cut;
-    const int mine = BY_UNIT ? (b0 + lane < p.batch ? p.hkv : 0) : parts * p.hkv;
-    const int own_slots = parts > 1 ? parts * p.hkv : 0;
-    const int incl = wave_scan(mine, lane), sincl = wave_scan(own_slots, lane);
-    const uint64_t hit = __ballot(items + incl > item);
-    if (hit) {
-      const int l = __ffsll((unsigned long long)hit) - 1;
-      const int local = item - items - __shfl(incl - mine, l, 64);
-      out.b = b0 + l;
-      out.parts = __shfl(parts, l, 64);
-      out.h = local % p.hkv;
-      out.part = local / p.hkv;
-      out.slot = slots + __shfl(sincl - own_slots, l, 64) + out.h * out.parts;
-      out.b = __builtin_amdgcn_readfirstlane(out.b);
-      out.h = __builtin_amdgcn_readfirstlane(out.h);
-      out.part = __builtin_amdgcn_readfirstlane(out.part);
-      out.parts = __builtin_amdgcn_readfirstlane(out.parts);
-      out.slot = __builtin_amdgcn_readfirstlane(out.slot);
-      return true;
-    }
-    items += __shfl(incl, 63, 64);
-    slots += __shfl(sincl, 63, 64);
-  }
-  return false;
-}
 
 // A tile as it comes from memory.
 template <int FORM>
@@ -127,15 +47,6 @@ struct Raw {
   std::conditional_t<kBf16, uint4, uint2> v[8];            // eight keys, eight dimensions
   uint32_t ks[2], vs[2];                                   // kCacheBlock: scale bytes of the groups
 };
-
-__device__ __forceinline__ bf16x8_t codes_to_bf16(uint32_t a, uint32_t b, float s) {
-  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-  const b2 x[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)a, s, false),
-                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)a, s, true),
-                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)b, s, false),
-                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)b, s, true)};
-  return __builtin_bit_cast(bf16x8_t, x);
-}
 
 // Whether a row's eight values hold an infinity or a NaN.
 __device__ __forceinline__ bool odd_values(uint4 v) {
@@ -508,58 +419,53 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(CacheProblem p, Cac
 }
 
 // Joins the parts of the units that were cut: a workgroup takes one packed
-// row, eight groups of 32 lanes every eighth part.
+// row. The maximum over the parts comes first, so that the sums are plain ones
+// with their loads in flight together (eight groups of 32 lanes, every eighth
+// part each).
 __global__ __launch_bounds__(256) void combine_kernel(CacheProblem p, CachePartials part, int rows_cap,
                                                       int max_rows, uint16_t* __restrict__ out,
                                                       float* __restrict__ lse) {
-  __shared__ float s_m[8], s_l[8];
+  __shared__ float s_m[4], s_l[8];
   __shared__ float4 s_a[8][32];
   Unit un;
   if (!find_item<true>(p, blockIdx.x / max_rows, un) || un.parts <= 1) return;
   const int pr = blockIdx.x % max_rows;
   const int q0 = ld_uniform(p.cu, un.b), Lq = ld_uniform(p.cu, un.b + 1) - q0;
   if (pr >= Lq * p.g) return;
-  const int grp = threadIdx.x >> 5, d = threadIdx.x & 31;
-  float m = kNoRef, l = 0.f;
-  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i = grp; i < un.parts; i += 8) {
-    const int64_t at = (int64_t)(un.slot + i) * rows_cap + pr;
-    const float2 ml = *(const float2*)(part.ml + 2 * at);
-    const float4 y = *(const float4*)(part.o + at * kHeadDim + 4 * d);
-    const float mn = fmaxf(m, ml.x);
-    const float f = fast_exp2(m - mn), g = fast_exp2(ml.x - mn);
-    m = mn;
-    l = l * f + ml.y * g;
-    a.x = a.x * f + y.x * g, a.y = a.y * f + y.y * g;
-    a.z = a.z * f + y.z * g, a.w = a.w * f + y.w * g;
-  }
-  if (d == 0) s_m[grp] = m, s_l[grp] = l;
-  s_a[grp][d] = a;
+  const int tid = threadIdx.x, grp = tid >> 5, d = tid & 31;
+  const float* ml = part.ml + 2 * ((int64_t)un.slot * rows_cap + pr);
+  const float* po = part.o + ((int64_t)un.slot * rows_cap + pr) * kHeadDim + 4 * d;
+  float m = kNoRef;
+  for (int i = tid; i < un.parts; i += 256) m = fmaxf(m, ml[(int64_t)2 * i * rows_cap]);
+  m = wave_max(m);
+  if ((tid & 63) == 0) s_m[tid >> 6] = m;
   __syncthreads();
-  if (threadIdx.x >= 32) return;
-  float mm = s_m[0];
-#pragma unroll
-  for (int i = 1; i < 8; ++i) mm = fmaxf(mm, s_m[i]);
-  float ll = 0.f;
-  a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float f = fast_exp2(s_m[i] - mm);
-    const float4 y = s_a[i][d];
-    ll += f * s_l[i];
+  m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+  float l = 0.f;
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int i = grp; i < un.parts; i += 8) {
+    const float2 x = *(const float2*)(ml + (int64_t)2 * i * rows_cap);
+    const float4 y = *(const float4*)(po + (int64_t)i * rows_cap * kHeadDim);
+    const float f = fast_exp2(x.x - m);
+    l += f * x.y;
     a.x += f * y.x, a.y += f * y.y, a.z += f * y.z, a.w += f * y.w;
   }
-  const float inv = (p.form == kCacheHead ? ld_uniform(p.v_head, un.h) : 1.f) / ll;
+  if (d == 0) s_l[grp] = l;
+  s_a[grp][d] = a;
+  __syncthreads();
+  if (tid >= 32) return;
+  for (int i = 1; i < 8; ++i) {
+    const float4 y = s_a[i][d];
+    l += d == 0 ? s_l[i] : 0.f;
+    a.x += y.x, a.y += y.y, a.z += y.z, a.w += y.w;
+  }
+  l = __shfl(l, 0, 32);
+  const float inv = (p.form == kCacheHead ? ld_uniform(p.v_head, un.h) : 1.f) / l;
   const int64_t at = (int64_t)(q0 + pr / p.g) * p.hq + un.h * p.g + pr % p.g;
   *(uint2*)(out + at * kHeadDim + 4 * d) =
       make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
-  if (lse && d == 0) lse[at] = (mm + fast_log2(ll)) * kLn2f;
-}
-
-// 16-row tiles of the bound of the rows.
-int row_tiles(const CacheProblem& p) {
-  const int rows = p.max_new * p.g;
-  return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  if (lse && d == 0) lse[at] = (m + fast_log2(l)) * kLn2f;
 }
 
 // Parts of a unit, at most.

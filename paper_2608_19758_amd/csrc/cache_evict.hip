@@ -103,9 +103,16 @@ __global__ __launch_bounds__(kThreads) void select_kernel(CacheProblem p, int bu
     const uint32_t above = d == 0 ? 0u : d == 1 ? 0xffe00000u : 0xfffffc00u;
     for (int i = tid; i < bins; i += kThreads) hist[i] = 0;
     __syncthreads();
-    for (int i = lo + tid; i < hi; i += kThreads) {
-      const uint32_t u = order_of(wr[i]);
-      if ((u & above) == edge) atomicAdd(&hist[(u >> shift) & (bins - 1)], 1);
+    for (int i0 = lo + tid; i0 < hi; i0 += 8 * kThreads) {
+      float x[8];                        // eight loads in flight
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = i0 + j * kThreads < hi ? wr[i0 + j * kThreads] : 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t u = order_of(x[j]);
+        if (i0 + j * kThreads < hi && (u & above) == edge)
+          atomicAdd(&hist[(u >> shift) & (bins - 1)], 1);
+      }
     }
     __syncthreads();
     // bins from the top, two a thread
@@ -119,37 +126,48 @@ __global__ __launch_bounds__(kThreads) void select_kernel(CacheProblem p, int bu
     left = s_need;
     __syncthreads();
   }
-  // tokens in order: heavier than the edge, or the first `left` at it
-  int put = 0, equal = 0;
-#pragma unroll 1
-  for (int i0 = 0; i0 < L; i0 += kThreads * kPer) {
-    float x[kPer];
-    int eq = 0, fixed = 0, over = 0;   // bit masks of this thread's tokens
+  // tokens in order: protected or heavier than the edge, or the first `left` at
+  // it. Both are counted by one sum a step, the second kind in the high half.
+  int over = 0, equal = 0;               // of the steps before
+  float x[kPer], y[kPer];
+  auto load = [&](int i0, float (&v)[kPer]) {
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       const int i = i0 + kPer * tid + j;
-      x[j] = i < L ? wr[i] : 0.f;
-      if (i >= L) continue;
-      const uint32_t u = order_of(x[j]);
-      if (i < lo || i >= hi) fixed |= 1 << j;
-      else if (need > 0 && u > edge) over |= 1 << j;
-      else if (need > 0 && u == edge) eq |= 1 << j;
+      v[j] = i < L ? wr[i] : 0.f;
     }
-    int eq_total, keep_total;
-    int rank = equal + block_scan(__popc(eq), tot, eq_total);
-    int keep = fixed | over;
+  };
+  load(0, x);
+#pragma unroll 1
+  for (int i0 = 0; i0 < L; i0 += kThreads * kPer) {
+    load(i0 + kThreads * kPer, y);       // of the next step
+    int eq = 0, up = 0;                  // bit masks of this thread's tokens
 #pragma unroll
-    for (int j = 0; j < kPer; ++j)
-      if (eq >> j & 1) keep |= rank++ < left ? 1 << j : 0;
-    int to = put + block_scan(__popc(keep), tot, keep_total);
+    for (int j = 0; j < kPer; ++j) {
+      const int i = i0 + kPer * tid + j;
+      const uint32_t u = order_of(x[j]);
+      const bool fixed = i < lo || i >= hi;
+      if (i < L && (fixed || (need > 0 && u > edge))) up |= 1 << j;
+      else if (i < L && need > 0 && u == edge) eq |= 1 << j;
+    }
+    int total;
+    const int before = block_scan(__popc(up) | __popc(eq) << 16, tot, total);
+    int o = over + (before & 0xffff), e = equal + (before >> 16);
 #pragma unroll
-    for (int j = 0; j < kPer; ++j)
-      if (keep >> j & 1) {
+    for (int j = 0; j < kPer; ++j) {
+      const bool is_up = up >> j & 1, is_eq = eq >> j & 1;
+      if (is_up || (is_eq && e < left)) {
+        const int to = o + min(e, left);
         kr[to] = i0 + kPer * tid + j;
-        wo[to++] = x[j];
+        wo[to] = x[j];
       }
-    equal += eq_total;
-    put += keep_total;
+      o += is_up;
+      e += is_eq;
+    }
+    over += total & 0xffff;
+    equal += total >> 16;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) x[j] = y[j];
   }
 }
 

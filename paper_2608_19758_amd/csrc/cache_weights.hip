@@ -1,18 +1,25 @@
 // The attention weight that cached tokens received of a call's queries: for
 // each KV head, the sum over the new tokens and the g query heads of
-// exp(scale q.k - lse), with the log-sum-exp that the attention returned.
+// exp(scale q.k - lse), with the log-sum-exp that the attention returned. Each
+// sum has one writer: no atomics, and the same result in every run.
 //
-// A workgroup takes 256 keys of a (sequence, head), a wave 64 of them as the
-// A operand of S^T = K Q^T (v_mfma_f32_32x32x16_bf16), which stay in registers
-// while the packed query rows that see them pass by, 32 at a time, through
-// LDS. A lane then holds query l % 32 and 32 keys and adds its probabilities
-// in fp32; at the end the 32 sums of a lane are exchanged and added over the
-// lanes, half of them a step (31 exchanges). Each sum has one writer: no
-// atomics, and the same result in every run.
+// few_kernel: at most 64 packed rows a sequence, bound by the keys' bytes. As
+// in the attention of few rows, parts of equal length fill the chip and a wave
+// takes tiles of 32 keys from global memory to the matrix cores; a lane then
+// holds one query and eight keys, whose sums over the 16 lanes of a group take
+// eight exchanges.
 //
-// Few rows: bound by the keys' bytes. Prompts: by the products and the
-// exponentials, half of the attention's work.
-#include "cache.h"
+// many_kernel: a workgroup takes 256 keys, a wave 64 of them as the A operand
+// of S^T = K Q^T (v_mfma_f32_32x32x16_bf16), which stay in registers while the
+// packed query rows that see them pass by, 32 at a time, through LDS. A lane
+// holds one query and 32 keys and adds its probabilities in fp32; at the end
+// the 32 sums of a lane are exchanged and added over the lanes, half of them a
+// step. Bound by the products and the exponentials, half of the attention's
+// work. Where the keys alone do not fill the chip the rows are cut into
+// segments too, whose sums sum_kernel adds in their order.
+#include <algorithm>
+
+#include "cache_few.h"
 
 namespace fp2 {
 
@@ -20,8 +27,164 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kWaves = 4;
-constexpr int kKeys = 64;                 // of a wave
+constexpr int kKeys = 64;                 // of a wave (many rows)
+constexpr int kChunk = kWaves * kKeys;
 constexpr int kRows = 32;                 // packed query rows of a step
+constexpr int kFill = 2048;               // workgroups that fill the chip evenly
+constexpr int kMaxSegs = 16;
+constexpr int kMinSteps = 8;              // steps of a segment, at least
+
+template <int FORM, int NT, bool GROUPED>
+__global__ __launch_bounds__(64 * kWaves) void few_kernel(CacheProblem p, const float* __restrict__ lse,
+                                                          const float* in, float* out, int64_t stride,
+                                                          bool all) {
+  constexpr bool kBf16 = FORM == kCacheBf16;
+  constexpr int ESZ = kBf16 ? 2 : 1;
+  constexpr int KC = kBf16 ? 4 : 2;            // 16-byte chunks of a key per lane
+  Unit un;
+  if (!find_item<false>(p, blockIdx.x, un, all)) return;
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c16 = lane & 15, kg = lane >> 4;
+  const int q0 = ld_uniform(p.cu, un.b), Lq = ld_uniform(p.cu, un.b + 1) - q0;
+  const int64_t tok0 = ld_uniform(p.cuk, un.b);
+  const int L = ld_uniform(p.cuk, un.b + 1) - (int)tok0;
+  const int first = L - Lq, last = L - 1, rows = Lq * p.g;
+  const Tiles tl = tiles_of(p, Lq, L, all);
+  const int lo = (int)((int64_t)tl.n * un.part / un.parts);
+  const int hi = (int)((int64_t)tl.n * (un.part + 1) / un.parts);
+  auto tile_at = [&](int i) { return i < tl.sinks ? i : tl.from + i - tl.sinks; };
+
+  bf16x8_t qb[NT][4];
+  int pos[NT];
+  float ref[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = 16 * nt + c16;
+    pos[nt] = r < rows ? first + r / p.g : -1;        // a row past the last sees nothing
+    ref[nt] = 0.f;
+    const int64_t qrow = (int64_t)(q0 + r / p.g) * p.hq + un.h * p.g + r % p.g;
+    if (r < rows) ref[nt] = lse[qrow] * kLog2e;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int d = kBf16 ? 32 * s + 8 * kg : 64 * (s >> 1) + 16 * kg + 8 * (s & 1);
+      uint4 x = make_uint4(0, 0, 0, 0);
+      if (r < rows) x = *(const uint4*)(p.q + qrow * kHeadDim + d);
+      qb[nt][s] = __builtin_bit_cast(bf16x8_t, x);
+    }
+  }
+  const float cs = p.scale_log2 * (FORM == kCacheHead ? ld_uniform(p.k_head, un.h) : 1.f);
+  const int64_t rowb = (int64_t)p.hkv * kHeadDim * ESZ;
+  const uint8_t* K = p.k + (int64_t)un.h * kHeadDim * ESZ;
+  const uint32_t koff = (uint32_t)(c16 * rowb + 16 * kg);
+  const int64_t wrow = ((int64_t)un.b * p.hkv + un.h) * stride;
+  // key of a tile that this lane writes
+  const int mine = 16 * (c16 >> 3) + 4 * kg + ((c16 >> 1) & 3);
+
+  struct Raw {
+    uint4 k[2][KC];
+    uint32_t ks[2];
+    float old;
+  };
+  auto seen = [&](int t0) { return t0 < p.sink || (t0 <= last && t0 + kTile - 1 > first - p.window); };
+  auto load = [&](int tile, Raw& x) {
+    const int t0 = kTile * tile;
+    x.old = in && t0 + mine <= last ? in[wrow + t0 + mine] : 0.f;
+    if (Lq <= 0 || !seen(t0)) return;
+    if constexpr (GROUPED) {
+      const int32_t* row = p.pm.table + (int64_t)un.b * p.pm.stride;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int t = u && t0 + 16 > last ? t0 : t0 + 16 * u;
+        const int pg = p.pm.shift >= 0 ? t >> p.pm.shift : t / p.pm.page;
+        const int64_t s = (int64_t)ld_uniform(row, pg) * p.pm.page + (t - pg * p.pm.page);
+        const uint8_t* kb = K + s * rowb;
+#pragma unroll
+        for (int c = 0; c < KC; ++c) x.k[u][c] = *(const uint4*)(kb + (koff + 64u * c));
+        if constexpr (FORM == kCacheBlock) x.ks[u] = p.k_block[(s >> p.sb_shift) * p.hkv + un.h];
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int64_t s = slot_of(p.pm, un.b, tok0, min(t0 + 16 * u + c16, last));
+#pragma unroll
+        for (int c = 0; c < KC; ++c) x.k[u][c] = *(const uint4*)(K + s * rowb + 16 * kg + 64 * c);
+      }
+    }
+  };
+  auto step = [&](int tile, const Raw& x) {
+    const int t0 = kTile * tile;
+    float sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+    if (Lq > 0 && seen(t0)) {
+      const bool masked = t0 + kTile - 1 > first || rows < 16 * NT ||
+                          (t0 <= last - p.window && t0 + kTile > p.sink);
+      bf16x8_t a[2][4];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if constexpr (kBf16) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) a[u][c] = __builtin_bit_cast(bf16x8_t, x.k[u][c]);
+        } else {
+          const float sc = FORM == kCacheBlock ? block_scale(x.ks[u]) : 1.f;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            a[u][2 * c] = codes_to_bf16(x.k[u][c].x, x.k[u][c].y, sc);
+            a[u][2 * c + 1] = codes_to_bf16(x.k[u][c].z, x.k[u][c].w, sc);
+          }
+        }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        f32x4_t s[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          s[u] = f32x4_t{};
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[u][c], qb[nt][c], s[u], 0, 0, 0);
+        }
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int key = t0 + 16 * (i >> 2) + 4 * kg + (i & 3);
+            const bool see = key <= pos[nt] && (key < p.sink || key > pos[nt] - p.window);
+            s[i >> 2][i & 3] = see ? s[i >> 2][i & 3] : -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += fast_exp2(fmaf(s[i >> 2][i & 3], cs, -ref[nt]));
+      }
+    }
+    // over the 16 lanes of a group: lanes 2 i and 2 i + 1 end with element i
+#pragma unroll
+    for (int n = 4; n > 0; n >>= 1) {
+      const bool up = c16 & (2 * n);
+#pragma unroll
+      for (int j = 0; j < n; ++j) {
+        const float send = up ? sum[j] : sum[j + n], keep = up ? sum[j + n] : sum[j];
+        sum[j] = keep + __shfl_xor(send, 2 * n, 64);
+      }
+    }
+    sum[0] += __shfl_xor(sum[0], 1, 64);
+    if (!(c16 & 1) && t0 + mine <= last) out[wrow + t0 + mine] = x.old + sum[0];
+  };
+
+  // two tiles ahead: few registers a tile, so loads in flight come cheap
+  if (lo + w < hi) {
+    Raw cur, n1, n2;
+    load(tile_at(lo + w), cur);
+    if (lo + w + kWaves < hi) load(tile_at(lo + w + kWaves), n1);
+#pragma unroll 1
+    for (int i = lo + w; i < hi; i += kWaves) {
+      if (i + 2 * kWaves < hi) load(tile_at(i + 2 * kWaves), n2);
+      step(tile_at(i), cur);
+      cur = n1;
+      n1 = n2;
+    }
+  }
+}
 
 __device__ __forceinline__ int place(int r, int c) { return r * 16 + (c ^ (r & 15)); }
 
@@ -30,41 +193,54 @@ struct Shared {
   float lse[2][kRows];
 };
 
+// Steps of rows, [from, to), that see some of the keys c0 .. c0 + kChunk - 1.
+struct Steps {
+  int from, to;
+};
+__device__ __forceinline__ Steps steps_of(const CacheProblem& p, int c0, int Lq, int L) {
+  // from the first query at or behind the keys to the last whose window
+  // reaches them (all where first tokens are among them)
+  const int P = L - Lq, kend = min(c0 + kChunk, L) - 1;
+  const int i_lo = max(c0 - P, 0);
+  const int i_hi = c0 < p.sink ? Lq - 1 : (int)min((int64_t)Lq - 1, (int64_t)kend + p.window - 1 - P);
+  const int from = i_lo * p.g / kRows;
+  return Steps{from, i_hi >= i_lo ? (i_hi * p.g + p.g - 1) / kRows + 1 : from};
+}
+
+// segs == 1: sums join `in` and go to `out`; else to part[seg][sequence, head][key].
 template <int FORM>
-__global__ __launch_bounds__(64 * kWaves) void weights_kernel(CacheProblem p,
+__global__ __launch_bounds__(64 * kWaves, 3) void many_kernel(CacheProblem p,
                                                               const float* __restrict__ lse,
                                                               const float* in, float* out,
-                                                              int64_t stride) {
+                                                              int64_t stride, float* part, int segs,
+                                                              int seg_steps, int chunks) {
   constexpr bool kBf16 = FORM == kCacheBf16;
   constexpr int ESZ = kBf16 ? 2 : 1;
   __shared__ Shared sh;
-  int64_t at = blockIdx.x;
+  int64_t at = blockIdx.x;             // the first keys are seen by most rows: they come first
   const int h = (int)(at % p.hkv);
   at /= p.hkv;
-  const int b = (int)(at % p.batch), c0 = (int)(at / p.batch) * kWaves * kKeys;
+  const int b = (int)(at % p.batch);
+  at /= p.batch;
+  const int seg = (int)(at % segs), c0 = (int)(at / segs) * kChunk;
   const int64_t tok0 = ld_uniform(p.cuk, b);
   const int L = ld_uniform(p.cuk, b + 1) - (int)tok0;
   if (c0 >= L) return;
   const int q0 = ld_uniform(p.cu, b), Lq = ld_uniform(p.cu, b + 1) - q0;
   const int P = L - Lq, rows = Lq * p.g;
+  const Steps st = steps_of(p, c0, Lq, L);
+  const int from = max(st.from, seg * seg_steps), to = min(st.to, (seg + 1) * seg_steps);
+  if (segs > 1 && from >= to) return;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, l32 = lane & 31;
   const int k0 = c0 + kKeys * w;              // the wave's first key
-
-  // rows of the workgroup's keys: from the first that lies at or behind them
-  // to the last whose window reaches them (all where they are first tokens)
-  const int kend = min(c0 + kWaves * kKeys, L) - 1;
-  const int i_lo = max(c0 - P, 0);
-  const int i_hi = c0 < p.sink ? Lq - 1 : min((int64_t)Lq - 1, (int64_t)kend + p.window - 1 - P);
-  const int t_lo = i_lo * p.g / kRows, t_hi = i_hi >= i_lo ? (i_hi * p.g + p.g - 1) / kRows + 1 : t_lo;
-
   float acc[32];
 #pragma unroll
   for (int i = 0; i < 32; ++i) acc[i] = 0.f;
 
-  if (t_lo < t_hi) {
+  if (from < to) {
     const int64_t rowb = (int64_t)p.hkv * kHeadDim * ESZ;
     const uint8_t* K = p.k + (int64_t)h * kHeadDim * ESZ;
     bf16x8_t a[2][8];
@@ -79,83 +255,79 @@ __global__ __launch_bounds__(64 * kWaves) void weights_kernel(CacheProblem p,
       } else {
         float sc = 1.f;
         if constexpr (FORM == kCacheBlock) sc = block_scale(p.k_block[(slot >> p.sb_shift) * p.hkv + h]);
-        typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint4 x = *(const uint4*)(row + 32 * j + 16 * half);
-          const uint32_t d[4] = {x.x, x.y, x.z, x.w};
-          b2 y[8];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            y[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)d[i], sc, false);
-            y[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)d[i], sc, true);
-          }
-          const b2 y0[4] = {y[0], y[1], y[2], y[3]}, y1[4] = {y[4], y[5], y[6], y[7]};
-          a[u][2 * j] = __builtin_bit_cast(bf16x8_t, y0);
-          a[u][2 * j + 1] = __builtin_bit_cast(bf16x8_t, y1);
+          a[u][2 * j] = codes_to_bf16(x.x, x.y, sc);
+          a[u][2 * j + 1] = codes_to_bf16(x.z, x.w, sc);
         }
       }
     }
     const float cs = p.scale_log2 * (FORM == kCacheHead ? ld_uniform(p.k_head, h) : 1.f);
 
-    // staging: thread -> row tid / 8 of a step, two 16-byte chunks
+    // staging: thread -> row tid / 8 of a step, two 16-byte chunks; g is a power of two
     const int r = tid >> 3, c = 2 * (tid & 7);
-    uint4 x[2];
+    const int gs = __builtin_ctz(p.g), gm = p.g - 1;
+    const uint16_t* Q = p.q + ((int64_t)q0 * p.hq + h * p.g) * kHeadDim;
+    const float* Z = lse + (int64_t)q0 * p.hq + h * p.g;
+    uint4 x0, x1;
     float ls = 0.f;
-    auto load = [&](int t) {
-      const int pr = min(kRows * t + r, rows - 1);
-      const uint16_t* src = p.q + ((int64_t)(q0 + pr / p.g) * p.hq + h * p.g + pr % p.g) * kHeadDim;
-      x[0] = *(const uint4*)(src + 8 * c);
-      x[1] = *(const uint4*)(src + 8 * c + 8);
-      if (tid < kRows) {
-        const int pl = min(kRows * t + tid, rows - 1);
-        ls = lse[(int64_t)(q0 + pl / p.g) * p.hq + h * p.g + pl % p.g] * kLog2e;
-      }
-    };
-    auto write = [&](int t) {
-      sh.q[t & 1][place(r, c)] = x[0];
-      sh.q[t & 1][place(r, c + 1)] = x[1];
-      if (tid < kRows) sh.lse[t & 1][tid] = ls;
-    };
-    load(t_lo);
-    write(t_lo);
-    if (t_lo + 1 < t_hi) load(t_lo + 1);
+#define LOAD(t)                                                                              \
+  do {                                                                                       \
+    const int pr = min(kRows * (t) + r, rows - 1);                                           \
+    const uint16_t* src = Q + ((int64_t)(pr >> gs) * p.hq + (pr & gm)) * kHeadDim + 8 * c;   \
+    x0 = *(const uint4*)src;                                                                 \
+    x1 = *(const uint4*)(src + 8);                                                           \
+    if (tid < kRows) {                                                                       \
+      const int pl = min(kRows * (t) + tid, rows - 1);                                       \
+      ls = Z[(int64_t)(pl >> gs) * p.hq + (pl & gm)] * kLog2e;                               \
+    }                                                                                        \
+  } while (0)
+#define STORE(t)                                                                             \
+  do {                                                                                       \
+    sh.q[(t) & 1][place(r, c)] = x0;                                                         \
+    sh.q[(t) & 1][place(r, c + 1)] = x1;                                                     \
+    if (tid < kRows) sh.lse[(t) & 1][tid] = ls;                                              \
+  } while (0)
+    LOAD(from);
+    STORE(from);
+    if (from + 1 < to) LOAD(from + 1);
 #pragma unroll 1
-    for (int t = t_lo; t < t_hi; ++t) {
+    for (int t = from; t < to; ++t) {
       lds_barrier();
-      if (t + 1 < t_hi) write(t + 1);
-      if (t + 2 < t_hi) load(t + 2);
-      const int pr = kRows * t + l32;
-      const int pos = pr < rows ? P + pr / p.g : -1;     // a row past the last sees nothing
-      const int first = P + kRows * t / p.g, last = P + min(kRows * t + kRows, rows) / p.g;
+      if (t + 1 < to) STORE(t + 1);
+      if (t + 2 < to) LOAD(t + 2);
+      const int first = P + ((kRows * t) >> gs), last = P + ((min(kRows * t + kRows, rows) - 1) >> gs);
       if (last < k0) continue;                           // (uniform) none of the wave's keys is seen
       const float ref = sh.lse[t & 1][l32];
       f32x16_t s[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) s[u] = f32x16_t{};
 #pragma unroll
-      for (int st = 0; st < 8; ++st) {
-        // dimensions 16 st + 8 half of bf16 keys, 32 (st / 2) + 16 half + 8 (st % 2) of codes
-        const int ch = kBf16 ? 2 * st + half : 4 * (st >> 1) + 2 * half + (st & 1);
+      for (int d = 0; d < 8; ++d) {
+        // dimensions 16 d + 8 half of bf16 keys, 32 (d / 2) + 16 half + 8 (d % 2) of codes
+        const int ch = kBf16 ? 2 * d + half : 4 * (d >> 1) + 2 * half + (d & 1);
         const bf16x8_t q = __builtin_bit_cast(bf16x8_t, sh.q[t & 1][place(l32, ch)]);
 #pragma unroll
         for (int u = 0; u < 2; ++u)
-          s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[u][st], q, s[u], 0, 0, 0);
+          s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[u][d], q, s[u], 0, 0, 0);
       }
-      const bool masked = k0 + kKeys - 1 > first || kRows * t + kRows > rows ||
-                          (k0 <= last - p.window && k0 + kKeys > p.sink);
+      if (k0 + kKeys - 1 > first || kRows * t + kRows > rows ||
+          (k0 <= last - p.window && k0 + kKeys > p.sink)) {
+        const int pr = kRows * t + l32;
+        const int pos = pr < rows ? P + (pr >> gs) : -1;   // a row past the last sees nothing
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float v = fast_exp2(fmaf(s[u][e], cs, -ref));
-          if (masked) {
-            const int key = k0 + 32 * u + 8 * (e >> 2) + 4 * half + (e & 3);
-            v = key <= pos && (key < p.sink || key > pos - p.window) ? v : 0.f;
-          }
-          acc[16 * u + e] += v;
+        for (int i = 0; i < 32; ++i) {
+          const int e = i & 15, key = k0 + 32 * (i >> 4) + 8 * (e >> 2) + 4 * half + (e & 3);
+          const bool see = key <= pos && (key < p.sink || key > pos - p.window);
+          s[i >> 4][e] = see ? s[i >> 4][e] : -INFINITY;
         }
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i) acc[i] += fast_exp2(fmaf(s[i >> 4][i & 15], cs, -ref));
     }
+#undef LOAD
+#undef STORE
   }
   // sums over the 32 lanes of a half: lane l32 keeps that of element l32
 #pragma unroll
@@ -167,27 +339,97 @@ __global__ __launch_bounds__(64 * kWaves) void weights_kernel(CacheProblem p,
       acc[j] = keep + __shfl_xor(send, n, 64);
     }
   }
-  const int u = l32 >> 4, e = l32 & 15;
-  const int key = k0 + 32 * u + 8 * (e >> 2) + 4 * half + (e & 3);
-  if (key < L) {
-    const int64_t to = ((int64_t)b * p.hkv + h) * stride + key;
-    out[to] = (in ? in[to] : 0.f) + acc[0];
+  const int e = l32 & 15, key = k0 + 32 * (l32 >> 4) + 8 * (e >> 2) + 4 * half + (e & 3);
+  const int64_t bh = (int64_t)b * p.hkv + h;
+  if (segs > 1) {
+    part[((int64_t)seg * p.batch * p.hkv + bh) * ((int64_t)chunks * kChunk) + key] = acc[0];
+  } else if (key < L) {
+    out[bh * stride + key] = (in ? in[bh * stride + key] : 0.f) + acc[0];
   }
+}
+
+// The segments' sums of a key, in their order.
+__global__ __launch_bounds__(kChunk) void sum_kernel(CacheProblem p, const float* in, float* out,
+                                                     int64_t stride, const float* __restrict__ part,
+                                                     int segs, int seg_steps, int chunks) {
+  const int bh = blockIdx.x % (p.batch * p.hkv), c0 = blockIdx.x / (p.batch * p.hkv) * kChunk;
+  const int b = bh / p.hkv;
+  const int L = ld_uniform(p.cuk, b + 1) - ld_uniform(p.cuk, b);
+  const int key = c0 + threadIdx.x;
+  if (key >= L) return;
+  const Steps st = steps_of(p, c0, ld_uniform(p.cu, b + 1) - ld_uniform(p.cu, b), L);
+  float sum = 0.f;
+  for (int s = 0; s < segs; ++s)
+    if (max(st.from, s * seg_steps) < min(st.to, (s + 1) * seg_steps))
+      sum += part[((int64_t)s * p.batch * p.hkv + bh) * ((int64_t)chunks * kChunk) + key];
+  const int64_t to = (int64_t)bh * stride + key;
+  out[to] = (in ? in[to] : 0.f) + sum;
+}
+
+int chunks_of(const CacheProblem& p) { return (p.max_kv + kChunk - 1) / kChunk; }
+
+// Segments of the rows, and steps of each.
+int segments(const CacheProblem& p, int* steps) {
+  const int all = (int)(((int64_t)p.max_new * p.g + kRows - 1) / kRows);
+  const int64_t groups = std::max<int64_t>(1, (int64_t)p.batch * p.hkv * chunks_of(p));
+  const int segs = (int)std::max<int64_t>(1, std::min<int64_t>({kFill / groups, all / kMinSteps, kMaxSegs}));
+  *steps = (all + segs - 1) / segs;
+  return segs;
+}
+
+bool few_rows(const CacheProblem& p) { return (int64_t)p.max_new * p.g <= kFewRows; }
+
+template <int FORM>
+hipError_t launch_few(const CacheProblem& p, const float* lse, const float* in, float* out,
+                      int64_t stride, hipStream_t s) {
+  // added in place, tiles that no query sees stay as they are; else all are written
+  const bool all = in != out;
+  const int64_t units = (int64_t)p.batch * p.hkv;
+  const int64_t mp = (p.max_kv / kTile + 1 + kMinTiles - 1) / kMinTiles;
+  const int64_t grid = p.splits ? units * p.splits : std::min(units * mp, units + kParts);
+  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  const dim3 g((unsigned)grid), t(64 * kWaves);
+  const int nt = row_tiles(p);
+  if (FORM == kCacheBlock || p.pm.page % 16 == 0) {
+    if (nt == 1) few_kernel<FORM, 1, true><<<g, t, 0, s>>>(p, lse, in, out, stride, all);
+    else if (nt == 2) few_kernel<FORM, 2, true><<<g, t, 0, s>>>(p, lse, in, out, stride, all);
+    else few_kernel<FORM, 4, true><<<g, t, 0, s>>>(p, lse, in, out, stride, all);
+  } else if constexpr (FORM != kCacheBlock) {
+    if (nt == 1) few_kernel<FORM, 1, false><<<g, t, 0, s>>>(p, lse, in, out, stride, all);
+    else if (nt == 2) few_kernel<FORM, 2, false><<<g, t, 0, s>>>(p, lse, in, out, stride, all);
+    else few_kernel<FORM, 4, false><<<g, t, 0, s>>>(p, lse, in, out, stride, all);
+  }
+  return hipGetLastError();
+}
+
+template <int FORM>
+hipError_t launch(const CacheProblem& p, const float* lse, const float* in, float* out, int64_t stride,
+                  float* part, hipStream_t s) {
+  if (few_rows(p)) return launch_few<FORM>(p, lse, in, out, stride, s);
+  int steps;
+  const int segs = segments(p, &steps), chunks = chunks_of(p);
+  const int64_t groups = (int64_t)p.batch * p.hkv * chunks;
+  if (groups * segs > 0x7fffffff) return hipErrorInvalidValue;
+  many_kernel<FORM><<<(unsigned)(groups * segs), 64 * kWaves, 0, s>>>(p, lse, in, out, stride, part, segs,
+                                                                      steps, chunks);
+  if (segs > 1)
+    sum_kernel<<<(unsigned)groups, kChunk, 0, s>>>(p, in, out, stride, part, segs, steps, chunks);
+  return hipGetLastError();
 }
 
 }  // namespace
 
+int64_t cache_weights_partials(const CacheProblem& p) {
+  int steps;
+  const int segs = few_rows(p) ? 1 : segments(p, &steps);
+  return segs > 1 ? (int64_t)segs * p.batch * p.hkv * chunks_of(p) * kChunk : 0;
+}
+
 hipError_t launch_cache_weights(const CacheProblem& p, const float* lse, const float* in, float* out,
-                                int64_t stride, hipStream_t s) {
-  const int64_t grid = (int64_t)p.batch * p.hkv * ((p.max_kv + kWaves * kKeys - 1) / (kWaves * kKeys));
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  if (p.form == kCacheBf16)
-    weights_kernel<kCacheBf16><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, lse, in, out, stride);
-  else if (p.form == kCacheHead)
-    weights_kernel<kCacheHead><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, lse, in, out, stride);
-  else
-    weights_kernel<kCacheBlock><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, lse, in, out, stride);
-  return hipGetLastError();
+                                int64_t stride, float* part, hipStream_t s) {
+  return p.form == kCacheBf16   ? launch<kCacheBf16>(p, lse, in, out, stride, part, s)
+         : p.form == kCacheHead ? launch<kCacheHead>(p, lse, in, out, stride, part, s)
+                                : launch<kCacheBlock>(p, lse, in, out, stride, part, s);
 }
 
 }  // namespace fp2

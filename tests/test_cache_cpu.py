@@ -47,7 +47,7 @@ def call(op, p, **over):
                                   a["ws"], a["wsb"], None)
     if op == "weights":
         return L.fp2_cache_weights(ref_p, a["q"], a["lse"], a["cu"], cuh, a["cuk"], cukh, c, a["table"], a["win"],
-                                   a["w"], a["stride"], None)
+                                   a["w"], a["stride"], a["ws"], a["wsb"], None)
     return L.fp2_cache_evict(ref_p, c, a["cuk"], cukh, a["table"], a["target"], a["pages"], a["budget"],
                              a["recent"], a["w"], a["wout"], a["stride"], a["kept"], a["cuo"], None)
 
@@ -125,13 +125,17 @@ def test_attend_workspace():
     assert call("attend", p, ws=FAKE, wsb=need - 1) == fp2.EWORKSPACE
     assert call("attend", p, ws=FAKE + 16, wsb=need) == fp2.EWORKSPACE
     assert "workspace" in fp2.last_error()
+    p = base(max_seq_len=1000)                                       # rows of the weights are cut too
+    need = fp2.cache_workspace_bytes(p)
+    assert need > 0 and call("weights", p) == fp2.EWORKSPACE
+    assert call("weights", p, ws=FAKE + 16, wsb=need) == fp2.EWORKSPACE
 
 
 def test_workspace_bounds():
     """Nothing where no keys are cut; else bounded whatever the sizes."""
     assert fp2.cache_workspace_bytes(base(max_kv_len=400)) == 0
     assert fp2.cache_workspace_bytes(base(kv_splits=1)) == 0
-    assert fp2.cache_workspace_bytes(base(max_seq_len=2000, max_kv_len=2000, batch=64)) == 0
+    assert fp2.cache_workspace_bytes(base(max_seq_len=2000, max_kv_len=8000, batch=64)) == 0
     for kw in (dict(batch=65536), dict(max_seq_len=8), dict(max_seq_len=17, max_kv_len=1 << 20),
                dict(num_q_heads=64, max_seq_len=8, max_kv_len=1 << 20, batch=256), dict(window_tokens=100)):
         assert fp2.cache_workspace_bytes(base(**kw)) <= 70 << 20, kw
