@@ -446,7 +446,7 @@ fp2_status_t fp2_prefill_noalloc(const fp2_params_t* params, const void* q,
  * hold (streams, capture, errors).
  */
 typedef struct {
-  int32_t batch;              /* number of sequences, 0 .. 65536 */
+  int32_t batch;              /* number of sequences, 0 .. 65536; batch * (max_kv_len + 4096) <= 2^35 */
   int32_t num_q_heads;        /* H_q, a multiple of num_kv_heads */
   int32_t num_kv_heads;       /* 1 .. 1024; g = H_q / H_kv is 1, 2, 4 or 8 */
   int32_t head_dim;           /* must be 128 */
@@ -517,7 +517,7 @@ fp2_status_t fp2_cache_attend(const fp2_cache_params_t* params, const void* q,
  * with q as in fp2_cache_attend and the lse that it returned. weights and
  * weights_in (nullable = zeros; may be weights itself) are fp32 [batch,
  * num_kv_heads, weights_stride], weights_stride >= max_kv_len; entries past a
- * sequence are left alone. No values are read: cache->v may be null. The
+ * sequence are those of weights_in (zeros without it). No values are read: cache->v may be null. The
  * result does not depend on the order of anything (no atomics). */
 fp2_status_t fp2_cache_weights(const fp2_cache_params_t* params, const void* q, const float* lse,
                                const int32_t* cu_seqlens, const int32_t* cu_seqlens_host,

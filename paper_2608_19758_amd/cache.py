@@ -10,14 +10,13 @@ for it.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import dataclasses
 from typing import Optional
 
 import torch
 
-from . import (_INT32, _F32, BF16, FP8_E4M3, HEAD_DIM, _check, _host_ptr, _need, _ptr, lib)
+from . import _F32, _INT32, BF16, FP8_E4M3, HEAD_DIM, _check, _host_ptr, lib
 
 
 class CacheParams(ctypes.Structure):
@@ -89,142 +88,138 @@ def alloc_cache(p: CacheParams, num_pages: int, device="cuda", k_scale=None, v_s
 
 _ROWS = {BF16: (torch.bfloat16,), FP8_E4M3: (torch.uint8, torch.float8_e4m3fn)}
 _BF16 = (torch.bfloat16,)
+_U8 = (torch.uint8,)
+_BYTES = (torch.uint8, torch.int8)
 
 
-def _check_cache(p: CacheParams, c: KVCache, need_v=True):
-    row = p.num_kv_heads * p.head_dim
-    slots = c.k.numel() // max(1, row)
-    for name, t, s in (("k", c.k, c.k_scale), ("v", c.v, c.v_scale)):
-        if t is None and not need_v and name == "v":
-            continue
-        _need(t, "cache." + name, dtypes=_ROWS.get(p.dtype), divisible=max(1, row * p.page_size))
-        if t.numel() != c.k.numel():
+class _Args:
+    """Checks tensors one by one and gives their addresses: CUDA tensors on one device, dense, of the
+    right type and of at least `least` elements. The C ABI sees only pointers."""
+
+    def __init__(self):
+        self.dev = None
+        self.odd = None     # first tensor that is not on the device of the others, refused at the end
+
+    def __call__(self, name, t, dtypes, least=0, multiple=1):
+        if t is None:
+            return None
+        if not isinstance(t, torch.Tensor):
+            raise ValueError("%s must be a torch tensor" % name)
+        n = t.numel()
+        if t.dtype not in dtypes:
+            raise ValueError("%s must have dtype in %s, got %s" % (name, dtypes, t.dtype))
+        if not t.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
+        if n < least or n % multiple:
+            raise ValueError("%s holds %d elements, needs at least %d and a multiple of %d"
+                             % (name, n, least, multiple))
+        if self.dev is None:
+            self.dev = t.device
+        if (t.device != self.dev or not t.is_cuda) and self.odd is None:
+            self.odd = (name, t.device)
+        return t.data_ptr()
+
+    def table(self, p, name, t, width):
+        if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.shape[1] != width or t.shape[0] < p.batch:
+            raise ValueError("%s must be int32 [>= batch, %d], got %s"
+                             % (name, width, tuple(getattr(t, "shape", ()))))
+        return self(name, t, _INT32)
+
+    def weights(self, p, name, w):
+        if w is None:
+            return None
+        if w.dim() != 3 or w.shape[0] < p.batch or w.shape[1] != p.num_kv_heads or w.shape[2] < p.max_kv_len:
+            raise ValueError("%s must be fp32 [>= batch, num_kv_heads, >= max_kv_len], got %s"
+                             % (name, tuple(w.shape)))
+        return self(name, w, _F32)
+
+    def cache(self, p, c, need_v=True):
+        """fp2_kv_cache_t of the cache."""
+        row = max(1, p.num_kv_heads * p.head_dim * max(1, p.page_size))
+        rows = _ROWS.get(p.dtype, ())
+        k = self("cache.k", c.k, rows, 0, row)
+        v = self("cache.v", c.v, rows, 0, row) if need_v or c.v is not None else None
+        if v is not None and c.v.numel() != c.k.numel():
             raise ValueError("cache.k and cache.v differ in size")
         if p.dtype != FP8_E4M3:
-            continue
-        if s is None:
-            raise ValueError("cache.%s_scale is missing" % name)
+            return _CachePointers(k, v, None, None, None, None)
+        if c.k_scale is None or (need_v and c.v_scale is None):
+            raise ValueError("cache.k_scale or cache.v_scale is missing")
         if p.scale_tokens > 0:
-            _need(s, "cache.%s_scale" % name, dtypes=(torch.uint8,),
-                  min_numel=slots // p.scale_tokens * p.num_kv_heads)
+            least = c.k.numel() // (p.scale_tokens * p.head_dim)
+            ks, vs = self("cache.k_scale", c.k_scale, _U8, least), self("cache.v_scale", c.v_scale, _U8, least)
+            return _CachePointers(k, v, None, None, ks, vs)
+        ks, vs = (self("cache.k_scale", c.k_scale, _F32, p.num_kv_heads),
+                  self("cache.v_scale", c.v_scale, _F32, p.num_kv_heads))
+        return _CachePointers(k, v, ks, vs, None, None)
+
+    def lengths(self, p, cu, cuk, host, host_k):
+        for name, t in (("cu_seqlens_host", host), ("cu_seqlens_k_host", host_k)):
+            if t is None:
+                continue
+            torch_t = isinstance(t, torch.Tensor)
+            if (t.dtype != torch.int32 or t.is_cuda) if torch_t else t.dtype != "int32":
+                raise ValueError("%s must be a host int32 array" % name)
+            if (t.numel() if torch_t else t.size) < p.batch + 1:
+                raise ValueError("%s must have batch + 1 entries" % name)
+        return (self("cu_seqlens", cu, _INT32, p.batch + 1), _host_ptr(host),
+                self("cu_seqlens_k", cuk, _INT32, p.batch + 1), _host_ptr(host_k))
+
+    def call(self, name, stream, *args):
+        """The entry point on `stream` (the current one of the tensors' device if None), with that
+        device made current."""
+        if self.odd is not None:
+            raise ValueError("%s must be a CUDA tensor on the device of the others (%s), got one on %s"
+                             % (self.odd[0], self.dev, self.odd[1]))
+        if stream is None:
+            stream = torch.cuda.current_stream(self.dev)
+        elif stream.device != self.dev:
+            raise ValueError("stream is on %s, the tensors on %s" % (stream.device, self.dev))
+        if torch.cuda.current_device() == self.dev.index:
+            st = getattr(lib(), name)(*args, stream.cuda_stream)
         else:
-            _need(s, "cache.%s_scale" % name, dtypes=_F32, min_numel=p.num_kv_heads)
-
-
-def _check_table(p: CacheParams, name, t, width):
-    _need(t, name, dtypes=_INT32)
-    if t.dim() != 2 or t.shape[1] != width or t.shape[0] < p.batch:
-        raise ValueError("%s must be int32 [>= batch, %d], got %s" % (name, width, tuple(t.shape)))
-
-
-def _pointers(p: CacheParams, c: KVCache):
-    block = p.scale_tokens > 0
-    ks, vs = _ptr(c.k_scale), _ptr(c.v_scale)
-    return _CachePointers(_ptr(c.k), _ptr(c.v), None if block else ks, None if block else vs,
-                          ks if block else None, vs if block else None)
-
-
-def _same_device(named):
-    """Every tensor is a CUDA tensor, all on one device, which is returned."""
-    dev = None
-    for name, t in named:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("%s must be a CUDA tensor" % name)
-        dev = t.device if dev is None else dev
-        if t.device != dev:
-            raise ValueError("%s is on %s, other arguments on %s" % (name, t.device, dev))
-    return dev
-
-
-def _on(dev, stream):
-    """The device made current for the call, and the stream to use (dev's current one if None)."""
-    if stream is None:
-        stream = torch.cuda.current_stream(dev)
-    elif stream.device != dev:
-        raise ValueError("stream is on %s, the tensors on %s" % (stream.device, dev))
-    same = torch.cuda.current_device() == dev.index
-    return (contextlib.nullcontext() if same else torch.cuda.device(dev)), ctypes.c_void_p(stream.cuda_stream)
-
-
-def _lengths(p, cu_seqlens, cu_seqlens_k, host, host_k):
-    for name, t in (("cu_seqlens", cu_seqlens), ("cu_seqlens_k", cu_seqlens_k)):
-        _need(t, name, dtypes=_INT32, min_numel=p.batch + 1)
-    for name, t in (("cu_seqlens_host", host), ("cu_seqlens_k_host", host_k)):
-        if t is None:
-            continue
-        size = t.numel() if isinstance(t, torch.Tensor) else t.size
-        if str(t.dtype).replace("torch.", "") != "int32" or size < p.batch + 1 \
-                or (isinstance(t, torch.Tensor) and t.is_cuda):
-            raise ValueError("%s must be a host int32 array of batch + 1 entries" % name)
-
-
-def _queries(p, q, name="q"):
-    _need(q, name, dtypes=_BF16, divisible=p.num_q_heads * p.head_dim)
-    return q.numel() // (p.num_q_heads * p.head_dim)
+            with torch.cuda.device(self.dev):
+                st = getattr(lib(), name)(*args, stream.cuda_stream)
+        _check(name, st)
 
 
 def cache_append(p: CacheParams, k_new, v_new, cache: KVCache, cu_seqlens, cu_seqlens_k, block_table,
                  *, cu_seqlens_host=None, cu_seqlens_k_host=None, stream=None) -> None:
     """fp2_cache_append: k_new and v_new bf16 [new tokens, num_kv_heads, 128] into the
     cache's pages, in its type."""
-    _check_cache(p, cache)
-    for name, t in (("k_new", k_new), ("v_new", v_new)):
-        _need(t, name, dtypes=_BF16, divisible=p.num_kv_heads * p.head_dim)
+    a = _Args()
+    c = a.cache(p, cache)
+    row = p.num_kv_heads * p.head_dim
+    k, v = a("k_new", k_new, _BF16, 0, row), a("v_new", v_new, _BF16, 0, row)
     if k_new.numel() != v_new.numel():
         raise ValueError("k_new and v_new differ in size")
-    _lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host)
-    _check_table(p, "block_table", block_table, p.max_pages_per_seq)
-    dev = _same_device((("cache.k", cache.k), ("cache.v", cache.v), ("cache.k_scale", cache.k_scale),
-                        ("cache.v_scale", cache.v_scale), ("k_new", k_new), ("v_new", v_new),
-                        ("cu_seqlens", cu_seqlens), ("cu_seqlens_k", cu_seqlens_k),
-                        ("block_table", block_table)))
-    c = _pointers(p, cache)
-    guard, s = _on(dev, stream)
-    with guard:
-        _check("fp2_cache_append", lib().fp2_cache_append(
-            ctypes.byref(p), _ptr(k_new), _ptr(v_new), _ptr(cu_seqlens), _host_ptr(cu_seqlens_host),
-            _ptr(cu_seqlens_k), _host_ptr(cu_seqlens_k_host), ctypes.byref(c), _ptr(block_table), s))
+    lens = a.lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host)
+    table = a.table(p, "block_table", block_table, p.max_pages_per_seq)
+    a.call("fp2_cache_append", stream, ctypes.byref(p), k, v, *lens, ctypes.byref(c), table)
 
 
 def cache_attend(p: CacheParams, q, cache: KVCache, cu_seqlens, cu_seqlens_k, block_table, *, out=None,
                  lse=None, want_lse=False, workspace=None, cu_seqlens_host=None,
                  cu_seqlens_k_host=None, stream=None):
     """fp2_cache_attend: returns (out bf16 like q, lse fp32 [tokens, num_q_heads] or None)."""
-    rows = _queries(p, q)
-    _check_cache(p, cache)
-    _lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host)
-    _check_table(p, "block_table", block_table, p.max_pages_per_seq)
+    a = _Args()
+    row = p.num_q_heads * p.head_dim
+    qp = a("q", q, _BF16, 0, row)
+    rows = q.numel() // row
+    c = a.cache(p, cache)
+    lens = a.lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host)
+    table = a.table(p, "block_table", block_table, p.max_pages_per_seq)
     if out is None:
         out = torch.empty_like(q)
     if lse is None and want_lse:
         lse = torch.empty((rows, p.num_q_heads), dtype=torch.float32, device=q.device)
-    _need(out, "out", dtypes=_BF16, min_numel=q.numel())
-    _need(lse, "lse", dtypes=_F32, min_numel=rows * p.num_q_heads)
     if workspace is None:
         workspace = alloc_cache_workspace(p, q.device)
-    _need(workspace, "workspace", esz=1)
-    dev = _same_device((("q", q), ("cache.k", cache.k), ("cache.v", cache.v),
-                        ("cache.k_scale", cache.k_scale), ("cache.v_scale", cache.v_scale),
-                        ("cu_seqlens", cu_seqlens), ("cu_seqlens_k", cu_seqlens_k),
-                        ("block_table", block_table), ("out", out), ("lse", lse),
-                        ("workspace", workspace)))
-    c = _pointers(p, cache)
-    guard, s = _on(dev, stream)
-    with guard:
-        _check("fp2_cache_attend", lib().fp2_cache_attend(
-            ctypes.byref(p), _ptr(q), _ptr(cu_seqlens), _host_ptr(cu_seqlens_host),
-            _ptr(cu_seqlens_k), _host_ptr(cu_seqlens_k_host), ctypes.byref(c), _ptr(block_table),
-            _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(), s))
+    op, lp = a("out", out, _BF16, q.numel()), a("lse", lse, _F32, rows * p.num_q_heads)
+    ws = a("workspace", workspace, _BYTES)
+    a.call("fp2_cache_attend", stream, ctypes.byref(p), qp, *lens, ctypes.byref(c), table, op, lp, ws,
+           workspace.numel())
     return out, lse
-
-
-def _weight_rows(p: CacheParams, name, w):
-    _need(w, name, dtypes=_F32)
-    if w.dim() != 3 or w.shape[0] < p.batch or w.shape[1] != p.num_kv_heads or w.shape[2] < p.max_kv_len:
-        raise ValueError("%s must be fp32 [>= batch, num_kv_heads, >= max_kv_len], got %s"
-                         % (name, tuple(w.shape)))
 
 
 def cache_weights(p: CacheParams, q, lse, cache: KVCache, cu_seqlens, cu_seqlens_k, block_table, *,
@@ -232,35 +227,26 @@ def cache_weights(p: CacheParams, q, lse, cache: KVCache, cu_seqlens, cu_seqlens
                   cu_seqlens_k_host=None, stream=None):
     """fp2_cache_weights: weights = weights_in (zeros if None) plus what each cached token
     received of these queries, fp32 [batch, num_kv_heads, max_kv_len or more]. To add in
-    place give the same tensor as both. A result that is allocated here starts as a copy of
-    weights_in (zeros without one), so entries past a sequence are defined."""
-    rows = _queries(p, q)
-    _check_cache(p, cache, need_v=False)
-    _lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host)
-    _check_table(p, "block_table", block_table, p.max_pages_per_seq)
-    _need(lse, "lse", dtypes=_F32, min_numel=rows * p.num_q_heads)
-    if weights_in is not None:
-        _weight_rows(p, "weights_in", weights_in)
+    place give the same tensor as both."""
+    a = _Args()
+    row = p.num_q_heads * p.head_dim
+    qp = a("q", q, _BF16, 0, row)
+    lp = a("lse", lse, _F32, q.numel() // p.head_dim)
+    c = a.cache(p, cache, need_v=False)
+    lens = a.lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host)
+    table = a.table(p, "block_table", block_table, p.max_pages_per_seq)
+    wi = a.weights(p, "weights_in", weights_in)
     if weights is None:
-        weights = (torch.zeros((p.batch, p.num_kv_heads, p.max_kv_len), dtype=torch.float32, device=q.device)
-                   if weights_in is None else weights_in.clone())
-    _weight_rows(p, "weights", weights)
+        shape = (p.batch, p.num_kv_heads, p.max_kv_len if weights_in is None else weights_in.shape[2])
+        weights = torch.empty(shape, dtype=torch.float32, device=q.device)
+    w = a.weights(p, "weights", weights)
     if weights_in is not None and weights_in.shape[2] != weights.shape[2]:
         raise ValueError("weights and weights_in differ in their last size")
     if workspace is None:
         workspace = alloc_cache_workspace(p, q.device)
-    _need(workspace, "workspace", esz=1)
-    dev = _same_device((("q", q), ("lse", lse), ("cache.k", cache.k), ("cache.k_scale", cache.k_scale),
-                        ("cu_seqlens", cu_seqlens), ("cu_seqlens_k", cu_seqlens_k),
-                        ("block_table", block_table), ("weights", weights), ("weights_in", weights_in),
-                        ("workspace", workspace)))
-    c = _pointers(p, cache)
-    guard, s = _on(dev, stream)
-    with guard:
-        _check("fp2_cache_weights", lib().fp2_cache_weights(
-            ctypes.byref(p), _ptr(q), _ptr(lse), _ptr(cu_seqlens), _host_ptr(cu_seqlens_host),
-            _ptr(cu_seqlens_k), _host_ptr(cu_seqlens_k_host), ctypes.byref(c), _ptr(block_table),
-            _ptr(weights_in), _ptr(weights), weights.shape[2], _ptr(workspace), workspace.numel(), s))
+    ws = a("workspace", workspace, _BYTES)
+    a.call("fp2_cache_weights", stream, ctypes.byref(p), qp, lp, *lens, ctypes.byref(c), table, wi, w,
+           weights.shape[2], ws, workspace.numel())
     return weights
 
 
@@ -270,37 +256,25 @@ def cache_evict(p: CacheParams, cache: KVCache, weights, cu_seqlens_k, block_tab
     """fp2_cache_evict: the `budget` tokens of each sequence and KV head that stay go to the
     pages of target_table (int32 [batch, pages], other pages than block_table's). Returns
     (kept int32 [batch, num_kv_heads, budget], the new cu_seqlens_k, the weights that stay)."""
-    _check_cache(p, cache)
-    _need(cu_seqlens_k, "cu_seqlens_k", dtypes=_INT32, min_numel=p.batch + 1)
-    _lengths(p, None, None, None, cu_seqlens_k_host)
-    _check_table(p, "block_table", block_table, p.max_pages_per_seq)
-    if not (isinstance(target_table, torch.Tensor) and target_table.dim() == 2):
-        raise ValueError("target_table must be int32 [>= batch, pages]")
-    _check_table(p, "target_table", target_table, target_table.shape[1])
-    _weight_rows(p, "weights", weights)
-    dev = cache.k.device
+    a = _Args()
+    c = a.cache(p, cache)
+    _, _, cuk, cuk_host = a.lengths(p, None, cu_seqlens_k, None, cu_seqlens_k_host)
+    table = a.table(p, "block_table", block_table, p.max_pages_per_seq)
+    pages = target_table.shape[1] if isinstance(target_table, torch.Tensor) and target_table.dim() == 2 else -1
+    target = a.table(p, "target_table", target_table, pages)
+    w = a.weights(p, "weights", weights)
+    dev, heads = cache.k.device, p.batch * p.num_kv_heads
     if kept is None:
         kept = torch.empty((p.batch, p.num_kv_heads, max(1, budget)), dtype=torch.int32, device=dev)
     if cu_seqlens_k_out is None:
         cu_seqlens_k_out = torch.empty(p.batch + 1, dtype=torch.int32, device=dev)
     if weights_out is None:
         weights_out = torch.empty_like(weights)
-    _need(kept, "kept", dtypes=_INT32, min_numel=p.batch * p.num_kv_heads * budget)
-    _need(cu_seqlens_k_out, "cu_seqlens_k_out", dtypes=_INT32, min_numel=p.batch + 1)
-    _weight_rows(p, "weights_out", weights_out)
+    wo = a.weights(p, "weights_out", weights_out)
     if weights_out.shape[2] != weights.shape[2]:
         raise ValueError("weights and weights_out differ in their last size")
-    dev = _same_device((("cache.k", cache.k), ("cache.v", cache.v), ("cache.k_scale", cache.k_scale),
-                        ("cache.v_scale", cache.v_scale), ("weights", weights),
-                        ("cu_seqlens_k", cu_seqlens_k), ("block_table", block_table),
-                        ("target_table", target_table), ("kept", kept),
-                        ("cu_seqlens_k_out", cu_seqlens_k_out), ("weights_out", weights_out)))
-    c = _pointers(p, cache)
-    guard, s = _on(dev, stream)
-    with guard:
-        _check("fp2_cache_evict", lib().fp2_cache_evict(
-            ctypes.byref(p), ctypes.byref(c), _ptr(cu_seqlens_k), _host_ptr(cu_seqlens_k_host),
-            _ptr(block_table), _ptr(target_table), target_table.shape[1], int(budget),
-            int(recent_tokens), _ptr(weights), _ptr(weights_out), weights.shape[2], _ptr(kept),
-            _ptr(cu_seqlens_k_out), s))
+    kp = a("kept", kept, _INT32, heads * budget)
+    co = a("cu_seqlens_k_out", cu_seqlens_k_out, _INT32, p.batch + 1)
+    a.call("fp2_cache_evict", stream, ctypes.byref(p), ctypes.byref(c), cuk, cuk_host, table, target,
+           target_table.shape[1], int(budget), int(recent_tokens), w, wo, weights.shape[2], kp, co)
     return kept, cu_seqlens_k_out, weights_out

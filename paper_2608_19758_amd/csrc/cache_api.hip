@@ -49,6 +49,8 @@ fp2_status_t check_params(const fp2_cache_params_t* p) {
     return fail(FP2_EINVAL, "max_pages_per_seq %d < ceil(max_kv_len / page_size) = %d",
                 p->max_pages_per_seq, pages);
   if (p->dtype != FP2_BF16 && p->dtype != FP2_FP8_E4M3) return fail(FP2_EINVAL, "dtype %d unknown", p->dtype);
+  if ((int64_t)p->batch * (p->max_kv_len + 4096ll) > 1ll << 35)   // tiles of 32 keys are counted in 31 bits
+    return fail(FP2_EUNSUPPORTED, "batch %d x max_kv_len %d > 2^35 - 4096 batch", p->batch, p->max_kv_len);
   const int sb = p->scale_tokens;
   if (sb != 0) {
     if (p->dtype != FP2_FP8_E4M3) return fail(FP2_EINVAL, "scale_tokens %d with a bf16 cache", sb);

@@ -7,11 +7,12 @@
 // read once for all of them, so the call is bound by memory, 2 * 128 bytes a
 // key and head in 8 bits, twice that in bf16.
 //
-// * Work: the visible keys of a unit come in tiles of 32; units are cut into
-//   parts of about equal length, as many as fill the chip over all sequences
-//   (every workgroup works that out from the lengths, which are on the device
-//   only), and combine_kernel joins the parts. A workgroup takes one part, its
-//   four waves alternate tiles and join in LDS.
+// * Work: the visible keys of a sequence come in tiles of 32. All tiles of the
+//   call are dealt to the workgroups in equal shares (each works its own out
+//   from the lengths, which are on the device only); the four waves of a
+//   workgroup alternate tiles and join in LDS, and combine_kernel joins
+//   sequences that lie in several shares. More than 32 rows are halved between
+//   the waves, which then read the same keys (the second time from cache).
 // * A wave goes from global memory to the matrix cores without LDS.
 //   S^T = K Q^T on v_mfma_f32_16x16x32_bf16: A holds 16 keys, and which of the
 //   128 dimensions stands at which place of a product is free, so four lanes
@@ -35,7 +36,8 @@ namespace fp2 {
 namespace {
 
 constexpr float kLn2f = 0.69314718055994530942f;
-constexpr int kWaves = 4;
+constexpr int kWaves = kFewWaves;
+constexpr int kShares = 256;     // workgroups that a call is dealt to: one a compute unit
 constexpr float kTau = 8.0f;
 constexpr float kNoRef = -1e30f; // maximum of a row that saw no key
 
@@ -48,79 +50,88 @@ struct Raw {
   uint32_t ks[2], vs[2];                                   // kCacheBlock: scale bytes of the groups
 };
 
-// Whether a row's eight values hold an infinity or a NaN.
+// Infinities and NaN among packed values, with no compare a value: adding the
+// lowest exponent bit (bf16), or one (codes), to a magnitude carries into the
+// sign's place only from them. The top bit of each odd value is returned.
+__device__ __forceinline__ uint32_t odd_bf16(uint32_t x) {
+  return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+}
+__device__ __forceinline__ uint32_t odd_codes(uint32_t x) {
+  return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+}
 __device__ __forceinline__ bool odd_values(uint4 v) {
-  bool bad = false;
-  const uint32_t d[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    bad |= (d[i] & 0x7f800000u) == 0x7f800000u || (d[i] & 0x7f80u) == 0x7f80u;
-  return bad;
+  return (odd_bf16(v.x) | odd_bf16(v.y) | odd_bf16(v.z) | odd_bf16(v.w)) != 0;
 }
-__device__ __forceinline__ bool odd_values(uint2 v) {
-  bool bad = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    bad |= ((v.x >> (8 * i)) & 0x7f) == 0x7f || ((v.y >> (8 * i)) & 0x7f) == 0x7f;
-  return bad;
-}
-// The same with those values set to zero.
+__device__ __forceinline__ bool odd_values(uint2 v) { return (odd_codes(v.x) | odd_codes(v.y)) != 0; }
+// The values with those set to zero.
 __device__ __forceinline__ uint4 even_values(uint4 v) {
-  uint32_t d[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if ((d[i] & 0x7f800000u) == 0x7f800000u) d[i] &= 0xffffu;
-    if ((d[i] & 0x7f80u) == 0x7f80u) d[i] &= 0xffff0000u;
-  }
-  return make_uint4(d[0], d[1], d[2], d[3]);
+  auto f = [](uint32_t x) { return x & ~((odd_bf16(x) >> 15) * 0xffffu); };
+  return make_uint4(f(v.x), f(v.y), f(v.z), f(v.w));
 }
 __device__ __forceinline__ uint2 even_values(uint2 v) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (((v.x >> (8 * i)) & 0x7f) == 0x7f) v.x &= ~(0xffu << (8 * i));
-    if (((v.y >> (8 * i)) & 0x7f) == 0x7f) v.y &= ~(0xffu << (8 * i));
-  }
-  return v;
+  auto f = [](uint32_t x) { return x & ~((odd_codes(x) >> 7) * 0xffu); };
+  return make_uint2(f(v.x), f(v.y));
 }
-// Value e of the eight where it is an infinity or NaN, else zero.
-__device__ __forceinline__ float odd_value(uint4 v, int e) {
-  const uint32_t d = e < 2 ? v.x : e < 4 ? v.y : e < 6 ? v.z : v.w;
-  const uint32_t u = e & 1 ? d & 0xffff0000u : d << 16;
-  return (u & 0x7f800000u) == 0x7f800000u ? __uint_as_float(u) : 0.f;
+// fp32 bits of value e of the eight where it is odd, else zero.
+__device__ __forceinline__ uint32_t odd_value(uint4 v, int e) {
+  const uint32_t d = e < 2 ? v.x : e < 4 ? v.y : e < 6 ? v.z : v.w, o = odd_bf16(d) >> 15;
+  return e & 1 ? d & ((o >> 16) * 0xffff0000u) : (d << 16) & ((o & 1) * 0xffff0000u);
 }
-__device__ __forceinline__ float odd_value(uint2 v, int e) {
-  const uint32_t c = ((e < 4 ? v.x : v.y) >> (8 * (e & 3))) & 0x7f;
-  return c == 0x7f ? __uint_as_float(0x7fc00000u) : 0.f;
+__device__ __forceinline__ uint32_t odd_value(uint2 v, int e) {
+  return ((odd_codes(e < 4 ? v.x : v.y) >> (8 * (e & 3) + 7)) & 1) * 0x7fc00000u;
 }
 
-// FORM: the cache's type. NT: 16-row tiles of query rows. GROUPED: pages hold
-// a multiple of 16 tokens, so the 16 keys of a group lie one after the other
-// and their address is uniform (scalar); otherwise every key has its own.
-template <int FORM, int NT, bool GROUPED>
-__global__ __launch_bounds__(64 * kWaves) void decode_kernel(CacheProblem p, CachePartials part,
-                                                             uint16_t* __restrict__ out,
-                                                             float* __restrict__ lse) {
+// FORM: the cache's type. NT: 16-row tiles of query rows of a wave. RS: waves
+// that share the rows of a tile of keys. GROUPED: pages hold a multiple of 16
+// tokens, so the 16 keys of a group lie one after the other and their address
+// is uniform (scalar); otherwise every key has its own. ONE: one new token a
+// sequence, so that every row sees the same keys.
+template <int FORM, int NT, int RS, bool GROUPED, bool ONE>
+__global__ __launch_bounds__(64 * kWaves, FORM == kCacheBf16 && NT > 1 ? 1 : 2) void decode_kernel(CacheProblem p, CachePartials part,
+                                                                int shares, uint16_t* __restrict__ out,
+                                                                float* __restrict__ lse) {
   constexpr bool kBf16 = FORM == kCacheBf16;
   constexpr int ESZ = kBf16 ? 2 : 1;
   constexpr int KC = kBf16 ? 4 : 2;            // 16-byte chunks of a key per lane
   constexpr int LDR = kHeadDim + 4;            // LDS row, padded against bank conflicts
+  constexpr int KS = kWaves / RS;              // waves that alternate tiles
   __shared__ float s_o[kWaves][16][LDR];
   __shared__ float s_ml[kWaves][16][2];
-  Unit un;
-  if (!find_item<false>(p, blockIdx.x, un)) return;
+  const int h = blockIdx.x % p.hkv, index = blockIdx.x / p.hkv;
+  Share sh;
+  if (!find_share<false>(p, shares, index, sh)) return;
 
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int ks = w / RS, rs = w % RS;          // this wave's place among tiles and rows
   const int c16 = lane & 15, kg = lane >> 4;
-  const int q0 = ld_uniform(p.cu, un.b), Lq = ld_uniform(p.cu, un.b + 1) - q0;
-  const int64_t tok0 = ld_uniform(p.cuk, un.b);
-  const int L = ld_uniform(p.cuk, un.b + 1) - (int)tok0;
+  float cs = p.scale_log2, vsc = 1.f;
+  if constexpr (FORM == kCacheHead) {
+    cs *= ld_uniform(p.k_head, h);
+    vsc = ld_uniform(p.v_head, h);
+  }
+  const int64_t rowb = (int64_t)p.hkv * kHeadDim * ESZ;
+  const int64_t hoff = (int64_t)h * kHeadDim * ESZ;
+  const uint8_t* K = p.k + hoff;
+  const uint8_t* V = p.v + hoff;
+  const uint32_t koff = (uint32_t)(c16 * rowb + 16 * kg);
+  const uint32_t voff = (uint32_t)(4 * kg * rowb + 8 * ESZ * c16);
+
+  int b = sh.b, base = sh.base;
+#pragma unroll 1
+  for (bool again = false;; again = true) {
+  if (again) {
+    sh.q0 = ld_uniform(p.cu, b);
+    sh.Lq = ld_uniform(p.cu, b + 1) - sh.q0;
+    sh.L = ld_uniform(p.cuk, b + 1) - ld_uniform(p.cuk, b);
+  }
+  const int q0 = sh.q0, Lq = ONE ? 1 : sh.Lq, L = sh.L;
   const int first = L - Lq, last = L - 1;      // positions of the first and the last row
   const int rows = Lq * p.g;
-  const Tiles tl = tiles_of(p, Lq, L);
-  const int lo = (int)((int64_t)tl.n * un.part / un.parts);
-  const int hi = (int)((int64_t)tl.n * (un.part + 1) / un.parts);
+  const Tiles tl = tiles_of(p, sh.Lq, L);
+  const int lo = max(sh.lo, base) - base, hi = min(sh.hi, base + tl.n) - base;
   auto tile_at = [&](int i) { return i < tl.sinks ? i : tl.from + i - tl.sinks; };
+  if (lo < hi) {
 
   // queries: the B operand of score product s holds, for lane group kg, eight
   // of the dimensions that the key operand holds there
@@ -128,9 +139,9 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(CacheProblem p, Cac
   int pos[NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int r = 16 * nt + c16;
-    pos[nt] = first + r / p.g;
-    const uint16_t* qrow = p.q + ((int64_t)(q0 + min(r / p.g, Lq - 1)) * p.hq + un.h * p.g + r % p.g) *
+    const int r = 16 * (NT * rs + nt) + c16;
+    pos[nt] = first + (ONE ? 0 : r / p.g);
+    const uint16_t* qrow = p.q + ((int64_t)(q0 + (ONE ? 0 : min(r / p.g, Lq - 1))) * p.hq + h * p.g + r % p.g) *
                                      kHeadDim;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
@@ -149,18 +160,6 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(CacheProblem p, Cac
     m[nt] = kNoRef;
     l[nt] = 0.f;
   }
-  float cs = p.scale_log2, vsc = 1.f;
-  if constexpr (FORM == kCacheHead) {
-    cs *= ld_uniform(p.k_head, un.h);
-    vsc = ld_uniform(p.v_head, un.h);
-  }
-
-  const int64_t rowb = (int64_t)p.hkv * kHeadDim * ESZ;
-  const int64_t hoff = (int64_t)un.h * kHeadDim * ESZ;
-  const uint8_t* K = p.k + hoff;
-  const uint8_t* V = p.v + hoff;
-  const uint32_t koff = (uint32_t)(c16 * rowb + 16 * kg);
-  const uint32_t voff = (uint32_t)(4 * kg * rowb + 8 * ESZ * c16);
 
   // where the keys of a tile lie: the slots of its two groups' first keys, or
   // that of key lane % 32. Keys past the sequence stand on valid ones.
@@ -171,7 +170,7 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(CacheProblem p, Cac
     Where a;
     const int t0 = kTile * tile;
     if constexpr (GROUPED) {
-      const int32_t* row = p.pm.table + (int64_t)un.b * p.pm.stride;
+      const int32_t* row = p.pm.table + (int64_t)b * p.pm.stride;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int t = u && t0 + 16 > last ? t0 : t0 + 16 * u;
@@ -179,7 +178,7 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(CacheProblem p, Cac
         a.s[u] = (int64_t)ld_uniform(row, pg) * p.pm.page + (t - pg * p.pm.page);
       }
     } else {
-      a.s[0] = slot_of(p.pm, un.b, tok0, min(t0 + (lane & 31), last));
+      a.s[0] = slot_of(p.pm, b, 0, min(t0 + (lane & 31), last));
       a.s[1] = 0;
     }
     return a;
@@ -196,7 +195,7 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(CacheProblem p, Cac
 #pragma unroll
         for (int e = 0; e < 4; ++e) x.v[4 * u + e] = *(const vrow_t*)(vb + e * rowb + voff);
         if constexpr (FORM == kCacheBlock) {
-          const int64_t at = (a.s[u] >> p.sb_shift) * p.hkv + un.h;
+          const int64_t at = (a.s[u] >> p.sb_shift) * p.hkv + h;
           x.ks[u] = p.k_block[at];
           x.vs[u] = p.v_block[at];
         }
@@ -253,9 +252,8 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(CacheProblem p, Cac
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int key = t0 + 16 * u + 4 * kg + i;
-            const bool see = key <= pos[nt] && (key < p.sink || key > pos[nt] - p.window);
-            s[nt][u][i] = see ? s[nt][u][i] : -INFINITY;
+            s[nt][u][i] = sees(p, pos[nt], t0 + 16 * u + 4 * kg + i) ? s[nt][u][i] : -INFINITY;
+            s[nt][u][i] = pinned(s[nt][u][i]);
           }
       // values that no row sees (the pool holds anything there) must not meet
       // the zero probabilities; nor infinities and NaN that some row does not see
@@ -265,29 +263,36 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(CacheProblem p, Cac
         const int key = t0 + 16 * (e >> 2) + 4 * kg + (e & 3);
         const bool any = key <= last && (key < p.sink || key > first - p.window);
         if (!any) x.v[e] = vrow_t{};
-        if (Lq > 1) bad |= odd_values(x.v[e]);
+        if constexpr (!ONE) bad |= odd_values(x.v[e]);
+        x.v[e].x = pinned(x.v[e].x);
       }
-      if (Lq > 1 && __any(bad)) {
+      if (!ONE && Lq > 1 && __any(bad)) {
         // rare: such values are added to the rows that see them by hand
 #pragma unroll 1
         for (int k = 0; k < kTile; ++k) {
           const int key = t0 + k;
           if (key > last || !(key < p.sink || key > first - p.window)) continue;
-          const uint8_t* row = V + slot_of(p.pm, un.b, tok0, key) * rowb;
+          const uint8_t* row = V + slot_of(p.pm, b, 0, key) * rowb;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const vrow_t v = *(const vrow_t*)(row + (32 * kg + 8 * i) * ESZ);
             if (!odd_values(v)) continue;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              const bool see = key <= pos[nt] && (key < p.sink || key > pos[nt] - p.window);
+              const uint32_t see = sees(p, pos[nt], key) ? ~0u : 0u;
 #pragma unroll
-              for (int t = 0; t < 8; ++t) o[nt][t][i] += see ? odd_value(v, t) : 0.f;
+              for (int t = 0; t < 8; ++t) {
+                o[nt][t][i] += __uint_as_float(odd_value(v, t) & see);
+                o[nt][t][i] = pinned(o[nt][t][i]);
+              }
             }
           }
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x.v[e] = even_values(x.v[e]);
+        for (int e = 0; e < 8; ++e) {
+          x.v[e] = even_values(x.v[e]);
+          x.v[e].x = pinned(x.v[e].x);
+        }
       }
     }
     // values: pair (2p, 2p + 1) of keys, dimension 8 c16 + t -> word p of
@@ -356,27 +361,29 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(CacheProblem p, Cac
   };
 
   // the next tile's rows are on their way while a tile is computed
-  if (lo + w < hi) {
+  if (lo + ks < hi) {
     Raw<FORM> cur, nxt;
-    load(where(tile_at(lo + w)), cur);
-    Where ahead = where(tile_at(min(lo + w + kWaves, hi - 1)));
+    load(where(tile_at(lo + ks)), cur);
+    Where ahead = where(tile_at(min(lo + ks + KS, hi - 1)));
 #pragma unroll 1
-    for (int i = lo + w; i < hi; i += kWaves) {
-      if (i + kWaves < hi) load(ahead, nxt);
-      ahead = where(tile_at(min(i + 2 * kWaves, hi - 1)));
+    for (int i = lo + ks; i < hi; i += KS) {
+      if (i + KS < hi) load(ahead, nxt);
+      ahead = where(tile_at(min(i + 2 * KS, hi - 1)));
       step(tile_at(i), cur);
       cur = nxt;
     }
   }
 
-  // the four waves' parts, joined 16 rows at a time
-  const bool split = un.parts > 1;
+  // the waves' parts of the rows, joined 16 rows a wave at a time. A sequence
+  // in several shares leaves its part in slot 2 * share, if it started in an
+  // earlier one, or 2 * share + 1 (kv_splits: the share's own).
+  const bool split = p.splits ? hi - lo < tl.n : base < sh.lo || base + tl.n > sh.hi;
+  const int64_t slot = (p.splits ? (int64_t)index : 2 * (int64_t)index + (base >= sh.lo)) * p.hkv + h;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    if (16 * nt >= rows) break;
     l[nt] += __shfl_xor(l[nt], 16, 64);
     l[nt] += __shfl_xor(l[nt], 32, 64);
-    if (nt) __syncthreads();
+    if (nt || again) __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float* d = &s_o[w][c16][32 * kg + 8 * i];
@@ -388,33 +395,38 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(CacheProblem p, Cac
       s_ml[w][c16][1] = l[nt];
     }
     __syncthreads();
-    for (int x = threadIdx.x; x < 16 * 32; x += 64 * kWaves) {
-      const int r = x >> 5, d = 4 * (x & 31), pr = 16 * nt + r;
+    for (int x = threadIdx.x; x < RS * 16 * 32; x += 64 * kWaves) {
+      const int r = (x >> 5) & 15, d = 4 * (x & 31), rh = x >> 9, pr = 16 * (NT * rh + nt) + r;
       if (pr >= rows) continue;
-      float mm = s_ml[0][r][0];
+      float mm = s_ml[rh][r][0];
 #pragma unroll
-      for (int v = 1; v < kWaves; ++v) mm = fmaxf(mm, s_ml[v][r][0]);
+      for (int v = 1; v < KS; ++v) mm = fmaxf(mm, s_ml[v * RS + rh][r][0]);
       float ll = 0.f;
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) {
-        const float f = fast_exp2(s_ml[v][r][0] - mm);
-        const float4 y = *(const float4*)&s_o[v][r][d];
-        ll += f * s_ml[v][r][1];
+      for (int v = 0; v < KS; ++v) {
+        const float f = fast_exp2(s_ml[v * RS + rh][r][0] - mm);
+        const float4 y = *(const float4*)&s_o[v * RS + rh][r][d];
+        ll += f * s_ml[v * RS + rh][r][1];
         a.x += f * y.x, a.y += f * y.y, a.z += f * y.z, a.w += f * y.w;
       }
       if (split) {
-        const int64_t at = (int64_t)(un.slot + un.part) * (16 * NT) + pr;
+        const int64_t at = slot * (16 * NT * RS) + pr;
         *(float4*)(part.o + at * kHeadDim + d) = a;
         if (d == 0) *(float2*)(part.ml + 2 * at) = make_float2(mm, ll);
       } else {
         const float inv = vsc / ll;
-        const int64_t at = (int64_t)(q0 + pr / p.g) * p.hq + un.h * p.g + pr % p.g;
+        const int64_t at = (int64_t)(q0 + pr / p.g) * p.hq + h * p.g + pr % p.g;
         *(uint2*)(out + at * kHeadDim + d) =
             make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
         if (lse && d == 0) lse[at] = (mm + fast_log2(ll)) * kLn2f;
       }
     }
+  }
+  }
+  base += tl.n;
+  if (p.splits || base >= sh.hi) break;
+  ++b;
   }
 }
 
@@ -422,21 +434,39 @@ __global__ __launch_bounds__(64 * kWaves) void decode_kernel(CacheProblem p, Cac
 // row. The maximum over the parts comes first, so that the sums are plain ones
 // with their loads in flight together (eight groups of 32 lanes, every eighth
 // part each).
-__global__ __launch_bounds__(256) void combine_kernel(CacheProblem p, CachePartials part, int rows_cap,
-                                                      int max_rows, uint16_t* __restrict__ out,
+__global__ __launch_bounds__(256) void combine_kernel(CacheProblem p, CachePartials part, int shares,
+                                                      int rows_cap, int max_rows,
+                                                      uint16_t* __restrict__ out,
                                                       float* __restrict__ lse) {
   __shared__ float s_m[4], s_l[8];
   __shared__ float4 s_a[8][32];
-  Unit un;
-  if (!find_item<true>(p, blockIdx.x / max_rows, un) || un.parts <= 1) return;
-  const int pr = blockIdx.x % max_rows;
-  const int q0 = ld_uniform(p.cu, un.b), Lq = ld_uniform(p.cu, un.b + 1) - q0;
-  if (pr >= Lq * p.g) return;
+  const int pr = blockIdx.x % max_rows, bh = blockIdx.x / max_rows;
+  const int b = bh / p.hkv, h = bh % p.hkv;
+  Share sh;
+  if (!find_share<true>(p, shares, b, sh)) return;
+  const int q0 = sh.q0;
+  if (pr >= sh.Lq * p.g) return;
+  // the sequence's parts: slots `s0`, then every second share's (kv_splits:
+  // its own shares')
+  int parts;
+  int64_t s0, step;
+  if (p.splits) {
+    parts = min(p.splits, sh.hi - sh.lo);
+    s0 = (int64_t)b * p.splits;
+    step = 1;
+  } else {
+    const int from = sh.lo / sh.len;
+    parts = (sh.hi - 1) / sh.len - from + 1;
+    s0 = 2 * (int64_t)from;      // the first part, at 2 from + 1, is one slot further
+    step = 2;
+  }
+  if (parts <= 1) return;
+  const int odd = p.splits ? 0 : 1;
+  // row `pr` of part i, among the rows of all slots
+  auto row = [&](int i) { return ((s0 + step * i + (i ? 0 : odd)) * p.hkv + h) * rows_cap + pr; };
   const int tid = threadIdx.x, grp = tid >> 5, d = tid & 31;
-  const float* ml = part.ml + 2 * ((int64_t)un.slot * rows_cap + pr);
-  const float* po = part.o + ((int64_t)un.slot * rows_cap + pr) * kHeadDim + 4 * d;
   float m = kNoRef;
-  for (int i = tid; i < un.parts; i += 256) m = fmaxf(m, ml[(int64_t)2 * i * rows_cap]);
+  for (int i = tid; i < parts; i += 256) m = fmaxf(m, part.ml[2 * row(i)]);
   m = wave_max(m);
   if ((tid & 63) == 0) s_m[tid >> 6] = m;
   __syncthreads();
@@ -444,9 +474,9 @@ __global__ __launch_bounds__(256) void combine_kernel(CacheProblem p, CacheParti
   float l = 0.f;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
-  for (int i = grp; i < un.parts; i += 8) {
-    const float2 x = *(const float2*)(ml + (int64_t)2 * i * rows_cap);
-    const float4 y = *(const float4*)(po + (int64_t)i * rows_cap * kHeadDim);
+  for (int i = grp; i < parts; i += 8) {
+    const float2 x = *(const float2*)(part.ml + 2 * row(i));
+    const float4 y = *(const float4*)(part.o + row(i) * kHeadDim + 4 * d);
     const float f = fast_exp2(x.x - m);
     l += f * x.y;
     a.x += f * y.x, a.y += f * y.y, a.z += f * y.z, a.w += f * y.w;
@@ -461,66 +491,65 @@ __global__ __launch_bounds__(256) void combine_kernel(CacheProblem p, CacheParti
     a.x += y.x, a.y += y.y, a.z += y.z, a.w += y.w;
   }
   l = __shfl(l, 0, 32);
-  const float inv = (p.form == kCacheHead ? ld_uniform(p.v_head, un.h) : 1.f) / l;
-  const int64_t at = (int64_t)(q0 + pr / p.g) * p.hq + un.h * p.g + pr % p.g;
+  const float inv = (p.form == kCacheHead ? ld_uniform(p.v_head, h) : 1.f) / l;
+  const int64_t at = (int64_t)(q0 + pr / p.g) * p.hq + h * p.g + pr % p.g;
   *(uint2*)(out + at * kHeadDim + 4 * d) =
       make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
   if (lse && d == 0) lse[at] = (m + fast_log2(l)) * kLn2f;
 }
 
-// Parts of a unit, at most.
-int64_t max_parts(const CacheProblem& p) {
-  const int seen = (int)std::min((int64_t)p.max_kv, (int64_t)p.window + p.max_new + p.sink);
-  const int tiles = seen / kTile + 3;   // ends of the two ranges inside a tile
-  return p.splits ? std::min(p.splits, tiles) : (tiles + kMinTiles - 1) / kMinTiles;
+// Rows that a workgroup holds: 16, 32 or 64.
+int rows_cap(const CacheProblem& p) {
+  const int rows = p.max_new * p.g;
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
 }
 
-template <int FORM, int NT, bool GROUPED>
+template <int FORM, int NT, int RS, bool GROUPED, bool ONE>
 hipError_t launch(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse,
                   hipStream_t s) {
-  const int64_t units = (int64_t)p.batch * p.hkv, mp = max_parts(p);
-  // a unit of n tiles is cut into ceil(n / cut) parts, cut >= all tiles / kParts
-  const int64_t grid = p.splits ? units * mp : std::min(units * mp, units + kParts);
-  const int max_rows = p.max_new * p.g;
-  if (grid > 0x7fffffff || units * max_rows > 0x7fffffff) return hipErrorInvalidValue;
-  decode_kernel<FORM, NT, GROUPED><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, part, out, lse);
-  if (mp > 1)
-    combine_kernel<<<(unsigned)(units * max_rows), 256, 0, s>>>(p, part, 16 * NT, max_rows, out, lse);
+  const int shares = shares_of(p, kShares), max_rows = p.max_new * p.g;
+  const int64_t grid = (int64_t)shares * p.hkv, joins = (int64_t)p.batch * p.hkv * max_rows;
+  if (grid > 0x7fffffff || joins > 0x7fffffff) return hipErrorInvalidValue;
+  decode_kernel<FORM, NT, RS, GROUPED, ONE>
+      <<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, part, shares, out, lse);
+  if (p.splits != 1)
+    combine_kernel<<<(unsigned)joins, 256, 0, s>>>(p, part, shares, 16 * NT * RS, max_rows, out, lse);
   return hipGetLastError();
 }
 
-template <int FORM, int NT>
-hipError_t launch_pages(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse,
-                        hipStream_t s) {
-  // scales of blocks imply pages of a multiple of 16 tokens
-  if constexpr (FORM == kCacheBlock) return launch<FORM, NT, true>(p, part, out, lse, s);
-  else if (p.pm.page % 16 == 0) return launch<FORM, NT, true>(p, part, out, lse, s);
-  else return launch<FORM, NT, false>(p, part, out, lse, s);
+template <int FORM, bool GROUPED>
+hipError_t launch_rows(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse,
+                       hipStream_t s) {
+  const int rows = rows_cap(p);
+  return p.max_new == 1 ? launch<FORM, 1, 1, GROUPED, true>(p, part, out, lse, s)
+         : rows == 16   ? launch<FORM, 1, 1, GROUPED, false>(p, part, out, lse, s)
+         : rows == 32   ? launch<FORM, 2, 1, GROUPED, false>(p, part, out, lse, s)
+                        : launch<FORM, 2, 2, GROUPED, false>(p, part, out, lse, s);
 }
 
 template <int FORM>
-hipError_t launch_rows(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse,
-                       hipStream_t s) {
-  const int nt = row_tiles(p);
-  return nt == 1   ? launch_pages<FORM, 1>(p, part, out, lse, s)
-         : nt == 2 ? launch_pages<FORM, 2>(p, part, out, lse, s)
-                   : launch_pages<FORM, 4>(p, part, out, lse, s);
+hipError_t launch_pages(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse,
+                        hipStream_t s) {
+  // scales of blocks imply pages of a multiple of 16 tokens
+  if constexpr (FORM == kCacheBlock) return launch_rows<FORM, true>(p, part, out, lse, s);
+  else if (p.pm.page % 16 == 0) return launch_rows<FORM, true>(p, part, out, lse, s);
+  else return launch_rows<FORM, false>(p, part, out, lse, s);
 }
 
 }  // namespace
 
-void cache_decode_partials(const CacheProblem& p, int64_t* slots, int* rows) {
-  const int64_t units = (int64_t)p.batch * p.hkv, mp = max_parts(p);
-  // parts of cut units only: ceil(n / cut) < 2 n / cut where n > cut
-  *slots = mp <= 1 ? 0 : p.splits ? units * mp : std::min(units * mp, (int64_t)2 * kParts);
-  *rows = 16 * row_tiles(p);
+void cache_decode_partials(const CacheProblem& problem, int64_t* slots, int* rows) {
+  const CacheProblem p = dealt(problem);
+  *slots = p.splits == 1 ? 0 : (int64_t)shares_of(p, kShares) * (p.splits ? 1 : 2) * p.hkv;
+  *rows = rows_cap(p);
 }
 
-hipError_t launch_cache_decode(const CacheProblem& p, const CachePartials& part, uint16_t* out,
+hipError_t launch_cache_decode(const CacheProblem& problem, const CachePartials& part, uint16_t* out,
                                float* lse, hipStream_t s) {
-  return p.form == kCacheBf16   ? launch_rows<kCacheBf16>(p, part, out, lse, s)
-         : p.form == kCacheHead ? launch_rows<kCacheHead>(p, part, out, lse, s)
-                                : launch_rows<kCacheBlock>(p, part, out, lse, s);
+  const CacheProblem p = dealt(problem);
+  return p.form == kCacheBf16   ? launch_pages<kCacheBf16>(p, part, out, lse, s)
+         : p.form == kCacheHead ? launch_pages<kCacheHead>(p, part, out, lse, s)
+                                : launch_pages<kCacheBlock>(p, part, out, lse, s);
 }
 
 }  // namespace fp2

@@ -8,8 +8,9 @@ namespace fp2 {
 namespace {
 
 constexpr int kTile = 32;        // keys per wave and step
-constexpr int kParts = 1024;     // parts that a call's keys are cut for: four workgroups a compute unit
-constexpr int kMinTiles = 16;    // tiles of a part, at least
+constexpr int kFewWaves = 4;
+constexpr int kMinTiles = 4;     // tiles of a share, at least: one a wave
+constexpr int kWholeTiles = 16;  // sequences of at most as many are not cut
 
 // Tiles of a sequence that some row sees: `sinks` leading ones, then those
 // from `from` on.
@@ -17,11 +18,9 @@ struct Tiles {
   int sinks, from, n;
 };
 
-// With `all`, every tile of the sequence.
-__device__ __forceinline__ Tiles tiles_of(const CacheProblem& p, int Lq, int L, bool all = false) {
+__device__ __forceinline__ Tiles tiles_of(const CacheProblem& p, int Lq, int L) {
   Tiles t{0, 0, 0};
-  if (all) t.n = (L + kTile - 1) / kTile;
-  if (all || Lq <= 0 || L <= 0) return t;
+  if (Lq <= 0 || L <= 0) return t;
   const int lo = max(L - Lq - p.window + 1, 0);
   t.sinks = (min(p.sink, L) + kTile - 1) / kTile;
   t.from = max(lo / kTile, t.sinks);
@@ -29,64 +28,115 @@ __device__ __forceinline__ Tiles tiles_of(const CacheProblem& p, int Lq, int L, 
   return t;
 }
 
-__device__ __forceinline__ int wave_scan(int v, int lane) {   // inclusive
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(v, o, 64);
-    if (lane >= o) v += u;
-  }
-  return v;
+// Whether the query at `pos` sees `key`.
+__device__ __forceinline__ bool sees(const CacheProblem& p, int pos, int key) {
+  return (uint32_t)(key - pos + p.window - 1) < (uint32_t)p.window || (key < p.sink && key <= pos);
 }
 
-struct Unit {
-  int b, h, part, parts, slot;   // slot: first partial slot of the unit, if parts > 1
+// Keeps the compiler from computing many masks (a pair of scalar registers
+// each) before it uses the first: x is needed here.
+template <class T>
+__device__ __forceinline__ T pinned(T x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// The tiles of a call, one sequence after the other, form a line, which is cut
+// into equal shares; a workgroup takes one share of one head, so that all have
+// the same work whatever the lengths. A share may hold the end of one
+// sequence, whole ones, and the start of another. With kv_splits n >= 1 every
+// sequence is cut into at most n shares of its own instead.
+struct Share {
+  int lo, hi;       // tiles of the line
+  int b;            // sequence of the first
+  int base;         // and where that one starts
+  int len;          // tiles of a share (kv_splits 0)
+  int q0, Lq, L;    // the sequence's first query and its lengths
 };
 
-// The `item`-th (sequence, part, head) of the call, or, with by_unit, the
-// unit (sequence, head) of that number. Wave-uniform; false past the last.
-template <bool BY_UNIT>
-__device__ __forceinline__ bool find_item(const CacheProblem& p, int item, Unit& out,
-                                          bool all = false) {
+// Sequences of at most kWholeTiles tiles, by the bounds of the call, are taken
+// whole: there is nothing to even out, and nothing to join.
+inline CacheProblem dealt(CacheProblem p) {
+  const int64_t a = p.max_kv, b = (int64_t)p.window + p.max_new + p.sink;
+  if (p.splits == 0 && (a < b ? a : b) / kTile + 3 <= kWholeTiles) p.splits = 1;
+  return p;
+}
+
+// Shares of the line for `wgs` workgroups.
+inline __host__ __device__ int shares_of(const CacheProblem& p, int wgs) {
+  return p.splits ? p.batch * p.splits : (wgs + p.hkv - 1) / p.hkv;
+}
+
+__device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+
+// Share `index` of the call, or, with BY_SEQ, sequence `index` (lo .. hi then
+// are all its tiles). Wave-uniform; false where there is none. A call has
+// fewer than 2^31 tiles (the host's check).
+template <bool BY_SEQ>
+__device__ __forceinline__ bool find_share(const CacheProblem& p, int shares, int index, Share& out) {
   const int lane = threadIdx.x & 63;
+  int q0, Lq, L;
   auto tiles_at = [&](int b) {
-    return b < p.batch ? tiles_of(p, p.cu[b + 1] - p.cu[b], p.cuk[b + 1] - p.cuk[b], all).n : 0;
+    q0 = Lq = L = 0;
+    if (b < p.batch) {
+      q0 = p.cu[b];
+      Lq = p.cu[b + 1] - q0;
+      L = p.cuk[b + 1] - p.cuk[b];
+    }
+    return tiles_of(p, Lq, L).n;
   };
-  int64_t total = 0;   // tiles of the call
-  int cut = 0;         // tiles of a part
-  const int n0 = tiles_at(lane);
-  if (p.splits == 0) {
-    for (int b0 = 0; b0 < p.batch; b0 += 64) {
-      int64_t s = b0 ? tiles_at(b0 + lane) : n0;
-      for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-      total += s;
-    }
-    total *= p.hkv;
-    cut = max((int)((total + kParts - 1) / kParts), kMinTiles);
+  auto take = [&](int l) {
+    out.q0 = lane_value(q0, l);
+    out.Lq = lane_value(Lq, l);
+    out.L = lane_value(L, l);
+  };
+  if (p.splits) {
+    const int b = BY_SEQ ? index : index / p.splits, part = BY_SEQ ? 0 : index % p.splits;
+    const int n = lane_value(tiles_at(b), 0);
+    const int parts = BY_SEQ ? 1 : min(p.splits, n);
+    if (part >= parts) return false;
+    out.lo = (int)((int64_t)n * part / parts);
+    out.hi = (int)((int64_t)n * (part + 1) / parts);
+    out.b = b;
+    out.base = out.len = 0;
+    take(0);
+    return out.lo < out.hi;
   }
-  int items = 0, slots = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += 64) {
-    const int n = b0 ? tiles_at(b0 + lane) : n0;
-    const int parts = p.splits ? min(p.splits, n) : (n + cut - 1) / cut;
-    const int mine = BY_UNIT ? (b0 + lane < p.batch ? p.hkv : 0) : parts * p.hkv;
-    const int own_slots = parts > 1 ? parts * p.hkv : 0;
-    const int incl = wave_scan(mine, lane), sincl = wave_scan(own_slots, lane);
-    const uint64_t hit = __ballot(items + incl > item);
-    if (hit) {
-      const int l = __ffsll((unsigned long long)hit) - 1;
-      const int local = item - items - __shfl(incl - mine, l, 64);
-      out.b = b0 + l;
-      out.parts = __shfl(parts, l, 64);
-      out.h = local % p.hkv;
-      out.part = local / p.hkv;
-      out.slot = slots + __shfl(sincl - own_slots, l, 64) + out.h * out.parts;
-      out.b = __builtin_amdgcn_readfirstlane(out.b);
-      out.h = __builtin_amdgcn_readfirstlane(out.h);
-      out.part = __builtin_amdgcn_readfirstlane(out.part);
-      out.parts = __builtin_amdgcn_readfirstlane(out.parts);
-      out.slot = __builtin_amdgcn_readfirstlane(out.slot);
-      return true;
+  // tiles before each sequence, 64 of them at a time; up to 64 are looked at once
+  auto scan = [&](int n) {
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(n, o, 64);
+      if (lane >= o) n += u;
     }
-    items += __shfl(incl, 63, 64);
-    slots += __shfl(sincl, 63, 64);
+    return n;
+  };
+  int n = tiles_at(lane), incl = scan(n), total = lane_value(incl, 63);
+  for (int b0 = 64; b0 < p.batch; b0 += 64) {
+    int s = tiles_at(b0 + lane);
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    total += __builtin_amdgcn_readfirstlane(s);
+  }
+  out.len = max((int)(((int64_t)total + shares - 1) / shares), kMinTiles);
+  out.lo = (int)min((int64_t)index * out.len, (int64_t)total);
+  out.hi = (int)min((int64_t)out.lo + out.len, (int64_t)total);
+  if (!BY_SEQ && out.lo >= out.hi) return false;
+  int before = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += 64) {
+    if (p.batch > 64) {
+      n = tiles_at(b0 + lane);
+      incl = before + scan(n);
+    }
+    const uint64_t hit = __ballot(BY_SEQ ? b0 + lane == index : incl > out.lo);
+    if (hit) {
+      const int l = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)hit) - 1);
+      const int nl = lane_value(n, l);
+      out.b = b0 + l;
+      out.base = lane_value(incl, l) - nl;
+      take(l);
+      if (BY_SEQ) out.lo = out.base, out.hi = out.base + nl;
+      return out.lo < out.hi;
+    }
+    before = lane_value(incl, 63);
   }
   return false;
 }
@@ -98,12 +148,6 @@ __device__ __forceinline__ bf16x8_t codes_to_bf16(uint32_t a, uint32_t b, float 
                    __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)b, s, false),
                    __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)b, s, true)};
   return __builtin_bit_cast(bf16x8_t, x);
-}
-
-// 16-row tiles of the bound of the rows of a sequence.
-inline int row_tiles(const CacheProblem& p) {
-  const int rows = p.max_new * p.g;
-  return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
 }
 
 }  // namespace

@@ -4,8 +4,8 @@
 // sum has one writer: no atomics, and the same result in every run.
 //
 // few_kernel: at most 64 packed rows a sequence, bound by the keys' bytes. As
-// in the attention of few rows, parts of equal length fill the chip and a wave
-// takes tiles of 32 keys from global memory to the matrix cores; a lane then
+// in the attention of few rows, the call's tiles are dealt in equal shares and a
+// wave takes tiles of 32 keys from global memory to the matrix cores; a lane then
 // holds one query and eight keys, whose sums over the 16 lanes of a group take
 // eight exchanges.
 //
@@ -26,7 +26,9 @@ namespace fp2 {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr int kWaves = 4;
+constexpr int kWaves = kFewWaves;
+constexpr int kShares = 1024;             // workgroups that a call of few rows is dealt to
+constexpr int kCopy = 4096;               // entries of a workgroup's turn in the copy
 constexpr int kKeys = 64;                 // of a wave (many rows)
 constexpr int kChunk = kWaves * kKeys;
 constexpr int kRows = 32;                 // packed query rows of a step
@@ -37,23 +39,52 @@ constexpr int kMinSteps = 8;              // steps of a segment, at least
 template <int FORM, int NT, bool GROUPED>
 __global__ __launch_bounds__(64 * kWaves) void few_kernel(CacheProblem p, const float* __restrict__ lse,
                                                           const float* in, float* out, int64_t stride,
-                                                          bool all) {
+                                                          int shares) {
   constexpr bool kBf16 = FORM == kCacheBf16;
   constexpr int ESZ = kBf16 ? 2 : 1;
   constexpr int KC = kBf16 ? 4 : 2;            // 16-byte chunks of a key per lane
-  Unit un;
-  if (!find_item<false>(p, blockIdx.x, un, all)) return;
+  const int h = blockIdx.x % p.hkv, index = blockIdx.x / p.hkv;
+  // not in place: what no query sees, and what lies past the sequences
+  if (in != out) {
+    const int per = (int)((stride + kCopy - 1) / kCopy);
+    for (int64_t i = blockIdx.x; i < (int64_t)p.batch * p.hkv * per; i += gridDim.x) {
+      const int64_t row = i / per, from = i % per * kCopy;
+      const int sb = (int)(row / p.hkv);
+      const int Ls = ld_uniform(p.cuk, sb + 1) - ld_uniform(p.cuk, sb);
+      const Tiles t = tiles_of(p, ld_uniform(p.cu, sb + 1) - ld_uniform(p.cu, sb), Ls);
+      // tiles sinks .. until - 1 are unseen, and the entries from Ls on
+      const int until = t.n ? t.from : (Ls + kTile - 1) / kTile;
+      for (int64_t j = from + threadIdx.x; j < min(from + kCopy, stride); j += 64 * kWaves)
+        if (j >= Ls || (j / kTile >= t.sinks && j / kTile < until))
+          out[row * stride + j] = in ? in[row * stride + j] : 0.f;
+    }
+  }
+  Share sh;
+  if (!find_share<false>(p, shares, index, sh)) return;
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, kg = lane >> 4;
-  const int q0 = ld_uniform(p.cu, un.b), Lq = ld_uniform(p.cu, un.b + 1) - q0;
-  const int64_t tok0 = ld_uniform(p.cuk, un.b);
-  const int L = ld_uniform(p.cuk, un.b + 1) - (int)tok0;
+  const float cs = p.scale_log2 * (FORM == kCacheHead ? ld_uniform(p.k_head, h) : 1.f);
+  const int64_t rowb = (int64_t)p.hkv * kHeadDim * ESZ;
+  const uint8_t* K = p.k + (int64_t)h * kHeadDim * ESZ;
+  const uint32_t koff = (uint32_t)(c16 * rowb + 16 * kg);
+  // key of a tile that this lane writes
+  const int mine = 16 * (c16 >> 3) + 4 * kg + ((c16 >> 1) & 3);
+
+  int b = sh.b, base = sh.base;
+#pragma unroll 1
+  for (bool again = false;; again = true) {
+  if (again) {
+    sh.q0 = ld_uniform(p.cu, b);
+    sh.Lq = ld_uniform(p.cu, b + 1) - sh.q0;
+    sh.L = ld_uniform(p.cuk, b + 1) - ld_uniform(p.cuk, b);
+  }
+  const int q0 = sh.q0, Lq = sh.Lq, L = sh.L;
   const int first = L - Lq, last = L - 1, rows = Lq * p.g;
-  const Tiles tl = tiles_of(p, Lq, L, all);
-  const int lo = (int)((int64_t)tl.n * un.part / un.parts);
-  const int hi = (int)((int64_t)tl.n * (un.part + 1) / un.parts);
+  const Tiles tl = tiles_of(p, Lq, L);
+  const int lo = max(sh.lo, base) - base, hi = min(sh.hi, base + tl.n) - base;
   auto tile_at = [&](int i) { return i < tl.sinks ? i : tl.from + i - tl.sinks; };
+  const int64_t wrow = ((int64_t)b * p.hkv + h) * stride;
 
   bf16x8_t qb[NT][4];
   int pos[NT];
@@ -63,7 +94,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(CacheProblem p, const 
     const int r = 16 * nt + c16;
     pos[nt] = r < rows ? first + r / p.g : -1;        // a row past the last sees nothing
     ref[nt] = 0.f;
-    const int64_t qrow = (int64_t)(q0 + r / p.g) * p.hq + un.h * p.g + r % p.g;
+    const int64_t qrow = (int64_t)(q0 + r / p.g) * p.hq + h * p.g + r % p.g;
     if (r < rows) ref[nt] = lse[qrow] * kLog2e;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
@@ -73,26 +104,16 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(CacheProblem p, const 
       qb[nt][s] = __builtin_bit_cast(bf16x8_t, x);
     }
   }
-  const float cs = p.scale_log2 * (FORM == kCacheHead ? ld_uniform(p.k_head, un.h) : 1.f);
-  const int64_t rowb = (int64_t)p.hkv * kHeadDim * ESZ;
-  const uint8_t* K = p.k + (int64_t)un.h * kHeadDim * ESZ;
-  const uint32_t koff = (uint32_t)(c16 * rowb + 16 * kg);
-  const int64_t wrow = ((int64_t)un.b * p.hkv + un.h) * stride;
-  // key of a tile that this lane writes
-  const int mine = 16 * (c16 >> 3) + 4 * kg + ((c16 >> 1) & 3);
-
   struct Raw {
     uint4 k[2][KC];
     uint32_t ks[2];
     float old;
   };
-  auto seen = [&](int t0) { return t0 < p.sink || (t0 <= last && t0 + kTile - 1 > first - p.window); };
   auto load = [&](int tile, Raw& x) {
     const int t0 = kTile * tile;
     x.old = in && t0 + mine <= last ? in[wrow + t0 + mine] : 0.f;
-    if (Lq <= 0 || !seen(t0)) return;
     if constexpr (GROUPED) {
-      const int32_t* row = p.pm.table + (int64_t)un.b * p.pm.stride;
+      const int32_t* row = p.pm.table + (int64_t)b * p.pm.stride;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int t = u && t0 + 16 > last ? t0 : t0 + 16 * u;
@@ -101,12 +122,12 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(CacheProblem p, const 
         const uint8_t* kb = K + s * rowb;
 #pragma unroll
         for (int c = 0; c < KC; ++c) x.k[u][c] = *(const uint4*)(kb + (koff + 64u * c));
-        if constexpr (FORM == kCacheBlock) x.ks[u] = p.k_block[(s >> p.sb_shift) * p.hkv + un.h];
+        if constexpr (FORM == kCacheBlock) x.ks[u] = p.k_block[(s >> p.sb_shift) * p.hkv + h];
       }
     } else {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int64_t s = slot_of(p.pm, un.b, tok0, min(t0 + 16 * u + c16, last));
+        const int64_t s = slot_of(p.pm, b, 0, min(t0 + 16 * u + c16, last));
 #pragma unroll
         for (int c = 0; c < KC; ++c) x.k[u][c] = *(const uint4*)(K + s * rowb + 16 * kg + 64 * c);
       }
@@ -117,7 +138,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(CacheProblem p, const 
     float sum[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.f;
-    if (Lq > 0 && seen(t0)) {
+    {
       const bool masked = t0 + kTile - 1 > first || rows < 16 * NT ||
                           (t0 <= last - p.window && t0 + kTile > p.sink);
       bf16x8_t a[2][4];
@@ -149,8 +170,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(CacheProblem p, const 
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int key = t0 + 16 * (i >> 2) + 4 * kg + (i & 3);
-            const bool see = key <= pos[nt] && (key < p.sink || key > pos[nt] - p.window);
-            s[i >> 2][i & 3] = see ? s[i >> 2][i & 3] : -INFINITY;
+            s[i >> 2][i & 3] = sees(p, pos[nt], key) ? s[i >> 2][i & 3] : -INFINITY;
           }
         }
 #pragma unroll
@@ -183,6 +203,10 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(CacheProblem p, const 
       cur = n1;
       n1 = n2;
     }
+  }
+  base += tl.n;
+  if (p.splits || base >= sh.hi) break;
+  ++b;
   }
 }
 
@@ -225,7 +249,13 @@ __global__ __launch_bounds__(64 * kWaves, 3) void many_kernel(CacheProblem p,
   const int seg = (int)(at % segs), c0 = (int)(at / segs) * kChunk;
   const int64_t tok0 = ld_uniform(p.cuk, b);
   const int L = ld_uniform(p.cuk, b + 1) - (int)tok0;
-  if (c0 >= L) return;
+  if (c0 >= L) {                       // past the sequence, not in place
+    if (segs == 1 && in != out) {
+      const int64_t to = ((int64_t)b * p.hkv + h) * stride + c0 + threadIdx.x;
+      if (c0 + threadIdx.x < stride) out[to] = in ? in[to] : 0.f;
+    }
+    return;
+  }
   const int q0 = ld_uniform(p.cu, b), Lq = ld_uniform(p.cu, b + 1) - q0;
   const int P = L - Lq, rows = Lq * p.g;
   const Steps st = steps_of(p, c0, Lq, L);
@@ -319,8 +349,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void many_kernel(CacheProblem p,
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
           const int e = i & 15, key = k0 + 32 * (i >> 4) + 8 * (e >> 2) + 4 * half + (e & 3);
-          const bool see = key <= pos && (key < p.sink || key > pos - p.window);
-          s[i >> 4][e] = see ? s[i >> 4][e] : -INFINITY;
+          s[i >> 4][e] = sees(p, pos, key) ? s[i >> 4][e] : -INFINITY;
+          s[i >> 4][e] = pinned(s[i >> 4][e]);
         }
       }
 #pragma unroll
@@ -343,8 +373,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void many_kernel(CacheProblem p,
   const int64_t bh = (int64_t)b * p.hkv + h;
   if (segs > 1) {
     part[((int64_t)seg * p.batch * p.hkv + bh) * ((int64_t)chunks * kChunk) + key] = acc[0];
-  } else if (key < L) {
-    out[bh * stride + key] = (in ? in[bh * stride + key] : 0.f) + acc[0];
+  } else if (key < L || (in != out && key < stride)) {
+    out[bh * stride + key] = (in ? in[bh * stride + key] : 0.f) + (key < L ? acc[0] : 0.f);
   }
 }
 
@@ -356,11 +386,11 @@ __global__ __launch_bounds__(kChunk) void sum_kernel(CacheProblem p, const float
   const int b = bh / p.hkv;
   const int L = ld_uniform(p.cuk, b + 1) - ld_uniform(p.cuk, b);
   const int key = c0 + threadIdx.x;
-  if (key >= L) return;
+  if (key >= (in != out ? stride : (int64_t)L)) return;
   const Steps st = steps_of(p, c0, ld_uniform(p.cu, b + 1) - ld_uniform(p.cu, b), L);
   float sum = 0.f;
   for (int s = 0; s < segs; ++s)
-    if (max(st.from, s * seg_steps) < min(st.to, (s + 1) * seg_steps))
+    if (key < L && max(st.from, s * seg_steps) < min(st.to, (s + 1) * seg_steps))
       sum += part[((int64_t)s * p.batch * p.hkv + bh) * ((int64_t)chunks * kChunk) + key];
   const int64_t to = (int64_t)bh * stride + key;
   out[to] = (in ? in[to] : 0.f) + sum;
@@ -380,24 +410,22 @@ int segments(const CacheProblem& p, int* steps) {
 bool few_rows(const CacheProblem& p) { return (int64_t)p.max_new * p.g <= kFewRows; }
 
 template <int FORM>
-hipError_t launch_few(const CacheProblem& p, const float* lse, const float* in, float* out,
+hipError_t launch_few(const CacheProblem& problem, const float* lse, const float* in, float* out,
                       int64_t stride, hipStream_t s) {
-  // added in place, tiles that no query sees stay as they are; else all are written
-  const bool all = in != out;
-  const int64_t units = (int64_t)p.batch * p.hkv;
-  const int64_t mp = (p.max_kv / kTile + 1 + kMinTiles - 1) / kMinTiles;
-  const int64_t grid = p.splits ? units * p.splits : std::min(units * mp, units + kParts);
+  const CacheProblem p = dealt(problem);
+  const int shares = shares_of(p, kShares), rows = p.max_new * p.g;
+  const int nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  const int64_t grid = (int64_t)shares * p.hkv;
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
   const dim3 g((unsigned)grid), t(64 * kWaves);
-  const int nt = row_tiles(p);
   if (FORM == kCacheBlock || p.pm.page % 16 == 0) {
-    if (nt == 1) few_kernel<FORM, 1, true><<<g, t, 0, s>>>(p, lse, in, out, stride, all);
-    else if (nt == 2) few_kernel<FORM, 2, true><<<g, t, 0, s>>>(p, lse, in, out, stride, all);
-    else few_kernel<FORM, 4, true><<<g, t, 0, s>>>(p, lse, in, out, stride, all);
+    if (nt == 1) few_kernel<FORM, 1, true><<<g, t, 0, s>>>(p, lse, in, out, stride, shares);
+    else if (nt == 2) few_kernel<FORM, 2, true><<<g, t, 0, s>>>(p, lse, in, out, stride, shares);
+    else few_kernel<FORM, 4, true><<<g, t, 0, s>>>(p, lse, in, out, stride, shares);
   } else if constexpr (FORM != kCacheBlock) {
-    if (nt == 1) few_kernel<FORM, 1, false><<<g, t, 0, s>>>(p, lse, in, out, stride, all);
-    else if (nt == 2) few_kernel<FORM, 2, false><<<g, t, 0, s>>>(p, lse, in, out, stride, all);
-    else few_kernel<FORM, 4, false><<<g, t, 0, s>>>(p, lse, in, out, stride, all);
+    if (nt == 1) few_kernel<FORM, 1, false><<<g, t, 0, s>>>(p, lse, in, out, stride, shares);
+    else if (nt == 2) few_kernel<FORM, 2, false><<<g, t, 0, s>>>(p, lse, in, out, stride, shares);
+    else few_kernel<FORM, 4, false><<<g, t, 0, s>>>(p, lse, in, out, stride, shares);
   }
   return hipGetLastError();
 }
@@ -408,12 +436,16 @@ hipError_t launch(const CacheProblem& p, const float* lse, const float* in, floa
   if (few_rows(p)) return launch_few<FORM>(p, lse, in, out, stride, s);
   int steps;
   const int segs = segments(p, &steps), chunks = chunks_of(p);
-  const int64_t groups = (int64_t)p.batch * p.hkv * chunks;
-  if (groups * segs > 0x7fffffff) return hipErrorInvalidValue;
+  // not in place, the entries past the sequences are written too
+  const int64_t all = in != out ? (stride + kChunk - 1) / kChunk : chunks;
+  const int64_t groups = (int64_t)p.batch * p.hkv * (segs > 1 ? chunks : all);
+  if (all > 0x7fffffff / kChunk || groups * segs > 0x7fffffff || (int64_t)p.batch * p.hkv * all > 0x7fffffff)
+    return hipErrorInvalidValue;
   many_kernel<FORM><<<(unsigned)(groups * segs), 64 * kWaves, 0, s>>>(p, lse, in, out, stride, part, segs,
                                                                       steps, chunks);
   if (segs > 1)
-    sum_kernel<<<(unsigned)groups, kChunk, 0, s>>>(p, in, out, stride, part, segs, steps, chunks);
+    sum_kernel<<<(unsigned)(p.batch * p.hkv * all), kChunk, 0, s>>>(p, in, out, stride, part, segs, steps,
+                                                                    chunks);
   return hipGetLastError();
 }
 

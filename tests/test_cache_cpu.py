@@ -59,6 +59,7 @@ OPS = ["append", "attend", "weights", "evict"]
 @pytest.mark.parametrize("kw,status", [
     (dict(batch=-1), fp2.EINVAL),
     (dict(batch=65537), fp2.EUNSUPPORTED),
+    (dict(batch=65536, max_kv_len=1 << 20), fp2.EUNSUPPORTED),
     (dict(num_kv_heads=0), fp2.EINVAL),
     (dict(num_kv_heads=2048, num_q_heads=2048), fp2.EUNSUPPORTED),
     (dict(num_q_heads=30), fp2.EINVAL),
@@ -133,7 +134,7 @@ def test_attend_workspace():
 
 def test_workspace_bounds():
     """Nothing where no keys are cut; else bounded whatever the sizes."""
-    assert fp2.cache_workspace_bytes(base(max_kv_len=400)) == 0
+    assert fp2.cache_workspace_bytes(base(max_kv_len=400)) == 0      # short sequences are taken whole
     assert fp2.cache_workspace_bytes(base(kv_splits=1)) == 0
     assert fp2.cache_workspace_bytes(base(max_seq_len=2000, max_kv_len=8000, batch=64)) == 0
     for kw in (dict(batch=65536), dict(max_seq_len=8), dict(max_seq_len=17, max_kv_len=1 << 20),

@@ -77,13 +77,17 @@ def run_attend(c, hq, new, window=0, sink=0, splits=0, seed=1, scale=0.0, pad=3,
     w = dev(before).clone()
     fp2.cache_weights(p, dev(q), lse, cache, *args, weights=w, weights_in=w)
     fresh = fp2.cache_weights(p, dev(q), lse, cache, *args, weights=torch.full_like(w, -1.0))
+    moved = fp2.cache_weights(p, dev(q), lse, cache, *args, weights_in=dev(before))
     _, _, _, _, want = ref.attend(c, q[:n], new, window, sink, scale or None,
                                   lse[:n].double().cpu().numpy())
     for b, L in enumerate(c.lens):
         close(fresh[b, :, :L], want[b][0], want[b][1] + 1e-30, "weights of %d" % b)
         both = want[b][0] + before[b, :, :L].double().numpy()
+        other = moved[b].cpu()
+        assert torch.equal(other[:, L:], before[b, :, L:])
+        close(other[:, :L], both, want[b][1] + 2 * ref.U32 * both, "weights of %d added elsewhere" % b)
         close(w[b, :, :L], both, want[b][1] + 2 * ref.U32 * both, "added weights of %d" % b)
-        assert bool((fresh[b, :, L:] == -1).all()) and torch.equal(w[b, :, L:].cpu(), before[b, :, L:])
+        assert not bool(fresh[b, :, L:].any()) and torch.equal(w[b, :, L:].cpu(), before[b, :, L:])
     return out, lse
 
 
