@@ -475,7 +475,7 @@ typedef struct {
 
 /* Bytes of workspace (256-byte aligned) that fp2_cache_attend and
  * fp2_cache_weights need for `params`: the partial results of sequences whose
- * keys (or queries) are cut into parts, at most 70 MB where kv_splits is 0. 0
+ * keys (or queries) are cut into parts, at most 140 MB where kv_splits is 0. 0
  * where none is needed, and for an invalid params. One workspace serves calls
  * in order on a stream; calls that overlap, and graphs that may, need their
  * own. */

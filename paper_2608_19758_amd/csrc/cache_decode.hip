@@ -9,10 +9,11 @@
 //
 // * Work: the visible keys of a sequence come in tiles of 32. All tiles of the
 //   call are dealt to the workgroups in equal shares (each works its own out
-//   from the lengths, which are on the device only); the four waves of a
-//   workgroup alternate tiles and join in LDS, and combine_kernel joins
-//   sequences that lie in several shares. More than 32 rows are halved between
-//   the waves, which then read the same keys (the second time from cache).
+//   from the lengths, which are on the device only); combine_kernel joins
+//   sequences that lie in several shares. The waves of a workgroup take
+//   different heads of the same tokens; where there are fewer heads they
+//   alternate tiles and join in LDS, and many rows are halved between waves,
+//   which then read the same keys (all but one from cache).
 // * A wave goes from global memory to the matrix cores without LDS.
 //   S^T = K Q^T on v_mfma_f32_16x16x32_bf16: A holds 16 keys, and which of the
 //   128 dimensions stands at which place of a product is free, so four lanes
@@ -37,7 +38,6 @@ namespace {
 
 constexpr float kLn2f = 0.69314718055994530942f;
 constexpr int kWaves = kFewWaves;
-constexpr int kShares = 256;     // workgroups that a call is dealt to: one a compute unit
 constexpr float kTau = 8.0f;
 constexpr float kNoRef = -1e30f; // maximum of a row that saw no key
 
@@ -87,23 +87,24 @@ __device__ __forceinline__ uint32_t odd_value(uint2 v, int e) {
 // is uniform (scalar); otherwise every key has its own. ONE: one new token a
 // sequence, so that every row sees the same keys.
 template <int FORM, int NT, int RS, bool GROUPED, bool ONE>
-__global__ __launch_bounds__(64 * kWaves, FORM == kCacheBf16 && NT > 1 ? 1 : 2) void decode_kernel(CacheProblem p, CachePartials part,
+__global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(CacheProblem p, CachePartials part,
                                                                 int shares, uint16_t* __restrict__ out,
                                                                 float* __restrict__ lse) {
   constexpr bool kBf16 = FORM == kCacheBf16;
   constexpr int ESZ = kBf16 ? 2 : 1;
   constexpr int KC = kBf16 ? 4 : 2;            // 16-byte chunks of a key per lane
   constexpr int LDR = kHeadDim + 4;            // LDS row, padded against bank conflicts
-  constexpr int KS = kWaves / RS;              // waves that alternate tiles
   __shared__ float s_o[kWaves][16][LDR];
   __shared__ float s_ml[kWaves][16][2];
-  const int h = blockIdx.x % p.hkv, index = blockIdx.x / p.hkv;
+  const WaveSplit ws = wave_split(p, RS);
+  const int groups = p.hkv / ws.heads, index = blockIdx.x / groups, KS = ws.keys;
   Share sh;
   if (!find_share<false>(p, shares, index, sh)) return;
 
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int ks = w / RS, rs = w % RS;          // this wave's place among tiles and rows
+  const int h = blockIdx.x % groups * ws.heads + w % ws.heads;
+  const int rs = w / ws.heads % RS, ks = w / (ws.heads * RS);   // place among rows and tiles
   const int c16 = lane & 15, kg = lane >> 4;
   float cs = p.scale_log2, vsc = 1.f;
   if constexpr (FORM == kCacheHead) {
@@ -186,19 +187,25 @@ __global__ __launch_bounds__(64 * kWaves, FORM == kCacheBf16 && NT > 1 ? 1 : 2) 
   typedef std::conditional_t<kBf16, uint4, uint2> vrow_t;
   auto load = [&](const Where& a, Raw<FORM>& x) {
     if constexpr (GROUPED) {
+      if constexpr (FORM == kCacheBlock) {   // before the rows: loads come back in order
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int64_t at = (a.s[u] >> p.sb_shift) * p.hkv + h;
+          x.ks[u] = p.k_block[at];
+          x.vs[u] = p.v_block[at];
+        }
+      }
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const uint8_t* kb = K + a.s[u] * rowb;
 #pragma unroll
         for (int c = 0; c < KC; ++c) x.k[u][c] = *(const uint4*)(kb + (koff + 64u * c));
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
         const uint8_t* vb = V + a.s[u] * rowb;
 #pragma unroll
         for (int e = 0; e < 4; ++e) x.v[4 * u + e] = *(const vrow_t*)(vb + e * rowb + voff);
-        if constexpr (FORM == kCacheBlock) {
-          const int64_t at = (a.s[u] >> p.sb_shift) * p.hkv + h;
-          x.ks[u] = p.k_block[at];
-          x.vs[u] = p.v_block[at];
-        }
       }
     } else {
       const int slot = (int)a.s[0];
@@ -360,29 +367,60 @@ __global__ __launch_bounds__(64 * kWaves, FORM == kCacheBf16 && NT > 1 ? 1 : 2) 
     }
   };
 
-  // the next tile's rows are on their way while a tile is computed
+  // The next tile's rows are on their way while a tile is computed. Loads are
+  // never left out (past the end they repeat the last tile): behind a load that
+  // may not have been issued the compiler can only wait for all of them.
   if (lo + ks < hi) {
-    Raw<FORM> cur, nxt;
-    load(where(tile_at(lo + ks)), cur);
-    Where ahead = where(tile_at(min(lo + ks + KS, hi - 1)));
+    Raw<FORM> r0, r1;
+    const int end = hi - 1;
+    load(where(tile_at(lo + ks)), r0);
+    Where a0 = where(tile_at(min(lo + ks + KS, end))), a1;
 #pragma unroll 1
-    for (int i = lo + ks; i < hi; i += KS) {
-      if (i + KS < hi) load(ahead, nxt);
-      ahead = where(tile_at(min(i + 2 * KS, hi - 1)));
-      step(tile_at(i), cur);
-      cur = nxt;
+    for (int i = lo + ks; i < hi; i += 2 * KS) {
+      load(a0, r1);
+      a1 = where(tile_at(min(i + 2 * KS, end)));
+      step(tile_at(i), r0);
+      load(a1, r0);
+      a0 = where(tile_at(min(i + 3 * KS, end)));
+      if (i + KS < hi) step(tile_at(i + KS), r1);
     }
   }
 
-  // the waves' parts of the rows, joined 16 rows a wave at a time. A sequence
-  // in several shares leaves its part in slot 2 * share, if it started in an
-  // earlier one, or 2 * share + 1 (kv_splits: the share's own).
+  // A sequence in several shares leaves its part in slot 2 * share, if it
+  // started in an earlier one, or 2 * share + 1 (kv_splits: the share's own).
   const bool split = p.splits ? hi - lo < tl.n : base < sh.lo || base + tl.n > sh.hi;
-  const int64_t slot = (p.splits ? (int64_t)index : 2 * (int64_t)index + (base >= sh.lo)) * p.hkv + h;
+  const int64_t slot = (p.splits ? (int64_t)index : 2 * (int64_t)index + (base >= sh.lo)) * p.hkv;
+  // eight values of packed row pr of head hh, from dimension d on
+  auto put = [&](int hh, int pr, int d, float mm, float ll, float4 x, float4 y) {
+    if (split) {
+      const int64_t at = (slot + hh) * (16 * NT * RS) + pr;
+      *(float4*)(part.o + at * kHeadDim + d) = x;
+      *(float4*)(part.o + at * kHeadDim + d + 4) = y;
+      if (d == 0) *(float2*)(part.ml + 2 * at) = make_float2(mm, ll);
+    } else {
+      const float inv = vsc / ll;
+      const int64_t at = (int64_t)(q0 + (ONE ? 0 : pr / p.g)) * p.hq + hh * p.g + (ONE ? pr : pr % p.g);
+      *(uint4*)(out + at * kHeadDim + d) =
+          make_uint4(pack_bf16x2(x.x * inv, x.y * inv), pack_bf16x2(x.z * inv, x.w * inv),
+                     pack_bf16x2(y.x * inv, y.y * inv), pack_bf16x2(y.z * inv, y.w * inv));
+      if (lse && d == 0) lse[at] = (mm + fast_log2(ll)) * kLn2f;
+    }
+  };
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     l[nt] += __shfl_xor(l[nt], 16, 64);
     l[nt] += __shfl_xor(l[nt], 32, 64);
+    const int pr = 16 * (NT * rs + nt) + c16;
+    if (KS == 1) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (pr < rows)
+          put(h, pr, 32 * kg + 8 * i, m[nt], l[nt],
+              make_float4(o[nt][0][i], o[nt][1][i], o[nt][2][i], o[nt][3][i]),
+              make_float4(o[nt][4][i], o[nt][5][i], o[nt][6][i], o[nt][7][i]));
+      continue;
+    }
+    // the waves of a head and its rows, joined 16 rows a wave at a time
     if (nt || again) __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -395,32 +433,24 @@ __global__ __launch_bounds__(64 * kWaves, FORM == kCacheBf16 && NT > 1 ? 1 : 2) 
       s_ml[w][c16][1] = l[nt];
     }
     __syncthreads();
-    for (int x = threadIdx.x; x < RS * 16 * 32; x += 64 * kWaves) {
-      const int r = (x >> 5) & 15, d = 4 * (x & 31), rh = x >> 9, pr = 16 * (NT * rh + nt) + r;
-      if (pr >= rows) continue;
-      float mm = s_ml[rh][r][0];
-#pragma unroll
-      for (int v = 1; v < KS; ++v) mm = fmaxf(mm, s_ml[v * RS + rh][r][0]);
+    // wave w joins some of the rows of its own head and rows: ks-th of KS shares of the 16 x 16 pieces
+    const int w0 = w % (ws.heads * RS), stepw = ws.heads * RS;
+    for (int x = 64 * ks + lane; x < 16 * 16; x += 64 * KS) {
+      const int r = x >> 4, d = 8 * (x & 15), jr = 16 * (NT * rs + nt) + r;
+      if (jr >= rows) continue;
+      float mm = kNoRef;
+      for (int v = 0; v < KS; ++v) mm = fmaxf(mm, s_ml[w0 + v * stepw][r][0]);
       float ll = 0.f;
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f), c = a;
       for (int v = 0; v < KS; ++v) {
-        const float f = fast_exp2(s_ml[v * RS + rh][r][0] - mm);
-        const float4 y = *(const float4*)&s_o[v * RS + rh][r][d];
-        ll += f * s_ml[v * RS + rh][r][1];
+        const float* src = &s_o[w0 + v * stepw][r][d];
+        const float f = fast_exp2(s_ml[w0 + v * stepw][r][0] - mm);
+        const float4 y = *(const float4*)src, z = *(const float4*)(src + 4);
+        ll += f * s_ml[w0 + v * stepw][r][1];
         a.x += f * y.x, a.y += f * y.y, a.z += f * y.z, a.w += f * y.w;
+        c.x += f * z.x, c.y += f * z.y, c.z += f * z.z, c.w += f * z.w;
       }
-      if (split) {
-        const int64_t at = slot * (16 * NT * RS) + pr;
-        *(float4*)(part.o + at * kHeadDim + d) = a;
-        if (d == 0) *(float2*)(part.ml + 2 * at) = make_float2(mm, ll);
-      } else {
-        const float inv = vsc / ll;
-        const int64_t at = (int64_t)(q0 + pr / p.g) * p.hq + h * p.g + pr % p.g;
-        *(uint2*)(out + at * kHeadDim + d) =
-            make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
-        if (lse && d == 0) lse[at] = (mm + fast_log2(ll)) * kLn2f;
-      }
+      put(h, jr, d, mm, ll, a, c);
     }
   }
   }
@@ -504,11 +534,24 @@ int rows_cap(const CacheProblem& p) {
   return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
 }
 
+// How the rows are held: 16-row tiles of a wave and waves that share the rows
+// of a tile of keys. A bf16 tile of keys takes twice the registers of one of
+// codes, so its waves hold 16 rows.
+struct Rows {
+  int tiles, waves;
+};
+Rows rows_for(const CacheProblem& p) {
+  const int n = rows_cap(p) / 16;
+  return p.form == kCacheBf16 || n == 1 ? Rows{1, n} : Rows{2, n / 2};
+}
+
 template <int FORM, int NT, int RS, bool GROUPED, bool ONE>
-hipError_t launch(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse,
+hipError_t launch(const CacheProblem& problem, const CachePartials& part, uint16_t* out, float* lse,
                   hipStream_t s) {
-  const int shares = shares_of(p, kShares), max_rows = p.max_new * p.g;
-  const int64_t grid = (int64_t)shares * p.hkv, joins = (int64_t)p.batch * p.hkv * max_rows;
+  const CacheProblem p = dealt(problem, RS);
+  const int shares = shares_of(p, RS), max_rows = p.max_new * p.g;
+  const int64_t grid = (int64_t)shares * (p.hkv / wave_split(p, RS).heads);
+  const int64_t joins = (int64_t)p.batch * p.hkv * max_rows;
   if (grid > 0x7fffffff || joins > 0x7fffffff) return hipErrorInvalidValue;
   decode_kernel<FORM, NT, RS, GROUPED, ONE>
       <<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, part, shares, out, lse);
@@ -520,11 +563,16 @@ hipError_t launch(const CacheProblem& p, const CachePartials& part, uint16_t* ou
 template <int FORM, bool GROUPED>
 hipError_t launch_rows(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse,
                        hipStream_t s) {
-  const int rows = rows_cap(p);
-  return p.max_new == 1 ? launch<FORM, 1, 1, GROUPED, true>(p, part, out, lse, s)
-         : rows == 16   ? launch<FORM, 1, 1, GROUPED, false>(p, part, out, lse, s)
-         : rows == 32   ? launch<FORM, 2, 1, GROUPED, false>(p, part, out, lse, s)
-                        : launch<FORM, 2, 2, GROUPED, false>(p, part, out, lse, s);
+  if (p.max_new == 1) return launch<FORM, 1, 1, GROUPED, true>(p, part, out, lse, s);
+  const int waves = rows_for(p).waves;
+  if constexpr (FORM == kCacheBf16)
+    return waves == 1   ? launch<FORM, 1, 1, GROUPED, false>(p, part, out, lse, s)
+           : waves == 2 ? launch<FORM, 1, 2, GROUPED, false>(p, part, out, lse, s)
+                        : launch<FORM, 1, 4, GROUPED, false>(p, part, out, lse, s);
+  else
+    return rows_for(p).tiles == 1 ? launch<FORM, 1, 1, GROUPED, false>(p, part, out, lse, s)
+           : waves == 1           ? launch<FORM, 2, 1, GROUPED, false>(p, part, out, lse, s)
+                                  : launch<FORM, 2, 2, GROUPED, false>(p, part, out, lse, s);
 }
 
 template <int FORM>
@@ -539,14 +587,14 @@ hipError_t launch_pages(const CacheProblem& p, const CachePartials& part, uint16
 }  // namespace
 
 void cache_decode_partials(const CacheProblem& problem, int64_t* slots, int* rows) {
-  const CacheProblem p = dealt(problem);
-  *slots = p.splits == 1 ? 0 : (int64_t)shares_of(p, kShares) * (p.splits ? 1 : 2) * p.hkv;
+  const int waves = rows_for(problem).waves;
+  const CacheProblem p = dealt(problem, waves);
+  *slots = p.splits == 1 ? 0 : (int64_t)shares_of(p, waves) * (p.splits ? 1 : 2) * p.hkv;
   *rows = rows_cap(p);
 }
 
-hipError_t launch_cache_decode(const CacheProblem& problem, const CachePartials& part, uint16_t* out,
+hipError_t launch_cache_decode(const CacheProblem& p, const CachePartials& part, uint16_t* out,
                                float* lse, hipStream_t s) {
-  const CacheProblem p = dealt(problem);
   return p.form == kCacheBf16   ? launch_pages<kCacheBf16>(p, part, out, lse, s)
          : p.form == kCacheHead ? launch_pages<kCacheHead>(p, part, out, lse, s)
                                 : launch_pages<kCacheBlock>(p, part, out, lse, s);

@@ -8,9 +8,9 @@ namespace fp2 {
 namespace {
 
 constexpr int kTile = 32;        // keys per wave and step
-constexpr int kFewWaves = 4;
-constexpr int kMinTiles = 4;     // tiles of a share, at least: one a wave
-constexpr int kWholeTiles = 16;  // sequences of at most as many are not cut
+constexpr int kFewWaves = 8;     // waves of a workgroup
+constexpr int kFewGroups = 256;  // workgroups that a call is dealt to: one a compute unit
+constexpr int kWholeTiles = 16;  // sequences of at most as many are not cut, if there are many
 
 // Tiles of a sequence that some row sees: `sinks` leading ones, then those
 // from `from` on.
@@ -41,8 +41,23 @@ __device__ __forceinline__ T pinned(T x) {
   return x;
 }
 
+// The heads of a token lie side by side in the pool, so the waves of a
+// workgroup take different heads of the same tokens where they can: memory is
+// then read in runs of heads x 128 codes (reading a pool of 8 heads this way
+// reaches 6.2 TB/s, with the heads in different workgroups 5.5). `heads` of a
+// workgroup's waves are heads, `rows` halves or quarters of the query rows, and
+// the others (`keys`) alternate tiles of the same head.
+struct WaveSplit {
+  int heads, rows, keys;
+};
+inline __host__ __device__ WaveSplit wave_split(const CacheProblem& p, int rows) {
+  int heads = kFewWaves / rows;
+  while (p.hkv % heads) heads >>= 1;
+  return WaveSplit{heads, rows, kFewWaves / rows / heads};
+}
+
 // The tiles of a call, one sequence after the other, form a line, which is cut
-// into equal shares; a workgroup takes one share of one head, so that all have
+// into equal shares; a workgroup takes one share of its heads, so that all have
 // the same work whatever the lengths. A share may hold the end of one
 // sequence, whole ones, and the start of another. With kv_splits n >= 1 every
 // sequence is cut into at most n shares of its own instead.
@@ -54,17 +69,20 @@ struct Share {
   int q0, Lq, L;    // the sequence's first query and its lengths
 };
 
-// Sequences of at most kWholeTiles tiles, by the bounds of the call, are taken
-// whole: there is nothing to even out, and nothing to join.
-inline CacheProblem dealt(CacheProblem p) {
+// Short sequences, by the bounds of the call, are taken whole if they are
+// enough to fill the chip: there is nothing to even out, and nothing to join.
+inline CacheProblem dealt(CacheProblem p, int rows) {
   const int64_t a = p.max_kv, b = (int64_t)p.window + p.max_new + p.sink;
-  if (p.splits == 0 && (a < b ? a : b) / kTile + 3 <= kWholeTiles) p.splits = 1;
+  if (p.splits == 0 && (a < b ? a : b) / kTile + 3 <= kWholeTiles &&
+      (int64_t)p.batch * (p.hkv / wave_split(p, rows).heads) >= kFewGroups)
+    p.splits = 1;
   return p;
 }
 
-// Shares of the line for `wgs` workgroups.
-inline __host__ __device__ int shares_of(const CacheProblem& p, int wgs) {
-  return p.splits ? p.batch * p.splits : (wgs + p.hkv - 1) / p.hkv;
+// Shares of the line.
+inline __host__ __device__ int shares_of(const CacheProblem& p, int rows) {
+  const int groups = p.hkv / wave_split(p, rows).heads;
+  return p.splits ? p.batch * p.splits : (kFewGroups + groups - 1) / groups;
 }
 
 __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
@@ -116,7 +134,7 @@ __device__ __forceinline__ bool find_share(const CacheProblem& p, int shares, in
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
     total += __builtin_amdgcn_readfirstlane(s);
   }
-  out.len = max((int)(((int64_t)total + shares - 1) / shares), kMinTiles);
+  out.len = max((int)(((int64_t)total + shares - 1) / shares), 1);
   out.lo = (int)min((int64_t)index * out.len, (int64_t)total);
   out.hi = (int)min((int64_t)out.lo + out.len, (int64_t)total);
   if (!BY_SEQ && out.lo >= out.hi) return false;

@@ -26,43 +26,42 @@ namespace fp2 {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr int kWaves = kFewWaves;
-constexpr int kShares = 1024;             // workgroups that a call of few rows is dealt to
+constexpr int kWaves = 4;                 // of a workgroup (many rows)
 constexpr int kCopy = 4096;               // entries of a workgroup's turn in the copy
 constexpr int kKeys = 64;                 // of a wave (many rows)
 constexpr int kChunk = kWaves * kKeys;
 constexpr int kRows = 32;                 // packed query rows of a step
-constexpr int kFill = 2048;               // workgroups that fill the chip evenly
-constexpr int kMaxSegs = 16;
+constexpr int kFill = 8192;               // workgroups that fill the chip evenly
+constexpr int kMaxSegs = 64;
 constexpr int kMinSteps = 8;              // steps of a segment, at least
 
 template <int FORM, int NT, bool GROUPED>
-__global__ __launch_bounds__(64 * kWaves) void few_kernel(CacheProblem p, const float* __restrict__ lse,
+__global__ __launch_bounds__(64 * kFewWaves) void few_kernel(CacheProblem p, const float* __restrict__ lse,
                                                           const float* in, float* out, int64_t stride,
                                                           int shares) {
   constexpr bool kBf16 = FORM == kCacheBf16;
   constexpr int ESZ = kBf16 ? 2 : 1;
   constexpr int KC = kBf16 ? 4 : 2;            // 16-byte chunks of a key per lane
-  const int h = blockIdx.x % p.hkv, index = blockIdx.x / p.hkv;
-  // not in place: what no query sees, and what lies past the sequences
-  if (in != out) {
-    const int per = (int)((stride + kCopy - 1) / kCopy);
-    for (int64_t i = blockIdx.x; i < (int64_t)p.batch * p.hkv * per; i += gridDim.x) {
-      const int64_t row = i / per, from = i % per * kCopy;
-      const int sb = (int)(row / p.hkv);
-      const int Ls = ld_uniform(p.cuk, sb + 1) - ld_uniform(p.cuk, sb);
-      const Tiles t = tiles_of(p, ld_uniform(p.cu, sb + 1) - ld_uniform(p.cu, sb), Ls);
-      // tiles sinks .. until - 1 are unseen, and the entries from Ls on
-      const int until = t.n ? t.from : (Ls + kTile - 1) / kTile;
-      for (int64_t j = from + threadIdx.x; j < min(from + kCopy, stride); j += 64 * kWaves)
-        if (j >= Ls || (j / kTile >= t.sinks && j / kTile < until))
-          out[row * stride + j] = in ? in[row * stride + j] : 0.f;
-    }
+  const WaveSplit ws = wave_split(p, 1);
+  const int groups = p.hkv / ws.heads, index = blockIdx.x / groups, KS = ws.keys;
+  if (index >= shares) {   // not in place: what no query sees, and what lies past the sequences
+    const int64_t turn = blockIdx.x - (int64_t)shares * groups, per = (stride + kCopy - 1) / kCopy;
+    const int64_t row = turn / per, from = turn % per * kCopy;
+    const int sb = (int)(row / p.hkv);
+    const int Ls = ld_uniform(p.cuk, sb + 1) - ld_uniform(p.cuk, sb);
+    const Tiles t = tiles_of(p, ld_uniform(p.cu, sb + 1) - ld_uniform(p.cu, sb), Ls);
+    // tiles sinks .. until - 1 are unseen, and the entries from Ls on
+    const int until = t.n ? t.from : (Ls + kTile - 1) / kTile;
+    for (int64_t j = from + threadIdx.x; j < min(from + kCopy, stride); j += 64 * kFewWaves)
+      if (j >= Ls || (j / kTile >= t.sinks && j / kTile < until))
+        out[row * stride + j] = in ? in[row * stride + j] : 0.f;
+    return;
   }
   Share sh;
   if (!find_share<false>(p, shares, index, sh)) return;
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = blockIdx.x % groups * ws.heads + w % ws.heads, ks = w / ws.heads;
   const int c16 = lane & 15, kg = lane >> 4;
   const float cs = p.scale_log2 * (FORM == kCacheHead ? ld_uniform(p.k_head, h) : 1.f);
   const int64_t rowb = (int64_t)p.hkv * kHeadDim * ESZ;
@@ -85,6 +84,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(CacheProblem p, const 
   const int lo = max(sh.lo, base) - base, hi = min(sh.hi, base + tl.n) - base;
   auto tile_at = [&](int i) { return i < tl.sinks ? i : tl.from + i - tl.sinks; };
   const int64_t wrow = ((int64_t)b * p.hkv + h) * stride;
+  const float* old_row = (in ? in : out) + wrow;   // loaded in any case, used where there is one
 
   bf16x8_t qb[NT][4];
   int pos[NT];
@@ -111,18 +111,26 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(CacheProblem p, const 
   };
   auto load = [&](int tile, Raw& x) {
     const int t0 = kTile * tile;
-    x.old = in && t0 + mine <= last ? in[wrow + t0 + mine] : 0.f;
+    x.old = old_row[min(t0 + mine, last)];
     if constexpr (GROUPED) {
       const int32_t* row = p.pm.table + (int64_t)b * p.pm.stride;
+      int64_t s[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int t = u && t0 + 16 > last ? t0 : t0 + 16 * u;
         const int pg = p.pm.shift >= 0 ? t >> p.pm.shift : t / p.pm.page;
-        const int64_t s = (int64_t)ld_uniform(row, pg) * p.pm.page + (t - pg * p.pm.page);
-        const uint8_t* kb = K + s * rowb;
+        s[u] = (int64_t)ld_uniform(row, pg) * p.pm.page + (t - pg * p.pm.page);
+      }
+      // the scales first: loads come back in order
+      if constexpr (FORM == kCacheBlock) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) x.ks[u] = p.k_block[(s[u] >> p.sb_shift) * p.hkv + h];
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint8_t* kb = K + s[u] * rowb;
 #pragma unroll
         for (int c = 0; c < KC; ++c) x.k[u][c] = *(const uint4*)(kb + (koff + 64u * c));
-        if constexpr (FORM == kCacheBlock) x.ks[u] = p.k_block[(s >> p.sb_shift) * p.hkv + h];
       }
     } else {
 #pragma unroll
@@ -188,20 +196,22 @@ __global__ __launch_bounds__(64 * kWaves) void few_kernel(CacheProblem p, const 
       }
     }
     sum[0] += __shfl_xor(sum[0], 1, 64);
-    if (!(c16 & 1) && t0 + mine <= last) out[wrow + t0 + mine] = x.old + sum[0];
+    if (!(c16 & 1) && t0 + mine <= last) out[wrow + t0 + mine] = (in ? x.old : 0.f) + sum[0];
   };
 
-  // two tiles ahead: few registers a tile, so loads in flight come cheap
-  if (lo + w < hi) {
-    Raw cur, n1, n2;
-    load(tile_at(lo + w), cur);
-    if (lo + w + kWaves < hi) load(tile_at(lo + w + kWaves), n1);
+  // a tile ahead, with loads never left out (past the end they repeat the last
+  // tile): behind a load that may not have been issued the compiler can only
+  // wait for all of them
+  if (lo + ks < hi) {
+    Raw r0, r1;
+    const int end = hi - 1;
+    load(tile_at(lo + ks), r0);
 #pragma unroll 1
-    for (int i = lo + w; i < hi; i += kWaves) {
-      if (i + 2 * kWaves < hi) load(tile_at(i + 2 * kWaves), n2);
-      step(tile_at(i), cur);
-      cur = n1;
-      n1 = n2;
+    for (int i = lo + ks; i < hi; i += 2 * KS) {
+      load(tile_at(min(i + KS, end)), r1);
+      step(tile_at(i), r0);
+      load(tile_at(min(i + 2 * KS, end)), r0);
+      if (i + KS < hi) step(tile_at(i + KS), r1);
     }
   }
   base += tl.n;
@@ -412,12 +422,13 @@ bool few_rows(const CacheProblem& p) { return (int64_t)p.max_new * p.g <= kFewRo
 template <int FORM>
 hipError_t launch_few(const CacheProblem& problem, const float* lse, const float* in, float* out,
                       int64_t stride, hipStream_t s) {
-  const CacheProblem p = dealt(problem);
-  const int shares = shares_of(p, kShares), rows = p.max_new * p.g;
+  const CacheProblem p = dealt(problem, 1);
+  const int shares = shares_of(p, 1), rows = p.max_new * p.g;
   const int nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  const int64_t grid = (int64_t)shares * p.hkv;
+  const int64_t copies = in != out ? (int64_t)p.batch * p.hkv * ((stride + kCopy - 1) / kCopy) : 0;
+  const int64_t grid = (int64_t)shares * (p.hkv / wave_split(p, 1).heads) + copies;
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 g((unsigned)grid), t(64 * kWaves);
+  const dim3 g((unsigned)grid), t(64 * kFewWaves);
   if (FORM == kCacheBlock || p.pm.page % 16 == 0) {
     if (nt == 1) few_kernel<FORM, 1, true><<<g, t, 0, s>>>(p, lse, in, out, stride, shares);
     else if (nt == 2) few_kernel<FORM, 2, true><<<g, t, 0, s>>>(p, lse, in, out, stride, shares);
