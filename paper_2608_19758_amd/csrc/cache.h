@@ -32,6 +32,7 @@ struct CacheProblem {
   int32_t max_new, max_kv;  // bounds of the lengths
   int32_t splits;           // 0: by the work of the call, n: n parts
   float scale_log2;         // softmax scale * log2(e)
+  int32_t heads;            // few rows: heads that the waves of a workgroup take side by side
 };
 
 constexpr int kNoWindow = 1 << 30;
@@ -75,6 +76,28 @@ __device__ __forceinline__ void e4m3x4_to_f32(uint32_t w, float (&x)[4]) {
   const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
   const f32x2_t hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
   x[0] = lo[0]; x[1] = lo[1]; x[2] = hi[0]; x[3] = hi[1];
+}
+
+// Inclusive sum over the lanes of a wave, by the vector ALU's lane shifts (six
+// exchanges through LDS take some six times as long).
+__device__ __forceinline__ int wave_scan(int v) {
+#define FP2_STEP(ctrl, rows) v += __builtin_amdgcn_update_dpp(0, v, ctrl, rows, 0xf, false)
+  FP2_STEP(0x111, 0xf);   // row_shr 1, 2, 4, 8: within 16 lanes
+  FP2_STEP(0x112, 0xf);
+  FP2_STEP(0x114, 0xf);
+  FP2_STEP(0x118, 0xf);
+  FP2_STEP(0x142, 0xa);   // row_bcast 15: the second and fourth row take the row before
+  FP2_STEP(0x143, 0xc);   // row_bcast 31: the upper half takes the lower one
+#undef FP2_STEP
+  return v;
+}
+
+// Keeps the compiler from computing many masks (a pair of scalar registers
+// each) before it uses the first: x is needed here.
+template <class T>
+__device__ __forceinline__ T pinned(T x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
 
 // Partial outputs of sequences whose keys are cut into parts.

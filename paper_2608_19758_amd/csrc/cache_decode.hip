@@ -12,8 +12,7 @@
 //   from the lengths, which are on the device only); combine_kernel joins
 //   sequences that lie in several shares. The waves of a workgroup take
 //   different heads of the same tokens; where there are fewer heads they
-//   alternate tiles and join in LDS, and many rows are halved between waves,
-//   which then read the same keys (all but one from cache).
+//   alternate tiles and join in LDS.
 // * A wave goes from global memory to the matrix cores without LDS.
 //   S^T = K Q^T on v_mfma_f32_16x16x32_bf16: A holds 16 keys, and which of the
 //   128 dimensions stands at which place of a product is free, so four lanes
@@ -37,7 +36,6 @@ namespace fp2 {
 namespace {
 
 constexpr float kLn2f = 0.69314718055994530942f;
-constexpr int kWaves = kFewWaves;
 constexpr float kTau = 8.0f;
 constexpr float kNoRef = -1e30f; // maximum of a row that saw no key
 
@@ -81,30 +79,29 @@ __device__ __forceinline__ uint32_t odd_value(uint2 v, int e) {
   return ((odd_codes(e < 4 ? v.x : v.y) >> (8 * (e & 3) + 7)) & 1) * 0x7fc00000u;
 }
 
-// FORM: the cache's type. NT: 16-row tiles of query rows of a wave. RS: waves
-// that share the rows of a tile of keys. GROUPED: pages hold a multiple of 16
+// FORM: the cache's type. NT: 16-row tiles of query rows. W: waves (many
+// registers a wave: four, one a SIMD). GROUPED: pages hold a multiple of 16
 // tokens, so the 16 keys of a group lie one after the other and their address
 // is uniform (scalar); otherwise every key has its own. ONE: one new token a
 // sequence, so that every row sees the same keys.
-template <int FORM, int NT, int RS, bool GROUPED, bool ONE>
-__global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(CacheProblem p, CachePartials part,
-                                                                int shares, uint16_t* __restrict__ out,
-                                                                float* __restrict__ lse) {
+template <int FORM, int NT, int W, bool GROUPED, bool ONE>
+__global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, CachePartials part,
+                                                               int shares, uint16_t* __restrict__ out,
+                                                               float* __restrict__ lse) {
   constexpr bool kBf16 = FORM == kCacheBf16;
   constexpr int ESZ = kBf16 ? 2 : 1;
   constexpr int KC = kBf16 ? 4 : 2;            // 16-byte chunks of a key per lane
   constexpr int LDR = kHeadDim + 4;            // LDS row, padded against bank conflicts
-  __shared__ float s_o[kWaves][16][LDR];
-  __shared__ float s_ml[kWaves][16][2];
-  const WaveSplit ws = wave_split(p, RS);
-  const int groups = p.hkv / ws.heads, index = blockIdx.x / groups, KS = ws.keys;
+  __shared__ float s_o[W][16][LDR];
+  __shared__ float s_ml[W][16][2];
+  const int groups = p.hkv / p.heads, index = blockIdx.x / groups, KS = W / p.heads;
   Share sh;
   if (!find_share<false>(p, shares, index, sh)) return;
 
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h = blockIdx.x % groups * ws.heads + w % ws.heads;
-  const int rs = w / ws.heads % RS, ks = w / (ws.heads * RS);   // place among rows and tiles
+  const int h = blockIdx.x % groups * p.heads + w % p.heads;
+  const int ks = w / p.heads;                  // place among the head's tiles
   const int c16 = lane & 15, kg = lane >> 4;
   float cs = p.scale_log2, vsc = 1.f;
   if constexpr (FORM == kCacheHead) {
@@ -140,7 +137,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(CacheProblem p, 
   int pos[NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int r = 16 * (NT * rs + nt) + c16;
+    const int r = 16 * nt + c16;
     pos[nt] = first + (ONE ? 0 : r / p.g);
     const uint16_t* qrow = p.q + ((int64_t)(q0 + (ONE ? 0 : min(r / p.g, Lq - 1))) * p.hq + h * p.g + r % p.g) *
                                      kHeadDim;
@@ -162,53 +159,34 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(CacheProblem p, 
     l[nt] = 0.f;
   }
 
-  // where the keys of a tile lie: the slots of its two groups' first keys, or
-  // that of key lane % 32. Keys past the sequence stand on valid ones.
-  struct Where {
-    int64_t s[2];
-  };
-  auto where = [&](int tile) {
-    Where a;
-    const int t0 = kTile * tile;
-    if constexpr (GROUPED) {
-      const int32_t* row = p.pm.table + (int64_t)b * p.pm.stride;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int t = u && t0 + 16 > last ? t0 : t0 + 16 * u;
-        const int pg = p.pm.shift >= 0 ? t >> p.pm.shift : t / p.pm.page;
-        a.s[u] = (int64_t)ld_uniform(row, pg) * p.pm.page + (t - pg * p.pm.page);
-      }
-    } else {
-      a.s[0] = slot_of(p.pm, b, 0, min(t0 + (lane & 31), last));
-      a.s[1] = 0;
-    }
-    return a;
-  };
+  const int32_t* table = p.pm.table + (int64_t)b * p.pm.stride;
+  auto where = [&](int tile) { return where_at<GROUPED>(p.pm, table, tile, last, lane); };
   typedef std::conditional_t<kBf16, uint4, uint2> vrow_t;
-  auto load = [&](const Where& a, Raw<FORM>& x) {
+  auto load = [&](const Where& a, Raw<FORM>& x, uint32_t on) {   // on: ~0, or 0 to read one row over and over
     if constexpr (GROUPED) {
+      const int64_t slot[2] = {a.slot(p.pm, 0), a.slot(p.pm, 1)};
       if constexpr (FORM == kCacheBlock) {   // before the rows: loads come back in order
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const int64_t at = (a.s[u] >> p.sb_shift) * p.hkv + h;
+          const int64_t at = (slot[u] >> p.sb_shift) * p.hkv + h;
           x.ks[u] = p.k_block[at];
           x.vs[u] = p.v_block[at];
         }
       }
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const uint8_t* kb = K + a.s[u] * rowb;
+        const uint8_t* kb = K + slot[u] * rowb;
 #pragma unroll
-        for (int c = 0; c < KC; ++c) x.k[u][c] = *(const uint4*)(kb + (koff + 64u * c));
+        for (int c = 0; c < KC; ++c) x.k[u][c] = *(const uint4*)(kb + ((koff & on) + 64u * c));
       }
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const uint8_t* vb = V + a.s[u] * rowb;
+        const uint8_t* vb = V + slot[u] * rowb;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x.v[4 * u + e] = *(const vrow_t*)(vb + e * rowb + voff);
+        for (int e = 0; e < 4; ++e) x.v[4 * u + e] = *(const vrow_t*)(vb + e * rowb + (voff & on));
       }
     } else {
-      const int slot = (int)a.s[0];
+      const int slot = (int)a.slot(p.pm, 0);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const uint8_t* kb = K + (int64_t)__shfl(slot, 16 * u + c16, 64) * rowb + 16 * kg;
@@ -368,20 +346,20 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(CacheProblem p, 
   };
 
   // The next tile's rows are on their way while a tile is computed. Loads are
-  // never left out (past the end they repeat the last tile): behind a load that
-  // may not have been issued the compiler can only wait for all of them.
+  // never left out (past the end they repeat a row): behind a load that may not
+  // have been issued the compiler can only wait for all of them.
   if (lo + ks < hi) {
     Raw<FORM> r0, r1;
-    const int end = hi - 1;
-    load(where(tile_at(lo + ks)), r0);
-    Where a0 = where(tile_at(min(lo + ks + KS, end))), a1;
+    auto where_to = [&](int i) { return where(tile_at(min(i, hi - 1))); };
+    load(where_to(lo + ks), r0, ~0u);
+    Where a0 = where_to(lo + ks + KS), a1;
 #pragma unroll 1
     for (int i = lo + ks; i < hi; i += 2 * KS) {
-      load(a0, r1);
-      a1 = where(tile_at(min(i + 2 * KS, end)));
+      load(a0, r1, i + KS < hi ? ~0u : 0u);
+      a1 = where_to(i + 2 * KS);
       step(tile_at(i), r0);
-      load(a1, r0);
-      a0 = where(tile_at(min(i + 3 * KS, end)));
+      load(a1, r0, i + 2 * KS < hi ? ~0u : 0u);
+      a0 = where_to(i + 3 * KS);
       if (i + KS < hi) step(tile_at(i + KS), r1);
     }
   }
@@ -393,7 +371,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(CacheProblem p, 
   // eight values of packed row pr of head hh, from dimension d on
   auto put = [&](int hh, int pr, int d, float mm, float ll, float4 x, float4 y) {
     if (split) {
-      const int64_t at = (slot + hh) * (16 * NT * RS) + pr;
+      const int64_t at = (slot + hh) * (16 * NT) + pr;
       *(float4*)(part.o + at * kHeadDim + d) = x;
       *(float4*)(part.o + at * kHeadDim + d + 4) = y;
       if (d == 0) *(float2*)(part.ml + 2 * at) = make_float2(mm, ll);
@@ -410,7 +388,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(CacheProblem p, 
   for (int nt = 0; nt < NT; ++nt) {
     l[nt] += __shfl_xor(l[nt], 16, 64);
     l[nt] += __shfl_xor(l[nt], 32, 64);
-    const int pr = 16 * (NT * rs + nt) + c16;
+    const int pr = 16 * nt + c16;
     if (KS == 1) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -420,7 +398,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(CacheProblem p, 
               make_float4(o[nt][4][i], o[nt][5][i], o[nt][6][i], o[nt][7][i]));
       continue;
     }
-    // the waves of a head and its rows, joined 16 rows a wave at a time
+    if (16 * nt >= rows) continue;
+    // the waves of a head, joined 16 rows at a time
     if (nt || again) __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -433,10 +412,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(CacheProblem p, 
       s_ml[w][c16][1] = l[nt];
     }
     __syncthreads();
-    // wave w joins some of the rows of its own head and rows: ks-th of KS shares of the 16 x 16 pieces
-    const int w0 = w % (ws.heads * RS), stepw = ws.heads * RS;
+    // the ks-th of them joins that share of the pieces of eight dimensions
+    const int w0 = w % p.heads, stepw = p.heads;
     for (int x = 64 * ks + lane; x < 16 * 16; x += 64 * KS) {
-      const int r = x >> 4, d = 8 * (x & 15), jr = 16 * (NT * rs + nt) + r;
+      const int r = x >> 4, d = 8 * (x & 15), jr = 16 * nt + r;
       if (jr >= rows) continue;
       float mm = kNoRef;
       for (int v = 0; v < KS; ++v) mm = fmaxf(mm, s_ml[w0 + v * stepw][r][0]);
@@ -461,15 +440,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(CacheProblem p, 
 }
 
 // Joins the parts of the units that were cut: a workgroup takes one packed
-// row. The maximum over the parts comes first, so that the sums are plain ones
-// with their loads in flight together (eight groups of 32 lanes, every eighth
-// part each).
-__global__ __launch_bounds__(256) void combine_kernel(CacheProblem p, CachePartials part, int shares,
+// row, groups of 32 lanes the parts in turn, eight of them a step with all
+// their loads in flight; the groups are joined in LDS.
+__global__ __launch_bounds__(1024) void combine_kernel(CacheProblem p, CachePartials part, int shares,
                                                       int rows_cap, int max_rows,
                                                       uint16_t* __restrict__ out,
                                                       float* __restrict__ lse) {
-  __shared__ float s_m[4], s_l[8];
-  __shared__ float4 s_a[8][32];
+  __shared__ float s_m[32], s_l[32];
+  __shared__ float4 s_a[32][32];
   const int pr = blockIdx.x % max_rows, bh = blockIdx.x / max_rows;
   const int b = bh / p.hkv, h = bh % p.hkv;
   Share sh;
@@ -495,32 +473,52 @@ __global__ __launch_bounds__(256) void combine_kernel(CacheProblem p, CacheParti
   // row `pr` of part i, among the rows of all slots
   auto row = [&](int i) { return ((s0 + step * i + (i ? 0 : odd)) * p.hkv + h) * rows_cap + pr; };
   const int tid = threadIdx.x, grp = tid >> 5, d = tid & 31;
-  float m = kNoRef;
-  for (int i = tid; i < parts; i += 256) m = fmaxf(m, part.ml[2 * row(i)]);
-  m = wave_max(m);
-  if ((tid & 63) == 0) s_m[tid >> 6] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-  float l = 0.f;
+  const int groups = blockDim.x >> 5;
+  float m = kNoRef, l = 0.f;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-  for (int i = grp; i < parts; i += 8) {
-    const float2 x = *(const float2*)(part.ml + 2 * row(i));
-    const float4 y = *(const float4*)(part.o + row(i) * kHeadDim + 4 * d);
-    const float f = fast_exp2(x.x - m);
-    l += f * x.y;
-    a.x += f * y.x, a.y += f * y.y, a.z += f * y.z, a.w += f * y.w;
+#pragma unroll 1
+  for (int i0 = grp; i0 < parts; i0 += 8 * groups) {
+    float2 x[8];
+    float4 y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int64_t at = row(min(i0 + j * groups, parts - 1));
+      x[j] = *(const float2*)(part.ml + 2 * at);
+      y[j] = *(const float4*)(part.o + at * kHeadDim + 4 * d);
+    }
+    float mn = m;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[j].x = i0 + j * groups < parts ? x[j].x : -INFINITY;
+      mn = fmaxf(mn, x[j].x);
+    }
+    const float f = fast_exp2(m - mn);
+    m = mn;
+    l *= f;
+    a.x *= f, a.y *= f, a.z *= f, a.w *= f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (i0 + j * groups >= parts) break;
+      const float g = fast_exp2(x[j].x - m);
+      l += g * x[j].y;
+      a.x += g * y[j].x, a.y += g * y[j].y, a.z += g * y[j].z, a.w += g * y[j].w;
+    }
   }
-  if (d == 0) s_l[grp] = l;
+  if (d == 0) s_m[grp] = m, s_l[grp] = l;
   s_a[grp][d] = a;
   __syncthreads();
   if (tid >= 32) return;
-  for (int i = 1; i < 8; ++i) {
+  const float own = m;
+  for (int i = 1; i < groups; ++i) m = fmaxf(m, s_m[i]);
+  const float f = fast_exp2(own - m);
+  l = s_l[0] * f;
+  a.x *= f, a.y *= f, a.z *= f, a.w *= f;
+  for (int i = 1; i < groups; ++i) {
+    const float g = fast_exp2(s_m[i] - m);
     const float4 y = s_a[i][d];
-    l += d == 0 ? s_l[i] : 0.f;
-    a.x += y.x, a.y += y.y, a.z += y.z, a.w += y.w;
+    l += g * s_l[i];
+    a.x += g * y.x, a.y += g * y.y, a.z += g * y.z, a.w += g * y.w;
   }
-  l = __shfl(l, 0, 32);
   const float inv = (p.form == kCacheHead ? ld_uniform(p.v_head, h) : 1.f) / l;
   const int64_t at = (int64_t)(q0 + pr / p.g) * p.hq + h * p.g + pr % p.g;
   *(uint2*)(out + at * kHeadDim + 4 * d) =
@@ -534,45 +532,37 @@ int rows_cap(const CacheProblem& p) {
   return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
 }
 
-// How the rows are held: 16-row tiles of a wave and waves that share the rows
-// of a tile of keys. A bf16 tile of keys takes twice the registers of one of
-// codes, so its waves hold 16 rows.
-struct Rows {
-  int tiles, waves;
-};
-Rows rows_for(const CacheProblem& p) {
-  const int n = rows_cap(p) / 16;
-  return p.form == kCacheBf16 || n == 1 ? Rows{1, n} : Rows{2, n / 2};
+// Waves of a workgroup: a tile of bf16 keys takes twice the registers of one
+// of codes.
+int waves_for(const CacheProblem& p) {
+  return rows_cap(p) <= (p.form == kCacheBf16 ? 16 : 32) ? 8 : 4;
 }
 
-template <int FORM, int NT, int RS, bool GROUPED, bool ONE>
+template <int FORM, int NT, int W, bool GROUPED, bool ONE>
 hipError_t launch(const CacheProblem& problem, const CachePartials& part, uint16_t* out, float* lse,
                   hipStream_t s) {
-  const CacheProblem p = dealt(problem, RS);
-  const int shares = shares_of(p, RS), max_rows = p.max_new * p.g;
-  const int64_t grid = (int64_t)shares * (p.hkv / wave_split(p, RS).heads);
+  const CacheProblem p = dealt(problem, W);
+  const int shares = shares_of(p), max_rows = p.max_new * p.g;
+  const int64_t grid = (int64_t)shares * (p.hkv / p.heads);
   const int64_t joins = (int64_t)p.batch * p.hkv * max_rows;
   if (grid > 0x7fffffff || joins > 0x7fffffff) return hipErrorInvalidValue;
-  decode_kernel<FORM, NT, RS, GROUPED, ONE>
-      <<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, part, shares, out, lse);
-  if (p.splits != 1)
-    combine_kernel<<<(unsigned)joins, 256, 0, s>>>(p, part, shares, 16 * NT * RS, max_rows, out, lse);
+  decode_kernel<FORM, NT, W, GROUPED, ONE><<<(unsigned)grid, 64 * W, 0, s>>>(p, part, shares, out, lse);
+  if (p.splits == 1) return hipGetLastError();
+  // few joins have many parts each, and a compute unit to themselves
+  const int threads = joins <= kFewGroups ? 1024 : 256;
+  combine_kernel<<<(unsigned)joins, threads, 0, s>>>(p, part, shares, 16 * NT, max_rows, out, lse);
   return hipGetLastError();
 }
 
 template <int FORM, bool GROUPED>
 hipError_t launch_rows(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse,
                        hipStream_t s) {
-  if (p.max_new == 1) return launch<FORM, 1, 1, GROUPED, true>(p, part, out, lse, s);
-  const int waves = rows_for(p).waves;
-  if constexpr (FORM == kCacheBf16)
-    return waves == 1   ? launch<FORM, 1, 1, GROUPED, false>(p, part, out, lse, s)
-           : waves == 2 ? launch<FORM, 1, 2, GROUPED, false>(p, part, out, lse, s)
-                        : launch<FORM, 1, 4, GROUPED, false>(p, part, out, lse, s);
-  else
-    return rows_for(p).tiles == 1 ? launch<FORM, 1, 1, GROUPED, false>(p, part, out, lse, s)
-           : waves == 1           ? launch<FORM, 2, 1, GROUPED, false>(p, part, out, lse, s)
-                                  : launch<FORM, 2, 2, GROUPED, false>(p, part, out, lse, s);
+  constexpr int W2 = FORM == kCacheBf16 ? 4 : 8;   // waves_for 32 rows
+  const int rows = rows_cap(p);
+  return p.max_new == 1 ? launch<FORM, 1, 8, GROUPED, true>(p, part, out, lse, s)
+         : rows == 16   ? launch<FORM, 1, 8, GROUPED, false>(p, part, out, lse, s)
+         : rows == 32   ? launch<FORM, 2, W2, GROUPED, false>(p, part, out, lse, s)
+                        : launch<FORM, 4, 4, GROUPED, false>(p, part, out, lse, s);
 }
 
 template <int FORM>
@@ -587,9 +577,8 @@ hipError_t launch_pages(const CacheProblem& p, const CachePartials& part, uint16
 }  // namespace
 
 void cache_decode_partials(const CacheProblem& problem, int64_t* slots, int* rows) {
-  const int waves = rows_for(problem).waves;
-  const CacheProblem p = dealt(problem, waves);
-  *slots = p.splits == 1 ? 0 : (int64_t)shares_of(p, waves) * (p.splits ? 1 : 2) * p.hkv;
+  const CacheProblem p = dealt(problem, waves_for(problem));
+  *slots = p.splits == 1 ? 0 : (int64_t)shares_of(p) * (p.splits ? 1 : 2) * p.hkv;
   *rows = rows_cap(p);
 }
 

@@ -4,13 +4,16 @@
 //
 // select_kernel: one workgroup a (sequence, head). The weight that just stays
 // is found digit by digit (11, 11 and 10 bits of the order-preserving bits of
-// the weights, a histogram in LDS each), then one pass over the tokens writes
-// the ones that stay, ties by the lowest index.
-// move_kernel: 128 rows of the new layout a workgroup, as the append. bf16
-// rows and codes with a scale per head are copied; with a scale per block a
-// new block holds rows of several old ones: its scale is again the smallest
-// power of two for its largest value, and the codes are moved by the
-// difference of the powers, exact but for what becomes subnormal.
+// the weights, a histogram in LDS each), then one more pass writes the tokens
+// that stay, ties by the lowest index. What bounds it is how much of the row a
+// compute unit has in flight: 16 bytes a lane and four loads at once.
+// move_kernel: a wave takes a run of rows of the new layout of one head, keys
+// or values, and the waves beside it the other heads, whose rows lie side by
+// side in the new pages and near each other in the old ones. bf16 rows and
+// codes with a scale per head are copied; with a scale per block a new block
+// holds rows of several old ones: its scale is again the smallest power of two
+// for its largest value, and the codes are moved by the difference of the
+// powers, exact but for what becomes subnormal.
 #include <algorithm>
 #include <type_traits>
 
@@ -21,9 +24,10 @@ namespace fp2 {
 namespace {
 
 constexpr int kThreads = 1024;
+constexpr int kSteps = 4;                         // loads of a thread at once, of four tokens each
+constexpr int kRound = kSteps * kThreads * 4;     // tokens of them
 constexpr int kBins = 2048;
-constexpr int kPer = 4;            // consecutive tokens of a thread
-constexpr int kRows = 128;
+constexpr int kCopies = 4;         // histograms, so that the lanes of a wave seldom meet at a bin
 constexpr int kWaves = 8;
 
 // Bits whose order is that of the numbers; NaN below all, -0 as 0.
@@ -33,26 +37,16 @@ __device__ __forceinline__ uint32_t order_of(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-__device__ __forceinline__ int wave_scan(int v, int lane) {   // inclusive
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(v, o, 64);
-    if (lane >= o) v += u;
-  }
-  return v;
-}
-
 // Exclusive sum over the workgroup's threads and the total. tot: LDS, one a wave.
 __device__ __forceinline__ int block_scan(int v, int* tot, int& total) {
+  constexpr int W = kThreads / 64;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int incl = wave_scan(v, lane);
+  const int incl = wave_scan(v);
   if (lane == 63) tot[w] = incl;
   __syncthreads();
-  int before = 0;
-  total = 0;
-  for (int i = 0; i < kThreads / 64; ++i) {
-    before += i < w ? tot[i] : 0;
-    total += tot[i];
-  }
+  const int sums = wave_scan(lane < W ? tot[lane] : 0);
+  total = __builtin_amdgcn_readlane(sums, W - 1);
+  const int before = w ? __shfl(sums, w - 1, 64) : 0;
   __syncthreads();
   return before + incl - v;
 }
@@ -62,9 +56,10 @@ __global__ __launch_bounds__(kThreads) void select_kernel(CacheProblem p, int bu
                                                           int64_t stride, float* __restrict__ weights_out,
                                                           int64_t out_stride, int32_t* __restrict__ kept,
                                                           int32_t* __restrict__ cu_out) {
-  __shared__ int hist[kBins];
+  __shared__ int hist[kCopies][kBins];
+  __shared__ int cnt[2][kSteps * kThreads / 64];
   __shared__ int tot[kThreads / 64];
-  __shared__ int s_bin, s_need;
+  __shared__ int s_bin, s_need, s_size;
   const int tid = threadIdx.x, lane = tid & 63;
   if (blockIdx.x == 0 && tid < 64) {   // the new lengths
     int base = 0;
@@ -72,7 +67,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(CacheProblem p, int bu
     for (int b0 = 0; b0 < p.batch; b0 += 64) {
       const int b = b0 + lane;
       const int n = b < p.batch ? min(p.cuk[b + 1] - p.cuk[b], budget) : 0;
-      const int incl = wave_scan(n, lane);
+      const int incl = wave_scan(n);
       if (b < p.batch) cu_out[b + 1] = base + incl;
       base += __shfl(incl, 63, 64);
     }
@@ -94,156 +89,211 @@ __global__ __launch_bounds__(kThreads) void select_kernel(CacheProblem p, int bu
   }
   const int lo = min(p.sink, budget), hi = L - recent;   // the tokens between are ranked
   int need = budget - lo - recent;                       // of them stay
+  // four weights a load from the 16-byte line that the row starts in: element e
+  // of line v is token 4 v + e - skew
+  const int skew = (int)((uintptr_t)wr >> 2 & 3), lines = (L + skew + 3) / 4;
+  const float4* line = (const float4*)(wr - skew);
+  auto load = [&](int v0, float4 (&x)[kSteps]) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) x[s] = line[min(v0 + s * kThreads + tid, lines - 1)];
+  };
+  float4 x[kSteps];
+  load(0, x);
+  const bool once = lines <= kRound / 4;                 // then they are loaded once
+  auto at = [](const float4& x, int e) { return e == 0 ? x.x : e == 1 ? x.y : e == 2 ? x.z : x.w; };
   // bits of the weight that just stays, found from the top
-  uint32_t edge = 0;
+  uint32_t edge = 0, mask = 0;                           // and which of its bits are known
   int left = need;                                       // of those equal to `edge` so far
 #pragma unroll 1
   for (int d = 0; d < 3 && need > 0; ++d) {
     const int shift = d == 0 ? 21 : d == 1 ? 10 : 0, bins = d == 2 ? 1024 : 2048;
-    const uint32_t above = d == 0 ? 0u : d == 1 ? 0xffe00000u : 0xfffffc00u;
-    for (int i = tid; i < bins; i += kThreads) hist[i] = 0;
+    for (int i = tid; i < kCopies * kBins; i += kThreads) hist[0][i] = 0;
     __syncthreads();
-    for (int i0 = lo + tid; i0 < hi; i0 += 8 * kThreads) {
-      float x[8];                        // eight loads in flight
+#pragma unroll 1
+    for (int v0 = 0; v0 < lines; v0 += kRound / 4) {
+      if (!once) load(v0, x);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = i0 + j * kThreads < hi ? wr[i0 + j * kThreads] : 0.f;
+      for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t u = order_of(x[j]);
-        if (i0 + j * kThreads < hi && (u & above) == edge)
-          atomicAdd(&hist[(u >> shift) & (bins - 1)], 1);
-      }
+        for (int e = 0; e < 4; ++e) {
+          const int i = 4 * (v0 + s * kThreads + tid) + e - skew;
+          const uint32_t u = order_of(at(x[s], e));
+          if (i >= lo && i < hi && (u & mask) == edge)
+            atomicAdd(&hist[tid % kCopies][(u >> shift) & (bins - 1)], 1);
+        }
     }
     __syncthreads();
     // bins from the top, two a thread
-    const int b1 = bins - 1 - 2 * tid, n1 = b1 >= 0 ? hist[b1] : 0, n2 = b1 >= 1 ? hist[b1 - 1] : 0;
+    const int b1 = bins - 1 - 2 * tid;
+    int n1 = 0, n2 = 0;
+    for (int c = 0; c < kCopies && b1 > 0; ++c) n1 += hist[c][b1], n2 += hist[c][b1 - 1];
     int total;
     const int before = block_scan(n1 + n2, tot, total);
-    if (before < left && before + n1 >= left) s_bin = b1, s_need = left - before;
-    else if (before + n1 < left && before + n1 + n2 >= left) s_bin = b1 - 1, s_need = left - before - n1;
+    if (before < left && before + n1 >= left) s_bin = b1, s_need = left - before, s_size = n1;
+    else if (before + n1 < left && before + n1 + n2 >= left)
+      s_bin = b1 - 1, s_need = left - before - n1, s_size = n2;
     __syncthreads();
     edge |= (uint32_t)s_bin << shift;
+    mask |= (uint32_t)(bins - 1) << shift;
     left = s_need;
+    const bool all = s_size == left;     // every weight with these bits stays: no need for the others
     __syncthreads();
+    if (all) break;
   }
-  // tokens in order: protected or heavier than the edge, or the first `left` at
-  // it. Both are counted by one sum a step, the second kind in the high half.
-  int over = 0, equal = 0;               // of the steps before
-  float x[kPer], y[kPer];
-  auto load = [&](int i0, float (&v)[kPer]) {
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int i = i0 + kPer * tid + j;
-      v[j] = i < L ? wr[i] : 0.f;
-    }
-  };
-  load(0, x);
+  // in order: tokens that are protected or heavier than the edge, and the
+  // first `left` at it. A round counts both (the second kind in the high half)
+  // for every wave and step, and one sum over those gives every place.
+  const int w = tid >> 6;
+  int over = 0, equal = 0;               // of the rounds before
 #pragma unroll 1
-  for (int i0 = 0; i0 < L; i0 += kThreads * kPer) {
-    load(i0 + kThreads * kPer, y);       // of the next step
-    int eq = 0, up = 0;                  // bit masks of this thread's tokens
+  for (int v0 = 0, odd = 0; v0 < lines; v0 += kRound / 4, odd ^= 1) {
+    if (!once) load(v0, x);
+    int up[kSteps], eq[kSteps], incl[kSteps];            // bits of this thread's tokens
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int i = i0 + kPer * tid + j;
-      const uint32_t u = order_of(x[j]);
-      const bool fixed = i < lo || i >= hi;
-      if (i < L && (fixed || (need > 0 && u > edge))) up |= 1 << j;
-      else if (i < L && need > 0 && u == edge) eq |= 1 << j;
-    }
-    int total;
-    const int before = block_scan(__popc(up) | __popc(eq) << 16, tot, total);
-    int o = over + (before & 0xffff), e = equal + (before >> 16);
+    for (int s = 0; s < kSteps; ++s) {
+      up[s] = eq[s] = 0;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const bool is_up = up >> j & 1, is_eq = eq >> j & 1;
-      if (is_up || (is_eq && e < left)) {
-        const int to = o + min(e, left);
-        kr[to] = i0 + kPer * tid + j;
-        wo[to] = x[j];
+      for (int e = 0; e < 4; ++e) {
+        const int i = 4 * (v0 + s * kThreads + tid) + e - skew;
+        const uint32_t u = order_of(at(x[s], e)) & mask;
+        const bool fixed = i < lo || i >= hi, in = i >= 0 && i < L;
+        up[s] |= in && (fixed || (need > 0 && u > edge)) ? 1 << e : 0;
+        eq[s] |= in && !fixed && need > 0 && u == edge ? 1 << e : 0;
       }
-      o += is_up;
-      e += is_eq;
+      incl[s] = wave_scan(__popc(up[s]) | __popc(eq[s]) << 16);
+      if (lane == 63) cnt[odd][s * (kThreads / 64) + w] = incl[s];
+    }
+    __syncthreads();
+    static_assert(kSteps * kThreads / 64 == 64, "a lane each");
+    const int own = cnt[odd][lane], sum = wave_scan(own), total = __builtin_amdgcn_readlane(sum, 63);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int before = __shfl(sum - own, s * (kThreads / 64) + w, 64) + incl[s] -
+                         (__popc(up[s]) | __popc(eq[s]) << 16);
+      int o = over + (before & 0xffff), n = equal + (before >> 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool is_up = up[s] >> e & 1, is_eq = eq[s] >> e & 1;
+        if (is_up || (is_eq && n < left)) {
+          const int to = o + min(n, left);
+          kr[to] = 4 * (v0 + s * kThreads + tid) + e - skew;
+          wo[to] = at(x[s], e);
+        }
+        o += is_up;
+        n += is_eq;
+      }
     }
     over += total & 0xffff;
     equal += total >> 16;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) x[j] = y[j];
   }
 }
 
-template <int FORM>
+// SB: tokens with one scale (blocks), else 0.
+template <int FORM, int SB>
 __global__ __launch_bounds__(64 * kWaves) void move_kernel(CacheProblem p, PageMap to, int budget,
-                                                           int chunks, const int32_t* __restrict__ kept) {
+                                                           int runs, int64_t total,
+                                                           const int32_t* __restrict__ kept) {
   constexpr int ESZ = FORM == kCacheBf16 ? 2 : 1;
-  __shared__ float s_amax[kWaves];
-  int64_t at = blockIdx.x;
+  constexpr int RUN = SB > 32 ? SB : 32;         // rows of a wave
+  constexpr int LPR = kHeadDim * ESZ / 16;       // lanes of a row, 16 bytes each
+  constexpr int RPL = 64 / LPR;                  // rows of a load
+  constexpr int N = RUN / RPL;
+  int64_t at = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (at >= total) return;
   const int h = (int)(at % p.hkv);
   at /= p.hkv;
   const bool is_v = at & 1;
   at >>= 1;
-  const int first = (int)(at % chunks) * kRows, b = (int)(at / chunks);
-  const int L = ld_uniform(p.cuk, b + 1) - ld_uniform(p.cuk, b);
-  const int stay = min(L, budget);
+  const int first = (int)(at % runs) * RUN, b = (int)(at / runs);
+  const int stay = min(ld_uniform(p.cuk, b + 1) - ld_uniform(p.cuk, b), budget);
   if (first >= stay) return;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = lane & 15;
+  const int lane = threadIdx.x & 63, c = lane % LPR, r0 = lane / LPR;
+  const int64_t rowb = (int64_t)p.hkv * kHeadDim * ESZ, hoff = (int64_t)h * kHeadDim * ESZ + 16 * c;
+  const int32_t* kr = kept + ((int64_t)b * p.hkv + h) * budget;
+  // slots of the rows: every lane looks up some, the loads below ask it
+  constexpr int LOOK = (RUN + 63) / 64;
+  int64_t from[LOOK], dest[LOOK];
+#pragma unroll
+  for (int i = 0; i < LOOK; ++i) {
+    const int r = min(first + 64 * i + lane, stay - 1);
+    from[i] = slot_of(p.pm, b, 0, kr[r]);
+    dest[i] = slot_of(to, b, 0, r);
+  }
   uint8_t* pool = is_v ? p.v : p.k;
   uint8_t* scales = is_v ? p.v_block : p.k_block;
-  const int64_t rowb = (int64_t)p.hkv * kHeadDim * ESZ, hoff = (int64_t)h * kHeadDim * ESZ;
-  const int32_t* kr = kept + ((int64_t)b * p.hkv + h) * budget;
-  typedef std::conditional_t<FORM == kCacheBf16, uint4, uint2> row_t;
-  row_t x[4];
-  float sc[4];
+  i32x4_t x[N];   // (a vector, not the struct: a copied struct would be kept in LDS)
+  uint32_t old[N];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = first + 16 * w + 4 * i + (lane >> 4);
-    x[i] = row_t{};
-    sc[i] = 0.f;
-    if (r < stay) {
-      const int64_t slot = slot_of(p.pm, b, 0, kr[r]);
-      x[i] = *(const row_t*)(pool + slot * rowb + hoff + sizeof(row_t) * c);
-      if constexpr (FORM == kCacheBlock) sc[i] = block_scale(scales[(slot >> p.sb_shift) * p.hkv + h]);
-    }
+  for (int i = 0; i < N; ++i) {
+    const int r = RPL * i + r0;
+    const int64_t slot = __shfl(from[RPL * i / 64], r & 63, 64);
+    x[i] = *(const i32x4_t*)(pool + slot * rowb + hoff);
+    if constexpr (FORM == kCacheBlock) old[i] = scales[(slot >> p.sb_shift) * p.hkv + h];
   }
-  float inv = 0.f;
   if constexpr (FORM == kCacheBlock) {
-    float amax = 0.f;
+    constexpr int PER = SB / RPL;              // loads of a block
+    float amax[N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float y[4], z[4];
-      e4m3x4_to_f32(x[i].x, y);
-      e4m3x4_to_f32(x[i].y, z);
+    for (int i = 0; i < N; ++i) {
+      const uint32_t d[4] = {(uint32_t)x[i][0], (uint32_t)x[i][1], (uint32_t)x[i][2], (uint32_t)x[i][3]};
+      float m = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {   // NaN codes do not count
-        const float g = fabsf(y[e]), f = fabsf(z[e]);
-        amax = fmaxf(amax, g <= 448.f ? g * sc[i] : 0.f);
-        amax = fmaxf(amax, f <= 448.f ? f * sc[i] : 0.f);
+      for (int j = 0; j < 4; ++j) {
+        float y[4];
+        e4m3x4_to_f32(d[j], y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = fmaxf(m, fabsf(y[e]));   // a NaN is left out
       }
+      // rows behind the last repeat it: they change no maximum
+      amax[i] = m * block_scale(old[i]);
     }
-    amax = wave_max(amax);
-    if (lane == 0) s_amax[w] = amax;
-    __syncthreads();
-    const int wpb = 1 << (p.sb_shift - 4), w0 = w & ~(wpb - 1);
-    for (int j = 0; j < wpb; ++j) amax = fmaxf(amax, s_amax[w0 + j]);
-    const int byte = scale_byte(amax), tb = first + 16 * w0;
-    if (w == w0 && lane == 0 && tb < stay)
-      scales[(slot_of(to, b, 0, tb) >> p.sb_shift) * p.hkv + h] = (uint8_t)byte;
-    inv = __uint_as_float((uint32_t)(254 - byte) << 23);
+    int byte = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (i % PER == 0) {
+        float m = amax[i];
+#pragma unroll
+        for (int j = 1; j < PER; ++j) m = fmaxf(m, amax[i + j]);
+        byte = scale_byte(wave_max(m));
+        const int64_t slot = __shfl(dest[RPL * i / 64], RPL * i & 63, 64);
+        if (lane == 0 && first + RPL * i < stay)
+          scales[(slot >> p.sb_shift) * p.hkv + h] = (uint8_t)byte;
+      }
+      // what a code is times: 2^(old - new), at most 448 in the end
+      const float f = block_scale(old[i]) * __uint_as_float((uint32_t)(254 - byte) << 23);
+      // converted once more: kept from above they would take 16 registers a load
+      uint32_t d[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) d[j] = (uint32_t)pinned((int)x[i][j]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float y[4];
+        e4m3x4_to_f32(d[j], y);
+        const uint32_t nan = ((d[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;   // top bits of NaN codes
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] * f, y[1] * f, 0, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] * f, y[3] * f, w, true);
+        d[j] = ((uint32_t)w & ~((nan >> 7) * 0xffu)) | (nan - (nan >> 7));
+      }
+      x[i] = (i32x4_t){(int)d[0], (int)d[1], (int)d[2], (int)d[3]};
+    }
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = first + 16 * w + 4 * i + (lane >> 4);
-    if (r >= stay) continue;
-    row_t v = x[i];
-    if constexpr (FORM == kCacheBlock) {
-      float y[4], z[4], s[4], t[4];
-      e4m3x4_to_f32(v.x, y);
-      e4m3x4_to_f32(v.y, z);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] = y[e] * sc[i] * inv, t[e] = z[e] * sc[i] * inv;
-      v = make_uint2(e4m3x4(y, s), e4m3x4(z, t));
-    }
-    *(row_t*)(pool + slot_of(to, b, 0, r) * rowb + hoff + sizeof(row_t) * c) = v;
+  for (int i = 0; i < N; ++i) {
+    const int r = RPL * i + r0;
+    const int64_t slot = __shfl(dest[RPL * i / 64], r & 63, 64);
+    if (first + r < stay) *(i32x4_t*)(pool + slot * rowb + hoff) = x[i];
   }
+}
+
+template <int FORM, int SB>
+hipError_t launch_move(const CacheProblem& p, const PageMap& to, int budget, const int32_t* kept,
+                       hipStream_t s) {
+  constexpr int RUN = SB > 32 ? SB : 32;
+  const int runs = (std::min(budget, p.max_kv) + RUN - 1) / RUN;
+  const int64_t total = (int64_t)p.batch * p.hkv * 2 * runs, grid = (total + kWaves - 1) / kWaves;
+  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  move_kernel<FORM, SB><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, to, budget, runs, total, kept);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -251,18 +301,17 @@ __global__ __launch_bounds__(64 * kWaves) void move_kernel(CacheProblem p, PageM
 hipError_t launch_cache_evict(const CacheProblem& p, const PageMap& to, int budget, int recent,
                               const float* weights, int64_t stride, float* weights_out,
                               int64_t out_stride, int32_t* kept, int32_t* cu_out, hipStream_t s) {
-  const int chunks = (std::min(budget, p.max_kv) + kRows - 1) / kRows;
-  const int64_t heads = (int64_t)p.batch * p.hkv, grid = heads * 2 * chunks;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  const int64_t heads = (int64_t)p.batch * p.hkv;
   select_kernel<<<(unsigned)heads, kThreads, 0, s>>>(p, budget, recent, weights, stride, weights_out,
                                                      out_stride, kept, cu_out);
-  if (p.form == kCacheBf16)
-    move_kernel<kCacheBf16><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, to, budget, chunks, kept);
-  else if (p.form == kCacheHead)
-    move_kernel<kCacheHead><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, to, budget, chunks, kept);
-  else
-    move_kernel<kCacheBlock><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, to, budget, chunks, kept);
-  return hipGetLastError();
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (p.form == kCacheBf16) return launch_move<kCacheBf16, 0>(p, to, budget, kept, s);
+  if (p.form == kCacheHead) return launch_move<kCacheHead, 0>(p, to, budget, kept, s);
+  return p.sb_shift == 4   ? launch_move<kCacheBlock, 16>(p, to, budget, kept, s)
+         : p.sb_shift == 5 ? launch_move<kCacheBlock, 32>(p, to, budget, kept, s)
+         : p.sb_shift == 6 ? launch_move<kCacheBlock, 64>(p, to, budget, kept, s)
+                           : launch_move<kCacheBlock, 128>(p, to, budget, kept, s);
 }
 
 }  // namespace fp2

@@ -8,9 +8,8 @@ namespace fp2 {
 namespace {
 
 constexpr int kTile = 32;        // keys per wave and step
-constexpr int kFewWaves = 8;     // waves of a workgroup
 constexpr int kFewGroups = 256;  // workgroups that a call is dealt to: one a compute unit
-constexpr int kWholeTiles = 16;  // sequences of at most as many are not cut, if there are many
+constexpr int kWholeTiles = 48;  // sequences of at most as many (half of it in bf16) are not cut
 
 // Tiles of a sequence that some row sees: `sinks` leading ones, then those
 // from `from` on.
@@ -33,29 +32,6 @@ __device__ __forceinline__ bool sees(const CacheProblem& p, int pos, int key) {
   return (uint32_t)(key - pos + p.window - 1) < (uint32_t)p.window || (key < p.sink && key <= pos);
 }
 
-// Keeps the compiler from computing many masks (a pair of scalar registers
-// each) before it uses the first: x is needed here.
-template <class T>
-__device__ __forceinline__ T pinned(T x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
-
-// The heads of a token lie side by side in the pool, so the waves of a
-// workgroup take different heads of the same tokens where they can: memory is
-// then read in runs of heads x 128 codes (reading a pool of 8 heads this way
-// reaches 6.2 TB/s, with the heads in different workgroups 5.5). `heads` of a
-// workgroup's waves are heads, `rows` halves or quarters of the query rows, and
-// the others (`keys`) alternate tiles of the same head.
-struct WaveSplit {
-  int heads, rows, keys;
-};
-inline __host__ __device__ WaveSplit wave_split(const CacheProblem& p, int rows) {
-  int heads = kFewWaves / rows;
-  while (p.hkv % heads) heads >>= 1;
-  return WaveSplit{heads, rows, kFewWaves / rows / heads};
-}
-
 // The tiles of a call, one sequence after the other, form a line, which is cut
 // into equal shares; a workgroup takes one share of its heads, so that all have
 // the same work whatever the lengths. A share may hold the end of one
@@ -69,19 +45,28 @@ struct Share {
   int q0, Lq, L;    // the sequence's first query and its lengths
 };
 
-// Short sequences, by the bounds of the call, are taken whole if they are
-// enough to fill the chip: there is nothing to even out, and nothing to join.
-inline CacheProblem dealt(CacheProblem p, int rows) {
+// The heads of a token lie side by side in the pool, so the waves of a
+// workgroup take `heads` different heads of the same tokens, and memory is read
+// in runs of heads x 128 codes (reading a pool of 8 heads this way reaches 6.2
+// TB/s, with the heads in different workgroups 5.5); the other waves alternate
+// tiles. Short sequences, by the bounds of the call, are taken whole, with
+// fewer heads a workgroup where those would not fill the chip: joining parts
+// is a second kernel and costs about 8 us, a compute unit reads some 100 KB in
+// that time.
+inline CacheProblem dealt(CacheProblem p, int waves) {
+  p.heads = waves;
+  while (p.hkv % p.heads) p.heads >>= 1;
   const int64_t a = p.max_kv, b = (int64_t)p.window + p.max_new + p.sink;
-  if (p.splits == 0 && (a < b ? a : b) / kTile + 3 <= kWholeTiles &&
-      (int64_t)p.batch * (p.hkv / wave_split(p, rows).heads) >= kFewGroups)
+  if (p.splits == 0 && (a < b ? a : b) / kTile + 3 <= kWholeTiles >> (p.form == kCacheBf16)) {
     p.splits = 1;
+    while (p.heads > 1 && (int64_t)p.batch * (p.hkv / p.heads) < kFewGroups) p.heads >>= 1;
+  }
   return p;
 }
 
 // Shares of the line.
-inline __host__ __device__ int shares_of(const CacheProblem& p, int rows) {
-  const int groups = p.hkv / wave_split(p, rows).heads;
+inline __host__ __device__ int shares_of(const CacheProblem& p) {
+  const int groups = p.hkv / p.heads;
   return p.splits ? p.batch * p.splits : (kFewGroups + groups - 1) / groups;
 }
 
@@ -121,18 +106,9 @@ __device__ __forceinline__ bool find_share(const CacheProblem& p, int shares, in
     return out.lo < out.hi;
   }
   // tiles before each sequence, 64 of them at a time; up to 64 are looked at once
-  auto scan = [&](int n) {
-    for (int o = 1; o < 64; o <<= 1) {
-      const int u = __shfl_up(n, o, 64);
-      if (lane >= o) n += u;
-    }
-    return n;
-  };
-  int n = tiles_at(lane), incl = scan(n), total = lane_value(incl, 63);
+  int n = tiles_at(lane), incl = wave_scan(n), total = lane_value(incl, 63);
   for (int b0 = 64; b0 < p.batch; b0 += 64) {
-    int s = tiles_at(b0 + lane);
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-    total += __builtin_amdgcn_readfirstlane(s);
+    total += lane_value(wave_scan(tiles_at(b0 + lane)), 63);
   }
   out.len = max((int)(((int64_t)total + shares - 1) / shares), 1);
   out.lo = (int)min((int64_t)index * out.len, (int64_t)total);
@@ -142,7 +118,7 @@ __device__ __forceinline__ bool find_share(const CacheProblem& p, int shares, in
   for (int b0 = 0; b0 < p.batch; b0 += 64) {
     if (p.batch > 64) {
       n = tiles_at(b0 + lane);
-      incl = before + scan(n);
+      incl = before + wave_scan(n);
     }
     const uint64_t hit = __ballot(BY_SEQ ? b0 + lane == index : incl > out.lo);
     if (hit) {
@@ -157,6 +133,30 @@ __device__ __forceinline__ bool find_share(const CacheProblem& p, int shares, in
     before = lane_value(incl, 63);
   }
   return false;
+}
+
+// Where the keys of a tile lie: the pages of its two groups of 16 and the
+// places in them (GROUPED), or the page and place of key lane % 32. The table's
+// entries are kept as loaded and used a tile later, so that nothing waits for
+// them. Keys past the sequence stand on valid ones.
+struct Where {
+  int page[2], off[2];
+  __device__ __forceinline__ int64_t slot(const PageMap& pm, int u) const {
+    return (int64_t)page[u] * pm.page + off[u];
+  }
+};
+template <bool GROUPED>
+__device__ __forceinline__ Where where_at(const PageMap& pm, const int32_t* table, int tile, int last, int lane) {
+  Where a;
+  const int t0 = kTile * tile;
+#pragma unroll
+  for (int u = 0; u < (GROUPED ? 2 : 1); ++u) {
+    const int t = !GROUPED ? min(t0 + (lane & 31), last) : u && t0 + 16 > last ? t0 : t0 + 16 * u;
+    const int pg = pm.shift >= 0 ? t >> pm.shift : t / pm.page;
+    a.page[u] = GROUPED ? ld_uniform(table, pg) : table[pg];
+    a.off[u] = t - pg * pm.page;
+  }
+  return a;
 }
 
 __device__ __forceinline__ bf16x8_t codes_to_bf16(uint32_t a, uint32_t b, float s) {

@@ -26,7 +26,8 @@ namespace fp2 {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr int kWaves = 4;                 // of a workgroup (many rows)
+constexpr int kFewWaves = 8;              // waves of a workgroup (few rows)
+constexpr int kWaves = 4;                 // (many rows)
 constexpr int kCopy = 4096;               // entries of a workgroup's turn in the copy
 constexpr int kKeys = 64;                 // of a wave (many rows)
 constexpr int kChunk = kWaves * kKeys;
@@ -42,8 +43,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(CacheProblem p, con
   constexpr bool kBf16 = FORM == kCacheBf16;
   constexpr int ESZ = kBf16 ? 2 : 1;
   constexpr int KC = kBf16 ? 4 : 2;            // 16-byte chunks of a key per lane
-  const WaveSplit ws = wave_split(p, 1);
-  const int groups = p.hkv / ws.heads, index = blockIdx.x / groups, KS = ws.keys;
+  const int groups = p.hkv / p.heads, index = blockIdx.x / groups, KS = kFewWaves / p.heads;
   if (index >= shares) {   // not in place: what no query sees, and what lies past the sequences
     const int64_t turn = blockIdx.x - (int64_t)shares * groups, per = (stride + kCopy - 1) / kCopy;
     const int64_t row = turn / per, from = turn % per * kCopy;
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(CacheProblem p, con
   if (!find_share<false>(p, shares, index, sh)) return;
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h = blockIdx.x % groups * ws.heads + w % ws.heads, ks = w / ws.heads;
+  const int h = blockIdx.x % groups * p.heads + w % p.heads, ks = w / p.heads;
   const int c16 = lane & 15, kg = lane >> 4;
   const float cs = p.scale_log2 * (FORM == kCacheHead ? ld_uniform(p.k_head, h) : 1.f);
   const int64_t rowb = (int64_t)p.hkv * kHeadDim * ESZ;
@@ -109,18 +109,12 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(CacheProblem p, con
     uint32_t ks[2];
     float old;
   };
-  auto load = [&](int tile, Raw& x) {
-    const int t0 = kTile * tile;
-    x.old = old_row[min(t0 + mine, last)];
+  const int32_t* table = p.pm.table + (int64_t)b * p.pm.stride;
+  auto where = [&](int tile) { return where_at<GROUPED>(p.pm, table, tile, last, lane); };
+  auto load = [&](int tile, const Where& at, Raw& x, uint32_t on) {   // on: ~0, or 0 to read one row over and over
+    x.old = old_row[min(kTile * tile + mine, last)];
     if constexpr (GROUPED) {
-      const int32_t* row = p.pm.table + (int64_t)b * p.pm.stride;
-      int64_t s[2];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int t = u && t0 + 16 > last ? t0 : t0 + 16 * u;
-        const int pg = p.pm.shift >= 0 ? t >> p.pm.shift : t / p.pm.page;
-        s[u] = (int64_t)ld_uniform(row, pg) * p.pm.page + (t - pg * p.pm.page);
-      }
+      const int64_t s[2] = {at.slot(p.pm, 0), at.slot(p.pm, 1)};
       // the scales first: loads come back in order
       if constexpr (FORM == kCacheBlock) {
 #pragma unroll
@@ -130,14 +124,15 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(CacheProblem p, con
       for (int u = 0; u < 2; ++u) {
         const uint8_t* kb = K + s[u] * rowb;
 #pragma unroll
-        for (int c = 0; c < KC; ++c) x.k[u][c] = *(const uint4*)(kb + (koff + 64u * c));
+        for (int c = 0; c < KC; ++c) x.k[u][c] = *(const uint4*)(kb + ((koff & on) + 64u * c));
       }
     } else {
+      const int slot = (int)at.slot(p.pm, 0);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int64_t s = slot_of(p.pm, b, 0, min(t0 + 16 * u + c16, last));
+        const uint8_t* kb = K + (int64_t)__shfl(slot, 16 * u + c16, 64) * rowb + 16 * kg;
 #pragma unroll
-        for (int c = 0; c < KC; ++c) x.k[u][c] = *(const uint4*)(K + s * rowb + 16 * kg + 64 * c);
+        for (int c = 0; c < KC; ++c) x.k[u][c] = *(const uint4*)(kb + 64 * c);
       }
     }
   };
@@ -199,18 +194,22 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(CacheProblem p, con
     if (!(c16 & 1) && t0 + mine <= last) out[wrow + t0 + mine] = (in ? x.old : 0.f) + sum[0];
   };
 
-  // a tile ahead, with loads never left out (past the end they repeat the last
-  // tile): behind a load that may not have been issued the compiler can only
+  // a tile ahead, with loads never left out (past the end they repeat a
+  // row): behind a load that may not have been issued the compiler can only
   // wait for all of them
   if (lo + ks < hi) {
     Raw r0, r1;
     const int end = hi - 1;
-    load(tile_at(lo + ks), r0);
+    auto tile_to = [&](int i) { return tile_at(min(i, end)); };
+    load(tile_at(lo + ks), where(tile_at(lo + ks)), r0, ~0u);
+    Where a0 = where(tile_to(lo + ks + KS)), a1;
 #pragma unroll 1
     for (int i = lo + ks; i < hi; i += 2 * KS) {
-      load(tile_at(min(i + KS, end)), r1);
+      load(tile_to(i + KS), a0, r1, i + KS < hi ? ~0u : 0u);
+      a1 = where(tile_to(i + 2 * KS));
       step(tile_at(i), r0);
-      load(tile_at(min(i + 2 * KS, end)), r0);
+      load(tile_to(i + 2 * KS), a1, r0, i + 2 * KS < hi ? ~0u : 0u);
+      a0 = where(tile_to(i + 3 * KS));
       if (i + KS < hi) step(tile_at(i + KS), r1);
     }
   }
@@ -422,11 +421,11 @@ bool few_rows(const CacheProblem& p) { return (int64_t)p.max_new * p.g <= kFewRo
 template <int FORM>
 hipError_t launch_few(const CacheProblem& problem, const float* lse, const float* in, float* out,
                       int64_t stride, hipStream_t s) {
-  const CacheProblem p = dealt(problem, 1);
-  const int shares = shares_of(p, 1), rows = p.max_new * p.g;
+  const CacheProblem p = dealt(problem, kFewWaves);
+  const int shares = shares_of(p), rows = p.max_new * p.g;
   const int nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   const int64_t copies = in != out ? (int64_t)p.batch * p.hkv * ((stride + kCopy - 1) / kCopy) : 0;
-  const int64_t grid = (int64_t)shares * (p.hkv / wave_split(p, 1).heads) + copies;
+  const int64_t grid = (int64_t)shares * (p.hkv / p.heads) + copies;
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
   const dim3 g((unsigned)grid), t(64 * kFewWaves);
   if (FORM == kCacheBlock || p.pm.page % 16 == 0) {
