@@ -107,7 +107,9 @@ struct Shared {
   int bad[4];               // a tile's values had infinities or NaN that some row does not see
 };
 
-template <int FORM>
+// FORM: the cache's type. WIDE: pages hold a multiple of 64 tokens, so a tile
+// lies in one and its address is uniform (scalar).
+template <int FORM, bool WIDE>
 __global__ __launch_bounds__(64 * kWaves, 1) void extend_kernel(CacheProblem p, CachePartials part,
                                                                 int nq, int parts,
                                                                 uint16_t* __restrict__ out,
@@ -160,22 +162,55 @@ __global__ __launch_bounds__(64 * kWaves, 1) void extend_kernel(CacheProblem p, 
     uint4 k[NJ], v[NJ];
     uint32_t ks, vs;
   };
-  auto slots_at = [&](int i, int64_t (&s)[NJ]) {
-    const int k0 = key0_at(i);
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) s[j] = slot_of(p.pm, u.b, u.tok0, min(k0 + r0 + 32 * j, u.L - 1));
+  // Where a tile lies (WIDE), or this thread's rows of it: the table's entries
+  // as loaded (used a tile later, so that nothing waits for them) and the places
+  // in the pages. Keys past the sequence stand on valid ones.
+  struct Where {
+    int page[NJ], off[NJ];
   };
-  auto load = [&](const int64_t (&s)[NJ], Regs& x) {
+  const int32_t* table = p.pm.table + (int64_t)u.b * p.pm.stride;
+  auto where = [&](int i) {
+    Where a;
+    const int k0 = key0_at(min(i, hi - 1));      // past the end the last tile again
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int64_t at = s[j] * rowb + hoff + 16 * c;
-      x.k[j] = *(const uint4*)(p.k + at);
-      x.v[j] = *(const uint4*)(p.v + at);
+      const int t = WIDE ? k0 : min(k0 + r0 + 32 * j, u.L - 1);
+      const int pg = p.pm.shift >= 0 ? t >> p.pm.shift : t / p.pm.page;
+      a.page[j] = WIDE ? ld_uniform(table, pg) : table[pg];
+      a.off[j] = t - pg * p.pm.page;
     }
-    if constexpr (FORM == kCacheBlock) {
-      const int64_t at = (s[0] >> p.sb_shift) * p.hkv + u.h;
-      x.ks = p.k_block[at];
-      x.vs = p.v_block[at];
+    return a;
+  };
+  const uint32_t roff = (uint32_t)(r0 * rowb + 16 * c);                  // WIDE: this thread's place in a tile
+  const uint32_t soff = (uint32_t)((r0 >> p.sb_shift) * p.hkv);          // and its scale's among the tile's
+  auto load = [&](const Where& a, Regs& x) {
+    if constexpr (WIDE) {
+      const int64_t s0 = (int64_t)a.page[0] * p.pm.page + a.off[0];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const int64_t at = (s0 + 32 * j) * rowb + hoff;
+        x.k[j] = *(const uint4*)(p.k + at + roff);
+        x.v[j] = *(const uint4*)(p.v + at + roff);
+      }
+      if constexpr (FORM == kCacheBlock) {
+        const int64_t at = (s0 >> p.sb_shift) * p.hkv + u.h;
+        x.ks = (p.k_block + at)[soff];
+        x.vs = (p.v_block + at)[soff];
+      }
+    } else {
+      int64_t s[NJ];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        s[j] = (int64_t)a.page[j] * p.pm.page + a.off[j];
+        const int64_t at = s[j] * rowb + hoff + 16 * c;
+        x.k[j] = *(const uint4*)(p.k + at);
+        x.v[j] = *(const uint4*)(p.v + at);
+      }
+      if constexpr (FORM == kCacheBlock) {
+        const int64_t at = (s[0] >> p.sb_shift) * p.hkv + u.h;
+        x.ks = p.k_block[at];
+        x.vs = p.v_block[at];
+      }
     }
   };
   auto widen = [](uint4 x, uint32_t byte, uint4 (&y)[2]) {   // 16 codes -> 16 bf16
@@ -193,19 +228,21 @@ __global__ __launch_bounds__(64 * kWaves, 1) void extend_kernel(CacheProblem p, 
     y[0] = make_uint4(z[0], z[1], z[2], z[3]);
     y[1] = make_uint4(z[4], z[5], z[6], z[7]);
   };
-  auto write = [&](int i, const Regs& x) {
-    const int k0 = key0_at(i);
-    uint4* ks = sh.k[i & 1];
-    uint4* vs = sh.v[i & 1];
-    uint4 kk[2], vv[2];
-    if constexpr (kBf16) {
-      kk[0] = x.k[0], kk[1] = x.k[1], vv[0] = x.v[0], vv[1] = x.v[1];
-    } else {
-      widen(x.k[0], x.ks, kk);
-      widen(x.v[0], x.vs, vv);
-    }
+  auto write_k = [&](int i, const Regs& x) {
+    uint4 y[2];
+    if constexpr (kBf16) y[0] = x.k[0], y[1] = x.k[NJ - 1];
+    else widen(x.k[0], x.ks, y);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      sh.k[i & 1][kplace(kBf16 ? r0 + 32 * j : r0, kBf16 ? c : 2 * c + j)] = y[j];
+  };
+  auto write_v = [&](int i, const Regs& x) {
+    uint4 y[2];
+    if constexpr (kBf16) y[0] = x.v[0], y[1] = x.v[NJ - 1];
+    else widen(x.v[0], x.vs, y);
     // values that no row of the unit sees (the pool holds anything there) must
     // not meet zero probabilities; nor infinities and NaN that only some see
+    const int k0 = key0_at(min(i, hi - 1));
     if (k0 + kStep - 1 > u.first || (k0 <= u.last - p.window && k0 + kStep > p.sink)) {
       bool bad = false;
 #pragma unroll
@@ -213,17 +250,14 @@ __global__ __launch_bounds__(64 * kWaves, 1) void extend_kernel(CacheProblem p, 
         const int key = k0 + r0 + (kBf16 ? 32 * j : 0);
         const bool any = key <= u.last && (key < p.sink || key > u.first - p.window);
         const bool all = key <= u.first && (key < p.sink || key > u.last - p.window);
-        if (!any) vv[j] = make_uint4(0, 0, 0, 0);
-        else if (!all) bad |= drop_odd(vv[j]);
+        if (!any) y[j] = make_uint4(0, 0, 0, 0);
+        else if (!all) bad |= drop_odd(y[j]);
       }
-      if (bad) sh.bad[i & 3] = 1;
+      if (bad && i < hi) sh.bad[i & 3] = 1;
     }
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int r = kBf16 ? r0 + 32 * j : r0, cc = kBf16 ? c : 2 * c + j;
-      ks[kplace(r, cc)] = kk[j];
-      vs[vplace(r, cc)] = vv[j];
-    }
+    for (int j = 0; j < 2; ++j)
+      sh.v[i & 1][vplace(kBf16 ? r0 + 32 * j : r0, kBf16 ? c : 2 * c + j)] = y[j];
   };
 
   // V^T fragment of 16 keys kg and output tile dt: place i' of lane half H is
@@ -242,11 +276,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void extend_kernel(CacheProblem p, 
     return __builtin_bit_cast(bf16x8_t, (i32x4_t){a[0], a[1], b[0], b[1]});
   };
 
-  auto compute = [&](int i) {
-    const int k0 = key0_at(i);
+  // scores of tile i: element e of s[uu] is key k0 + 32 uu + 8 (e / 4) + 4 half + e % 4
+  auto qk = [&](int i, f32x16_t (&s)[2]) {
     const uint4* kt = sh.k[i & 1];
-    const uint4* vt = sh.v[i & 1];
-    f32x16_t s[2];
 #pragma unroll
     for (int uu = 0; uu < 2; ++uu) {
       s[uu] = f32x16_t{};
@@ -255,16 +287,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void extend_kernel(CacheProblem p, 
         s[uu] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
             __builtin_bit_cast(bf16x8_t, kt[kplace(32 * uu + l32, 2 * ds + half)]), qb[ds], s[uu], 0, 0, 0);
     }
-    // element e of s[uu] is key k0 + 32 uu + 8 (e / 4) + 4 half + e % 4
-    if (k0 + kStep - 1 > wfirst || (k0 <= wlast - p.window && k0 + kStep > p.sink)) {
-#pragma unroll
-      for (int uu = 0; uu < 2; ++uu)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int key = k0 + 32 * uu + 8 * (e >> 2) + 4 * half + (e & 3);
-          s[uu][e] = sees(p, pos, key) ? s[uu][e] : -INFINITY;
-        }
-    }
+  };
+  // scores become probabilities, against a maximum that moves when a score passes it by more than kTau
+  auto softmax = [&](f32x16_t (&s)[2]) {
     float mx = -INFINITY;
 #pragma unroll
     for (int uu = 0; uu < 2; ++uu)
@@ -290,6 +315,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void extend_kernel(CacheProblem p, 
         sum[e & 3] += s[uu][e];
       }
     l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  };
+  auto pv = [&](int i, const f32x16_t (&s)[2]) {
+    const uint4* vt = sh.v[i & 1];
 #pragma unroll
     for (int kg = 0; kg < 4; ++kg) {
       uint32_t pw[4];
@@ -301,52 +329,77 @@ __global__ __launch_bounds__(64 * kWaves, 1) void extend_kernel(CacheProblem p, 
       for (int dt = 0; dt < 4; ++dt)
         o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vread(vt, kg, dt), pb, o[dt], 0, 0, 0);
     }
-    if (sh.bad[i & 3]) {   // rare: what drop_odd took, to the rows that see it
-#pragma unroll 1
-      for (int k = 0; k < kStep; ++k) {
-        const int key = k0 + k;
-        const bool any = key <= u.last && (key < p.sink || key > u.first - p.window);
-        const bool all = key <= u.first && (key < p.sink || key > u.last - p.window);
-        if (!any || all) continue;
-        const uint8_t* row = p.v + slot_of(p.pm, u.b, u.tok0, key) * rowb + hoff;
+  };
+  auto masked = [&](int k0) {
+    return k0 + kStep - 1 > wfirst || (k0 <= wlast - p.window && k0 + kStep > p.sink);
+  };
+  auto mask = [&](int k0, f32x16_t (&s)[2]) {
 #pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
+    for (int uu = 0; uu < 2; ++uu)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int d = 32 * dt + 8 * (e >> 2) + 4 * half + (e & 3);
-            float x;
-            if constexpr (kBf16) x = bf16_to_f32(((const uint16_t*)row)[d]);
-            else x = (row[d] & 0x7f) == 0x7f ? __uint_as_float(0x7fc00000u) : 0.f;
-            if (!(fabsf(x) < INFINITY) && sees(p, pos, key)) o[dt][e] += x;
-          }
+      for (int e = 0; e < 16; ++e) {
+        const int key = k0 + 32 * uu + 8 * (e >> 2) + 4 * half + (e & 3);
+        s[uu][e] = pinned(sees(p, pos, key) ? s[uu][e] : -INFINITY);
       }
+  };
+  // rare: what drop_odd took, to the rows that see it
+  auto add_odd = [&](int k0) {
+#pragma unroll 1
+    for (int k = 0; k < kStep; ++k) {
+      const int key = k0 + k;
+      const bool any = key <= u.last && (key < p.sink || key > u.first - p.window);
+      const bool all = key <= u.first && (key < p.sink || key > u.last - p.window);
+      if (!any || all) continue;
+      const uint8_t* row = p.v + slot_of(p.pm, u.b, u.tok0, key) * rowb + hoff;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int d = 32 * dt + 8 * (e >> 2) + 4 * half + (e & 3);
+          float x;
+          if constexpr (kBf16) x = bf16_to_f32(((const uint16_t*)row)[d]);
+          else x = (row[d] & 0x7f) == 0x7f ? __uint_as_float(0x7fc00000u) : 0.f;
+          o[dt][e] += pinned(!(fabsf(x) < INFINITY) && sees(p, pos, key) ? x : 0.f);
+        }
     }
   };
 
-  int64_t slots[NJ];
+  // Keys run one tile ahead of values: the scores of the next tile are computed
+  // while the softmax of this one runs on the vector ALUs.
   Regs regs;
   if (tid < 4) sh.bad[tid] = 0;
   __syncthreads();
-  slots_at(lo, slots);
-  load(slots, regs);
-  write(lo, regs);
-  if (lo + 1 < hi) {
-    slots_at(lo + 1, slots);
-    load(slots, regs);
-    slots_at(min(lo + 2, hi - 1), slots);
-  }
-#pragma unroll 1
-  for (int i = lo; i < hi; ++i) {
-    lds_barrier();   // tile i is there; every wave is done with tile i - 1
+  Where at = where(lo + 1);
+  load(where(lo), regs);
+  write_k(lo, regs);
+  write_v(lo, regs);
+  load(at, regs);
+  at = where(lo + 2);
+  lds_barrier();
+  f32x16_t s[2], t[2];
+  qk(lo, s);
+  write_k(lo + 1, regs);
+  // tile i, whose scores are in x, and the scores of the next one into y
+  auto step = [&](int i, f32x16_t (&x)[2], f32x16_t (&y)[2]) {
+    lds_barrier();   // keys of tile i + 1 and values of tile i are there; all are done with those before
     if (tid == 0) sh.bad[(i + 2) & 3] = 0;   // read last for tile i - 2, written next for i + 2
-    if (i + 1 < hi) write(i + 1, regs);
-    if (i + 2 < hi) {
-      load(slots, regs);
-      slots_at(min(i + 3, hi - 1), slots);
-    }
+    // (past the end the last tile is staged again)
+    write_v(i + 1, regs);
+    load(at, regs);
+    at = where(i + 3);
     const int k0 = key0_at(i);
-    const bool none = k0 > wlast || (k0 + kStep - 1 <= wfirst - p.window && k0 >= p.sink);
-    if (!none) compute(i);
+    qk(i + 1, y);
+    if (masked(k0)) mask(k0, x);
+    softmax(x);
+    pv(i, x);
+    if (sh.bad[i & 3]) add_odd(k0);
+    write_k(i + 2, regs);
+  };
+#pragma unroll 1
+  for (int i = lo; i < hi; i += 2) {
+    step(i, s, t);
+    if (i + 1 >= hi) break;
+    step(i + 1, t, s);
   }
 
   // ---- output
@@ -433,7 +486,11 @@ hipError_t launch(const CacheProblem& p, const CachePartials& part, uint16_t* ou
   const int nq = query_tiles(p), parts = parts_for(p);
   const int64_t units = (int64_t)p.batch * p.hkv * nq;
   if (units * parts > 0x7fffffff || units * (kRows / 8) > 0x7fffffff) return hipErrorInvalidValue;
-  extend_kernel<FORM><<<(unsigned)(units * parts), 64 * kWaves, 0, s>>>(p, part, nq, parts, out, lse);
+  const dim3 grid((unsigned)(units * parts)), threads(64 * kWaves);
+  if (p.pm.page % kStep == 0)
+    extend_kernel<FORM, true><<<grid, threads, 0, s>>>(p, part, nq, parts, out, lse);
+  else
+    extend_kernel<FORM, false><<<grid, threads, 0, s>>>(p, part, nq, parts, out, lse);
   if (parts > 1) join_kernel<<<(unsigned)(units * (kRows / 8)), 256, 0, s>>>(p, part, nq, parts, out, lse);
   return hipGetLastError();
 }
