@@ -9,12 +9,11 @@
 // holds one query and eight keys, whose sums over the 16 lanes of a group take
 // eight exchanges.
 //
-// many_kernel: a workgroup takes 256 keys, a wave 64 of them as the A operand
-// of S^T = K Q^T (v_mfma_f32_32x32x16_bf16), which stay in registers while the
+// many_kernel: a workgroup takes 256 keys, a wave 64 of them as the B operand
+// of S = Q K^T (v_mfma_f32_32x32x16_bf16), which stay in registers while the
 // packed query rows that see them pass by, 32 at a time, through LDS. A lane
-// holds one query and 32 keys and adds its probabilities in fp32; at the end
-// the 32 sums of a lane are exchanged and added over the lanes, half of them a
-// step. Bound by the products and the exponentials, half of the attention's
+// holds two keys with 16 queries each, whose probabilities it adds in fp32; its
+// sums take two registers (with keys as rows they took 32). Bound by the products and the exponentials, half of the attention's
 // work. Where the keys alone do not fill the chip the rows are cut into
 // segments too, whose sums sum_kernel adds in their order.
 #include <algorithm>
@@ -24,6 +23,10 @@
 namespace fp2 {
 
 namespace {
+
+#ifndef MOCC
+#define MOCC 3
+#endif
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kFewWaves = 8;              // waves of a workgroup (few rows)
@@ -242,7 +245,7 @@ __device__ __forceinline__ Steps steps_of(const CacheProblem& p, int c0, int Lq,
 
 // segs == 1: sums join `in` and go to `out`; else to part[seg][sequence, head][key].
 template <int FORM>
-__global__ __launch_bounds__(64 * kWaves, 3) void many_kernel(CacheProblem p,
+__global__ __launch_bounds__(64 * kWaves, MOCC) void many_kernel(CacheProblem p,
                                                               const float* __restrict__ lse,
                                                               const float* in, float* out,
                                                               int64_t stride, float* part, int segs,
@@ -275,9 +278,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void many_kernel(CacheProblem p,
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, l32 = lane & 31;
   const int k0 = c0 + kKeys * w;              // the wave's first key
-  float acc[32];
-#pragma unroll
-  for (int i = 0; i < 32; ++i) acc[i] = 0.f;
+  float acc[2] = {0.f, 0.f};
 
   if (from < to) {
     const int64_t rowb = (int64_t)p.hkv * kHeadDim * ESZ;
@@ -338,7 +339,6 @@ __global__ __launch_bounds__(64 * kWaves, 3) void many_kernel(CacheProblem p,
       if (t + 2 < to) LOAD(t + 2);
       const int first = P + ((kRows * t) >> gs), last = P + ((min(kRows * t + kRows, rows) - 1) >> gs);
       if (last < k0) continue;                           // (uniform) none of the wave's keys is seen
-      const float ref = sh.lse[t & 1][l32];
       f32x16_t s[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) s[u] = f32x16_t{};
@@ -349,41 +349,42 @@ __global__ __launch_bounds__(64 * kWaves, 3) void many_kernel(CacheProblem p,
         const bf16x8_t q = __builtin_bit_cast(bf16x8_t, sh.q[t & 1][place(l32, ch)]);
 #pragma unroll
         for (int u = 0; u < 2; ++u)
-          s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[u][d], q, s[u], 0, 0, 0);
+          s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, a[u][d], s[u], 0, 0, 0);
       }
+      // element e is row 8 (e / 4) + 4 half + e % 4 of the step, key k0 + 32 u + l32
       if (k0 + kKeys - 1 > first || kRows * t + kRows > rows ||
           (k0 <= last - p.window && k0 + kKeys > p.sink)) {
-        const int pr = kRows * t + l32;
-        const int pos = pr < rows ? P + (pr >> gs) : -1;   // a row past the last sees nothing
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const int e = i & 15, key = k0 + 32 * (i >> 4) + 8 * (e >> 2) + 4 * half + (e & 3);
-          s[i >> 4][e] = sees(p, pos, key) ? s[i >> 4][e] : -INFINITY;
-          s[i >> 4][e] = pinned(s[i >> 4][e]);
+        for (int e = 0; e < 16; ++e) {
+          const int pr = kRows * t + 8 * (e >> 2) + 4 * half + (e & 3);
+          const int pos = pr < rows ? P + (pr >> gs) : -1;   // a row past the last sees nothing
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+            s[u][e] = pinned(sees(p, pos, k0 + 32 * u + l32) ? s[u][e] : -INFINITY);
         }
       }
 #pragma unroll
-      for (int i = 0; i < 32; ++i) acc[i] += fast_exp2(fmaf(s[i >> 4][i & 15], cs, -ref));
+      for (int i = 0; i < 4; ++i) {
+        const float4 z = *(const float4*)&sh.lse[t & 1][8 * i + 4 * half];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          acc[u] += (fast_exp2(fmaf(s[u][4 * i], cs, -z.x)) + fast_exp2(fmaf(s[u][4 * i + 1], cs, -z.y))) +
+                    (fast_exp2(fmaf(s[u][4 * i + 2], cs, -z.z)) + fast_exp2(fmaf(s[u][4 * i + 3], cs, -z.w)));
+      }
     }
 #undef LOAD
 #undef STORE
   }
-  // sums over the 32 lanes of a half: lane l32 keeps that of element l32
-#pragma unroll
-  for (int n = 16; n > 0; n >>= 1) {
-    const bool up = l32 & n;
-#pragma unroll
-    for (int j = 0; j < n; ++j) {
-      const float send = up ? acc[j] : acc[j + n], keep = up ? acc[j + n] : acc[j];
-      acc[j] = keep + __shfl_xor(send, n, 64);
-    }
-  }
-  const int e = l32 & 15, key = k0 + 32 * (l32 >> 4) + 8 * (e >> 2) + 4 * half + (e & 3);
+  // the halves of a wave hold other rows of the same keys; each keeps one of the two
+  acc[0] += __shfl_xor(acc[0], 32, 64);
+  acc[1] += __shfl_xor(acc[1], 32, 64);
+  const float sum = half ? acc[1] : acc[0];
+  const int key = k0 + lane;
   const int64_t bh = (int64_t)b * p.hkv + h;
   if (segs > 1) {
-    part[((int64_t)seg * p.batch * p.hkv + bh) * ((int64_t)chunks * kChunk) + key] = acc[0];
+    part[((int64_t)seg * p.batch * p.hkv + bh) * ((int64_t)chunks * kChunk) + key] = sum;
   } else if (key < L || (in != out && key < stride)) {
-    out[bh * stride + key] = (in ? in[bh * stride + key] : 0.f) + (key < L ? acc[0] : 0.f);
+    out[bh * stride + key] = (in ? in[bh * stride + key] : 0.f) + (key < L ? sum : 0.f);
   }
 }
 
