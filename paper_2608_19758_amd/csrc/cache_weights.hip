@@ -24,10 +24,6 @@ namespace fp2 {
 
 namespace {
 
-#ifndef MOCC
-#define MOCC 3
-#endif
-
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kFewWaves = 8;              // waves of a workgroup (few rows)
 constexpr int kWaves = 4;                 // (many rows)
@@ -245,7 +241,7 @@ __device__ __forceinline__ Steps steps_of(const CacheProblem& p, int c0, int Lq,
 
 // segs == 1: sums join `in` and go to `out`; else to part[seg][sequence, head][key].
 template <int FORM>
-__global__ __launch_bounds__(64 * kWaves, MOCC) void many_kernel(CacheProblem p,
+__global__ __launch_bounds__(64 * kWaves, 3) void many_kernel(CacheProblem p,
                                                               const float* __restrict__ lse,
                                                               const float* in, float* out,
                                                               int64_t stride, float* part, int segs,
@@ -399,9 +395,12 @@ __global__ __launch_bounds__(kChunk) void sum_kernel(CacheProblem p, const float
   if (key >= (in != out ? stride : (int64_t)L)) return;
   const Steps st = steps_of(p, c0, ld_uniform(p.cu, b + 1) - ld_uniform(p.cu, b), L);
   float sum = 0.f;
-  for (int s = 0; s < segs; ++s)
-    if (key < L && max(st.from, s * seg_steps) < min(st.to, (s + 1) * seg_steps))
+  const int s0 = st.from / seg_steps, s1 = key < L ? (st.to + seg_steps - 1) / seg_steps : s0;
+  if (st.from < st.to) {
+#pragma unroll 8
+    for (int s = s0; s < s1; ++s)
       sum += part[((int64_t)s * p.batch * p.hkv + bh) * ((int64_t)chunks * kChunk) + key];
+  }
   const int64_t to = (int64_t)bh * stride + key;
   out[to] = (in ? in[to] : 0.f) + sum;
 }
