@@ -475,10 +475,12 @@ typedef struct {
 
 /* Bytes of workspace (256-byte aligned) that fp2_cache_attend and
  * fp2_cache_weights need for `params`: the partial results of sequences whose
- * keys (or queries) are cut into parts, at most 140 MB where kv_splits is 0. 0
- * where none is needed, and for an invalid params. One workspace serves calls
+ * keys (or queries) are cut into parts, at most FP2_CACHE_WORKSPACE_MAX where
+ * kv_splits is 0 (a smaller call may need more than a larger one). 0 where
+ * none is needed, and for an invalid params. One workspace serves calls
  * in order on a stream; calls that overlap, and graphs that may, need their
  * own. */
+#define FP2_CACHE_WORKSPACE_MAX ((size_t)140 << 20)
 size_t fp2_cache_workspace_bytes(const fp2_cache_params_t* params);
 
 /* Writes the new tokens' keys and values, bf16 [cu_seqlens[batch],

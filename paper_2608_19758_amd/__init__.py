@@ -495,5 +495,6 @@ def mask_to_csr(p: Params, block_mask, cu_seqlens, *, cu_seqlens_k=None, cu_seql
 
 
 # the paged cache's operators
-from .cache import (KVCache, alloc_cache, alloc_cache_workspace, cache_append, cache_attend,  # noqa: E402,F401
-                    cache_evict, cache_weights, cache_workspace_bytes, make_cache_params)
+from .cache import (CACHE_WORKSPACE_MAX, CacheParams, KVCache, alloc_cache,  # noqa: E402,F401
+                    alloc_cache_workspace, cache_append, cache_attend, cache_evict, cache_weights,
+                    cache_workspace_bytes, make_cache_params)

@@ -10,6 +10,7 @@ for it.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import dataclasses
 from typing import Optional
@@ -17,6 +18,9 @@ from typing import Optional
 import torch
 
 from . import _F32, _INT32, BF16, FP8_E4M3, HEAD_DIM, _check, _host_ptr, lib
+
+
+CACHE_WORKSPACE_MAX = 140 << 20     # FP2_CACHE_WORKSPACE_MAX
 
 
 class CacheParams(ctypes.Structure):
@@ -183,6 +187,12 @@ class _Args:
         _check(name, st)
 
 
+def on_stream(stream):
+    """What is allocated for a call belongs to the stream that it runs on: the allocator may give the
+    memory to later work there, and to no other stream's."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def cache_append(p: CacheParams, k_new, v_new, cache: KVCache, cu_seqlens, cu_seqlens_k, block_table,
                  *, cu_seqlens_host=None, cu_seqlens_k_host=None, stream=None) -> None:
     """fp2_cache_append: k_new and v_new bf16 [new tokens, num_kv_heads, 128] into the
@@ -209,12 +219,13 @@ def cache_attend(p: CacheParams, q, cache: KVCache, cu_seqlens, cu_seqlens_k, bl
     c = a.cache(p, cache)
     lens = a.lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host)
     table = a.table(p, "block_table", block_table, p.max_pages_per_seq)
-    if out is None:
-        out = torch.empty_like(q)
-    if lse is None and want_lse:
-        lse = torch.empty((rows, p.num_q_heads), dtype=torch.float32, device=q.device)
-    if workspace is None:
-        workspace = alloc_cache_workspace(p, q.device)
+    with on_stream(stream):
+        if out is None:
+            out = torch.empty_like(q)
+        if lse is None and want_lse:
+            lse = torch.empty((rows, p.num_q_heads), dtype=torch.float32, device=q.device)
+        if workspace is None:
+            workspace = alloc_cache_workspace(p, q.device)
     op, lp = a("out", out, _BF16, q.numel()), a("lse", lse, _F32, rows * p.num_q_heads)
     ws = a("workspace", workspace, _BYTES)
     a.call("fp2_cache_attend", stream, ctypes.byref(p), qp, *lens, ctypes.byref(c), table, op, lp, ws,
@@ -236,14 +247,15 @@ def cache_weights(p: CacheParams, q, lse, cache: KVCache, cu_seqlens, cu_seqlens
     lens = a.lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host)
     table = a.table(p, "block_table", block_table, p.max_pages_per_seq)
     wi = a.weights(p, "weights_in", weights_in)
-    if weights is None:
-        shape = (p.batch, p.num_kv_heads, p.max_kv_len if weights_in is None else weights_in.shape[2])
-        weights = torch.empty(shape, dtype=torch.float32, device=q.device)
+    with on_stream(stream):
+        if weights is None:
+            shape = (p.batch, p.num_kv_heads, p.max_kv_len if weights_in is None else weights_in.shape[2])
+            weights = torch.empty(shape, dtype=torch.float32, device=q.device)
+        if workspace is None:
+            workspace = alloc_cache_workspace(p, q.device)
     w = a.weights(p, "weights", weights)
     if weights_in is not None and weights_in.shape[2] != weights.shape[2]:
         raise ValueError("weights and weights_in differ in their last size")
-    if workspace is None:
-        workspace = alloc_cache_workspace(p, q.device)
     ws = a("workspace", workspace, _BYTES)
     a.call("fp2_cache_weights", stream, ctypes.byref(p), qp, lp, *lens, ctypes.byref(c), table, wi, w,
            weights.shape[2], ws, workspace.numel())
@@ -264,12 +276,13 @@ def cache_evict(p: CacheParams, cache: KVCache, weights, cu_seqlens_k, block_tab
     target = a.table(p, "target_table", target_table, pages)
     w = a.weights(p, "weights", weights)
     dev, heads = cache.k.device, p.batch * p.num_kv_heads
-    if kept is None:
-        kept = torch.empty((p.batch, p.num_kv_heads, max(1, budget)), dtype=torch.int32, device=dev)
-    if cu_seqlens_k_out is None:
-        cu_seqlens_k_out = torch.empty(p.batch + 1, dtype=torch.int32, device=dev)
-    if weights_out is None:
-        weights_out = torch.empty_like(weights)
+    with on_stream(stream):
+        if kept is None:
+            kept = torch.empty((p.batch, p.num_kv_heads, max(1, budget)), dtype=torch.int32, device=dev)
+        if cu_seqlens_k_out is None:
+            cu_seqlens_k_out = torch.empty(p.batch + 1, dtype=torch.int32, device=dev)
+        if weights_out is None:
+            weights_out = torch.empty((p.batch, p.num_kv_heads, weights.shape[2]), dtype=torch.float32, device=dev)
     wo = a.weights(p, "weights_out", weights_out)
     if weights_out.shape[2] != weights.shape[2]:
         raise ValueError("weights and weights_out differ in their last size")

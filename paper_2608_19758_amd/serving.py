@@ -1,4 +1,5 @@
-"""Serving-engine attention backend for the extend (prefill) phase.
+"""Serving-engine attention backends: the sparse extend (prefill) phase, and the
+dense paged cache that decoding goes on from.
 
 The shape a continuous-batching engine needs around fp2_prefill (Sec. 4: the
 sparse operator serves every extend of a request, chunked prefill included,
@@ -26,9 +27,18 @@ while decode attention stays dense):
 Cached prefixes may have any length (a prefix-cache hit is page-granular);
 ``plan_forward`` checks the lengths against the configured bounds before
 anything reaches the GPU.
+
+``CacheConfig`` and ``CacheBackend`` are the same shape around the fp2_cache_*
+operators: a forward of any mix of prompts, chunks and single tokens appends
+the new keys and values to each layer's cache, attends over it and, where the
+engine wants to shorten sequences later, adds up what every cached token
+received; ``evict`` then keeps the heaviest ``budget`` tokens of each sequence
+and KV head in new pages. A cache of codes with a scale per head is what
+``PrefillBackend`` reads, so a prompt may be extended sparsely and decoded here.
 """
 from __future__ import annotations
 
+import ctypes
 import dataclasses
 from typing import List, Optional, Sequence
 
@@ -127,6 +137,22 @@ class ForwardMetadata:
         return self.plan.params
 
 
+def _dense_table(block_table, n: int, w: int):
+    """The first n rows of an engine's page table as a dense one of w pages."""
+    import torch
+    if not (isinstance(block_table, torch.Tensor) and block_table.is_cuda
+            and block_table.dtype == torch.int32 and block_table.dim() == 2):
+        raise ValueError("block_table must be a CUDA int32 tensor [batch, pages]")
+    if block_table.shape[1] < w or block_table.shape[0] < n:
+        raise ValueError("block_table is %s, the forward needs [>= %d, >= %d]"
+                         % (tuple(block_table.shape), n, w))
+    # the library reads row b at b * max_pages_per_seq: hand it a dense
+    # table of exactly that width (a copy when the caller's is wider or strided)
+    if block_table.shape[1] != w or not block_table.is_contiguous():
+        block_table = block_table[:n, :w].contiguous()
+    return block_table
+
+
 class PrefillBackend:
     """Extend-phase attention of one stream (see the module docstring)."""
 
@@ -165,17 +191,7 @@ class PrefillBackend:
         pooled = np.array([c // BLOCK for c in cached], np.int32)
         host = np.concatenate([plan.cu_q, plan.cu_k, pooled]).astype(np.int32)
         dev = torch.from_numpy(host).to(self.device)
-        w = self.cfg.max_pages_per_seq
-        if not (isinstance(block_table, torch.Tensor) and block_table.is_cuda
-                and block_table.dtype == torch.int32 and block_table.dim() == 2):
-            raise ValueError("block_table must be a CUDA int32 tensor [batch, pages]")
-        if block_table.shape[1] < w or block_table.shape[0] < n:
-            raise ValueError("block_table is %s, the forward needs [>= %d, >= %d]"
-                             % (tuple(block_table.shape), n, w))
-        # the library reads row b at b * max_pages_per_seq: hand it a dense
-        # table of exactly that width (a copy when the caller's is wider or strided)
-        if block_table.shape[1] != w or not block_table.is_contiguous():
-            block_table = block_table[:n, :w].contiguous()
+        block_table = _dense_table(block_table, n, self.cfg.max_pages_per_seq)
         return ForwardMetadata(plan=plan, cu_q=dev[:n + 1], cu_k=dev[n + 1:2 * n + 2],
                                block_table=block_table, pooled_blocks=dev[2 * n + 2:])
 
@@ -219,3 +235,156 @@ class PrefillBackend:
 
     def forward_decode(self, *args, **kwargs):
         raise NotImplementedError("decode attention stays dense; this backend serves extends")
+
+
+@dataclasses.dataclass(frozen=True)
+class CacheConfig:
+    num_q_heads: int
+    num_kv_heads: int
+    page_size: int                 # tokens per KV page
+    max_batch: int                 # sequences per forward
+    max_extend_len: int            # new tokens of one sequence in one forward
+    max_kv_len: int                # cached + new tokens of one sequence
+    dtype: str = "bf16"            # of the cache: "bf16" | "fp8"
+    scale_tokens: int = 0          # fp8: tokens per power-of-two scale, 0: a scale per head
+    sink_tokens: int = 0           # first tokens that stay visible and are never evicted
+    window_tokens: int = 0         # 0: every earlier token is visible
+    softmax_scale: float = 0.0     # <= 0: 1/sqrt(128)
+
+    @property
+    def max_pages_per_seq(self) -> int:
+        return (self.max_kv_len + self.page_size - 1) // self.page_size
+
+    def params(self, batch: int, max_extend: int, max_kv: int) -> "fp2.CacheParams":
+        return fp2.make_cache_params(
+            batch=batch, num_q_heads=self.num_q_heads, num_kv_heads=self.num_kv_heads,
+            max_seq_len=max_extend, max_kv_len=max_kv, page_size=self.page_size,
+            max_pages_per_seq=self.max_pages_per_seq, dtype=self.dtype,
+            scale_tokens=self.scale_tokens, sink_tokens=self.sink_tokens,
+            window_tokens=self.window_tokens, softmax_scale=self.softmax_scale)
+
+    def worst_case_params(self) -> "fp2.CacheParams":
+        return self.params(self.max_batch, self.max_extend_len, self.max_kv_len)
+
+
+@dataclasses.dataclass
+class CacheMetadata:
+    plan: ForwardPlan
+    lengths: object                # device int32: cu_q and cu_k side by side
+    block_table: object            # device int32 [batch or more, max_pages_per_seq], dense
+
+    @property
+    def params(self):
+        return self.plan.params
+
+    @property
+    def cu_q(self):
+        return self.lengths[:len(self.plan.cu_q)]
+
+    @property
+    def cu_k(self):
+        return self.lengths[len(self.plan.cu_q):]
+
+
+class CacheBackend:
+    """Attention of one stream over paged caches, decoding included (see the
+    module docstring). It owns one workspace that fits every forward; calls
+    that overlap, and graphs that may, need backends of their own. Work runs
+    on `stream` (None: the current one of the device); the caller orders its
+    own tensors with it."""
+
+    def __init__(self, cfg: CacheConfig, device="cuda", stream=None):
+        import torch
+        self.cfg = cfg
+        self.device = torch.device(device)
+        self.stream = stream
+        if not 0 <= cfg.max_extend_len <= cfg.max_kv_len:
+            raise ValueError("max_extend_len %d outside [0, max_kv_len = %d]"
+                             % (cfg.max_extend_len, cfg.max_kv_len))
+        # a call without new tokens checks its parameters and has nothing to do
+        idle = cfg.params(cfg.max_batch, 0, cfg.max_kv_len)
+        if fp2.lib().fp2_cache_append(ctypes.byref(idle), *[None] * 9):
+            raise ValueError("configuration rejected by the library: " + fp2.last_error())
+        self.workspace = torch.empty(fp2.CACHE_WORKSPACE_MAX, dtype=torch.uint8, device=self.device)
+
+    def alloc_cache(self, num_pages: int, k_scale=None, v_scale=None) -> "fp2.KVCache":
+        """One layer's empty cache of num_pages pages."""
+        return fp2.alloc_cache(self.cfg.worst_case_params(), num_pages, self.device, k_scale, v_scale)
+
+    def alloc_weights(self):
+        """One layer's weights of empty sequences: zeros [max_batch, num_kv_heads, max_kv_len]."""
+        import torch
+        c = self.cfg
+        return torch.zeros((c.max_batch, c.num_kv_heads, c.max_kv_len), device=self.device)
+
+    def init_forward_metadata(self, extend_lens: Sequence[int], prefix_lens: Optional[Sequence[int]],
+                              block_table, replayed: bool = False) -> CacheMetadata:
+        """Once per forward, for all layers. replayed: the forward is captured in a graph
+        and replayed after update_forward_metadata; its bounds are then the longest of
+        these extends and the config's max_kv_len instead of these lengths'."""
+        import torch
+        plan = plan_forward(self.cfg, extend_lens, prefix_lens)
+        if replayed:
+            plan.params = self.cfg.params(plan.params.batch, plan.params.max_seq_len, self.cfg.max_kv_len)
+        with fp2.cache.on_stream(self.stream):
+            lengths = torch.from_numpy(np.concatenate([plan.cu_q, plan.cu_k])).to(self.device)
+            table = _dense_table(block_table, len(plan.cu_q) - 1, self.cfg.max_pages_per_seq)
+            if replayed:
+                table = table.clone()
+        return CacheMetadata(plan=plan, lengths=lengths, block_table=table)
+
+    def update_forward_metadata(self, meta: CacheMetadata, extend_lens: Sequence[int],
+                                prefix_lens: Optional[Sequence[int]], block_table) -> None:
+        """Other lengths and pages for a captured forward (metadata made with
+        replayed=True): as many sequences, extends within the first one's bound."""
+        import torch
+        plan = plan_forward(self.cfg, extend_lens, prefix_lens)
+        p = meta.params
+        if p.max_kv_len != self.cfg.max_kv_len:
+            raise ValueError("the metadata was not made with replayed=True")
+        if plan.params.batch != p.batch or plan.params.max_seq_len > p.max_seq_len:
+            raise ValueError("%d sequences with extends up to %d do not fit a forward of %d with up to %d"
+                             % (plan.params.batch, plan.params.max_seq_len, p.batch, p.max_seq_len))
+        plan.params = p
+        with fp2.cache.on_stream(self.stream):
+            meta.lengths.copy_(torch.from_numpy(np.concatenate([plan.cu_q, plan.cu_k])))
+            meta.block_table[:p.batch].copy_(
+                _dense_table(block_table, p.batch, self.cfg.max_pages_per_seq)[:p.batch])
+        meta.plan = plan
+
+    def forward(self, q, k_new, v_new, cache: "fp2.KVCache", meta: CacheMetadata, *, out=None, lse=None,
+                want_lse=False, weights=None):
+        """One layer: k_new and v_new bf16 [new tokens, Hkv, 128] go into the cache, q
+        [new tokens, Hq, 128] attends over it. weights (as from alloc_weights): what the
+        cached tokens received of these queries is added to it, row b for sequence b.
+        Returns (out, lse or None)."""
+        for name, t in (("q", q), ("k_new", k_new), ("v_new", v_new)):
+            if t.shape[0] < meta.plan.total_tokens:
+                raise ValueError("%s has %d rows, the forward has %d new tokens"
+                                 % (name, t.shape[0], meta.plan.total_tokens))
+        p, lens = meta.params, (meta.cu_q, meta.cu_k, meta.block_table)
+        host = dict(cu_seqlens_host=meta.plan.cu_q, cu_seqlens_k_host=meta.plan.cu_k, stream=self.stream)
+        fp2.cache_append(p, k_new, v_new, cache, *lens, **host)
+        out, lse = fp2.cache_attend(p, q, cache, *lens, out=out, lse=lse,
+                                    want_lse=want_lse or weights is not None,
+                                    workspace=self.workspace, **host)
+        if weights is not None:
+            fp2.cache_weights(p, q, lse, cache, *lens, weights=weights, weights_in=weights,
+                              workspace=self.workspace, **host)
+        return out, lse
+
+    def evict(self, cache: "fp2.KVCache", weights, meta: CacheMetadata, target_table, *, budget: int,
+              recent_tokens: int = 0):
+        """One layer, after a forward: the sequences of `meta` are cut to `budget` tokens per
+        KV head, in the pages of target_table (int32 [batch, pages]). Returns (the tokens
+        that stay, int32 [batch, Hkv, budget], their weights); the sequences' new lengths
+        are evicted_lens(meta, budget)."""
+        kept, _, w = fp2.cache_evict(meta.params, cache, weights, meta.cu_k, meta.block_table, target_table,
+                                     budget=budget, recent_tokens=recent_tokens,
+                                     cu_seqlens_k_host=meta.plan.cu_k, stream=self.stream)
+        return kept, w
+
+
+def evicted_lens(meta: CacheMetadata, budget: int) -> List[int]:
+    """Cached tokens of each sequence after an eviction to `budget`."""
+    return [min(int(n), budget) for n in np.diff(meta.plan.cu_k)]

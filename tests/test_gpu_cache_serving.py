@@ -1,0 +1,195 @@
+"""The cache backend on the GPU: forwards of layers through shared metadata against
+the operators called one by one, captured decode steps, eviction, and a prompt
+that the sparse backend extends over the cache which this one goes on with."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_19758_amd as fp2
+from paper_2608_19758_amd import serving
+from tests import cache_ref as ref
+from tests.test_gpu_cache import close, cu_of, dev
+
+pytestmark = pytest.mark.gpu
+
+HQ, HKV, PAGE = 8, 2, 64
+
+
+def config(form, **kw):
+    d = dict(num_q_heads=HQ, num_kv_heads=HKV, page_size=PAGE, max_batch=3, max_extend_len=600,
+             max_kv_len=1024, dtype="bf16" if form == "bf16" else "fp8",
+             scale_tokens=form if isinstance(form, int) else 0)
+    d.update(kw)
+    return serving.CacheConfig(**d)
+
+
+def scales(form):
+    return [torch.tensor([0.01, 0.013], device="cuda")] * 2 if form == "head" else [None, None]
+
+
+def tables(cfg, n, seed):
+    """n disjoint page tables [max_batch, pages], wider than the config needs."""
+    w = cfg.max_pages_per_seq
+    order = np.random.default_rng(seed).permutation(n * cfg.max_batch * w).astype(np.int32)
+    t = np.zeros((n, cfg.max_batch, w + 2), np.int32)
+    t[:, :, :w] = order.reshape(n, cfg.max_batch, w)
+    return dev(t), n * cfg.max_batch * w
+
+
+def rows(g, n):
+    return [torch.randn((n, h, 128), generator=g).bfloat16().cuda() for h in (HQ, HKV, HKV)]
+
+
+def call(cfg, ext, pre, table, cache, x, weights, max_kv):
+    """One layer by the operators themselves."""
+    p = cfg.params(len(ext), max(ext), max_kv)
+    args = (dev(cu_of(ext)), dev(cu_of([a + b for a, b in zip(ext, pre)])),
+            table[:len(ext), :cfg.max_pages_per_seq].contiguous())
+    fp2.cache_append(p, x[1], x[2], cache, *args)
+    out, lse = fp2.cache_attend(p, x[0], cache, *args, want_lse=True)
+    fp2.cache_weights(p, x[0], lse, cache, *args, weights=weights, weights_in=weights)
+    return out, lse
+
+
+def equal(a, b):
+    for n in ("k", "v", "k_scale", "v_scale"):
+        x, y = getattr(a, n), getattr(b, n)
+        assert (x is None and y is None) or torch.equal(x.view(torch.uint8), y.view(torch.uint8)), n
+
+
+@pytest.mark.parametrize("form", ["bf16", "head", 16, 64])
+@pytest.mark.parametrize("own_stream", [False, True])
+def test_forwards_and_eviction(form, own_stream):
+    cfg = config(form, window_tokens=300, sink_tokens=4)
+    stream = torch.cuda.Stream() if own_stream else None
+    be = serving.CacheBackend(cfg, stream=stream)
+    (table, target), pages = tables(cfg, 2, 3)
+    g = torch.Generator().manual_seed(1)
+    layers = [(be.alloc_cache(pages, *scales(form)), be.alloc_weights()) for _ in range(2)]
+    plain = [(be.alloc_cache(pages, *scales(form)), be.alloc_weights()) for _ in range(2)]
+    pre = [0, 0, 0]
+    for ext in ([600, 71, 1], [1, 1, 1], [40, 0, 3], [1, 1]):
+        prefix = pre[:len(ext)]
+        torch.cuda.synchronize()
+        meta = be.init_forward_metadata(ext, prefix, table)
+        for (cache, w), (cache2, w2) in zip(layers, plain):
+            x = rows(g, sum(ext))
+            torch.cuda.synchronize()
+            out, lse = be.forward(*x, cache, meta, weights=w)
+            torch.cuda.synchronize()
+            total = max(a + b for a, b in zip(ext, prefix))
+            want, want_lse = call(cfg, ext, prefix, table, cache2, x, w2, total)
+            assert torch.equal(out, want) and torch.equal(lse, want_lse) and torch.equal(w, w2)
+            equal(cache, cache2)
+        pre = [a + b for a, b in zip(ext, prefix)] + pre[len(ext):]
+    # the last forward had two sequences: those are cut, and go on in their new pages
+    torch.cuda.synchronize()
+    kept, left = be.evict(*layers[0], meta, target[:, :4].contiguous(), budget=200, recent_tokens=50)
+    torch.cuda.synchronize()
+    p = meta.params
+    kept2, cu, left2 = fp2.cache_evict(p, plain[0][0], plain[0][1], meta.cu_k, meta.block_table,
+                                       target[:, :4].contiguous(), budget=200, recent_tokens=50)
+    assert torch.equal(kept, kept2) and torch.equal(left, left2) and left.shape[0] == 2
+    equal(layers[0][0], plain[0][0])
+    lens = serving.evicted_lens(meta, 200)
+    assert cu.tolist() == [0, lens[0], lens[0] + lens[1]] and lens == [200, 73]
+    meta = be.init_forward_metadata([1, 2], lens, target)
+    x = rows(g, 3)
+    torch.cuda.synchronize()
+    out, _ = be.forward(*x, layers[0][0], meta, weights=left)
+    torch.cuda.synchronize()
+    want, _ = call(cfg, [1, 2], lens, target, plain[0][0], x, left2, 201)
+    assert torch.equal(out, want) and torch.equal(left, left2)
+
+
+@pytest.mark.parametrize("form", ["bf16", 64])
+def test_captured_decode(form):
+    """A decode step captured once and replayed with other lengths and pages."""
+    cfg = config(form)
+    be, eager = serving.CacheBackend(cfg), serving.CacheBackend(cfg)
+    (table,), pages = tables(cfg, 1, 4)
+    g = torch.Generator().manual_seed(2)
+    a, b = ((be.alloc_cache(pages), be.alloc_weights()) for _ in "ab")
+    lens = [70, 500, 3]
+    x = rows(g, sum(lens))
+    for e, (cache, w) in ((be, a), (eager, b)):
+        e.forward(*x, cache, e.init_forward_metadata(lens, None, table), weights=w)
+    meta = be.init_forward_metadata([1, 1, 1], lens, table, replayed=True)
+    static, out = rows(g, 3), torch.zeros((3, HQ, 128), dtype=torch.bfloat16, device="cuda")
+    saved = [t.clone() for t in (a[0].k, a[0].v, a[1])] + \
+        [None if t is None else t.clone() for t in (a[0].k_scale, a[0].v_scale)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        be.forward(*static, a[0], meta, out=out, weights=a[1])
+    for t, s in zip((a[0].k, a[0].v, a[1], a[0].k_scale, a[0].v_scale), saved):
+        assert t is None or torch.equal(t.view(torch.uint8), s.view(torch.uint8))    # captured, not run
+    order = [0, 1, 2]
+    for step in range(5):
+        if step == 3:                                  # the same sequences in another order
+            order = [2, 0, 1]
+            lens, tab = [lens[i] for i in order], table[order]
+            a[1].copy_(a[1][order]), b[1].copy_(b[1][order])
+        tab = table[order]
+        be.update_forward_metadata(meta, [1, 1, 1], lens, tab)
+        x = rows(g, 3)
+        for s, t in zip(static, x):
+            s.copy_(t)
+        graph.replay()
+        float(torch.randn(1 << 18, device="cuda").sum())
+        m2 = eager.init_forward_metadata([1, 1, 1], lens, tab, replayed=True)
+        want, _ = eager.forward(*x, b[0], m2, weights=b[1])
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(a[1], b[1]), step
+        equal(a[0], b[0])
+        lens = [n + 1 for n in lens]
+    with pytest.raises(ValueError, match="fit"):
+        be.update_forward_metadata(meta, [2, 1, 1], lens, table)
+    with pytest.raises(ValueError, match="replayed"):
+        be.update_forward_metadata(be.init_forward_metadata([1], [5], table), [1], [6], table)
+    with pytest.raises(ValueError, match="rows"):
+        be.forward(*[t[:2] for t in static], a[0], meta)
+
+
+@pytest.mark.parametrize("form", ["bf16", "head"])
+def test_after_a_sparse_prompt(form):
+    """A prompt of four blocks, all of them kept, extended by the sparse backend over the cache that
+    cache_append filled; then decoded. Its bars against dense attention are those of the sparse
+    kernels' parity tests: 2e-2, in codes 6e-2."""
+    n, cfg = 500, config(form)
+    be = serving.CacheBackend(cfg)
+    sparse = serving.PrefillBackend(serving.BackendConfig(
+        num_q_heads=HQ, num_kv_heads=HKV, page_size=PAGE, max_batch=1, max_extend_len=600, max_kv_len=1024,
+        dtype=cfg.dtype, window_blocks=8))
+    (table,), pages = tables(cfg, 1, 5)
+    g = torch.Generator().manual_seed(6)
+    q, k, v = rows(g, n)
+    cache = be.alloc_cache(pages, *scales(form))
+    meta = be.init_forward_metadata([n], None, table)
+    fp2.cache_append(meta.params, k, v, cache, meta.cu_q, meta.cu_k, meta.block_table)
+    smeta = sparse.init_forward_metadata([n], None, table)
+    if form == "bf16":
+        out, _ = sparse.forward_extend(q, cache.k, cache.v, smeta)
+        qd = q.cpu()
+    else:
+        qs = 0.01
+        codes = ref.to_codes(q.double().cpu().numpy() / qs)
+        out, _ = sparse.forward_extend(dev(codes), cache.k, cache.v, smeta,
+                                       q_scale=torch.full((HQ,), qs, device="cuda"),
+                                       k_scale=cache.k_scale, v_scale=cache.v_scale)
+        qd = torch.from_numpy(ref.VALUES[codes] * float(np.float32(qs)))
+    torch.cuda.synchronize()
+    c = ref.Cache([n], HKV, form, PAGE, room=500)
+    c.table = table[:, :cfg.max_pages_per_seq].cpu().numpy()
+    c.k, c.v = cache.k.cpu(), cache.v.cpu()
+    if form == "head":
+        c.ks, c.vs = cache.k_scale.cpu(), cache.v_scale.cpu()
+    want = ref.attend(c, qd, [n])[0]
+    assert np.abs(out.double().cpu().numpy() - want).max() <= (2e-2 if form == "bf16" else 6e-2)
+    x = rows(g, 1)
+    got, lse = be.forward(*x, cache, be.init_forward_metadata([1], [n], table), want_lse=True)
+    torch.cuda.synchronize()
+    c.lens, c.k, c.v = [n + 1], cache.k.cpu(), cache.v.cpu()
+    o, tol, z, ztol, _ = ref.attend(c, x[0].cpu(), [1])
+    close(got, o, tol, "out")
+    close(lse, z, ztol, "lse")
