@@ -437,8 +437,10 @@ fp2_status_t fp2_prefill_noalloc(const fp2_params_t* params, const void* q,
  * reads it. A sequence without new tokens takes no part in append and
  * attention. Lengths, tables and scales are read on the device, so a captured
  * call may be replayed with others inside the bounds of params. The caller
- * keeps cu_seqlens_k[b + 1] - cu_seqlens_k[b] >= the new tokens, table entries
- * inside the pool, and page_size whole slots behind each.
+ * keeps cu_seqlens_k[b + 1] - cu_seqlens_k[b] >= the new tokens, the table's
+ * entries for all tokens of a sequence (those that no query sees too) inside
+ * the pool, and page_size whole slots behind each. A call with batch 0, or
+ * without tokens by its bounds, is accepted and writes nothing.
  *
  * A query at position t sees key j <= t where window_tokens is 0; else where
  * also t - j < window_tokens or j < sink_tokens. What lies in slots that no
@@ -501,7 +503,7 @@ fp2_status_t fp2_cache_append(const fp2_cache_params_t* params, const void* k_ne
 
 /* out = softmax(scale * q k^T) v over the keys that each query sees; q and
  * out bf16 [cu_seqlens[batch], num_q_heads, 128], lse (nullable) fp32 [...,
- * num_q_heads], the natural log of the sum. Probabilities are rounded to bf16
+ * num_q_heads], the natural log of the sum. out must not overlap q. Probabilities are rounded to bf16
  * for the value product. Rows past cu_seqlens[batch] are not touched. Where
  * max_seq_len * g <= 64 the keys are read once for all rows of a sequence;
  * results depend on kv_splits, and with 0 on the other sequences of a call,
@@ -517,7 +519,7 @@ fp2_status_t fp2_cache_attend(const fp2_cache_params_t* params, const void* q,
  *   weights[b][h][j] = weights_in[b][h][j] + sum over the new tokens that see
  *       j and the g query heads of h of exp(scale * q.k_j - lse)
  * with q as in fp2_cache_attend and the lse that it returned. weights and
- * weights_in (nullable = zeros; may be weights itself) are fp32 [batch,
+ * weights_in (nullable = zeros; weights itself, or no memory of it) are fp32 [batch,
  * num_kv_heads, weights_stride], weights_stride >= max_kv_len; entries past a
  * sequence are those of weights_in (zeros without it). No values are read: cache->v may be null. The
  * result does not depend on the order of anything (no atomics). */
@@ -528,7 +530,7 @@ fp2_status_t fp2_cache_weights(const fp2_cache_params_t* params, const void* q, 
                                const float* weights_in, float* weights, int64_t weights_stride,
                                void* workspace, size_t workspace_bytes, void* stream);
 
-/* Cuts the sequences to at most `budget` tokens per KV head: the first
+/* Cuts the sequences to at most `budget` (1 .. 1048576) tokens per KV head: the first
  * sink_tokens, the last recent_tokens and, of the others, the heaviest by
  * weights [batch][num_kv_heads][weights_stride] (fp32; equal ones by the
  * lowest index, NaN last). sink_tokens + recent_tokens <= budget. A sequence
@@ -536,10 +538,11 @@ fp2_status_t fp2_cache_weights(const fp2_cache_params_t* params, const void* q, 
  * tokens.
  *   kept       int32 [batch][num_kv_heads][budget]: the indexes that stay,
  *              ascending, -1 behind them;
- *   cu_seqlens_k_out  int32 [batch + 1]: the new lengths min(L, budget);
+ *   cu_seqlens_k_out  int32 [batch + 1]: the new lengths min(L, budget),
+ *              summed up (not cu_seqlens_k itself);
  *   weights_out  fp32 [batch][num_kv_heads][weights_stride]: weights of the
  *              tokens that stay, zeros behind them (every entry is written;
- *              not weights itself).
+ *              no memory of weights).
  * The rows that stay are written to slots target_table[b][i / page_size] *
  * page_size + i % page_size of the same pool, i = 0, 1, ...; target_table
  * int32 [batch][target_pages], target_pages >= ceil(min(budget, max_kv_len) /

@@ -157,7 +157,8 @@ class _Args:
                   self("cache.v_scale", c.v_scale, _F32, p.num_kv_heads))
         return _CachePointers(k, v, ks, vs, None, None)
 
-    def lengths(self, p, cu, cuk, host, host_k):
+    def lengths(self, p, cu, cuk, host, host_k, rows=None):
+        """Device and host lengths; `rows`: new tokens that the call's tensors hold."""
         for name, t in (("cu_seqlens_host", host), ("cu_seqlens_k_host", host_k)):
             if t is None:
                 continue
@@ -166,6 +167,8 @@ class _Args:
                 raise ValueError("%s must be a host int32 array" % name)
             if (t.numel() if torch_t else t.size) < p.batch + 1:
                 raise ValueError("%s must have batch + 1 entries" % name)
+            if t is host and rows is not None and int(t[p.batch]) > rows:
+                raise ValueError("%d new tokens, tensors hold %d" % (int(t[p.batch]), rows))
         return (self("cu_seqlens", cu, _INT32, p.batch + 1), _host_ptr(host),
                 self("cu_seqlens_k", cuk, _INT32, p.batch + 1), _host_ptr(host_k))
 
@@ -203,7 +206,7 @@ def cache_append(p: CacheParams, k_new, v_new, cache: KVCache, cu_seqlens, cu_se
     k, v = a("k_new", k_new, _BF16, 0, row), a("v_new", v_new, _BF16, 0, row)
     if k_new.numel() != v_new.numel():
         raise ValueError("k_new and v_new differ in size")
-    lens = a.lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host)
+    lens = a.lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host, k_new.numel() // row)
     table = a.table(p, "block_table", block_table, p.max_pages_per_seq)
     a.call("fp2_cache_append", stream, ctypes.byref(p), k, v, *lens, ctypes.byref(c), table)
 
@@ -217,7 +220,7 @@ def cache_attend(p: CacheParams, q, cache: KVCache, cu_seqlens, cu_seqlens_k, bl
     qp = a("q", q, _BF16, 0, row)
     rows = q.numel() // row
     c = a.cache(p, cache)
-    lens = a.lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host)
+    lens = a.lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host, q.numel() // row)
     table = a.table(p, "block_table", block_table, p.max_pages_per_seq)
     with on_stream(stream):
         if out is None:
@@ -244,7 +247,7 @@ def cache_weights(p: CacheParams, q, lse, cache: KVCache, cu_seqlens, cu_seqlens
     qp = a("q", q, _BF16, 0, row)
     lp = a("lse", lse, _F32, q.numel() // p.head_dim)
     c = a.cache(p, cache, need_v=False)
-    lens = a.lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host)
+    lens = a.lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host, q.numel() // row)
     table = a.table(p, "block_table", block_table, p.max_pages_per_seq)
     wi = a.weights(p, "weights_in", weights_in)
     with on_stream(stream):
@@ -259,6 +262,12 @@ def cache_weights(p: CacheParams, q, lse, cache: KVCache, cu_seqlens, cu_seqlens
     ws = a("workspace", workspace, _BYTES)
     a.call("fp2_cache_weights", stream, ctypes.byref(p), qp, lp, *lens, ctypes.byref(c), table, wi, w,
            weights.shape[2], ws, workspace.numel())
+    if (p.batch == 0 or p.max_kv_len == 0) and weights is not weights_in:     # a call without tokens
+        with on_stream(stream):
+            if weights_in is None:
+                weights.zero_()
+            else:
+                weights[:p.batch].copy_(weights_in[:p.batch])
     return weights
 
 
@@ -290,4 +299,7 @@ def cache_evict(p: CacheParams, cache: KVCache, weights, cu_seqlens_k, block_tab
     co = a("cu_seqlens_k_out", cu_seqlens_k_out, _INT32, p.batch + 1)
     a.call("fp2_cache_evict", stream, ctypes.byref(p), ctypes.byref(c), cuk, cuk_host, table, target,
            target_table.shape[1], int(budget), int(recent_tokens), w, wo, weights.shape[2], kp, co)
+    if p.batch == 0 or p.max_kv_len == 0:                                      # a call without tokens
+        with on_stream(stream):
+            kept.fill_(-1), cu_seqlens_k_out.zero_(), weights_out.zero_()
     return kept, cu_seqlens_k_out, weights_out

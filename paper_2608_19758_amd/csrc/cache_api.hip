@@ -23,6 +23,13 @@ fp2_status_t fail(fp2_status_t st, const char* fmt, A... a) {
 fp2_status_t fail(fp2_status_t st, const char* msg) { return fp2::set_error(st, msg); }
 fp2_status_t ok() { return fp2::set_error(FP2_OK, ""); }
 
+// Whether n elements at a share memory with m at b.
+template <class T>
+bool overlap(const T* a, int64_t n, const T* b, int64_t m) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + (uint64_t)m * sizeof(T) && y < x + (uint64_t)n * sizeof(T);
+}
+
 bool aligned(const void* x, uintptr_t n) { return ((uintptr_t)x & (n - 1)) == 0; }
 
 fp2_status_t check_params(const fp2_cache_params_t* p) {
@@ -225,6 +232,7 @@ fp2_status_t fp2_cache_attend(const fp2_cache_params_t* params, const void* q,
   if ((st = check_cache(params, cache, block_table, true))) return st;
   if (!q || !out) return fail(FP2_EINVAL, "q or out is null");
   if (!aligned(q, 16) || !aligned(out, 16)) return fail(FP2_EINVAL, "q and out must be 16-byte aligned");
+  if (q == out) return fail(FP2_EINVAL, "out must not be q");
   const CacheProblem r = make_problem(params, q, cu_seqlens, cu_seqlens_k, cache, block_table);
   size_t ml;
   if ((st = check_workspace(workspace, workspace_bytes, attend_bytes(r, &ml)))) return st;
@@ -252,6 +260,9 @@ fp2_status_t fp2_cache_weights(const fp2_cache_params_t* params, const void* q, 
   if (weights_stride < params->max_kv_len)
     return fail(FP2_EINVAL, "weights_stride %lld < max_kv_len %d", (long long)weights_stride,
                 params->max_kv_len);
+  const int64_t entries = (int64_t)params->batch * params->num_kv_heads * weights_stride;
+  if (weights_in && weights_in != weights && overlap<float>(weights_in, entries, weights, entries))
+    return fail(FP2_EINVAL, "weights overlaps weights_in without being the same");
   const CacheProblem r = make_problem(params, q, cu_seqlens, cu_seqlens_k, cache, block_table);
   if ((st = check_workspace(workspace, workspace_bytes, weights_bytes(r)))) return st;
   return hip_status(fp2::launch_cache_weights(r, lse, weights_in, weights, weights_stride,
@@ -268,6 +279,7 @@ fp2_status_t fp2_cache_evict(const fp2_cache_params_t* params, const fp2_kv_cach
   fp2_status_t st = check_params(params);
   if (st != FP2_OK) return st;
   if (budget < 1) return fail(FP2_EINVAL, "budget %d < 1", budget);
+  if (budget > kMaxLen) return fail(FP2_EUNSUPPORTED, "budget %d > %d", budget, kMaxLen);
   if (recent_tokens < 0) return fail(FP2_EINVAL, "recent_tokens %d < 0", recent_tokens);
   if ((int64_t)params->sink_tokens + recent_tokens > budget)
     return fail(FP2_EINVAL, "sink_tokens %d + recent_tokens %d > budget %d", params->sink_tokens,
@@ -282,10 +294,14 @@ fp2_status_t fp2_cache_evict(const fp2_cache_params_t* params, const fp2_kv_cach
     return fail(FP2_EINVAL, "target_pages %d < %d for %d tokens", target_pages, pages, stay);
   if (!weights || !weights_out || !kept || !cu_seqlens_k_out)
     return fail(FP2_EINVAL, "weights, weights_out, kept or cu_seqlens_k_out is null");
-  if (weights == weights_out) return fail(FP2_EINVAL, "weights_out must not be weights");
   if (weights_stride < params->max_kv_len)
     return fail(FP2_EINVAL, "weights_stride %lld < max_kv_len %d", (long long)weights_stride,
                 params->max_kv_len);
+  const int64_t entries = (int64_t)params->batch * params->num_kv_heads * weights_stride;
+  if (overlap<float>(weights, entries, weights_out, entries))
+    return fail(FP2_EINVAL, "weights_out must not overlap weights");
+  if (overlap<int32_t>(cu_seqlens_k, params->batch + 1, cu_seqlens_k_out, params->batch + 1))
+    return fail(FP2_EINVAL, "cu_seqlens_k_out must not overlap cu_seqlens_k");
   CacheProblem r = make_problem(params, nullptr, nullptr, cu_seqlens_k, cache, block_table);
   r.sink = params->sink_tokens;
   fp2::PageMap to = r.pm;

@@ -14,7 +14,7 @@
 // probabilities go into the second product as they are, and the transposing
 // LDS reads give V^T. The running maximum moves when a score passes it by more
 // than 2^8. Probabilities are rounded to bf16 for the product; sums, maxima
-// and outputs are fp32. A wave leaves out tiles that none of its rows sees.
+// and outputs are fp32.
 //
 // Calls of few units cut each unit's tiles into equal parts, joined by
 // join_kernel.

@@ -395,7 +395,7 @@ __global__ __launch_bounds__(kChunk) void sum_kernel(CacheProblem p, const float
   if (key >= (in != out ? stride : (int64_t)L)) return;
   const Steps st = steps_of(p, c0, ld_uniform(p.cu, b + 1) - ld_uniform(p.cu, b), L);
   float sum = 0.f;
-  const int s0 = st.from / seg_steps, s1 = key < L ? (st.to + seg_steps - 1) / seg_steps : s0;
+  const int s0 = st.from / seg_steps, s1 = key < L ? min((st.to + seg_steps - 1) / seg_steps, segs) : s0;
   if (st.from < st.to) {
 #pragma unroll 8
     for (int s = s0; s < s1; ++s)

@@ -32,8 +32,8 @@ def host(x):
 
 def call(op, p, **over):
     a = dict(k_new=FAKE, v_new=FAKE, q=FAKE, cu=FAKE, cuh=None, cuk=FAKE, cukh=None, cache=pointers(), table=FAKE,
-             out=FAKE, lse=FAKE, ws=None, wsb=0, win=None, w=FAKE, stride=p.max_kv_len if p else 0, target=FAKE, pages=64,
-             budget=100, recent=10, wout=2 * FAKE, kept=FAKE, cuo=FAKE)
+             out=4 * FAKE, lse=FAKE, ws=None, wsb=0, win=None, w=FAKE, stride=p.max_kv_len if p else 0, target=FAKE, pages=64,
+             budget=100, recent=10, wout=2 * FAKE, kept=FAKE, cuo=3 * FAKE)
     a.update(over)
     held = [np.asarray(a[n], np.int32) if a[n] is not None else None for n in ("cuh", "cukh")]
     cuh, cukh = (None if x is None else x.ctypes.data for x in held)
@@ -152,6 +152,14 @@ def test_weights_and_eviction_refusals():
     assert call("evict", p, budget=13, recent=10) == fp2.EINVAL
     assert call("evict", p, budget=100, pages=1) == fp2.EINVAL
     assert call("evict", p, wout=FAKE) == fp2.EINVAL                # the weights themselves
+    row = 4 * 4096                                                  # bytes; 2 x 8 rows
+    for w in (FAKE + 15 * row, FAKE - 15 * row, FAKE + 4):
+        assert call("evict", p, wout=w) == fp2.EINVAL and "overlap" in fp2.last_error()
+        assert call("weights", p, win=w) == fp2.EINVAL and "overlap" in fp2.last_error()
+    for cu in (FAKE, FAKE + 8, FAKE - 8):
+        assert call("evict", p, cuo=cu) == fp2.EINVAL and "cu_seqlens_k_out" in fp2.last_error()
+    assert call("attend", p, out=FAKE) == fp2.EINVAL and "out must not be q" in fp2.last_error()
+    assert call("evict", p, budget=(1 << 20) + 1) == fp2.EUNSUPPORTED
 
 
 @pytest.mark.parametrize("op", OPS)
@@ -217,6 +225,18 @@ def test_binding_refuses(op):
             t["cache"].v = x
         with pytest.raises(ValueError, match=r"^(?!.*CUDA)"):
             binding(op, p, t)
+
+
+def test_rows_of_the_call():
+    """With host lengths the binding sees that the tensors hold the new tokens."""
+    p, h = base(), np.array([0, 4, 7], np.int32)
+    t = tensors(p)
+    with pytest.raises(ValueError, match="7 new tokens"):
+        fp2.cache_append(p, t["new"], t["new"], t["cache"], t["cu"], t["cu"], t["table"], cu_seqlens_host=h)
+    with pytest.raises(ValueError, match="7 new tokens"):
+        fp2.cache_attend(p, t["q"], t["cache"], t["cu"], t["cu"], t["table"], cu_seqlens_host=torch.from_numpy(h))
+    with pytest.raises(ValueError, match="7 new tokens"):
+        fp2.cache_weights(p, t["q"], t["lse"], t["cache"], t["cu"], t["cu"], t["table"], cu_seqlens_host=h)
 
 
 def test_alloc_cache():

@@ -339,6 +339,34 @@ def test_evict_order(kind):
     run_evict(ref.Cache([L], 2, 64, 64, seed=5), w, 4501, 3, 700)
 
 
+@pytest.mark.parametrize("batch,max_kv", [(0, 100), (2, 0)])
+def test_calls_without_tokens(batch, max_kv):
+    p = fp2.make_cache_params(batch=batch, num_q_heads=4, num_kv_heads=2, max_seq_len=0, max_kv_len=max_kv, page_size=16,
+                              max_pages_per_seq=7)
+    cache = fp2.alloc_cache(p, 2)
+    cu, table = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros((2, 7), dtype=torch.int32, device="cuda")
+    q, lse = torch.zeros((0, 4, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((0, 4), device="cuda")
+    w = torch.full((2, 2, 100), 3.0, device="cuda")
+    fp2.cache_append(p, q[:, :2].contiguous(), q[:, :2].contiguous(), cache, cu, cu, table)
+    assert fp2.cache_attend(p, q, cache, cu, cu, table)[0].shape == q.shape
+    got = fp2.cache_weights(p, q, lse, cache, cu, cu, table, weights_in=w)
+    assert got.shape[0] == batch and bool((got == 3).all())
+    assert bool((fp2.cache_weights(p, q, lse, cache, cu, cu, table) == 0).all())
+    kept, cu2, w2 = fp2.cache_evict(p, cache, w, cu, table, table.clone(), budget=20)
+    assert bool((kept == -1).all()) and cu2.tolist() == [0] * (batch + 1) and bool((w2 == 0).all())
+
+
+@pytest.mark.parametrize("form", ["bf16", 64])
+def test_many_sequences(form):
+    """More sequences than a wave looks at at once, some without new tokens or without any."""
+    r = np.random.default_rng(21)
+    lens = [int(n) for n in r.integers(0, 60, 150)]
+    new = [min(n, int(m)) for n, m in zip(lens, r.integers(0, 3, 150))]
+    lens[70], new[70] = 2500, 2                        # the call's bound: sequences are cut
+    run_attend(ref.Cache(lens, 2, form, 64, seed=22), 8, new)
+    run_attend(ref.Cache(lens, 3, form, 64, seed=23), 3, new, window=40, sink=3)
+
+
 # ---- together
 
 @pytest.mark.parametrize("form", ["bf16", "head", 16])
