@@ -357,7 +357,7 @@ def test_calls_without_tokens(batch, max_kv):
 
 
 @pytest.mark.parametrize("form", ["bf16", 64])
-def test_many_sequences(form):
+def test_more_sequences_than_lanes(form):
     """More sequences than a wave looks at at once, some without new tokens or without any."""
     r = np.random.default_rng(21)
     lens = [int(n) for n in r.integers(0, 60, 150)]
@@ -365,6 +365,80 @@ def test_many_sequences(form):
     lens[70], new[70] = 2500, 2                        # the call's bound: sequences are cut
     run_attend(ref.Cache(lens, 2, form, 64, seed=22), 8, new)
     run_attend(ref.Cache(lens, 3, form, 64, seed=23), 3, new, window=40, sink=3)
+
+
+@pytest.mark.parametrize("form,page", [("bf16", 1), ("bf16", 64), ("head", 24), (16, 64)])
+def test_slots_past_32_bits(form, page):
+    """The same calls on a small pool and at the end of one whose rows lie past 4 GiB."""
+    hkv, hq = 8, 16
+    row = hkv * 128 * (2 if form == "bf16" else 1)
+    c = ref.Cache([300, 41], hkv, form, page, room=80, seed=24)
+    spare = ref.Cache([100] * 2, hkv, form, page, seed=25)
+    small = on_gpu(c)
+    for n in ("k", "v") + (("ks", "vs") if c.sb else ()):
+        name = {"ks": "k_scale", "vs": "v_scale"}.get(n, n)
+        setattr(small, name, torch.cat([getattr(small, name), dev(getattr(spare, n))]))
+    skip = -(-((1 << 32) + (1 << 30)) // row // page) * page        # slots before the copy
+    pools = {}
+    for n in ("k", "v"):
+        t = getattr(small, n)
+        pools[n] = torch.empty((skip + t.shape[0],) + t.shape[1:], dtype=t.dtype, device="cuda")
+        pools[n][skip:] = t
+    scales = [small.k_scale, small.v_scale]
+    if c.sb:
+        scales = [torch.cat([torch.full((skip // c.sb, hkv), 255, dtype=torch.uint8, device="cuda"), t]) for t in scales]
+    large = fp2.KVCache(pools["k"], pools["v"], *scales)
+    g = torch.Generator().manual_seed(8)
+    w_shape = (2, hkv, 400)
+
+    def run(cache, shift):
+        g.manual_seed(8)
+        got, w = [], torch.zeros(w_shape, device="cuda")
+        lens = list(c.lens)
+        table = np.where(c.table < 2 ** 30, c.table + shift, 0).astype(np.int32)
+        for new in ([70, 3], [1, 1]):
+            lens = [a + b for a, b in zip(lens, new)]
+            p = params(c, hq, new, max_kv=max(lens))
+            q, k, v = (torch.randn((sum(new), h, 128), generator=g).bfloat16().cuda() for h in (hq, hkv, hkv))
+            args = (dev(cu_of(new)), dev(cu_of(lens)), dev(table))
+            fp2.cache_append(p, k, v, cache, *args)
+            out, lse = fp2.cache_attend(p, q, cache, *args, want_lse=True)
+            fp2.cache_weights(p, q, lse, cache, *args, weights=w, weights_in=w)
+            got += [out, lse]
+        target = (spare.table + c.pages + shift).astype(np.int32)
+        got += fp2.cache_evict(p, cache, w, args[1], args[2], dev(target), budget=100, recent_tokens=20)
+        p = params(c, hq, [1, 1], max_kv=100)
+        p.max_pages_per_seq = target.shape[1]
+        got.append(fp2.cache_attend(p, q, cache, args[0], dev(cu_of([100, 45])), dev(target))[0])
+        torch.cuda.synchronize()
+        return got + [w]
+
+    for a, b in zip(run(small, 0), run(large, skip // page)):
+        same(b, a.cpu(), "results")
+    same(large.k[skip:], small.k.cpu(), "k")
+    same(large.v[skip:], small.v.cpu(), "v")
+
+
+def test_two_calls_at_once():
+    """Calls on two streams, each with a workspace of its own, against the same calls one after the other."""
+    c = ref.Cache([3000, 2000], 2, 64, 64, seed=26)
+    cache, table, cuk = on_gpu(c), dev(c.table), dev(cu_of(c.lens))
+    g = torch.Generator().manual_seed(9)
+    calls = []
+    for new in ([1, 1], [100, 70]):
+        p = params(c, 8, new)
+        calls.append((p, torch.randn((sum(new), 8, 128), generator=g).bfloat16().cuda(), dev(cu_of(new)),
+                      fp2.alloc_cache_workspace(p)))
+    torch.cuda.synchronize()
+    want = [fp2.cache_attend(p, q, cache, cu, cuk, table, workspace=ws, want_lse=True) for p, q, cu, ws in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(3):
+        got = [fp2.cache_attend(p, q, cache, cu, cuk, table, workspace=ws, want_lse=True, stream=s)
+               for (p, q, cu, ws), s in zip(calls, streams)]
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
 # ---- together
