@@ -60,7 +60,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(CacheProblem p, int bu
   __shared__ int cnt[2][kSteps * kThreads / 64];
   __shared__ int tot[kThreads / 64];
   __shared__ int s_bin, s_need, s_size;
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (blockIdx.x == 0 && tid < 64) {   // the new lengths
     int base = 0;
     if (lane == 0) cu_out[0] = 0;
@@ -101,9 +101,20 @@ __global__ __launch_bounds__(kThreads) void select_kernel(CacheProblem p, int bu
   load(0, x);
   const bool once = lines <= kRound / 4;                 // then they are loaded once
   auto at = [](const float4& x, int e) { return e == 0 ? x.x : e == 1 ? x.y : e == 2 ? x.z : x.w; };
+  // the first token of a wave's load, and whether all of them are ranked: then
+  // none is looked at for its place
+  auto begins = [&](int v0, int s) { return 4 * (v0 + s * kThreads + (w << 6)) - skew; };
+  auto ranked = [&](int v0, int s) { return begins(v0, s) >= lo && begins(v0, s) + 256 <= hi; };
   // bits of the weight that just stays, found from the top
-  uint32_t edge = 0, mask = 0;                           // and which of its bits are known
-  int left = need;                                       // of those equal to `edge` so far
+  uint32_t edge = 0, span = 0;                           // it lies in [edge, edge + span)
+  int left = need;                                       // stay of those
+  // Weights in a range of positive finite ones are told by their own bits: two
+  // operations each, where putting them in order takes seven.
+  constexpr uint32_t kSign = 0x80000000u, kInf = 0x7f800000u;
+  bool plain = false;
+  auto from_edge = [&](float x, auto own) {              // 0 .. span - 1: in the range
+    return own ? __float_as_uint(x) - (edge ^ kSign) : order_of(x) - edge;
+  };
 #pragma unroll 1
   for (int d = 0; d < 3 && need > 0; ++d) {
     const int shift = d == 0 ? 21 : d == 1 ? 10 : 0, bins = d == 2 ? 1024 : 2048;
@@ -113,14 +124,27 @@ __global__ __launch_bounds__(kThreads) void select_kernel(CacheProblem p, int bu
     for (int v0 = 0; v0 < lines; v0 += kRound / 4) {
       if (!once) load(v0, x);
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s)
+      for (int s = 0; s < kSteps; ++s) {
+        auto count = [&](auto inside, auto first, auto own) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = 4 * (v0 + s * kThreads + tid) + e - skew;
-          const uint32_t u = order_of(at(x[s], e));
-          if (i >= lo && i < hi && (u & mask) == edge)
-            atomicAdd(&hist[tid % kCopies][(u >> shift) & (bins - 1)], 1);
+          for (int e = 0; e < 4; ++e) {
+            const int i = 4 * (v0 + s * kThreads + tid) + e - skew;
+            const uint32_t u = from_edge(at(x[s], e), own);
+            if ((inside || (i >= lo && i < hi)) && (first || u < span))
+              atomicAdd(&hist[tid % kCopies][u >> shift], 1);
+          }
+        };
+        using Y = std::true_type;
+        using N = std::false_type;
+        if (ranked(v0, s)) {
+          if (d == 0) count(Y{}, Y{}, N{});
+          else if (plain) count(Y{}, N{}, Y{});
+          else count(Y{}, N{}, N{});
+        } else if (begins(v0, s) < hi) {
+          if (d == 0) count(N{}, Y{}, N{});
+          else count(N{}, N{}, N{});
         }
+      }
     }
     __syncthreads();
     // bins from the top, two a thread
@@ -133,8 +157,9 @@ __global__ __launch_bounds__(kThreads) void select_kernel(CacheProblem p, int bu
     else if (before + n1 < left && before + n1 + n2 >= left)
       s_bin = b1 - 1, s_need = left - before - n1, s_size = n2;
     __syncthreads();
-    edge |= (uint32_t)s_bin << shift;
-    mask |= (uint32_t)(bins - 1) << shift;
+    edge += (uint32_t)s_bin << shift;
+    span = 1u << shift;
+    plain = edge > kSign && edge + span <= (kSign | kInf);
     left = s_need;
     const bool all = s_size == left;     // every weight with these bits stays: no need for the others
     __syncthreads();
@@ -143,7 +168,6 @@ __global__ __launch_bounds__(kThreads) void select_kernel(CacheProblem p, int bu
   // in order: tokens that are protected or heavier than the edge, and the
   // first `left` at it. A round counts both (the second kind in the high half)
   // for every wave and step, and one sum over those gives every place.
-  const int w = tid >> 6;
   int over = 0, equal = 0;               // of the rounds before
 #pragma unroll 1
   for (int v0 = 0, odd = 0; v0 < lines; v0 += kRound / 4, odd ^= 1) {
@@ -152,13 +176,23 @@ __global__ __launch_bounds__(kThreads) void select_kernel(CacheProblem p, int bu
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
       up[s] = eq[s] = 0;
+      auto sort = [&](auto inside, auto own) {
+        // heavier: behind the range, up to infinity
+        const uint32_t end = own ? kInf - (edge ^ kSign) - span : need > 0 ? ~edge - span : 0u;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int i = 4 * (v0 + s * kThreads + tid) + e - skew;
-        const uint32_t u = order_of(at(x[s], e)) & mask;
-        const bool fixed = i < lo || i >= hi, in = i >= 0 && i < L;
-        up[s] |= in && (fixed || (need > 0 && u > edge)) ? 1 << e : 0;
-        eq[s] |= in && !fixed && need > 0 && u == edge ? 1 << e : 0;
+        for (int e = 0; e < 4; ++e) {
+          const int i = 4 * (v0 + s * kThreads + tid) + e - skew;
+          const uint32_t u = from_edge(at(x[s], e), own);
+          const bool fixed = !inside && (i < lo || i >= hi), in = inside || (i >= 0 && i < L);
+          up[s] |= in && (fixed || (u - span <= end && (own || need > 0))) ? 1 << e : 0;
+          eq[s] |= in && !fixed && u < span ? 1 << e : 0;
+        }
+      };
+      if (ranked(v0, s)) {
+        if (plain) sort(std::true_type{}, std::true_type{});
+        else sort(std::true_type{}, std::false_type{});
+      } else if (begins(v0, s) < L) {
+        sort(std::false_type{}, std::false_type{});
       }
       incl[s] = wave_scan(__popc(up[s]) | __popc(eq[s]) << 16);
       if (lane == 63) cnt[odd][s * (kThreads / 64) + w] = incl[s];
@@ -171,6 +205,18 @@ __global__ __launch_bounds__(kThreads) void select_kernel(CacheProblem p, int bu
       const int before = __shfl(sum - own, s * (kThreads / 64) + w, 64) + incl[s] -
                          (__popc(up[s]) | __popc(eq[s]) << 16);
       int o = over + (before & 0xffff), n = equal + (before >> 16);
+      if (!__any(eq[s])) {
+        // (most loads)
+        const int base = o + min(n, left) , i0 = 4 * (v0 + s * kThreads + tid) - skew;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (up[s] >> e & 1) {
+            const int to = base + __popc(up[s] & ((1 << e) - 1));
+            kr[to] = i0 + e;
+            wo[to] = at(x[s], e);
+          }
+        continue;
+      }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const bool is_up = up[s] >> e & 1, is_eq = eq[s] >> e & 1;
