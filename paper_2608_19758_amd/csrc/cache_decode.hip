@@ -79,12 +79,12 @@ __device__ __forceinline__ uint32_t odd_value(uint2 v, int e) {
   return ((odd_codes(e < 4 ? v.x : v.y) >> (8 * (e & 3) + 7)) & 1) * 0x7fc00000u;
 }
 
-// FORM: the cache's type. NT: 16-row tiles of query rows. W: waves (many
-// registers a wave: four, one a SIMD). GROUPED: pages hold a multiple of 16
+// FORM: the cache's type. NT: 16-row tiles of query rows of a wave. RH: waves
+// that share the rows. W: waves (many registers a wave: four, one a SIMD). GROUPED: pages hold a multiple of 16
 // tokens, so the 16 keys of a group lie one after the other and their address
 // is uniform (scalar); otherwise every key has its own. ONE: one new token a
 // sequence, so that every row sees the same keys.
-template <int FORM, int NT, int W, bool GROUPED, bool ONE>
+template <int FORM, int NT, int RH, int W, bool GROUPED, bool ONE>
 __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, CachePartials part,
                                                                int shares, uint16_t* __restrict__ out,
                                                                float* __restrict__ lse) {
@@ -94,14 +94,16 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
   constexpr int LDR = kHeadDim + 4;            // LDS row, padded against bank conflicts
   __shared__ float s_o[W][16][LDR];
   __shared__ float s_ml[W][16][2];
-  const int groups = p.hkv / p.heads, index = blockIdx.x / groups, KS = W / p.heads;
+  const int groups = p.hkv / p.heads, index = blockIdx.x / groups;
+  const int units = p.heads * RH, KS = W / units;   // (head, half of the rows): how many waves alternate its tiles
   Share sh;
   if (!find_share<false>(p, shares, index, sh)) return;
 
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.x % groups * p.heads + w % p.heads;
-  const int ks = w / p.heads;                  // place among the head's tiles
+  const int ks = w / units;                    // place among the head's tiles
+  const int rb = RH == 1 ? 0 : w / p.heads % RH * 16 * NT;   // the wave's first packed row
   const int c16 = lane & 15, kg = lane >> 4;
   float cs = p.scale_log2, vsc = 1.f;
   if constexpr (FORM == kCacheHead) {
@@ -137,7 +139,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
   int pos[NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int r = 16 * nt + c16;
+    const int r = rb + 16 * nt + c16;
     pos[nt] = first + (ONE ? 0 : r / p.g);
     const uint16_t* qrow = p.q + ((int64_t)(q0 + (ONE ? 0 : min(r / p.g, Lq - 1))) * p.hq + h * p.g + r % p.g) *
                                      kHeadDim;
@@ -371,7 +373,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
   // eight values of packed row pr of head hh, from dimension d on
   auto put = [&](int hh, int pr, int d, float mm, float ll, float4 x, float4 y) {
     if (split) {
-      const int64_t at = (slot + hh) * (16 * NT) + pr;
+      const int64_t at = (slot + hh) * (16 * NT * RH) + pr;
       *(float4*)(part.o + at * kHeadDim + d) = x;
       *(float4*)(part.o + at * kHeadDim + d + 4) = y;
       if (d == 0) *(float2*)(part.ml + 2 * at) = make_float2(mm, ll);
@@ -388,7 +390,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
   for (int nt = 0; nt < NT; ++nt) {
     l[nt] += __shfl_xor(l[nt], 16, 64);
     l[nt] += __shfl_xor(l[nt], 32, 64);
-    const int pr = 16 * nt + c16;
+    const int pr = rb + 16 * nt + c16;
     if (KS == 1) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -413,9 +415,9 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
     }
     __syncthreads();
     // the ks-th of them joins that share of the pieces of eight dimensions
-    const int w0 = w % p.heads, stepw = p.heads;
+    const int w0 = w % units, stepw = units;
     for (int x = 64 * ks + lane; x < 16 * 16; x += 64 * KS) {
-      const int r = x >> 4, d = 8 * (x & 15), jr = 16 * nt + r;
+      const int r = x >> 4, d = 8 * (x & 15), jr = rb + 16 * nt + r;
       if (jr >= rows) continue;
       float mm = kNoRef;
       for (int v = 0; v < KS; ++v) mm = fmaxf(mm, s_ml[w0 + v * stepw][r][0]);
@@ -532,37 +534,41 @@ int rows_cap(const CacheProblem& p) {
   return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
 }
 
-// Waves of a workgroup: a tile of bf16 keys takes twice the registers of one
-// of codes.
-int waves_for(const CacheProblem& p) {
-  return rows_cap(p) <= (p.form == kCacheBf16 ? 16 : 32) ? 8 : 4;
-}
+// Heads that a workgroup takes side by side: many for long runs of memory, few
+// for few partial results, of which it leaves one for each head and row. 8
+// sequences of 5K to 38K tokens, codes, 32 rows: 78 us with 4 heads, 95 with 8;
+// 64 rows: 101 us with 2, 105 with 4.
+int heads_for(const CacheProblem& p) { return 128 / rows_cap(p); }
 
-template <int FORM, int NT, int W, bool GROUPED, bool ONE>
+template <int FORM, int NT, int RH, int W, bool GROUPED, bool ONE>
 hipError_t launch(const CacheProblem& problem, const CachePartials& part, uint16_t* out, float* lse,
                   hipStream_t s) {
-  const CacheProblem p = dealt(problem, W);
+  const CacheProblem p = dealt(problem, heads_for(problem));
   const int shares = shares_of(p), max_rows = p.max_new * p.g;
   const int64_t grid = (int64_t)shares * (p.hkv / p.heads);
   const int64_t joins = (int64_t)p.batch * p.hkv * max_rows;
   if (grid > 0x7fffffff || joins > 0x7fffffff) return hipErrorInvalidValue;
-  decode_kernel<FORM, NT, W, GROUPED, ONE><<<(unsigned)grid, 64 * W, 0, s>>>(p, part, shares, out, lse);
+  decode_kernel<FORM, NT, RH, W, GROUPED, ONE><<<(unsigned)grid, 64 * W, 0, s>>>(p, part, shares, out, lse);
   if (p.splits == 1) return hipGetLastError();
   // few joins have many parts each, and a compute unit to themselves
   const int threads = joins <= kFewGroups ? 1024 : 256;
-  combine_kernel<<<(unsigned)joins, threads, 0, s>>>(p, part, shares, 16 * NT, max_rows, out, lse);
+  combine_kernel<<<(unsigned)joins, threads, 0, s>>>(p, part, shares, 16 * NT * RH, max_rows, out, lse);
   return hipGetLastError();
 }
 
+// Waves of a workgroup: a tile of bf16 keys takes twice the registers of one
+// of codes. 64 rows need a wave's 512 registers; in bf16 not even those hold
+// them, and two waves share them (145 us, 170 with spilled registers; in codes
+// 108 instead of 101).
 template <int FORM, bool GROUPED>
 hipError_t launch_rows(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse,
                        hipStream_t s) {
-  constexpr int W2 = FORM == kCacheBf16 ? 4 : 8;   // waves_for 32 rows
+  constexpr bool kBf16 = FORM == kCacheBf16;
   const int rows = rows_cap(p);
-  return p.max_new == 1 ? launch<FORM, 1, 8, GROUPED, true>(p, part, out, lse, s)
-         : rows == 16   ? launch<FORM, 1, 8, GROUPED, false>(p, part, out, lse, s)
-         : rows == 32   ? launch<FORM, 2, W2, GROUPED, false>(p, part, out, lse, s)
-                        : launch<FORM, 4, 4, GROUPED, false>(p, part, out, lse, s);
+  return p.max_new == 1 ? launch<FORM, 1, 1, 8, GROUPED, true>(p, part, out, lse, s)
+         : rows == 16   ? launch<FORM, 1, 1, 8, GROUPED, false>(p, part, out, lse, s)
+         : rows == 32   ? launch<FORM, 2, 1, kBf16 ? 4 : 8, GROUPED, false>(p, part, out, lse, s)
+                        : launch<FORM, kBf16 ? 2 : 4, kBf16 ? 2 : 1, 4, GROUPED, false>(p, part, out, lse, s);
 }
 
 template <int FORM>
@@ -577,7 +583,7 @@ hipError_t launch_pages(const CacheProblem& p, const CachePartials& part, uint16
 }  // namespace
 
 void cache_decode_partials(const CacheProblem& problem, int64_t* slots, int* rows) {
-  const CacheProblem p = dealt(problem, waves_for(problem));
+  const CacheProblem p = dealt(problem, heads_for(problem));
   *slots = p.splits == 1 ? 0 : (int64_t)shares_of(p) * (p.splits ? 1 : 2) * p.hkv;
   *rows = rows_cap(p);
 }

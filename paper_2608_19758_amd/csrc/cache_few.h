@@ -46,15 +46,15 @@ struct Share {
 };
 
 // The heads of a token lie side by side in the pool, so the waves of a
-// workgroup take `heads` different heads of the same tokens, and memory is read
-// in runs of heads x 128 codes (reading a pool of 8 heads this way reaches 6.2
-// TB/s, with the heads in different workgroups 5.5); the other waves alternate
-// tiles. Short sequences, by the bounds of the call, are taken whole, with
+// workgroup take up to `heads` different heads of the same tokens, and memory
+// is read in runs of heads x 128 codes (reading a pool of 8 heads this way
+// reaches 6.2 TB/s, with the heads in different workgroups 5.5); the other
+// waves alternate tiles. Short sequences, by the bounds of the call, are taken whole, with
 // fewer heads a workgroup where those would not fill the chip: joining parts
 // is a second kernel and costs about 8 us, a compute unit reads some 100 KB in
 // that time.
-inline CacheProblem dealt(CacheProblem p, int waves) {
-  p.heads = waves;
+inline CacheProblem dealt(CacheProblem p, int heads) {
+  p.heads = heads;
   while (p.hkv % p.heads) p.heads >>= 1;
   const int64_t a = p.max_kv, b = (int64_t)p.window + p.max_new + p.sink;
   if (p.splits == 0 && (a < b ? a : b) / kTile + 3 <= kWholeTiles >> (p.form == kCacheBf16)) {
