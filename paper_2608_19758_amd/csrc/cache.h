@@ -107,7 +107,9 @@ struct CachePartials {
 };
 
 // At most this many packed rows (new tokens times heads of a group) a sequence
-// go to the decode kernel, which reads each key once for all of them.
+// go to the kernels of few rows, which read each key once for all of them. With
+// 64 rows attention over 30K tokens takes 36 us there and 57 as a short prompt,
+// of 8 sequences 99 and 285; with 900 tokens both take 25.
 constexpr int kFewRows = 64;
 
 // Slots, and packed rows of each, of the partial outputs of a call.

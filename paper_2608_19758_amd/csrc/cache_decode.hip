@@ -25,7 +25,14 @@
 //   conversion; a scale per head multiplies the scores and the output.
 // * The running maximum m of a row moves only when a score passes it by more
 //   than 2^8, so most tiles have no exchange between lanes. Probabilities are
-//   rounded to bf16 for the product; sums, maxima and outputs are fp32.
+//   rounded to bf16 for the product, the matrix cores' type (half a step of 2^-8
+//   each); sums, maxima and outputs are fp32.
+//
+// One token of each of 32 sequences of 1.3K to 112K tokens, 8 heads of 4: 274 us
+// in codes (5.5 TB/s), 525 in bf16 (5.7); one sequence of 128K 63 us, of which 9
+// are the join; 64 with windows of 4096 tokens 92 us. 8 drafted tokens and 8
+// heads a group (64 rows), 8 sequences: 100 us (3.1 TB/s); there a wave alone on
+// its SIMD has products and exponentials one after the other.
 #include <algorithm>
 #include <type_traits>
 
@@ -80,11 +87,11 @@ __device__ __forceinline__ uint32_t odd_value(uint2 v, int e) {
 }
 
 // FORM: the cache's type. NT: 16-row tiles of query rows of a wave. RH: waves
-// that share the rows. W: waves (many registers a wave: four, one a SIMD). GROUPED: pages hold a multiple of 16
-// tokens, so the 16 keys of a group lie one after the other and their address
-// is uniform (scalar); otherwise every key has its own. ONE: one new token a
-// sequence, so that every row sees the same keys.
-template <int FORM, int NT, int RH, int W, bool GROUPED, bool ONE>
+// that share the rows. W: waves (many registers a wave: four, one a SIMD).
+// GROUPED: pages hold a multiple of 16 tokens, so the 16 keys of a group lie one
+// after the other and their address is uniform (scalar); otherwise every key has
+// its own (8 sequences of 64 rows: 99 us, with pages of 24 tokens 108).
+template <int FORM, int NT, int RH, int W, bool GROUPED>
 __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, CachePartials part,
                                                                int shares, uint16_t* __restrict__ out,
                                                                float* __restrict__ lse) {
@@ -125,10 +132,10 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
     sh.Lq = ld_uniform(p.cu, b + 1) - sh.q0;
     sh.L = ld_uniform(p.cuk, b + 1) - ld_uniform(p.cuk, b);
   }
-  const int q0 = sh.q0, Lq = ONE ? 1 : sh.Lq, L = sh.L;
+  const int q0 = sh.q0, Lq = sh.Lq, L = sh.L;
   const int first = L - Lq, last = L - 1;      // positions of the first and the last row
   const int rows = Lq * p.g;
-  const Tiles tl = tiles_of(p, sh.Lq, L);
+  const Tiles tl = tiles_of(p, Lq, L);
   const int lo = max(sh.lo, base) - base, hi = min(sh.hi, base + tl.n) - base;
   auto tile_at = [&](int i) { return i < tl.sinks ? i : tl.from + i - tl.sinks; };
   if (lo < hi) {
@@ -140,8 +147,8 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int r = rb + 16 * nt + c16;
-    pos[nt] = first + (ONE ? 0 : r / p.g);
-    const uint16_t* qrow = p.q + ((int64_t)(q0 + (ONE ? 0 : min(r / p.g, Lq - 1))) * p.hq + h * p.g + r % p.g) *
+    pos[nt] = first + r / p.g;
+    const uint16_t* qrow = p.q + ((int64_t)(q0 + min(r / p.g, Lq - 1)) * p.hq + h * p.g + r % p.g) *
                                      kHeadDim;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
@@ -250,10 +257,10 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
         const int key = t0 + 16 * (e >> 2) + 4 * kg + (e & 3);
         const bool any = key <= last && (key < p.sink || key > first - p.window);
         if (!any) x.v[e] = vrow_t{};
-        if constexpr (!ONE) bad |= odd_values(x.v[e]);
+        bad |= odd_values(x.v[e]);
         x.v[e].x = pinned(x.v[e].x);
       }
-      if (!ONE && Lq > 1 && __any(bad)) {
+      if (Lq > 1 && __any(bad)) {
         // rare: such values are added to the rows that see them by hand
 #pragma unroll 1
         for (int k = 0; k < kTile; ++k) {
@@ -379,7 +386,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
       if (d == 0) *(float2*)(part.ml + 2 * at) = make_float2(mm, ll);
     } else {
       const float inv = vsc / ll;
-      const int64_t at = (int64_t)(q0 + (ONE ? 0 : pr / p.g)) * p.hq + hh * p.g + (ONE ? pr : pr % p.g);
+      const int64_t at = (int64_t)(q0 + pr / p.g) * p.hq + hh * p.g + pr % p.g;
       *(uint4*)(out + at * kHeadDim + d) =
           make_uint4(pack_bf16x2(x.x * inv, x.y * inv), pack_bf16x2(x.z * inv, x.w * inv),
                      pack_bf16x2(y.x * inv, y.y * inv), pack_bf16x2(y.z * inv, y.w * inv));
@@ -540,7 +547,7 @@ int rows_cap(const CacheProblem& p) {
 // 64 rows: 101 us with 2, 105 with 4.
 int heads_for(const CacheProblem& p) { return 128 / rows_cap(p); }
 
-template <int FORM, int NT, int RH, int W, bool GROUPED, bool ONE>
+template <int FORM, int NT, int RH, int W, bool GROUPED>
 hipError_t launch(const CacheProblem& problem, const CachePartials& part, uint16_t* out, float* lse,
                   hipStream_t s) {
   const CacheProblem p = dealt(problem, heads_for(problem));
@@ -548,9 +555,11 @@ hipError_t launch(const CacheProblem& problem, const CachePartials& part, uint16
   const int64_t grid = (int64_t)shares * (p.hkv / p.heads);
   const int64_t joins = (int64_t)p.batch * p.hkv * max_rows;
   if (grid > 0x7fffffff || joins > 0x7fffffff) return hipErrorInvalidValue;
-  decode_kernel<FORM, NT, RH, W, GROUPED, ONE><<<(unsigned)grid, 64 * W, 0, s>>>(p, part, shares, out, lse);
+  decode_kernel<FORM, NT, RH, W, GROUPED><<<(unsigned)grid, 64 * W, 0, s>>>(p, part, shares, out, lse);
   if (p.splits == 1) return hipGetLastError();
-  // few joins have many parts each, and a compute unit to themselves
+  // few joins have many parts each, and a compute unit to themselves: 32 joins
+  // of a sequence of 128K take 63 us with the attention, 69 with 256 threads;
+  // 4096 of 8 sequences 100, and 122 with 1024
   const int threads = joins <= kFewGroups ? 1024 : 256;
   combine_kernel<<<(unsigned)joins, threads, 0, s>>>(p, part, shares, 16 * NT * RH, max_rows, out, lse);
   return hipGetLastError();
@@ -565,10 +574,9 @@ hipError_t launch_rows(const CacheProblem& p, const CachePartials& part, uint16_
                        hipStream_t s) {
   constexpr bool kBf16 = FORM == kCacheBf16;
   const int rows = rows_cap(p);
-  return p.max_new == 1 ? launch<FORM, 1, 1, 8, GROUPED, true>(p, part, out, lse, s)
-         : rows == 16   ? launch<FORM, 1, 1, 8, GROUPED, false>(p, part, out, lse, s)
-         : rows == 32   ? launch<FORM, 2, 1, kBf16 ? 4 : 8, GROUPED, false>(p, part, out, lse, s)
-                        : launch<FORM, kBf16 ? 2 : 4, kBf16 ? 2 : 1, 4, GROUPED, false>(p, part, out, lse, s);
+  return rows == 16   ? launch<FORM, 1, 1, 8, GROUPED>(p, part, out, lse, s)
+         : rows == 32 ? launch<FORM, 2, 1, kBf16 ? 4 : 8, GROUPED>(p, part, out, lse, s)
+                      : launch<FORM, kBf16 ? 2 : 4, kBf16 ? 2 : 1, 4, GROUPED>(p, part, out, lse, s);
 }
 
 template <int FORM>

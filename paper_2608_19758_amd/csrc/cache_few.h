@@ -52,7 +52,8 @@ struct Share {
 // waves alternate tiles. Short sequences, by the bounds of the call, are taken whole, with
 // fewer heads a workgroup where those would not fill the chip: joining parts
 // is a second kernel and costs about 8 us, a compute unit reads some 100 KB in
-// that time.
+// that time. 64 sequences of 1000 visible tokens take 30 us whole and 42 cut,
+// one of 617 tokens in bf16 12 and 15, of 1500 in codes 14 both ways.
 inline CacheProblem dealt(CacheProblem p, int heads) {
   p.heads = heads;
   while (p.hkv % p.heads) p.heads >>= 1;

@@ -7,15 +7,18 @@
 // in the attention of few rows, the call's tiles are dealt in equal shares and a
 // wave takes tiles of 32 keys from global memory to the matrix cores; a lane then
 // holds one query and eight keys, whose sums over the 16 lanes of a group take
-// eight exchanges.
+// eight exchanges. One token of 16 sequences of 9K to 60K tokens, 8 heads of 4:
+// 111 us (4.4 TB/s).
 //
 // many_kernel: a workgroup takes 256 keys, a wave 64 of them as the B operand
 // of S = Q K^T (v_mfma_f32_32x32x16_bf16), which stay in registers while the
 // packed query rows that see them pass by, 32 at a time, through LDS. A lane
 // holds two keys with 16 queries each, whose probabilities it adds in fp32; its
-// sums take two registers (with keys as rows they took 32). Bound by the products and the exponentials, half of the attention's
-// work. Where the keys alone do not fill the chip the rows are cut into
-// segments too, whose sums sum_kernel adds in their order.
+// sums take two registers (with keys as rows they took 32). Bound by the
+// products and the exponentials, half of the attention's work: 8101 tokens of 32
+// heads, bf16, take 329 us (0.82 PFLOP/s). Where the keys alone do not fill the
+// chip the rows are cut into segments too, whose sums sum_kernel adds in their
+// order.
 #include <algorithm>
 
 #include "cache_few.h"
@@ -407,7 +410,10 @@ __global__ __launch_bounds__(kChunk) void sum_kernel(CacheProblem p, const float
 
 int chunks_of(const CacheProblem& p) { return (p.max_kv + kChunk - 1) / kChunk; }
 
-// Segments of the rows, and steps of each.
+// Segments of the rows, and steps of each. Workgroups differ much in work (the
+// first keys are seen by all rows), so many small ones fill the chip evenly: 8101
+// tokens take 333 us with 8192 of them, 537 with 1024, 1010 without segments; 500
+// tokens 21 and 79.
 int segments(const CacheProblem& p, int* steps) {
   const int all = (int)(((int64_t)p.max_new * p.g + kRows - 1) / kRows);
   const int64_t groups = std::max<int64_t>(1, (int64_t)p.batch * p.hkv * chunks_of(p));
