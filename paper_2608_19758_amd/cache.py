@@ -15,9 +15,10 @@ import ctypes
 import dataclasses
 from typing import Optional
 
+import numpy as np
 import torch
 
-from . import _F32, _INT32, BF16, FP8_E4M3, HEAD_DIM, _check, _host_ptr, lib
+from . import _F32, _INT32, BF16, FP8_E4M3, HEAD_DIM, _check, lib
 
 
 CACHE_WORKSPACE_MAX = 140 << 20     # FP2_CACHE_WORKSPACE_MAX
@@ -90,87 +91,105 @@ def alloc_cache(p: CacheParams, num_pages: int, device="cuda", k_scale=None, v_s
                    torch.zeros(shape, dtype=dt, device=device), k_scale, v_scale)
 
 
-_ROWS = {BF16: (torch.bfloat16,), FP8_E4M3: (torch.uint8, torch.float8_e4m3fn)}
-_BF16 = (torch.bfloat16,)
-_U8 = (torch.uint8,)
 _BYTES = (torch.uint8, torch.int8)
+_CODES = (torch.uint8, torch.float8_e4m3fn)
+_ONE_BF16, _ONE_U8, _ONE_F32, _ONE_I32 = ((t,) for t in (torch.bfloat16, torch.uint8, *_F32, *_INT32))
+_NUMPY_I32 = np.dtype(np.int32)
 
 
 class _Args:
     """Checks tensors one by one and gives their addresses: CUDA tensors on one device, dense, of the
-    right type and of at least `least` elements. The C ABI sees only pointers."""
+    right type and of at least `least` elements. The C ABI sees only pointers. (Half of a small call's
+    time is spent here, so each property of a tensor is asked for once.)"""
+    __slots__ = ("dev", "odd")
 
     def __init__(self):
-        self.dev = None
-        self.odd = None     # first tensor that is not on the device of the others, refused at the end
+        self.dev = None     # index of the first tensor's device
+        self.odd = None     # first tensor that is not on a CUDA device, or on another one; refused at the end
 
     def __call__(self, name, t, dtypes, least=0, multiple=1):
         if t is None:
             return None
         if not isinstance(t, torch.Tensor):
             raise ValueError("%s must be a torch tensor" % name)
-        n = t.numel()
         if t.dtype not in dtypes:
             raise ValueError("%s must have dtype in %s, got %s" % (name, dtypes, t.dtype))
         if not t.is_contiguous():
             raise ValueError("%s must be contiguous" % name)
-        if n < least or n % multiple:
-            raise ValueError("%s holds %d elements, needs at least %d and a multiple of %d"
-                             % (name, n, least, multiple))
-        if self.dev is None:
-            self.dev = t.device
-        if (t.device != self.dev or not t.is_cuda) and self.odd is None:
-            self.odd = (name, t.device)
+        if least or multiple > 1:
+            n = t.numel()
+            if n < least or n % multiple:
+                raise ValueError("%s holds %d elements, needs at least %d and a multiple of %d"
+                                 % (name, n, least, multiple))
+        dev = t.get_device()
+        if dev != self.dev or dev < 0:
+            if self.dev is None:
+                self.dev = dev
+            if (dev != self.dev or dev < 0) and self.odd is None:
+                self.odd = (name, t.device)
         return t.data_ptr()
 
-    def table(self, p, name, t, width):
-        if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.shape[1] != width or t.shape[0] < p.batch:
-            raise ValueError("%s must be int32 [>= batch, %d], got %s"
-                             % (name, width, tuple(getattr(t, "shape", ()))))
-        return self(name, t, _INT32)
+    def table(self, batch, name, t, width):
+        shape = t.shape if isinstance(t, torch.Tensor) else ()
+        if len(shape) != 2 or shape[1] != width or shape[0] < batch:
+            raise ValueError("%s must be int32 [>= batch, %d], got %s" % (name, width, tuple(shape)))
+        return self(name, t, _ONE_I32)
 
     def weights(self, p, name, w):
         if w is None:
             return None
-        if w.dim() != 3 or w.shape[0] < p.batch or w.shape[1] != p.num_kv_heads or w.shape[2] < p.max_kv_len:
+        shape = w.shape if isinstance(w, torch.Tensor) else ()
+        if len(shape) != 3 or shape[0] < p.batch or shape[1] != p.num_kv_heads or shape[2] < p.max_kv_len:
             raise ValueError("%s must be fp32 [>= batch, num_kv_heads, >= max_kv_len], got %s"
-                             % (name, tuple(w.shape)))
-        return self(name, w, _F32)
+                             % (name, tuple(shape)))
+        return self(name, w, _ONE_F32)
 
     def cache(self, p, c, need_v=True):
         """fp2_kv_cache_t of the cache."""
-        row = max(1, p.num_kv_heads * p.head_dim * max(1, p.page_size))
-        rows = _ROWS.get(p.dtype, ())
+        heads, scale_tokens, dtype = p.num_kv_heads, p.scale_tokens, p.dtype
+        row = max(1, heads * p.head_dim * max(1, p.page_size))
+        rows = _ONE_BF16 if dtype == BF16 else _CODES if dtype == FP8_E4M3 else ()
         k = self("cache.k", c.k, rows, 0, row)
-        v = self("cache.v", c.v, rows, 0, row) if need_v or c.v is not None else None
-        if v is not None and c.v.numel() != c.k.numel():
+        v = self("cache.v", c.v, rows) if need_v or c.v is not None else None
+        size = c.k.numel()
+        if v is not None and c.v.numel() != size:
             raise ValueError("cache.k and cache.v differ in size")
-        if p.dtype != FP8_E4M3:
+        if dtype != FP8_E4M3:
             return _CachePointers(k, v, None, None, None, None)
         if c.k_scale is None or (need_v and c.v_scale is None):
             raise ValueError("cache.k_scale or cache.v_scale is missing")
-        if p.scale_tokens > 0:
-            least = c.k.numel() // (p.scale_tokens * p.head_dim)
-            ks, vs = self("cache.k_scale", c.k_scale, _U8, least), self("cache.v_scale", c.v_scale, _U8, least)
+        if scale_tokens > 0:
+            least = size // (scale_tokens * p.head_dim)
+            ks, vs = (self("cache.k_scale", c.k_scale, _ONE_U8, least),
+                      self("cache.v_scale", c.v_scale, _ONE_U8, least))
             return _CachePointers(k, v, None, None, ks, vs)
-        ks, vs = (self("cache.k_scale", c.k_scale, _F32, p.num_kv_heads),
-                  self("cache.v_scale", c.v_scale, _F32, p.num_kv_heads))
+        ks, vs = self("cache.k_scale", c.k_scale, _ONE_F32, heads), self("cache.v_scale", c.v_scale, _ONE_F32, heads)
         return _CachePointers(k, v, ks, vs, None, None)
 
-    def lengths(self, p, cu, cuk, host, host_k, rows=None):
-        """Device and host lengths; `rows`: new tokens that the call's tensors hold."""
-        for name, t in (("cu_seqlens_host", host), ("cu_seqlens_k_host", host_k)):
-            if t is None:
-                continue
-            torch_t = isinstance(t, torch.Tensor)
-            if (t.dtype != torch.int32 or t.is_cuda) if torch_t else t.dtype != "int32":
-                raise ValueError("%s must be a host int32 array" % name)
-            if (t.numel() if torch_t else t.size) < p.batch + 1:
-                raise ValueError("%s must have batch + 1 entries" % name)
-            if t is host and rows is not None and int(t[p.batch]) > rows:
-                raise ValueError("%d new tokens, tensors hold %d" % (int(t[p.batch]), rows))
-        return (self("cu_seqlens", cu, _INT32, p.batch + 1), _host_ptr(host),
-                self("cu_seqlens_k", cuk, _INT32, p.batch + 1), _host_ptr(host_k))
+    @staticmethod
+    def host(name, t, batch, rows=None):
+        """Address of a host array of lengths; `rows`: new tokens that the call's tensors hold."""
+        if t is None:
+            return None
+        if isinstance(t, torch.Tensor):
+            ok = t.dtype == torch.int32 and not t.is_cuda and t.is_contiguous()
+            size, at = t.numel(), t.data_ptr()
+        else:
+            ok = t.dtype == _NUMPY_I32 and t.flags.c_contiguous
+            size, at = t.size, None
+        if not ok:
+            raise ValueError("%s must be a dense host int32 array" % name)
+        if size < batch + 1:
+            raise ValueError("%s must have batch + 1 entries" % name)
+        if rows is not None and t[batch] > rows:
+            raise ValueError("%d new tokens, tensors hold %d" % (int(t[batch]), rows))
+        if at is None:   # (.ctypes.data takes five times as long, and serves arrays that are read-only)
+            at = ctypes.byref(ctypes.c_int32.from_buffer(t)) if t.flags.writeable else t.ctypes.data
+        return at
+
+    def lengths(self, batch, cu, cuk, host, host_k, rows=None):
+        return (self("cu_seqlens", cu, _ONE_I32, batch + 1), self.host("cu_seqlens_host", host, batch, rows),
+                self("cu_seqlens_k", cuk, _ONE_I32, batch + 1), self.host("cu_seqlens_k_host", host_k, batch))
 
     def call(self, name, stream, *args):
         """The entry point on `stream` (the current one of the tensors' device if None), with that
@@ -179,15 +198,18 @@ class _Args:
             raise ValueError("%s must be a CUDA tensor on the device of the others (%s), got one on %s"
                              % (self.odd[0], self.dev, self.odd[1]))
         if stream is None:
-            stream = torch.cuda.current_stream(self.dev)
-        elif stream.device != self.dev:
-            raise ValueError("stream is on %s, the tensors on %s" % (stream.device, self.dev))
-        if torch.cuda.current_device() == self.dev.index:
-            st = getattr(lib(), name)(*args, stream.cuda_stream)
+            handle = torch._C._cuda_getCurrentRawStream(self.dev)
+        elif stream.device.index != self.dev:
+            raise ValueError("stream is on %s, the tensors on cuda:%d" % (stream.device, self.dev))
+        else:
+            handle = stream.cuda_stream
+        if torch.cuda.current_device() == self.dev:
+            st = getattr(lib(), name)(*args, handle)
         else:
             with torch.cuda.device(self.dev):
-                st = getattr(lib(), name)(*args, stream.cuda_stream)
-        _check(name, st)
+                st = getattr(lib(), name)(*args, handle)
+        if st:
+            _check(name, st)
 
 
 def on_stream(stream):
@@ -200,14 +222,15 @@ def cache_append(p: CacheParams, k_new, v_new, cache: KVCache, cu_seqlens, cu_se
                  *, cu_seqlens_host=None, cu_seqlens_k_host=None, stream=None) -> None:
     """fp2_cache_append: k_new and v_new bf16 [new tokens, num_kv_heads, 128] into the
     cache's pages, in its type."""
-    a = _Args()
+    a, batch = _Args(), p.batch
     c = a.cache(p, cache)
     row = p.num_kv_heads * p.head_dim
-    k, v = a("k_new", k_new, _BF16, 0, row), a("v_new", v_new, _BF16, 0, row)
-    if k_new.numel() != v_new.numel():
-        raise ValueError("k_new and v_new differ in size")
-    lens = a.lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host, k_new.numel() // row)
-    table = a.table(p, "block_table", block_table, p.max_pages_per_seq)
+    k, v = a("k_new", k_new, _ONE_BF16), a("v_new", v_new, _ONE_BF16)
+    size = k_new.numel()
+    if size != v_new.numel() or size % row:
+        raise ValueError("k_new and v_new must be of one size and hold rows of %d" % row)
+    lens = a.lengths(batch, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host, size // row)
+    table = a.table(batch, "block_table", block_table, p.max_pages_per_seq)
     a.call("fp2_cache_append", stream, ctypes.byref(p), k, v, *lens, ctypes.byref(c), table)
 
 
@@ -215,21 +238,22 @@ def cache_attend(p: CacheParams, q, cache: KVCache, cu_seqlens, cu_seqlens_k, bl
                  lse=None, want_lse=False, workspace=None, cu_seqlens_host=None,
                  cu_seqlens_k_host=None, stream=None):
     """fp2_cache_attend: returns (out bf16 like q, lse fp32 [tokens, num_q_heads] or None)."""
-    a = _Args()
-    row = p.num_q_heads * p.head_dim
-    qp = a("q", q, _BF16, 0, row)
-    rows = q.numel() // row
+    a, batch, heads = _Args(), p.batch, p.num_q_heads
+    row = heads * p.head_dim
+    qp = a("q", q, _ONE_BF16, 0, row)
+    size = q.numel()
+    rows = size // row
     c = a.cache(p, cache)
-    lens = a.lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host, q.numel() // row)
-    table = a.table(p, "block_table", block_table, p.max_pages_per_seq)
+    lens = a.lengths(batch, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host, rows)
+    table = a.table(batch, "block_table", block_table, p.max_pages_per_seq)
     with on_stream(stream):
         if out is None:
             out = torch.empty_like(q)
         if lse is None and want_lse:
-            lse = torch.empty((rows, p.num_q_heads), dtype=torch.float32, device=q.device)
+            lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device)
         if workspace is None:
             workspace = alloc_cache_workspace(p, q.device)
-    op, lp = a("out", out, _BF16, q.numel()), a("lse", lse, _F32, rows * p.num_q_heads)
+    op, lp = a("out", out, _ONE_BF16, size), a("lse", lse, _ONE_F32, rows * heads)
     ws = a("workspace", workspace, _BYTES)
     a.call("fp2_cache_attend", stream, ctypes.byref(p), qp, *lens, ctypes.byref(c), table, op, lp, ws,
            workspace.numel())
@@ -242,13 +266,14 @@ def cache_weights(p: CacheParams, q, lse, cache: KVCache, cu_seqlens, cu_seqlens
     """fp2_cache_weights: weights = weights_in (zeros if None) plus what each cached token
     received of these queries, fp32 [batch, num_kv_heads, max_kv_len or more]. To add in
     place give the same tensor as both."""
-    a = _Args()
+    a, batch = _Args(), p.batch
     row = p.num_q_heads * p.head_dim
-    qp = a("q", q, _BF16, 0, row)
-    lp = a("lse", lse, _F32, q.numel() // p.head_dim)
+    qp = a("q", q, _ONE_BF16, 0, row)
+    size = q.numel()
+    lp = a("lse", lse, _ONE_F32, size // p.head_dim)
     c = a.cache(p, cache, need_v=False)
-    lens = a.lengths(p, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host, q.numel() // row)
-    table = a.table(p, "block_table", block_table, p.max_pages_per_seq)
+    lens = a.lengths(batch, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host, size // row)
+    table = a.table(batch, "block_table", block_table, p.max_pages_per_seq)
     wi = a.weights(p, "weights_in", weights_in)
     with on_stream(stream):
         if weights is None:
@@ -277,28 +302,28 @@ def cache_evict(p: CacheParams, cache: KVCache, weights, cu_seqlens_k, block_tab
     """fp2_cache_evict: the `budget` tokens of each sequence and KV head that stay go to the
     pages of target_table (int32 [batch, pages], other pages than block_table's). Returns
     (kept int32 [batch, num_kv_heads, budget], the new cu_seqlens_k, the weights that stay)."""
-    a = _Args()
+    a, batch = _Args(), p.batch
     c = a.cache(p, cache)
-    _, _, cuk, cuk_host = a.lengths(p, None, cu_seqlens_k, None, cu_seqlens_k_host)
-    table = a.table(p, "block_table", block_table, p.max_pages_per_seq)
-    pages = target_table.shape[1] if isinstance(target_table, torch.Tensor) and target_table.dim() == 2 else -1
-    target = a.table(p, "target_table", target_table, pages)
+    _, _, cuk, cuk_host = a.lengths(batch, None, cu_seqlens_k, None, cu_seqlens_k_host)
+    table = a.table(batch, "block_table", block_table, p.max_pages_per_seq)
+    pages = target_table.shape[-1] if isinstance(target_table, torch.Tensor) and target_table.dim() else -1
+    target = a.table(batch, "target_table", target_table, pages)
     w = a.weights(p, "weights", weights)
-    dev, heads = cache.k.device, p.batch * p.num_kv_heads
+    heads, stride = p.num_kv_heads, weights.shape[2]
     with on_stream(stream):
         if kept is None:
-            kept = torch.empty((p.batch, p.num_kv_heads, max(1, budget)), dtype=torch.int32, device=dev)
+            kept = cache.k.new_empty((batch, heads, max(1, budget)), dtype=torch.int32)
         if cu_seqlens_k_out is None:
-            cu_seqlens_k_out = torch.empty(p.batch + 1, dtype=torch.int32, device=dev)
+            cu_seqlens_k_out = cache.k.new_empty(batch + 1, dtype=torch.int32)
         if weights_out is None:
-            weights_out = torch.empty((p.batch, p.num_kv_heads, weights.shape[2]), dtype=torch.float32, device=dev)
+            weights_out = weights.new_empty((batch, heads, stride))
     wo = a.weights(p, "weights_out", weights_out)
-    if weights_out.shape[2] != weights.shape[2]:
+    if weights_out.shape[2] != stride:
         raise ValueError("weights and weights_out differ in their last size")
-    kp = a("kept", kept, _INT32, heads * budget)
-    co = a("cu_seqlens_k_out", cu_seqlens_k_out, _INT32, p.batch + 1)
-    a.call("fp2_cache_evict", stream, ctypes.byref(p), ctypes.byref(c), cuk, cuk_host, table, target,
-           target_table.shape[1], int(budget), int(recent_tokens), w, wo, weights.shape[2], kp, co)
+    kp = a("kept", kept, _ONE_I32, batch * heads * budget)
+    co = a("cu_seqlens_k_out", cu_seqlens_k_out, _ONE_I32, batch + 1)
+    a.call("fp2_cache_evict", stream, ctypes.byref(p), ctypes.byref(c), cuk, cuk_host, table, target, pages,
+           int(budget), int(recent_tokens), w, wo, stride, kp, co)
     if p.batch == 0 or p.max_kv_len == 0:                                      # a call without tokens
         with on_stream(stream):
             kept.fill_(-1), cu_seqlens_k_out.zero_(), weights_out.zero_()

@@ -239,6 +239,28 @@ def test_rows_of_the_call():
         fp2.cache_weights(p, t["q"], t["lse"], t["cache"], t["cu"], t["cu"], t["table"], cu_seqlens_host=h)
 
 
+def test_host_lengths():
+    """Strided, short and mistyped host lengths are refused; read-only ones and torch's serve."""
+    p = base()
+    t = tensors(p)
+
+    def append(h, hk=None):
+        with pytest.raises(ValueError) as e:
+            fp2.cache_append(p, t["new"], t["new"], t["cache"], t["cu"], t["cu"], t["table"], cu_seqlens_host=h,
+                             cu_seqlens_k_host=hk)
+        return str(e.value)
+
+    z = np.zeros(6, np.int32)
+    for h in (z[::2], z.astype(np.int64), z.astype(np.float32), torch.zeros(6, dtype=torch.int32)[::2],
+              torch.zeros(3, dtype=torch.int64)):
+        assert "dense host int32" in append(h) and "dense host int32" in append(None, h)
+    assert "batch + 1" in append(z[:2]) and "batch + 1" in append(None, torch.zeros(2, dtype=torch.int32))
+    z.flags.writeable = False
+    for h in (z, torch.zeros(3, dtype=torch.int32)):
+        assert "must be a CUDA tensor" in append(h, h)       # all is well but for the device
+    assert fc._Args.host("x", z, 2) == z.ctypes.data
+
+
 def test_alloc_cache():
     p = base()
     c = fp2.alloc_cache(p, 10, device="cpu")
