@@ -17,9 +17,9 @@
 // cores' type (half a step of 2^-8 each); sums, maxima and outputs are fp32.
 //
 // Bound by the products and, beside them, a step's chain of exponentials: a
-// prompt of 32K tokens, 32 heads, window 4096, takes 2.17 ms from codes with
-// scales of 64 tokens (0.95 PFLOP/s; a large bf16 matrix product reaches 1.22)
-// and 2.43 from a bf16 cache, whose tiles take twice the loads.
+// prompt of 32K tokens, 32 heads, window 4096, takes 2.10 ms from codes with
+// scales of 64 tokens (0.98 PFLOP/s; a large bf16 matrix product reaches 1.22)
+// and 2.36 from a bf16 cache, whose tiles take twice the loads.
 //
 // Calls of few units cut each unit's tiles into equal parts, joined by
 // join_kernel.
@@ -113,8 +113,8 @@ struct Shared {
 };
 
 // FORM: the cache's type. WIDE: pages hold a multiple of 64 tokens, so a tile
-// lies in one and its address is uniform (scalar). The prompt above in bf16: 2.43
-// ms, from pages of 48 tokens 2.62.
+// lies in one and its address is uniform (scalar). The prompt above in bf16: 2.36
+// ms, from pages of 48 tokens 2.6.
 template <int FORM, bool WIDE>
 __global__ __launch_bounds__(64 * kWaves, 1) void extend_kernel(CacheProblem p, CachePartials part,
                                                                 int nq, int parts,
@@ -294,8 +294,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void extend_kernel(CacheProblem p, 
             __builtin_bit_cast(bf16x8_t, kt[kplace(32 * uu + l32, 2 * ds + half)]), qb[ds], s[uu], 0, 0, 0);
     }
   };
-  // scores become probabilities, against a maximum that moves when a score passes it by more than kTau
-  auto softmax = [&](f32x16_t (&s)[2]) {
+  // the maximum that scores become probabilities against moves when one passes it by more than kTau
+  auto move_max = [&](const f32x16_t (&s)[2]) {
     float mx = -INFINITY;
 #pragma unroll
     for (int uu = 0; uu < 2; ++uu)
@@ -312,6 +312,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void extend_kernel(CacheProblem p, 
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[dt][e] *= f;
     }
+  };
+  auto exponentials = [&](f32x16_t (&s)[2]) {
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int uu = 0; uu < 2; ++uu)
@@ -371,7 +373,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void extend_kernel(CacheProblem p, 
   };
 
   // Keys run one tile ahead of values: the scores of the next tile are computed
-  // while the softmax of this one runs on the vector ALUs.
+  // while the exponentials of this one run on the vector ALUs (in one block, behind
+  // the branch that moves the maximum: 2.10 ms, with the scores before it 2.13).
   Regs regs;
   if (tid < 4) sh.bad[tid] = 0;
   __syncthreads();
@@ -394,9 +397,10 @@ __global__ __launch_bounds__(64 * kWaves, 1) void extend_kernel(CacheProblem p, 
     load(at, regs);
     at = where(i + 3);
     const int k0 = key0_at(i);
-    qk(i + 1, y);
     if (masked(k0)) mask(k0, x);
-    softmax(x);
+    move_max(x);
+    qk(i + 1, y);
+    exponentials(x);
     pv(i, x);
     if (sh.bad[i & 3]) add_odd(k0);
     write_k(i + 2, regs);
@@ -477,7 +481,7 @@ __global__ __launch_bounds__(256) void join_kernel(CacheProblem p, CachePartials
 int query_tiles(const CacheProblem& p) { return (p.max_new * p.g + kRows - 1) / kRows; }
 
 // Parts of a unit: as many as fill the chip, of at least kMinTiles tiles. 256
-// tokens behind 30000 take 151 us, and 896 whole; 256 behind 1000 28 us, with
+// tokens behind 30000 take 141 us, and 896 whole; 256 behind 1000 28 us, with
 // parts of 8 tiles or more 36.
 int parts_for(const CacheProblem& p) {
   const int64_t units = (int64_t)p.batch * p.hkv * query_tiles(p);
