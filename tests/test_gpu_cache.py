@@ -243,6 +243,17 @@ def test_append(form, page, odd):
         run_append(c, k, v, new)
 
 
+@pytest.mark.parametrize("form,page", [("bf16", 24), ("head", 16), (16, 64), (32, 96), (128, 128)])
+@pytest.mark.parametrize("new", [16, 17])
+def test_append_few_tokens(form, page, new):
+    """Few new tokens of many sequences, over the edges of blocks, with scales that grow and that do not."""
+    lens = [0, 1, 15, 16, 31, 113, 120, 127, 128, 250]
+    count = [new, 16, 1, 0, 16, 16, 9, 1, 16, 7]
+    for size in (0.01, 1, 30.0):
+        c, k, v = grown(lens, count, form, page, seed=31, size=size)
+        run_append(c, k, v, count)
+
+
 @pytest.mark.parametrize("size", [1e-36, 1e-30, 1e30, 1e38])
 def test_append_extreme_sizes(size):
     c, k, v = grown([0, 20], [40, 3], 16, 16, size=size)
