@@ -104,6 +104,7 @@ __device__ __forceinline__ T pinned(T x) {
 struct CachePartials {
   float* o;                 // [slots, rows, d]
   float* ml;                // [slots, rows, 2] {running maximum (base 2), denominator}
+  int32_t* at;              // few rows, equal shares: [batch, 2] {first share, parts} of a sequence
 };
 
 // At most this many packed rows (new tokens times heads of a group) a sequence

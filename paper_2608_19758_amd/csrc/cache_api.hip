@@ -156,17 +156,19 @@ bool few_rows(const CacheProblem& r) { return (int64_t)r.max_new * r.g <= fp2::k
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Bytes that the attention needs, and the offset of the maxima behind the
-// partial outputs.
-size_t attend_bytes(const CacheProblem& r, size_t* ml) {
+// Bytes that the attention needs, and the offsets of the maxima and of the
+// sequences' parts behind the partial outputs.
+size_t attend_bytes(const CacheProblem& r, size_t* ml, size_t* at) {
   int64_t slots = 0;
   int rows = 0;
+  const bool few = few_rows(r);
   if (r.batch > 0 && r.max_new > 0) {
-    if (few_rows(r)) fp2::cache_decode_partials(r, &slots, &rows);
+    if (few) fp2::cache_decode_partials(r, &slots, &rows);
     else fp2::cache_extend_partials(r, &slots, &rows);
   }
   *ml = (size_t)slots * rows * fp2::kHeadDim * sizeof(float);   // a multiple of 256
-  return *ml + align256((size_t)slots * rows * 2 * sizeof(float));
+  *at = *ml + align256((size_t)slots * rows * 2 * sizeof(float));
+  return *at + (few && slots && !r.splits ? align256((size_t)r.batch * 2 * sizeof(int32_t)) : 0);
 }
 
 size_t weights_bytes(const CacheProblem& r) {
@@ -194,8 +196,8 @@ extern "C" {
 size_t fp2_cache_workspace_bytes(const fp2_cache_params_t* params) {
   if (check_params(params) != FP2_OK) return 0;
   const CacheProblem r = make_problem(params, nullptr, nullptr, nullptr, nullptr, nullptr);
-  size_t ml;
-  const size_t a = attend_bytes(r, &ml), w = weights_bytes(r);
+  size_t ml, at;
+  const size_t a = attend_bytes(r, &ml, &at), w = weights_bytes(r);
   return a > w ? a : w;
 }
 
@@ -234,9 +236,10 @@ fp2_status_t fp2_cache_attend(const fp2_cache_params_t* params, const void* q,
   if (!aligned(q, 16) || !aligned(out, 16)) return fail(FP2_EINVAL, "q and out must be 16-byte aligned");
   if (q == out) return fail(FP2_EINVAL, "out must not be q");
   const CacheProblem r = make_problem(params, q, cu_seqlens, cu_seqlens_k, cache, block_table);
-  size_t ml;
-  if ((st = check_workspace(workspace, workspace_bytes, attend_bytes(r, &ml)))) return st;
-  const fp2::CachePartials part{(float*)workspace, (float*)((char*)workspace + ml)};
+  size_t ml, at;
+  if ((st = check_workspace(workspace, workspace_bytes, attend_bytes(r, &ml, &at)))) return st;
+  const fp2::CachePartials part{(float*)workspace, (float*)((char*)workspace + ml),
+                                (int32_t*)((char*)workspace + at)};
   const hipError_t e =
       few_rows(r) ? fp2::launch_cache_decode(r, part, (uint16_t*)out, lse, (hipStream_t)stream)
                   : fp2::launch_cache_extend(r, part, (uint16_t*)out, lse, (hipStream_t)stream);

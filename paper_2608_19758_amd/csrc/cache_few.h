@@ -73,10 +73,8 @@ inline __host__ __device__ int shares_of(const CacheProblem& p) {
 
 __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
-// Share `index` of the call, or, with BY_SEQ, sequence `index` (lo .. hi then
-// are all its tiles). Wave-uniform; false where there is none. A call has
+// Share `index` of the call. Wave-uniform; false where there is none. A call has
 // fewer than 2^31 tiles (the host's check).
-template <bool BY_SEQ>
 __device__ __forceinline__ bool find_share(const CacheProblem& p, int shares, int index, Share& out) {
   const int lane = threadIdx.x & 63;
   int q0, Lq, L;
@@ -95,9 +93,9 @@ __device__ __forceinline__ bool find_share(const CacheProblem& p, int shares, in
     out.L = lane_value(L, l);
   };
   if (p.splits) {
-    const int b = BY_SEQ ? index : index / p.splits, part = BY_SEQ ? 0 : index % p.splits;
+    const int b = index / p.splits, part = index % p.splits;
     const int n = lane_value(tiles_at(b), 0);
-    const int parts = BY_SEQ ? 1 : min(p.splits, n);
+    const int parts = min(p.splits, n);
     if (part >= parts) return false;
     out.lo = (int)((int64_t)n * part / parts);
     out.hi = (int)((int64_t)n * (part + 1) / parts);
@@ -108,28 +106,29 @@ __device__ __forceinline__ bool find_share(const CacheProblem& p, int shares, in
   }
   // tiles before each sequence, 64 of them at a time; up to 64 are looked at once
   int n = tiles_at(lane), incl = wave_scan(n), total = lane_value(incl, 63);
-  for (int b0 = 64; b0 < p.batch; b0 += 64) {
-    total += lane_value(wave_scan(tiles_at(b0 + lane)), 63);
+  if (p.batch > 64) {
+    int more = 0;
+#pragma unroll 4
+    for (int b0 = 64; b0 < p.batch; b0 += 64) more += tiles_at(b0 + lane);
+    total += lane_value(wave_scan(more), 63);
   }
   out.len = max((int)(((int64_t)total + shares - 1) / shares), 1);
   out.lo = (int)min((int64_t)index * out.len, (int64_t)total);
   out.hi = (int)min((int64_t)out.lo + out.len, (int64_t)total);
-  if (!BY_SEQ && out.lo >= out.hi) return false;
+  if (out.lo >= out.hi) return false;
   int before = 0;
   for (int b0 = 0; b0 < p.batch; b0 += 64) {
     if (p.batch > 64) {
       n = tiles_at(b0 + lane);
       incl = before + wave_scan(n);
     }
-    const uint64_t hit = __ballot(BY_SEQ ? b0 + lane == index : incl > out.lo);
+    const uint64_t hit = __ballot(incl > out.lo);
     if (hit) {
       const int l = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)hit) - 1);
-      const int nl = lane_value(n, l);
       out.b = b0 + l;
-      out.base = lane_value(incl, l) - nl;
+      out.base = lane_value(incl, l) - lane_value(n, l);
       take(l);
-      if (BY_SEQ) out.lo = out.base, out.hi = out.base + nl;
-      return out.lo < out.hi;
+      return true;
     }
     before = lane_value(incl, 63);
   }

@@ -60,7 +60,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(CacheProblem p, con
     return;
   }
   Share sh;
-  if (!find_share<false>(p, shares, index, sh)) return;
+  if (!find_share(p, shares, index, sh)) return;
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.x % groups * p.heads + w % p.heads, ks = w / p.heads;
