@@ -31,7 +31,7 @@
 // One token of each of 32 sequences of 1.3K to 112K tokens, 8 heads of 4: 274 us
 // in codes (5.5 TB/s), 525 in bf16 (5.7); one sequence of 128K 63 us, of which 9
 // are the join; 64 with windows of 4096 tokens 92 us. 8 drafted tokens and 8
-// heads a group (64 rows), 8 sequences: 100 us (3.1 TB/s); there a wave alone on
+// heads a group (64 rows), 8 sequences: 96 us (3.2 TB/s); there a wave alone on
 // its SIMD has products and exponentials one after the other.
 #include <algorithm>
 #include <type_traits>
@@ -455,8 +455,9 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
 // Joins the parts of the units that were cut. Where a sequence's parts lie the
 // workgroup that took its start left in the workspace (looked for among the
 // lengths again, 2000 sequences of 1000 tokens take 1495 us instead of 767, 128 of
-// 8000 416 instead of 401). A workgroup takes one packed row, groups of 32 lanes the parts in turn, eight of them a step with all
-// their loads in flight; the groups are joined in LDS.
+// 8000 416 instead of 401). A workgroup takes one packed row, groups of 32 lanes
+// the parts in turn, eight of them a step with all their loads in flight; the
+// groups are joined in LDS.
 __global__ __launch_bounds__(1024) void combine_kernel(CacheProblem p, CachePartials part,
                                                       int rows_cap, int max_rows,
                                                       uint16_t* __restrict__ out,
@@ -522,12 +523,12 @@ __global__ __launch_bounds__(1024) void combine_kernel(CacheProblem p, CachePart
   s_a[grp][d] = a;
   __syncthreads();
   if (tid >= 32) return;
-  const float own = m;
-  for (int i = 1; i < groups; ++i) m = fmaxf(m, s_m[i]);
-  const float f = fast_exp2(own - m);
-  l = s_l[0] * f;
-  a.x *= f, a.y *= f, a.z *= f, a.w *= f;
-  for (int i = 1; i < groups; ++i) {
+#pragma unroll 8
+  for (int i = 0; i < groups; ++i) m = fmaxf(m, s_m[i]);
+  l = 0.f;
+  a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int i = 0; i < groups; ++i) {   // (8 or 32)
     const float g = fast_exp2(s_m[i] - m);
     const float4 y = s_a[i][d];
     l += g * s_l[i];
