@@ -519,10 +519,11 @@ fp2_status_t fp2_cache_attend(const fp2_cache_params_t* params, const void* q,
  *   weights[b][h][j] = weights_in[b][h][j] + sum over the new tokens that see
  *       j and the g query heads of h of exp(scale * q.k_j - lse)
  * with q as in fp2_cache_attend and the lse that it returned. weights and
- * weights_in (nullable = zeros; weights itself, or no memory of it) are fp32 [batch,
- * num_kv_heads, weights_stride], weights_stride >= max_kv_len; entries past a
- * sequence are those of weights_in (zeros without it). No values are read: cache->v may be null. The
- * result does not depend on the order of anything (no atomics). */
+ * weights_in (nullable = zeros; weights itself, or no memory of it) are fp32
+ * [batch, num_kv_heads, weights_stride], weights_stride >= max_kv_len; entries
+ * past a sequence are those of weights_in (zeros without it). No values are
+ * read: cache->v may be null, and q and lse where max_seq_len is 0. The result
+ * does not depend on the order of anything (no atomics). */
 fp2_status_t fp2_cache_weights(const fp2_cache_params_t* params, const void* q, const float* lse,
                                const int32_t* cu_seqlens, const int32_t* cu_seqlens_host,
                                const int32_t* cu_seqlens_k, const int32_t* cu_seqlens_k_host,

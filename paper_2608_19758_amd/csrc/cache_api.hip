@@ -258,7 +258,8 @@ fp2_status_t fp2_cache_weights(const fp2_cache_params_t* params, const void* q, 
   if ((st = check_lengths(params, cu_seqlens, cu_seqlens_host, cu_seqlens_k, cu_seqlens_k_host, true)))
     return st;
   if ((st = check_cache(params, cache, block_table, false))) return st;
-  if (!q || !lse || !weights) return fail(FP2_EINVAL, "q, lse or weights is null");
+  if ((params->max_seq_len > 0 && (!q || !lse)) || !weights)
+    return fail(FP2_EINVAL, "q, lse or weights is null");
   if (!aligned(q, 16)) return fail(FP2_EINVAL, "q must be 16-byte aligned");
   if (weights_stride < params->max_kv_len)
     return fail(FP2_EINVAL, "weights_stride %lld < max_kv_len %d", (long long)weights_stride,

@@ -272,6 +272,7 @@ class CacheMetadata:
     plan: ForwardPlan
     lengths: object                # device int32: cu_q and cu_k side by side
     block_table: object            # device int32 [batch or more, max_pages_per_seq], dense
+    replayed: bool = False         # lengths and table are the metadata's own, and may be updated
 
     @property
     def params(self):
@@ -305,17 +306,20 @@ class CacheBackend:
         idle = cfg.params(cfg.max_batch, 0, cfg.max_kv_len)
         if fp2.lib().fp2_cache_append(ctypes.byref(idle), *[None] * 9):
             raise ValueError("configuration rejected by the library: " + fp2.last_error())
-        self.workspace = torch.empty(fp2.CACHE_WORKSPACE_MAX, dtype=torch.uint8, device=self.device)
+        with fp2.cache.on_stream(stream):
+            self.workspace = torch.empty(fp2.CACHE_WORKSPACE_MAX, dtype=torch.uint8, device=self.device)
 
     def alloc_cache(self, num_pages: int, k_scale=None, v_scale=None) -> "fp2.KVCache":
         """One layer's empty cache of num_pages pages."""
-        return fp2.alloc_cache(self.cfg.worst_case_params(), num_pages, self.device, k_scale, v_scale)
+        with fp2.cache.on_stream(self.stream):
+            return fp2.alloc_cache(self.cfg.worst_case_params(), num_pages, self.device, k_scale, v_scale)
 
     def alloc_weights(self):
         """One layer's weights of empty sequences: zeros [max_batch, num_kv_heads, max_kv_len]."""
         import torch
         c = self.cfg
-        return torch.zeros((c.max_batch, c.num_kv_heads, c.max_kv_len), device=self.device)
+        with fp2.cache.on_stream(self.stream):
+            return torch.zeros((c.max_batch, c.num_kv_heads, c.max_kv_len), device=self.device)
 
     def init_forward_metadata(self, extend_lens: Sequence[int], prefix_lens: Optional[Sequence[int]],
                               block_table, replayed: bool = False) -> CacheMetadata:
@@ -331,7 +335,7 @@ class CacheBackend:
             table = _dense_table(block_table, len(plan.cu_q) - 1, self.cfg.max_pages_per_seq)
             if replayed:
                 table = table.clone()
-        return CacheMetadata(plan=plan, lengths=lengths, block_table=table)
+        return CacheMetadata(plan=plan, lengths=lengths, block_table=table, replayed=replayed)
 
     def update_forward_metadata(self, meta: CacheMetadata, extend_lens: Sequence[int],
                                 prefix_lens: Optional[Sequence[int]], block_table) -> None:
@@ -340,7 +344,7 @@ class CacheBackend:
         import torch
         plan = plan_forward(self.cfg, extend_lens, prefix_lens)
         p = meta.params
-        if p.max_kv_len != self.cfg.max_kv_len:
+        if not meta.replayed:
             raise ValueError("the metadata was not made with replayed=True")
         if plan.params.batch != p.batch or plan.params.max_seq_len > p.max_seq_len:
             raise ValueError("%d sequences with extends up to %d do not fit a forward of %d with up to %d"

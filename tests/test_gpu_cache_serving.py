@@ -147,6 +147,8 @@ def test_captured_decode(form):
         be.update_forward_metadata(meta, [2, 1, 1], lens, table)
     with pytest.raises(ValueError, match="replayed"):
         be.update_forward_metadata(be.init_forward_metadata([1], [5], table), [1], [6], table)
+    with pytest.raises(ValueError, match="replayed"):      # the longest sequence: the same bounds, another table
+        be.update_forward_metadata(be.init_forward_metadata([1], [cfg.max_kv_len - 1], table), [1], [6], table)
     with pytest.raises(ValueError, match="rows"):
         be.forward(*[t[:2] for t in static], a[0], meta)
 
@@ -193,3 +195,17 @@ def test_after_a_sparse_prompt(form):
     o, tol, z, ztol, _ = ref.attend(c, x[0].cpu(), [1])
     close(got, o, tol, "out")
     close(lse, z, ztol, "lse")
+
+
+@pytest.mark.parametrize("prefix", [[0, 0], [5, 70]])
+def test_forwards_without_new_tokens(prefix):
+    cfg = config(64)
+    be = serving.CacheBackend(cfg)
+    (table,), pages = tables(cfg, 1, 7)
+    cache, w = be.alloc_cache(pages), be.alloc_weights()
+    w += 2
+    meta = be.init_forward_metadata([0, 0], prefix, table)
+    out, lse = be.forward(*rows(torch.Generator().manual_seed(3), 0), cache, meta, weights=w)
+    torch.cuda.synchronize()
+    assert out.shape[0] == 0 and lse.shape[0] == 0
+    assert bool((w == 2).all()) and not bool(cache.k.any()) and bool((cache.k_scale == 127).all())
