@@ -209,6 +209,26 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
     }
   };
 
+  // the maximum that scores become probabilities against moves when one passes it by more than kTau
+  auto move_max = [&](int nt, const f32x4_t (&s)[2]) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[u][i]);
+    mx *= cs;
+    if (__any(mx > m[nt] + kTau)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float mn = mx > m[nt] + kTau ? mx : m[nt];
+      const float f = fast_exp2(m[nt] - mn);
+      m[nt] = mn;
+      l[nt] *= f;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) o[nt][t] *= f;
+    }
+  };
+
   auto step = [&](int tile, Raw<FORM>& x) {
     const int t0 = kTile * tile;
     // keys that some row does not see: behind the first row, or before the
@@ -261,7 +281,13 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
         x.v[e].x = pinned(x.v[e].x);
       }
       if (Lq > 1 && __any(bad)) {
-        // rare: such values are added to the rows that see them by hand
+        // rare: such values are added to the rows that see them by hand, infinities
+        // (codes have none) once the maximum is this tile's: times the factor of its
+        // move, which may be 0, they would become NaN
+        if constexpr (kBf16) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) move_max(nt, s[nt]);
+        }
 #pragma unroll 1
         for (int k = 0; k < kTile; ++k) {
           const int key = t0 + k;
@@ -323,22 +349,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
     }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float mx = -INFINITY;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[nt][u][i]);
-      mx *= cs;
-      if (__any(mx > m[nt] + kTau)) {
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float mn = mx > m[nt] + kTau ? mx : m[nt];
-        const float f = fast_exp2(m[nt] - mn);
-        m[nt] = mn;
-        l[nt] *= f;
-#pragma unroll
-        for (int t = 0; t < 8; ++t) o[nt][t] *= f;
-      }
+      move_max(nt, s[nt]);
       float e[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) e[i] = fast_exp2(fmaf(s[nt][i >> 2][i & 3], cs, -m[nt]));

@@ -1,0 +1,61 @@
+"""The paged cache's operators where infinities, NaN, scales and weights of places
+that no query sees, or that no token holds, could reach a result."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_19758_amd as fp2
+from tests import cache_ref as ref
+from tests.test_gpu_cache import close, cu_of, dev, on_gpu, params, run_attend, run_evict
+
+pytestmark = pytest.mark.gpu
+
+
+def queries(new, hq, pad=3):
+    """Those that run_attend draws."""
+    return torch.randn((sum(new) + pad, hq, 128), generator=torch.Generator().manual_seed(1)).bfloat16()
+
+
+@pytest.mark.parametrize("lens,new,window,sink,splits", [
+    ([3, 2, 5], [3, 2, 4], 0, 0, 0),             # the first tile is the last one
+    ([31, 100, 64], [2, 5, 8], 0, 0, 0),
+    ([400, 97], [4, 2], 60, 5, 0),
+    ([6000, 1500], [2, 3], 0, 0, 0),             # cut into shares
+    ([6000, 1500], [2, 3], 0, 0, 7),
+    ([300, 211], [120, 90], 0, 0, 0),            # prompts
+])
+@pytest.mark.parametrize("hq,hkv", [(8, 2), (8, 1), (16, 2)])
+def test_infinite_values_come_out_as_infinities(lens, new, window, sink, splits, hq, hkv):
+    """Infinities of both signs, some seen by all rows and some by the last ones, and NaN, each in
+    dimensions of its own; where both infinities meet, NaN."""
+    inf, nan = float("inf"), float("nan")
+    c = ref.Cache(lens, hkv, "bf16", 16, seed=41)
+    for b, (L, n) in enumerate(zip(lens, new)):
+        at = {d: c.slots(b, t) for d, t in ((0, L - 1), (1, L - 2), (2, L - n))}
+        c.v[at[0], :, 0:10] = inf
+        c.v[at[1], :, 20:30] = -inf
+        c.v[at[2], :, 40:50] = inf
+        c.v[at[0], :, 60:64] = -inf
+        c.v[at[2], :, 60:64] = inf
+        c.v[at[1], :, 100:104] = nan
+    want = ref.attend(c, queries(new, hq)[:sum(new)], new, window, sink)[0]
+    row = 0
+    for n in new:                                # what the definition gives has them
+        last, first = want[row + n - 1], want[row]
+        assert (last[:, 0:10] == np.inf).all() and (last[:, 40:50] == np.inf).all()
+        assert (first[:, 40:50] == np.inf).all() and np.isnan(last[:, 60:64]).all()
+        row += n
+    run_attend(c, hq, new, window, sink, splits, weights=False)
+
+
+@pytest.mark.parametrize("L,n", [(40, 2), (400, 3), (5000, 2), (300, 100)])
+def test_an_infinity_of_the_heaviest_key(L, n):
+    """The newest key outweighs all before it by more than fp32 holds, and its value is infinite."""
+    c, hq = ref.Cache([L], 2, "bf16", 16, seed=42), 8
+    q = queries([n], hq)
+    for h in range(2):
+        c.k[c.slots(0, L - 1), h] = (30 * q[n - 1, 4 * h].float()).bfloat16()
+    c.v[c.slots(0, L - 1), :, 5:9] = float("-inf")
+    want = ref.attend(c, q[:n], [n])[0]
+    assert (want[n - 1, ::4, 5:9] == -np.inf).all()
+    run_attend(c, hq, [n], weights=False)
