@@ -312,8 +312,10 @@ __global__ __launch_bounds__(64 * kWaves) void move_kernel(CacheProblem p, PageM
         if (lane == 0 && first + RPL * i < stay)
           scales[(slot >> p.sb_shift) * p.hkv + h] = (uint8_t)byte;
       }
-      // what a code is times: 2^(old - new), at most 448 in the end
-      const float f = block_scale(old[i]) * __uint_as_float((uint32_t)(254 - byte) << 23);
+      // What a code is times: 2^(old - new), which leaves at most 448. Codes that are not
+      // 0 need at most 2^17 for that; a row of zeros may come with any scale, and its
+      // power is held finite (below, 2^-126 leaves zeros too).
+      const float f = block_scale((uint32_t)min(max((int)old[i] - byte + 127, 1), 254));
       // converted once more: kept from above they would take 16 registers a load
       uint32_t d[4];
 #pragma unroll

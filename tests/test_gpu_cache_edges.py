@@ -59,3 +59,26 @@ def test_an_infinity_of_the_heaviest_key(L, n):
     want = ref.attend(c, q[:n], [n])[0]
     assert (want[n - 1, ::4, 5:9] == -np.inf).all()
     run_attend(c, hq, [n], weights=False)
+
+
+@pytest.mark.parametrize("form", [16, 32, 64, 128])
+def test_evicted_zeros_of_large_blocks(form):
+    """Rows of zeros from blocks with a large scale: beside rows of small blocks, and blocks of nothing
+    else. They stay zeros."""
+    for large in (128 + 27, 200, 245):
+        n = 6 * form + 3
+        c = ref.Cache([n, n], 2, form, form, seed=43)
+        r = np.random.default_rng(44)
+        w = r.random((2, 2, n)).astype(np.float32)
+        for b in range(2):
+            for i in range(0, n, form):
+                at = c.slots(b, np.arange(i, min(i + form, n)))
+                for name in ("k", "v"):
+                    pool, scale = getattr(c, name), getattr(c, name + "s")
+                    scale[at[0] // form] = 27 + i // form % 2 * (large - 27)
+                    if i // form % 2:
+                        pool[at] = 0
+                        pool[at[::2], :, ::3] = 0x80                       # zeros of both signs
+                if i // form % 2:
+                    w[b, 1, i:i + form] += 1                               # head 1 keeps them first
+        run_evict(c, w, 2 * form + form // 2, 0, 0)
