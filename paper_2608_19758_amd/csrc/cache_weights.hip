@@ -171,15 +171,17 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(CacheProblem p, con
           for (int c = 0; c < 4; ++c)
             s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[u][c], qb[nt][c], s[u], 0, 0, 0);
         }
-        if (masked) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i >> 2][i & 3] = fast_exp2(fmaf(s[i >> 2][i & 3], cs, -ref[nt]));
+        if (masked) {   // behind the exponentials: lse may be NaN or infinite too
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int key = t0 + 16 * (i >> 2) + 4 * kg + (i & 3);
-            s[i >> 2][i & 3] = sees(p, pos[nt], key) ? s[i >> 2][i & 3] : -INFINITY;
+            s[i >> 2][i & 3] = sees(p, pos[nt], key) ? s[i >> 2][i & 3] : 0.f;
           }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += fast_exp2(fmaf(s[i >> 2][i & 3], cs, -ref[nt]));
+        for (int i = 0; i < 8; ++i) sum[i] += s[i >> 2][i & 3];
       }
     }
     // over the 16 lanes of a group: lanes 2 i and 2 i + 1 end with element i
@@ -350,7 +352,19 @@ __global__ __launch_bounds__(64 * kWaves, 3) void many_kernel(CacheProblem p,
         for (int u = 0; u < 2; ++u)
           s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, a[u][d], s[u], 0, 0, 0);
       }
-      // element e is row 8 (e / 4) + 4 half + e % 4 of the step, key k0 + 32 u + l32
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 z = *(const float4*)&sh.lse[t & 1][8 * i + 4 * half];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          s[u][4 * i] = fast_exp2(fmaf(s[u][4 * i], cs, -z.x));
+          s[u][4 * i + 1] = fast_exp2(fmaf(s[u][4 * i + 1], cs, -z.y));
+          s[u][4 * i + 2] = fast_exp2(fmaf(s[u][4 * i + 2], cs, -z.z));
+          s[u][4 * i + 3] = fast_exp2(fmaf(s[u][4 * i + 3], cs, -z.w));
+        }
+      }
+      // element e is row 8 (e / 4) + 4 half + e % 4 of the step, key k0 + 32 u + l32;
+      // masked behind the exponentials: lse may be NaN or infinite too
       if (k0 + kKeys - 1 > first || kRows * t + kRows > rows ||
           (k0 <= last - p.window && k0 + kKeys > p.sink)) {
 #pragma unroll
@@ -359,17 +373,14 @@ __global__ __launch_bounds__(64 * kWaves, 3) void many_kernel(CacheProblem p,
           const int pos = pr < rows ? P + (pr >> gs) : -1;   // a row past the last sees nothing
 #pragma unroll
           for (int u = 0; u < 2; ++u)
-            s[u][e] = pinned(sees(p, pos, k0 + 32 * u + l32) ? s[u][e] : -INFINITY);
+            s[u][e] = pinned(sees(p, pos, k0 + 32 * u + l32) ? s[u][e] : 0.f);
         }
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 z = *(const float4*)&sh.lse[t & 1][8 * i + 4 * half];
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int u = 0; u < 2; ++u)
-          acc[u] += (fast_exp2(fmaf(s[u][4 * i], cs, -z.x)) + fast_exp2(fmaf(s[u][4 * i + 1], cs, -z.y))) +
-                    (fast_exp2(fmaf(s[u][4 * i + 2], cs, -z.z)) + fast_exp2(fmaf(s[u][4 * i + 3], cs, -z.w)));
-      }
+          acc[u] += (s[u][4 * i] + s[u][4 * i + 1]) + (s[u][4 * i + 2] + s[u][4 * i + 3]);
     }
 #undef LOAD
 #undef STORE

@@ -82,3 +82,44 @@ def test_evicted_zeros_of_large_blocks(form):
                 if i // form % 2:
                     w[b, 1, i:i + form] += 1                               # head 1 keeps them first
         run_evict(c, w, 2 * form + form // 2, 0, 0)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("-inf")])
+@pytest.mark.parametrize("form", ["bf16", "head", 16])
+@pytest.mark.parametrize("lens,new,window,sink", [
+    ([400, 97, 33], [1, 1, 1], 60, 3), ([400, 97, 33], [4, 1, 3], 0, 0), ([2500, 97], [8, 2], 300, 3),
+    ([300, 217], [20, 17], 0, 0),                # rows in one segment
+    ([600, 411], [600, 200], 130, 5),            # and in several
+])
+def test_odd_lse_reaches_only_keys_that_its_query_sees(bad, form, lens, new, window, sink):
+    """A query whose log-sum-exp is NaN or -inf: keys that it does not see have the weights that they
+    have without it."""
+    hkv, hq = 2, 8
+    c = ref.Cache(lens, hkv, form, 16, seed=45)
+    p = params(c, hq, new, window, sink)
+    q = torch.randn((sum(new), hq, 128), generator=torch.Generator().manual_seed(7)).bfloat16()
+    cu, cuk = cu_of(new), cu_of(lens)
+    cache, args = on_gpu(c), (dev(cu), dev(cuk), dev(c.table))
+    _, lse = fp2.cache_attend(p, dev(q), cache, *args, want_lse=True)
+    want = fp2.cache_weights(p, dev(q), lse, cache, *args).cpu().numpy()
+    odd = lse.clone()
+    for b, n in enumerate(new):
+        row = int(cu[b]) + n // 3                # a row that does not see the last keys, where there are several
+        odd[row, 1] = odd[row, 6] = bad          # a query head of each KV head
+        pos = np.array([lens[b] - n + n // 3])
+        want[b][:, :lens[b]][:, ref.sees(pos, np.arange(lens[b]), window, sink)[0]] = np.nan if bad != bad else np.inf
+    start = torch.zeros(want.shape, device="cuda")
+    for got in (fp2.cache_weights(p, dev(q), odd, cache, *args),
+                fp2.cache_weights(p, dev(q), odd, cache, *args, weights=start, weights_in=start)):
+        assert np.array_equal(got.cpu().numpy(), want, equal_nan=True)
+    assert np.isfinite(want).any() and not np.isfinite(want).all()
+
+
+@pytest.mark.parametrize("form", ["bf16", "head", 16])
+@pytest.mark.parametrize("new", [1, 4, 90])
+def test_weights_beside_keys_of_nan(form, new):
+    """Keys of NaN outside the window, in tiles of their own and in those of keys that are seen."""
+    c = ref.Cache([400], 2, form, 16, seed=47)
+    for t in range(5, 400 - new - 120):
+        c.k[c.slots(0, t)] = float("nan") if form == "bf16" else 0x7f
+    run_attend(c, 8, [new], 120, 5)
