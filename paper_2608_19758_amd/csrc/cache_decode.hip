@@ -271,6 +271,13 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
           }
       // values that no row sees (the pool holds anything there) must not meet
       // the zero probabilities; nor infinities and NaN that some row does not see
+      if constexpr (FORM == kCacheBlock) {   // (a scale of 255 makes NaN of zeros)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int key = t0 + 16 * u;
+          if (key > last || (key >= p.sink && key + 15 <= first - p.window)) x.vs[u] = 127;
+        }
+      }
       bool bad = false;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {

@@ -123,3 +123,21 @@ def test_weights_beside_keys_of_nan(form, new):
     for t in range(5, 400 - new - 120):
         c.k[c.slots(0, t)] = float("nan") if form == "bf16" else 0x7f
     run_attend(c, 8, [new], 120, 5)
+
+
+@pytest.mark.parametrize("byte", [255, 254, 246, 0])
+@pytest.mark.parametrize("new", [1, 3, 70])
+@pytest.mark.parametrize("place", [0, 3, 15])
+def test_scales_that_no_query_sees(byte, new, place):
+    """Blocks wholly outside the window, or behind the first tokens, with any scale byte and any codes,
+    also where they share a tile with keys that are seen."""
+    L, sink = 500, 5
+    first = 212 + place                                  # the first row's window begins in the second half of a tile
+    window = L - new + 1 - first
+    c = ref.Cache([L], 2, 16, 16, seed=46)
+    for t in range(16, first - 15, 16):
+        at = c.slots(0, np.arange(t, t + 16))
+        for name in ("k", "v"):
+            getattr(c, name + "s")[at[0] // 16] = byte
+            getattr(c, name)[at] = torch.tensor([0, 0x38, 0x7e, 0x7f] * 4, dtype=torch.uint8)[:, None, None]
+    run_attend(c, 8, [new], window, sink)
