@@ -440,7 +440,9 @@ fp2_status_t fp2_prefill_noalloc(const fp2_params_t* params, const void* q,
  * keeps cu_seqlens_k[b + 1] - cu_seqlens_k[b] >= the new tokens, the table's
  * entries for all tokens of a sequence (those that no query sees too) inside
  * the pool, and page_size whole slots behind each. A call with batch 0, or
- * without tokens by its bounds, is accepted and writes nothing.
+ * without tokens by its bounds, is accepted and writes nothing; one whose
+ * bounds ask for 2^32 threads of a kernel or more (some 2^23 workgroups) is
+ * refused with FP2_EUNSUPPORTED, as a whole.
  *
  * A query at position t sees key j <= t where window_tokens is 0; else where
  * also t - j < window_tokens or j < sink_tokens. What lies in slots that no

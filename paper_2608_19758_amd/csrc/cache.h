@@ -100,6 +100,10 @@ __device__ __forceinline__ T pinned(T x) {
   return x;
 }
 
+// Whether a launch of so many workgroups may be made: HIP counts its threads in
+// 32 bits. Asked for every kernel of a call before the first of them.
+inline bool launchable(int64_t groups, int threads) { return groups * threads < 1ll << 32; }
+
 // Partial outputs of sequences whose keys are cut into parts.
 struct CachePartials {
   float* o;                 // [slots, rows, d]
@@ -120,6 +124,7 @@ void cache_extend_partials(const CacheProblem& p, int64_t* slots, int* rows);
 // Floats of the partial weights of a call.
 int64_t cache_weights_partials(const CacheProblem& p);
 
+// hipErrorInvalidValue, and nothing launched, where the call is too large for it.
 hipError_t launch_cache_append(const CacheProblem& p, const uint16_t* k_new, const uint16_t* v_new,
                                hipStream_t s);
 hipError_t launch_cache_decode(const CacheProblem& p, const CachePartials& part, uint16_t* out,

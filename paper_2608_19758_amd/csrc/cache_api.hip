@@ -185,7 +185,7 @@ fp2_status_t check_workspace(const void* ws, size_t bytes, size_t need) {
 
 fp2_status_t hip_status(hipError_t e, const char* what) {
   if (e == hipSuccess) return ok();
-  if (e == hipErrorInvalidValue) return fail(FP2_EUNSUPPORTED, "%s: more workgroups than a launch takes", what);
+  if (e == hipErrorInvalidValue) return fail(FP2_EUNSUPPORTED, "%s: more threads than a launch takes (2^32 - 1)", what);
   return fail(FP2_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
 

@@ -248,15 +248,15 @@ __global__ __launch_bounds__(64 * kWaves) void append_few_kernel(CacheProblem p,
 template <int FORM>
 hipError_t launch(const CacheProblem& p, const uint16_t* k_new, const uint16_t* v_new, hipStream_t s) {
   if (p.max_new <= kFew) {
-    const int64_t total = (int64_t)p.batch * 2 * p.hkv;
-    append_few_kernel<FORM><<<(unsigned)((total + kWaves - 1) / kWaves), 64 * kWaves, 0, s>>>(p, k_new, v_new,
-                                                                                              total);
+    const int64_t total = (int64_t)p.batch * 2 * p.hkv, grid = (total + kWaves - 1) / kWaves;
+    if (!launchable(grid, 64 * kWaves)) return hipErrorInvalidValue;
+    append_few_kernel<FORM><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, k_new, v_new, total);
     return hipGetLastError();
   }
   // tokens of a sequence lie in at most this many runs of kRows
   const int chunks = (p.max_new + kRows - 2) / kRows + 1;
   const int64_t grid = (int64_t)p.batch * chunks * 2 * p.hkv;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  if (!launchable(grid, 64 * kWaves)) return hipErrorInvalidValue;
   append_kernel<FORM><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, k_new, v_new, chunks);
   return hipGetLastError();
 }

@@ -578,13 +578,13 @@ hipError_t launch(const CacheProblem& problem, const CachePartials& part, uint16
   const int shares = shares_of(p), max_rows = p.max_new * p.g;
   const int64_t grid = (int64_t)shares * (p.hkv / p.heads);
   const int64_t joins = (int64_t)p.batch * p.hkv * max_rows;
-  if (grid > 0x7fffffff || joins > 0x7fffffff) return hipErrorInvalidValue;
-  decode_kernel<FORM, NT, RH, W, GROUPED><<<(unsigned)grid, 64 * W, 0, s>>>(p, part, shares, out, lse);
-  if (p.splits == 1) return hipGetLastError();
   // few joins have many parts each, and a compute unit to themselves: 32 joins
   // of a sequence of 128K take 63 us with the attention, 69 with 256 threads;
   // 4096 of 8 sequences 100, and 122 with 1024
   const int threads = joins <= kFewGroups ? 1024 : 256;
+  if (!launchable(grid, 64 * W) || (p.splits != 1 && !launchable(joins, threads))) return hipErrorInvalidValue;
+  decode_kernel<FORM, NT, RH, W, GROUPED><<<(unsigned)grid, 64 * W, 0, s>>>(p, part, shares, out, lse);
+  if (p.splits == 1) return hipGetLastError();
   combine_kernel<<<(unsigned)joins, threads, 0, s>>>(p, part, 16 * NT * RH, max_rows, out, lse);
   return hipGetLastError();
 }

@@ -341,12 +341,18 @@ __global__ __launch_bounds__(64 * kWaves) void move_kernel(CacheProblem p, PageM
 }
 
 template <int FORM, int SB>
-hipError_t launch_move(const CacheProblem& p, const PageMap& to, int budget, const int32_t* kept,
-                       hipStream_t s) {
+hipError_t launch(const CacheProblem& p, const PageMap& to, int budget, int recent, const float* weights,
+                  int64_t stride, float* weights_out, int64_t out_stride, int32_t* kept, int32_t* cu_out,
+                  hipStream_t s) {
   constexpr int RUN = SB > 32 ? SB : 32;
   const int runs = (std::min(budget, p.max_kv) + RUN - 1) / RUN;
-  const int64_t total = (int64_t)p.batch * p.hkv * 2 * runs, grid = (total + kWaves - 1) / kWaves;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  const int64_t heads = (int64_t)p.batch * p.hkv;
+  const int64_t total = heads * 2 * runs, grid = (total + kWaves - 1) / kWaves;
+  if (!launchable(heads, kThreads) || !launchable(grid, 64 * kWaves)) return hipErrorInvalidValue;
+  select_kernel<<<(unsigned)heads, kThreads, 0, s>>>(p, budget, recent, weights, stride, weights_out,
+                                                     out_stride, kept, cu_out);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   move_kernel<FORM, SB><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, to, budget, runs, total, kept);
   return hipGetLastError();
 }
@@ -356,17 +362,15 @@ hipError_t launch_move(const CacheProblem& p, const PageMap& to, int budget, con
 hipError_t launch_cache_evict(const CacheProblem& p, const PageMap& to, int budget, int recent,
                               const float* weights, int64_t stride, float* weights_out,
                               int64_t out_stride, int32_t* kept, int32_t* cu_out, hipStream_t s) {
-  const int64_t heads = (int64_t)p.batch * p.hkv;
-  select_kernel<<<(unsigned)heads, kThreads, 0, s>>>(p, budget, recent, weights, stride, weights_out,
-                                                     out_stride, kept, cu_out);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  if (p.form == kCacheBf16) return launch_move<kCacheBf16, 0>(p, to, budget, kept, s);
-  if (p.form == kCacheHead) return launch_move<kCacheHead, 0>(p, to, budget, kept, s);
-  return p.sb_shift == 4   ? launch_move<kCacheBlock, 16>(p, to, budget, kept, s)
-         : p.sb_shift == 5 ? launch_move<kCacheBlock, 32>(p, to, budget, kept, s)
-         : p.sb_shift == 6 ? launch_move<kCacheBlock, 64>(p, to, budget, kept, s)
-                           : launch_move<kCacheBlock, 128>(p, to, budget, kept, s);
+  auto run = [&](auto f) {
+    return f(p, to, budget, recent, weights, stride, weights_out, out_stride, kept, cu_out, s);
+  };
+  if (p.form == kCacheBf16) return run(launch<kCacheBf16, 0>);
+  if (p.form == kCacheHead) return run(launch<kCacheHead, 0>);
+  return p.sb_shift == 4   ? run(launch<kCacheBlock, 16>)
+         : p.sb_shift == 5 ? run(launch<kCacheBlock, 32>)
+         : p.sb_shift == 6 ? run(launch<kCacheBlock, 64>)
+                           : run(launch<kCacheBlock, 128>);
 }
 
 }  // namespace fp2

@@ -497,13 +497,15 @@ hipError_t launch(const CacheProblem& p, const CachePartials& part, uint16_t* ou
                   hipStream_t s) {
   const int nq = query_tiles(p), parts = parts_for(p);
   const int64_t units = (int64_t)p.batch * p.hkv * nq;
-  if (units * parts > 0x7fffffff || units * (kRows / 8) > 0x7fffffff) return hipErrorInvalidValue;
+  const int64_t joins = units * (kRows / 8);
+  if (!launchable(units * parts, 64 * kWaves) || (parts > 1 && !launchable(joins, 256)))
+    return hipErrorInvalidValue;
   const dim3 grid((unsigned)(units * parts)), threads(64 * kWaves);
   if (p.pm.page % kStep == 0)
     extend_kernel<FORM, true><<<grid, threads, 0, s>>>(p, part, nq, parts, out, lse);
   else
     extend_kernel<FORM, false><<<grid, threads, 0, s>>>(p, part, nq, parts, out, lse);
-  if (parts > 1) join_kernel<<<(unsigned)(units * (kRows / 8)), 256, 0, s>>>(p, part, nq, parts, out, lse);
+  if (parts > 1) join_kernel<<<(unsigned)joins, 256, 0, s>>>(p, part, nq, parts, out, lse);
   return hipGetLastError();
 }
 

@@ -443,7 +443,7 @@ hipError_t launch_few(const CacheProblem& problem, const float* lse, const float
   const int nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   const int64_t copies = in != out ? (int64_t)p.batch * p.hkv * ((stride + kCopy - 1) / kCopy) : 0;
   const int64_t grid = (int64_t)shares * (p.hkv / p.heads) + copies;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  if (!launchable(grid, 64 * kFewWaves)) return hipErrorInvalidValue;
   const dim3 g((unsigned)grid), t(64 * kFewWaves);
   if (FORM == kCacheBlock || p.pm.page % 16 == 0) {
     if (nt == 1) few_kernel<FORM, 1, true><<<g, t, 0, s>>>(p, lse, in, out, stride, shares);
@@ -466,12 +466,14 @@ hipError_t launch(const CacheProblem& p, const float* lse, const float* in, floa
   // not in place, the entries past the sequences are written too
   const int64_t all = in != out ? (stride + kChunk - 1) / kChunk : chunks;
   const int64_t groups = (int64_t)p.batch * p.hkv * (segs > 1 ? chunks : all);
-  if (all > 0x7fffffff / kChunk || groups * segs > 0x7fffffff || (int64_t)p.batch * p.hkv * all > 0x7fffffff)
+  const int64_t sums = (int64_t)p.batch * p.hkv * all;
+  if (all > 0x7fffffff / kChunk || !launchable(groups * segs, 64 * kWaves) ||
+      (segs > 1 && !launchable(sums, kChunk)))
     return hipErrorInvalidValue;
   many_kernel<FORM><<<(unsigned)(groups * segs), 64 * kWaves, 0, s>>>(p, lse, in, out, stride, part, segs,
                                                                       steps, chunks);
   if (segs > 1)
-    sum_kernel<<<(unsigned)(p.batch * p.hkv * all), kChunk, 0, s>>>(p, in, out, stride, part, segs, steps,
+    sum_kernel<<<(unsigned)sums, kChunk, 0, s>>>(p, in, out, stride, part, segs, steps,
                                                                     chunks);
   return hipGetLastError();
 }
