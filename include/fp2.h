@@ -505,8 +505,9 @@ fp2_status_t fp2_cache_append(const fp2_cache_params_t* params, const void* k_ne
 
 /* out = softmax(scale * q k^T) v over the keys that each query sees; q and
  * out bf16 [cu_seqlens[batch], num_q_heads, 128], lse (nullable) fp32 [...,
- * num_q_heads], the natural log of the sum. out must not overlap q. Probabilities are rounded to bf16
- * for the value product. Rows past cu_seqlens[batch] are not touched. Where
+ * num_q_heads], the natural log of the sum. q, out and lse must not overlap
+ * (refused where cu_seqlens_host tells their rows). Probabilities are rounded
+ * to bf16 for the value product. Rows past cu_seqlens[batch] are not touched. Where
  * max_seq_len * g <= 64 the keys are read once for all rows of a sequence;
  * results depend on kv_splits, and with 0 on the other sequences of a call,
  * through rounding only. */

@@ -254,6 +254,12 @@ def cache_attend(p: CacheParams, q, cache: KVCache, cu_seqlens, cu_seqlens_k, bl
         if workspace is None:
             workspace = alloc_cache_workspace(p, q.device)
     op, lp = a("out", out, _ONE_BF16, size), a("lse", lse, _ONE_F32, rows * heads)
+    if op < qp + 2 * size and qp < op + 2 * size:
+        raise ValueError("out must not overlap q")
+    if lp is not None:
+        end = lp + 4 * rows * heads
+        if (lp < qp + 2 * size and qp < end) or (lp < op + 2 * size and op < end):
+            raise ValueError("lse must not overlap q or out")
     ws = a("workspace", workspace, _BYTES)
     a.call("fp2_cache_attend", stream, ctypes.byref(p), qp, *lens, ctypes.byref(c), table, op, lp, ws,
            workspace.numel())

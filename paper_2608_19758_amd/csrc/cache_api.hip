@@ -235,6 +235,14 @@ fp2_status_t fp2_cache_attend(const fp2_cache_params_t* params, const void* q,
   if (!q || !out) return fail(FP2_EINVAL, "q or out is null");
   if (!aligned(q, 16) || !aligned(out, 16)) return fail(FP2_EINVAL, "q and out must be 16-byte aligned");
   if (q == out) return fail(FP2_EINVAL, "out must not be q");
+  if (cu_seqlens_host) {   // then the rows that are read and written are known
+    const int64_t heads = (int64_t)cu_seqlens_host[params->batch] * params->num_q_heads;
+    const int64_t row = 2 * fp2::kHeadDim * heads, sums = sizeof(float) * heads;
+    const char *qb = (const char*)q, *ob = (const char*)out, *lb = (const char*)lse;
+    if (overlap(qb, row, ob, row)) return fail(FP2_EINVAL, "out must not overlap q");
+    if (lse && (overlap(qb, row, lb, sums) || overlap(ob, row, lb, sums)))
+      return fail(FP2_EINVAL, "lse must not overlap q or out");
+  }
   const CacheProblem r = make_problem(params, q, cu_seqlens, cu_seqlens_k, cache, block_table);
   size_t ml, at;
   if ((st = check_workspace(workspace, workspace_bytes, attend_bytes(r, &ml, &at)))) return st;

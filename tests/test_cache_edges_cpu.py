@@ -1,9 +1,10 @@
 """Calls of the paged cache's operators at the edges of what the host can see,
 refused before any launch (no GPU)."""
 import pytest
+import torch
 
 import paper_2608_19758_amd as fp2
-from tests.test_cache_cpu import FAKE, base, call
+from tests.test_cache_cpu import FAKE, base, call, tensors
 
 ROOM = dict(ws=FAKE, wsb=1 << 60)
 
@@ -26,3 +27,40 @@ def test_more_threads_than_a_launch_takes(op, kw, over):
     whole, before the first."""
     assert call(op, base(**kw), **over) == fp2.EUNSUPPORTED
     assert "threads" in fp2.last_error()
+
+
+@pytest.mark.parametrize("kw", [{}, dict(max_seq_len=100)])
+def test_outputs_over_the_queries(kw):
+    """Host lengths tell how many rows are read and written: none of them may be shared."""
+    p, h = base(**kw), [0, 4, 7]
+    q = 16 * FAKE
+    row, size = 32 * 128 * 2, 7 * 32 * 128 * 2
+    for out in (q + row, q - row, q + size - 16, q - size + 16):
+        assert call("attend", p, q=q, out=out, cuh=h, **ROOM) == fp2.EINVAL and "overlap q" in fp2.last_error()
+    for lse in (q, q + size - 4, q - 7 * 32 * 4 + 4, 2 * q, 2 * q + size - 4):
+        assert call("attend", p, q=q, out=2 * q, lse=lse, cuh=h, **ROOM) == fp2.EINVAL
+        assert "lse must not overlap" in fp2.last_error()
+    # side by side: refused only later, for want of a workspace
+    for out in (q + size, q - size):
+        assert call("attend", p, q=q, out=out, lse=4 * q, cuh=h) == fp2.EWORKSPACE
+
+
+def test_binding_refuses_outputs_over_the_queries():
+    """The binding knows the sizes without host lengths."""
+    p = base()
+    t = tensors(p)
+    both = torch.zeros(13, 32, 128, dtype=torch.bfloat16)
+    ws = torch.zeros(1, dtype=torch.uint8)
+
+    def attend(q, out, lse=None):
+        with pytest.raises(ValueError) as e:
+            fp2.cache_attend(p, q, t["cache"], t["cu"], t["cu"], t["table"], out=out, lse=lse, workspace=ws)
+        return str(e.value)
+
+    for q, out in ((both[:6], both[:6]), (both[:6], both[5:11]), (both[5:11], both[:6])):
+        assert "out must not overlap q" in attend(q, out)
+    assert "CUDA" in attend(both[:6], both[6:12])                        # side by side
+    flat = both.view(torch.float32).view(-1)                            # 2048 to a row
+    for at in (100, 2048 * 6 - 1, 2048 * 6, 2048 * 12 - 1):
+        assert "lse must not overlap" in attend(both[:6], both[6:12], flat[at:at + 192].view(6, 32))
+    assert "CUDA" in attend(both[:6], both[6:12], flat[2048 * 12:2048 * 12 + 192].view(6, 32))
