@@ -99,7 +99,8 @@ _NUMPY_I32 = np.dtype(np.int32)
 
 class _Args:
     """Checks tensors one by one and gives their addresses: CUDA tensors on one device, dense, of the
-    right type and of at least `least` elements. The C ABI sees only pointers. (Half of a small call's
+    right type and of at least `least` elements. The C ABI sees only pointers, and refuses a null one where
+    a call needs it, so `optional` says which this class lets through. (Half of a small call's
     time is spent here, so each property of a tensor is asked for once.)"""
     __slots__ = ("dev", "odd")
 
@@ -107,8 +108,8 @@ class _Args:
         self.dev = None     # index of the first tensor's device
         self.odd = None     # first tensor that is not on a CUDA device, or on another one; refused at the end
 
-    def __call__(self, name, t, dtypes, least=0, multiple=1):
-        if t is None:
+    def __call__(self, name, t, dtypes, least=0, multiple=1, optional=False):
+        if t is None and optional:
             return None
         if not isinstance(t, torch.Tensor):
             raise ValueError("%s must be a torch tensor" % name)
@@ -135,8 +136,8 @@ class _Args:
             raise ValueError("%s must be int32 [>= batch, %d], got %s" % (name, width, tuple(shape)))
         return self(name, t, _ONE_I32)
 
-    def weights(self, p, name, w):
-        if w is None:
+    def weights(self, p, name, w, optional=False):
+        if w is None and optional:
             return None
         shape = w.shape if isinstance(w, torch.Tensor) else ()
         if len(shape) != 3 or shape[0] < p.batch or shape[1] != p.num_kv_heads or shape[2] < p.max_kv_len:
@@ -146,11 +147,13 @@ class _Args:
 
     def cache(self, p, c, need_v=True):
         """fp2_kv_cache_t of the cache."""
+        if c is None:
+            raise ValueError("cache must be a KVCache")
         heads, scale_tokens, dtype = p.num_kv_heads, p.scale_tokens, p.dtype
         row = max(1, heads * p.head_dim * max(1, p.page_size))
         rows = _ONE_BF16 if dtype == BF16 else _CODES if dtype == FP8_E4M3 else ()
         k = self("cache.k", c.k, rows, 0, row)
-        v = self("cache.v", c.v, rows) if need_v or c.v is not None else None
+        v = self("cache.v", c.v, rows, optional=True)
         size = c.k.numel()
         if v is not None and c.v.numel() != size:
             raise ValueError("cache.k and cache.v differ in size")
@@ -161,9 +164,10 @@ class _Args:
         if scale_tokens > 0:
             least = size // (scale_tokens * p.head_dim)
             ks, vs = (self("cache.k_scale", c.k_scale, _ONE_U8, least),
-                      self("cache.v_scale", c.v_scale, _ONE_U8, least))
+                      self("cache.v_scale", c.v_scale, _ONE_U8, least, optional=not need_v))
             return _CachePointers(k, v, None, None, ks, vs)
-        ks, vs = self("cache.k_scale", c.k_scale, _ONE_F32, heads), self("cache.v_scale", c.v_scale, _ONE_F32, heads)
+        ks, vs = (self("cache.k_scale", c.k_scale, _ONE_F32, heads),
+                  self("cache.v_scale", c.v_scale, _ONE_F32, heads, optional=not need_v))
         return _CachePointers(k, v, ks, vs, None, None)
 
     @staticmethod
@@ -175,8 +179,8 @@ class _Args:
             ok = t.dtype == torch.int32 and not t.is_cuda and t.is_contiguous()
             size, at = t.numel(), t.data_ptr()
         else:
-            ok = t.dtype == _NUMPY_I32 and t.flags.c_contiguous
-            size, at = t.size, None
+            ok = isinstance(t, np.ndarray) and t.dtype == _NUMPY_I32 and t.flags.c_contiguous
+            size, at = t.size if ok else 0, None
         if not ok:
             raise ValueError("%s must be a dense host int32 array" % name)
         if size < batch + 1:
@@ -188,8 +192,8 @@ class _Args:
         return at
 
     def lengths(self, batch, cu, cuk, host, host_k, rows=None):
-        return (self("cu_seqlens", cu, _ONE_I32, batch + 1), self.host("cu_seqlens_host", host, batch, rows),
-                self("cu_seqlens_k", cuk, _ONE_I32, batch + 1), self.host("cu_seqlens_k_host", host_k, batch))
+        return (self("cu_seqlens", cu, _ONE_I32, batch + 1, optional=True), self.host("cu_seqlens_host", host, batch, rows),
+                self("cu_seqlens_k", cuk, _ONE_I32, batch + 1, optional=True), self.host("cu_seqlens_k_host", host_k, batch))
 
     def call(self, name, stream, *args):
         """The entry point on `stream` (the current one of the tensors' device if None), with that
@@ -253,7 +257,7 @@ def cache_attend(p: CacheParams, q, cache: KVCache, cu_seqlens, cu_seqlens_k, bl
             lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device)
         if workspace is None:
             workspace = alloc_cache_workspace(p, q.device)
-    op, lp = a("out", out, _ONE_BF16, size), a("lse", lse, _ONE_F32, rows * heads)
+    op, lp = a("out", out, _ONE_BF16, size), a("lse", lse, _ONE_F32, rows * heads, optional=True)
     if op < qp + 2 * size and qp < op + 2 * size:
         raise ValueError("out must not overlap q")
     if lp is not None:
@@ -276,11 +280,11 @@ def cache_weights(p: CacheParams, q, lse, cache: KVCache, cu_seqlens, cu_seqlens
     row = p.num_q_heads * p.head_dim
     qp = a("q", q, _ONE_BF16, 0, row)
     size = q.numel()
-    lp = a("lse", lse, _ONE_F32, size // p.head_dim)
+    lp = a("lse", lse, _ONE_F32, size // p.head_dim, optional=True)
     c = a.cache(p, cache, need_v=False)
     lens = a.lengths(batch, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host, size // row)
     table = a.table(batch, "block_table", block_table, p.max_pages_per_seq)
-    wi = a.weights(p, "weights_in", weights_in)
+    wi = a.weights(p, "weights_in", weights_in, optional=True)
     with on_stream(stream):
         if weights is None:
             shape = (p.batch, p.num_kv_heads, p.max_kv_len if weights_in is None else weights_in.shape[2])

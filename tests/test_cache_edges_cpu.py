@@ -1,10 +1,11 @@
 """Calls of the paged cache's operators at the edges of what the host can see,
 refused before any launch (no GPU)."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2608_19758_amd as fp2
-from tests.test_cache_cpu import FAKE, base, call, tensors
+from tests.test_cache_cpu import FAKE, OPS, base, binding, call, tensors
 
 ROOM = dict(ws=FAKE, wsb=1 << 60)
 
@@ -64,3 +65,40 @@ def test_binding_refuses_outputs_over_the_queries():
     for at in (100, 2048 * 6 - 1, 2048 * 6, 2048 * 12 - 1):
         assert "lse must not overlap" in attend(both[:6], both[6:12], flat[at:at + 192].view(6, 32))
     assert "CUDA" in attend(both[:6], both[6:12], flat[2048 * 12:2048 * 12 + 192].view(6, 32))
+
+
+@pytest.mark.parametrize("op", OPS)
+@pytest.mark.parametrize("x", [None, [1.0, 2.0], np.zeros((6, 8, 128), np.float32)])
+def test_binding_refuses_what_is_no_tensor(op, x):
+    """With the binding's own error, as for every other argument."""
+    p = base()
+    for name in {"append": ["new", "table"], "attend": ["q", "table"], "weights": ["q", "w", "table"],
+                 "evict": ["w", "table"]}[op]:
+        if name == "w" and op == "weights" and x is None:
+            continue                                                  # the result is allocated then
+        t = tensors(p)
+        t[name] = x
+        if name == "q" and op == "attend":
+            with pytest.raises(ValueError, match="q must be"):
+                fp2.cache_attend(p, x, t["cache"], t["cu"], t["cu"], t["table"])
+            continue
+        with pytest.raises(ValueError, match="must be"):
+            binding(op, p, t)
+    t = tensors(p)
+    t["cache"].k = x
+    with pytest.raises(ValueError, match="cache.k must be"):
+        binding(op, p, t)
+    t["cache"] = None
+    with pytest.raises(ValueError, match="cache must be"):
+        binding(op, p, t)
+
+
+def test_host_lengths_that_are_no_arrays():
+    p, t = base(), tensors(base())
+    for h in ([0, 1, 2], (0, 1, 2), 3, "012"):
+        for kw in (dict(cu_seqlens_host=h), dict(cu_seqlens_k_host=h)):
+            with pytest.raises(ValueError, match="dense host int32"):
+                fp2.cache_append(p, t["new"], t["new"], t["cache"], t["cu"], t["cu"], t["table"], **kw)
+            if "cu_seqlens_k_host" in kw:
+                with pytest.raises(ValueError, match="dense host int32"):
+                    fp2.cache_evict(p, t["cache"], t["w"], t["cu"], t["table"], t["table"], budget=100, **kw)
