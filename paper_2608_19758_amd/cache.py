@@ -300,9 +300,9 @@ def cache_weights(p: CacheParams, q, lse, cache: KVCache, cu_seqlens, cu_seqlens
     if (p.batch == 0 or p.max_kv_len == 0) and weights is not weights_in:     # a call without tokens
         with on_stream(stream):
             if weights_in is None:
-                weights.zero_()
+                weights[:batch].zero_()
             else:
-                weights[:p.batch].copy_(weights_in[:p.batch])
+                weights[:batch].copy_(weights_in[:batch])
     return weights
 
 
@@ -336,5 +336,7 @@ def cache_evict(p: CacheParams, cache: KVCache, weights, cu_seqlens_k, block_tab
            int(budget), int(recent_tokens), w, wo, stride, kp, co)
     if p.batch == 0 or p.max_kv_len == 0:                                      # a call without tokens
         with on_stream(stream):
-            kept.fill_(-1), cu_seqlens_k_out.zero_(), weights_out.zero_()
+            kept.view(-1)[:batch * heads * budget].fill_(-1)
+            cu_seqlens_k_out.view(-1)[:batch + 1].zero_()
+            weights_out[:batch].zero_()
     return kept, cu_seqlens_k_out, weights_out

@@ -141,3 +141,26 @@ def test_scales_that_no_query_sees(byte, new, place):
             getattr(c, name + "s")[at[0] // 16] = byte
             getattr(c, name)[at] = torch.tensor([0, 0x38, 0x7e, 0x7f] * 4, dtype=torch.uint8)[:, None, None]
     run_attend(c, 8, [new], window, sink)
+
+
+@pytest.mark.parametrize("batch,max_kv", [(0, 100), (2, 0)])
+def test_calls_without_tokens_leave_the_rows_behind_the_batch(batch, max_kv):
+    """Results that are larger than the call: what lies behind its sequences stays."""
+    p = fp2.make_cache_params(batch=batch, num_q_heads=4, num_kv_heads=2, max_seq_len=0, max_kv_len=max_kv,
+                              page_size=16, max_pages_per_seq=7)
+    cache = fp2.alloc_cache(p, 2)
+    cu, table = torch.zeros(5, dtype=torch.int32, device="cuda"), torch.zeros((4, 7), dtype=torch.int32, device="cuda")
+    q, lse = torch.zeros((0, 4, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((0, 4), device="cuda")
+    before = torch.full((4, 2, 100), 3.0, device="cuda")
+    for given, value in ((None, 0), (before, 3)):
+        w = torch.full((4, 2, 100), 7.0, device="cuda")
+        assert fp2.cache_weights(p, q, lse, cache, cu, cu, table, weights=w, weights_in=given) is w
+        assert bool((w[:batch] == value).all()) and bool((w[batch:] == 7).all())
+    left = torch.full((4, 2, 100), 7.0, device="cuda")
+    kept = torch.full((4, 2, 20), 7, dtype=torch.int32, device="cuda")
+    cu_out = torch.full((5,), 7, dtype=torch.int32, device="cuda")
+    fp2.cache_evict(p, cache, before, cu, table, table.clone(), budget=20, kept=kept, weights_out=left,
+                    cu_seqlens_k_out=cu_out)
+    assert not bool(left[:batch].any()) and bool((left[batch:] == 7).all())
+    assert bool((kept[:batch] == -1).all()) and bool((kept[batch:] == 7).all())
+    assert cu_out.tolist() == [0] * (batch + 1) + [7] * (4 - batch)
