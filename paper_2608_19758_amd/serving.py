@@ -273,6 +273,7 @@ class CacheMetadata:
     lengths: object                # device int32: cu_q and cu_k side by side
     block_table: object            # device int32 [batch or more, max_pages_per_seq], dense
     replayed: bool = False         # lengths and table are the metadata's own, and may be updated
+    rows: Optional[int] = None     # of the tensors of the forwards captured with it, the fewest
 
     @property
     def params(self):
@@ -340,7 +341,8 @@ class CacheBackend:
     def update_forward_metadata(self, meta: CacheMetadata, extend_lens: Sequence[int],
                                 prefix_lens: Optional[Sequence[int]], block_table) -> None:
         """Other lengths and pages for a captured forward (metadata made with
-        replayed=True): as many sequences, extends within the first one's bound."""
+        replayed=True): as many sequences, extends within the first one's bound, and no more new
+        tokens in all than the captured tensors have rows."""
         import torch
         plan = plan_forward(self.cfg, extend_lens, prefix_lens)
         p = meta.params
@@ -349,6 +351,9 @@ class CacheBackend:
         if plan.params.batch != p.batch or plan.params.max_seq_len > p.max_seq_len:
             raise ValueError("%d sequences with extends up to %d do not fit a forward of %d with up to %d"
                              % (plan.params.batch, plan.params.max_seq_len, p.batch, p.max_seq_len))
+        if meta.rows is not None and plan.total_tokens > meta.rows:
+            raise ValueError("%d new tokens, the captured forward's tensors have %d rows"
+                             % (plan.total_tokens, meta.rows))
         plan.params = p
         with fp2.cache.on_stream(self.stream):
             meta.lengths.copy_(torch.from_numpy(np.concatenate([plan.cu_q, plan.cu_k])))
@@ -366,6 +371,13 @@ class CacheBackend:
             if t.shape[0] < meta.plan.total_tokens:
                 raise ValueError("%s has %d rows, the forward has %d new tokens"
                                  % (name, t.shape[0], meta.plan.total_tokens))
+        if meta.replayed:
+            import torch
+            with fp2.cache.on_stream(self.stream):
+                captured = torch.cuda.is_current_stream_capturing()
+            if captured:     # later lengths are held to these tensors
+                rows = [t.shape[0] for t in (q, k_new, v_new)] + [meta.rows] * (meta.rows is not None)
+                meta.rows = min(rows)
         p, lens = meta.params, (meta.cu_q, meta.cu_k, meta.block_table)
         host = dict(cu_seqlens_host=meta.plan.cu_q, cu_seqlens_k_host=meta.plan.cu_k, stream=self.stream)
         fp2.cache_append(p, k_new, v_new, cache, *lens, **host)

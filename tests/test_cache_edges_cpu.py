@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2608_19758_amd as fp2
+from paper_2608_19758_amd import serving
 from tests.test_cache_cpu import FAKE, OPS, base, binding, call, tensors
 
 ROOM = dict(ws=FAKE, wsb=1 << 60)
@@ -102,3 +103,19 @@ def test_host_lengths_that_are_no_arrays():
             if "cu_seqlens_k_host" in kw:
                 with pytest.raises(ValueError, match="dense host int32"):
                     fp2.cache_evict(p, t["cache"], t["w"], t["cu"], t["table"], t["table"], budget=100, **kw)
+
+
+def test_updates_over_the_captured_rows():
+    """A forward captured with four rows goes on reading those: more new tokens are refused, though each
+    sequence stays within its bound."""
+    cfg = serving.CacheConfig(num_q_heads=8, num_kv_heads=2, page_size=16, max_batch=2, max_extend_len=40,
+                              max_kv_len=256)
+    be = serving.CacheBackend(cfg, device="cpu")
+    lengths, table = torch.zeros(6, dtype=torch.int32), torch.zeros((2, 16), dtype=torch.int32)
+    meta = serving.CacheMetadata(serving.plan_forward(cfg, [1, 3], [30, 10]), lengths, table, replayed=True)
+    meta.rows = 4
+    for new in ([3, 2], [3, 3]):
+        with pytest.raises(ValueError, match="5 new tokens.*4 rows|6 new tokens.*4 rows"):
+            be.update_forward_metadata(meta, new, [30, 10], None)
+    with pytest.raises(ValueError, match="block_table"):                  # fits
+        be.update_forward_metadata(meta, [3, 1], [30, 10], None)

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2608_19758_amd as fp2
+from paper_2608_19758_amd import serving
 from tests import cache_ref as ref
 from tests.test_gpu_cache import close, cu_of, dev, on_gpu, params, run_attend, run_evict
 
@@ -164,3 +165,40 @@ def test_calls_without_tokens_leave_the_rows_behind_the_batch(batch, max_kv):
     assert not bool(left[:batch].any()) and bool((left[batch:] == 7).all())
     assert bool((kept[:batch] == -1).all()) and bool((kept[batch:] == 7).all())
     assert cu_out.tolist() == [0] * (batch + 1) + [7] * (4 - batch)
+
+
+def test_updates_are_held_to_the_captured_rows():
+    """A captured forward goes on reading its tensors: lengths of more tokens than they have rows are
+    refused, others give the eager results."""
+    cfg = serving.CacheConfig(num_q_heads=8, num_kv_heads=2, page_size=16, max_batch=2, max_extend_len=40,
+                              max_kv_len=256)
+    be, eager = serving.CacheBackend(cfg), serving.CacheBackend(cfg)
+    table = torch.arange(32, dtype=torch.int32, device="cuda").view(2, 16)
+    g = torch.Generator().manual_seed(11)
+    caches = [be.alloc_cache(32) for _ in "ab"]
+    x = [torch.randn((40, h, 128), generator=g).bfloat16().cuda() for h in (8, 2, 2)]
+    for cache in caches:
+        eager.forward(*x, cache, eager.init_forward_metadata([30, 10], None, table))
+    new, lens = [1, 3], [30, 10]
+    meta = be.init_forward_metadata(new, lens, table, replayed=True)
+    static = [t[:4].clone() for t in x]
+    be.forward(*[t[:40] for t in x], be.alloc_cache(32), meta)          # not captured: holds nothing
+    out = torch.zeros_like(static[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        be.forward(*static, caches[0], meta, out=out)
+    for step, new in enumerate(([1, 3], [3, 1], [0, 2], [2, 2])):
+        be.update_forward_metadata(meta, new, lens, table)
+        for s, t in zip(static, x):
+            s.copy_(t[4 * step:4 * step + 4])
+        graph.replay()
+        float(torch.randn(1 << 18, device="cuda").sum())
+        m = eager.init_forward_metadata(new, lens, table, replayed=True)
+        want, _ = eager.forward(*[t[4 * step:4 * step + 4].contiguous() for t in x], caches[1], m)
+        torch.cuda.synchronize()
+        assert torch.equal(out[:sum(new)], want[:sum(new)]) and torch.equal(caches[0].k, caches[1].k), step
+        lens = [a + b for a, b in zip(lens, new)]
+    for new in ([3, 2], [3, 3]):
+        with pytest.raises(ValueError, match="rows"):
+            be.update_forward_metadata(meta, new, lens, table)
