@@ -356,9 +356,9 @@ class CacheBackend:
                              % (plan.total_tokens, meta.rows))
         plan.params = p
         with fp2.cache.on_stream(self.stream):
+            table = _dense_table(block_table, p.batch, self.cfg.max_pages_per_seq)   # refused before any change
             meta.lengths.copy_(torch.from_numpy(np.concatenate([plan.cu_q, plan.cu_k])))
-            meta.block_table[:p.batch].copy_(
-                _dense_table(block_table, p.batch, self.cfg.max_pages_per_seq)[:p.batch])
+            meta.block_table[:p.batch].copy_(table[:p.batch])
         meta.plan = plan
 
     def forward(self, q, k_new, v_new, cache: "fp2.KVCache", meta: CacheMetadata, *, out=None, lse=None,

@@ -119,3 +119,16 @@ def test_updates_over_the_captured_rows():
             be.update_forward_metadata(meta, new, [30, 10], None)
     with pytest.raises(ValueError, match="block_table"):                  # fits
         be.update_forward_metadata(meta, [3, 1], [30, 10], None)
+
+
+def test_a_refused_update_changes_nothing():
+    cfg = serving.CacheConfig(num_q_heads=8, num_kv_heads=2, page_size=16, max_batch=2, max_extend_len=40,
+                              max_kv_len=256)
+    be = serving.CacheBackend(cfg, device="cpu")
+    lengths, table = torch.full((6,), 7, dtype=torch.int32), torch.full((2, 16), 7, dtype=torch.int32)
+    plan = serving.plan_forward(cfg, [1, 3], [30, 10])
+    meta = serving.CacheMetadata(plan, lengths, table, replayed=True)
+    for bad in (None, table, table[:1]):                                  # (on the host)
+        with pytest.raises(ValueError, match="block_table"):
+            be.update_forward_metadata(meta, [3, 1], [30, 10], bad)
+    assert bool((lengths == 7).all()) and bool((table == 7).all()) and meta.plan is plan
