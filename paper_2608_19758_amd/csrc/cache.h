@@ -44,6 +44,14 @@ __device__ __forceinline__ float block_scale(uint32_t byte) { return __uint_as_f
 // and the smallest code times the smallest a normal one.
 constexpr int kMinScaleByte = 127 - 100, kMaxScaleByte = 127 + 118;
 
+// The scale of a head's scores (base 2). Never 0, which a masked score, minus
+// infinity, would make NaN; at 2^-126 the scores of queries up to 2^80 are below 2^-30.
+template <int FORM>
+__device__ __forceinline__ float score_scale(const CacheProblem& p, int h) {
+  if constexpr (FORM != kCacheHead) return p.scale_log2;
+  else return fmaxf(p.scale_log2 * ld_uniform(p.k_head, h), 0x1p-126f);
+}
+
 // Byte of the scale for values of at most amax (finite, >= 0): the smallest
 // power of two that is at least amax / 448. 448 = 0.875 * 2^9, so it is read
 // off the bits of amax = 1.m * 2^x: 2^(x - 8) where 1.m <= 1.75, else twice

@@ -112,11 +112,9 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
   const int ks = w / units;                    // place among the head's tiles
   const int rb = RH == 1 ? 0 : w / p.heads % RH * 16 * NT;   // the wave's first packed row
   const int c16 = lane & 15, kg = lane >> 4;
-  float cs = p.scale_log2, vsc = 1.f;
-  if constexpr (FORM == kCacheHead) {
-    cs *= ld_uniform(p.k_head, h);
-    vsc = ld_uniform(p.v_head, h);
-  }
+  const float cs = score_scale<FORM>(p, h);
+  float vsc = 1.f;
+  if constexpr (FORM == kCacheHead) vsc = ld_uniform(p.v_head, h);
   const int64_t rowb = (int64_t)p.hkv * kHeadDim * ESZ;
   const int64_t hoff = (int64_t)h * kHeadDim * ESZ;
   const uint8_t* K = p.k + hoff;

@@ -154,11 +154,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void extend_kernel(CacheProblem p, 
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt) o[dt] = f32x16_t{};
   float m = kNoRef, l = 0.f;
-  float cs = p.scale_log2, vsc = 1.f;
-  if constexpr (FORM == kCacheHead) {
-    cs *= ld_uniform(p.k_head, u.h);
-    vsc = ld_uniform(p.v_head, u.h);
-  }
+  const float cs = score_scale<FORM>(p, u.h);
+  float vsc = 1.f;
+  if constexpr (FORM == kCacheHead) vsc = ld_uniform(p.v_head, u.h);
 
   // ---- staging
   const int64_t rowb = (int64_t)p.hkv * kHeadDim * ESZ;

@@ -65,7 +65,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(CacheProblem p, con
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.x % groups * p.heads + w % p.heads, ks = w / p.heads;
   const int c16 = lane & 15, kg = lane >> 4;
-  const float cs = p.scale_log2 * (FORM == kCacheHead ? ld_uniform(p.k_head, h) : 1.f);
+  const float cs = score_scale<FORM>(p, h);
   const int64_t rowb = (int64_t)p.hkv * kHeadDim * ESZ;
   const uint8_t* K = p.k + (int64_t)h * kHeadDim * ESZ;
   const uint32_t koff = (uint32_t)(c16 * rowb + 16 * kg);
@@ -304,7 +304,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void many_kernel(CacheProblem p,
         }
       }
     }
-    const float cs = p.scale_log2 * (FORM == kCacheHead ? ld_uniform(p.k_head, h) : 1.f);
+    const float cs = score_scale<FORM>(p, h);
 
     // staging: thread -> row tid / 8 of a step, two 16-byte chunks; g is a power of two
     const int r = tid >> 3, c = 2 * (tid & 7);

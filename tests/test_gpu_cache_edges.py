@@ -144,6 +144,16 @@ def test_scales_that_no_query_sees(byte, new, place):
     run_attend(c, 8, [new], window, sink)
 
 
+@pytest.mark.parametrize("new", [1, 3, 70])
+@pytest.mark.parametrize("window", [0, 60])
+def test_the_smallest_scale_of_a_head(new, window):
+    """Key scales whose product with the softmax scale fp32 does not hold: every key seen weighs the same,
+    the others nothing."""
+    c = ref.Cache([300, 90], 2, "head", 16, seed=48)
+    c.ks[:] = torch.tensor([1e-45, 1e-40])
+    run_attend(c, 8, [new, 2], window, 5)
+
+
 @pytest.mark.parametrize("batch,max_kv", [(0, 100), (2, 0)])
 def test_calls_without_tokens_leave_the_rows_behind_the_batch(batch, max_kv):
     """Results that are larger than the call: what lies behind its sequences stays."""
