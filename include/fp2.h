@@ -446,7 +446,9 @@ fp2_status_t fp2_prefill_noalloc(const fp2_params_t* params, const void* q,
  *
  * A query at position t sees key j <= t where window_tokens is 0; else where
  * also t - j < window_tokens or j < sink_tokens. What lies in slots that no
- * query sees never reaches an output. The conventions at the top of this file
+ * query sees, and in the scales of blocks that no query sees, never reaches an
+ * output. Scores and sums are fp32: |scale q.k| up to 2^24 and values up to
+ * 2^98 keep them finite. The conventions at the top of this file
  * hold (streams, capture, errors).
  */
 typedef struct {
@@ -508,7 +510,10 @@ fp2_status_t fp2_cache_append(const fp2_cache_params_t* params, const void* k_ne
  * num_q_heads], the natural log of the sum. q, out and lse must not overlap
  * (refused where cu_seqlens_host tells their rows). Probabilities are rounded
  * to bf16 for the value product. Rows past cu_seqlens[batch] are not touched. Where
- * max_seq_len * g <= 64 the keys are read once for all rows of a sequence;
+ * max_seq_len * g <= 64 the keys are read once for all rows of a sequence, in
+ * parts by many workgroups; else a workgroup takes 256 rows, and single tokens
+ * beside a long chunk take as long as its keys take one workgroup, so a mixed
+ * batch is faster as two calls;
  * results depend on kv_splits, and with 0 on the other sequences of a call,
  * through rounding only. */
 fp2_status_t fp2_cache_attend(const fp2_cache_params_t* params, const void* q,
@@ -537,7 +542,7 @@ fp2_status_t fp2_cache_weights(const fp2_cache_params_t* params, const void* q, 
 /* Cuts the sequences to at most `budget` (1 .. 1048576) tokens per KV head: the first
  * sink_tokens, the last recent_tokens and, of the others, the heaviest by
  * weights [batch][num_kv_heads][weights_stride] (fp32; equal ones by the
- * lowest index, NaN last). sink_tokens + recent_tokens <= budget. A sequence
+ * lowest index, NaN last; the 16-byte lines that hold them are read whole). sink_tokens + recent_tokens <= budget. A sequence
  * of at most `budget` tokens keeps them all. Different heads keep different
  * tokens.
  *   kept       int32 [batch][num_kv_heads][budget]: the indexes that stay,

@@ -19,10 +19,11 @@
 // Bound by the products and, beside them, a step's chain of exponentials: a
 // prompt of 32K tokens, 32 heads, window 4096, takes 2.10 ms from codes with
 // scales of 64 tokens (0.98 PFLOP/s; a large bf16 matrix product reaches 1.22)
-// and 2.36 from a bf16 cache, whose tiles take twice the loads.
+// and 2.34 from a bf16 cache, whose tiles take twice the loads.
 //
 // Calls of few units cut each unit's tiles into equal parts, joined by
-// join_kernel.
+// join_kernel. From 129 units on none is cut, and a unit of few rows (a single
+// token beside a chunk) goes through all its keys alone.
 #include <algorithm>
 
 #include "cache.h"
@@ -113,7 +114,7 @@ struct Shared {
 };
 
 // FORM: the cache's type. WIDE: pages hold a multiple of 64 tokens, so a tile
-// lies in one and its address is uniform (scalar). The prompt above in bf16: 2.36
+// lies in one and its address is uniform (scalar). The prompt above in bf16: 2.34
 // ms, from pages of 48 tokens 2.6.
 template <int FORM, bool WIDE>
 __global__ __launch_bounds__(64 * kWaves, 1) void extend_kernel(CacheProblem p, CachePartials part,
@@ -479,7 +480,7 @@ __global__ __launch_bounds__(256) void join_kernel(CacheProblem p, CachePartials
 int query_tiles(const CacheProblem& p) { return (p.max_new * p.g + kRows - 1) / kRows; }
 
 // Parts of a unit: as many as fill the chip, of at least kMinTiles tiles. 256
-// tokens behind 30000 take 141 us, and 896 whole; 256 behind 1000 28 us, with
+// tokens behind 30000 take 156 us, and 896 whole; 256 behind 1000 28 us, with
 // parts of 8 tiles or more 36.
 int parts_for(const CacheProblem& p) {
   const int64_t units = (int64_t)p.batch * p.hkv * query_tiles(p);

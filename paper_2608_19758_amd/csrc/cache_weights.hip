@@ -16,7 +16,7 @@
 // holds two keys with 16 queries each, whose probabilities it adds in fp32; its
 // sums take two registers (with keys as rows they took 32). Bound by the
 // products and the exponentials, half of the attention's work: 8101 tokens of 32
-// heads, bf16, take 329 us (0.82 PFLOP/s). Where the keys alone do not fill the
+// heads, bf16, take 330 us (0.82 PFLOP/s). Where the keys alone do not fill the
 // chip the rows are cut into segments too, whose sums sum_kernel adds in their
 // order.
 #include <algorithm>

@@ -212,3 +212,17 @@ def test_updates_are_held_to_the_captured_rows():
     for new in ([3, 2], [3, 3]):
         with pytest.raises(ValueError, match="rows"):
             be.update_forward_metadata(meta, new, lens, table)
+
+
+@pytest.mark.parametrize("form", ["bf16", 16])
+@pytest.mark.parametrize("new", [1, 5, 100])
+def test_values_and_scores_at_their_bounds(form, new):
+    """Values of about 2^98 and scores up to some 2^24: every output is a finite one."""
+    c = ref.Cache([3000, 600], 2, form, 16, seed=49)
+    for scale in (0.0, 2.0 ** 19):
+        if form == "bf16":
+            c.v = (c.v.float().clamp(-4, 4) * (2.0 ** 96 if scale == 0 else 1)).bfloat16()
+        elif scale == 0:
+            c.vs = torch.where(c.vs < 255, 88 + 127, 255).to(torch.uint8)
+        out, lse = run_attend(c, 8, [new, 2], scale=scale, weights=False)
+        assert bool(out.isfinite().all()) and bool(lse.isfinite().all())
