@@ -331,6 +331,8 @@ def cache_evict(p: CacheParams, cache: KVCache, weights, cu_seqlens_k, block_tab
     if weights_out.shape[2] != stride:
         raise ValueError("weights and weights_out differ in their last size")
     kp = a("kept", kept, _ONE_I32, batch * heads * budget)
+    if kept.dim() == 3 and tuple(kept.shape[1:]) != (heads, max(1, budget)):     # rows lie `budget` apart
+        raise ValueError("kept must be int32 [>= batch, %d, %d], got %s" % (heads, budget, tuple(kept.shape)))
     co = a("cu_seqlens_k_out", cu_seqlens_k_out, _ONE_I32, batch + 1)
     a.call("fp2_cache_evict", stream, ctypes.byref(p), ctypes.byref(c), cuk, cuk_host, table, target, pages,
            int(budget), int(recent_tokens), w, wo, stride, kp, co)

@@ -132,3 +132,13 @@ def test_a_refused_update_changes_nothing():
         with pytest.raises(ValueError, match="block_table"):
             be.update_forward_metadata(meta, [3, 1], [30, 10], bad)
     assert bool((lengths == 7).all()) and bool((table == 7).all()) and meta.plan is plan
+
+
+def test_indexes_of_another_budget():
+    """The indexes that stay lie `budget` apart: a tensor of another last size would be misread."""
+    p, t = base(), tensors(base())
+    for shape, says in (((2, 8, 101), "kept must be"), ((2, 8, 200), "kept must be"), ((2, 16, 100), "kept must be"),
+                        ((1, 8, 100), "kept holds"), ((2, 8, 100), "CUDA"), ((5, 8, 100), "CUDA"), ((1600,), "CUDA")):
+        with pytest.raises(ValueError, match=says):
+            fp2.cache_evict(p, t["cache"], t["w"], t["cu"], t["table"], t["table"], budget=100,
+                            kept=torch.zeros(shape, dtype=torch.int32))
