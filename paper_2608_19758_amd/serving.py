@@ -34,8 +34,9 @@ the new keys and values to each layer's cache, attends over it and, where the
 engine wants to shorten sequences later, adds up what every cached token
 received; ``evict`` then keeps the heaviest ``budget`` tokens of each sequence
 and KV head in new pages. One kernel serves a forward, by its longest extend: single
-tokens beside a long chunk are faster in a forward of their own. A cache of codes with a scale per head is what
-``PrefillBackend`` reads, so a prompt may be extended sparsely and decoded here.
+tokens beside a long chunk are faster in a forward of their own. A cache of codes with
+a scale per head is what ``PrefillBackend`` reads, so a prompt may be extended sparsely
+and decoded here.
 """
 from __future__ import annotations
 
