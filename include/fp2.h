@@ -28,6 +28,14 @@
  *   fp2_cache_weights = the attention weight that each cached token received;
  *   fp2_cache_evict   = the heaviest tokens of each head moved to other pages.
  *
+ * And, around the cache, positions and states of another length (see "Rotary
+ * positions" and "Reading, moving, cross attention" below):
+ *   fp2_rotary        = queries and keys turned by their positions;
+ *   fp2_cache_append_rotary = the same on the way into the cache, one pass;
+ *   fp2_cache_read    = cached tokens as bf16 rows, the turn taken back if asked;
+ *   fp2_cache_move    = cached tokens to other pages or positions;
+ *   fp2_cache_cross   = attention over all keys of another sequence.
+ *
  * Conventions shared by every entry point
  * ---------------------------------------
  * - All tensor pointers are DEVICE pointers (hipMalloc'd or torch CUDA
@@ -568,6 +576,112 @@ fp2_status_t fp2_cache_evict(const fp2_cache_params_t* params, const fp2_kv_cach
                              int32_t target_pages, int32_t budget, int32_t recent_tokens,
                              const float* weights, float* weights_out, int64_t weights_stride,
                              int32_t* kept, int32_t* cu_seqlens_k_out, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Rotary positions
+ * ---------------------------------------------------------------------------
+ * The pair (x, y) of dimensions (i, i + dim / 2), or (2 i, 2 i + 1) where
+ * `interleaved`, i < dim / 2, of a row at position n becomes
+ *   scale * (x cos t - y sin t),  scale * (x sin t + y cos t),   t = f_i n;
+ * dimensions from dim on stay as they are. Frequencies come as fractions of a
+ * turn in 64-bit fixed point, turns[i] = f_i / (2 pi) * 2^64 modulo 2^64, so the
+ * angle is exact at any position, negative ones too (its cosine and sine are
+ * fp32). An infinity or NaN spoils its pair and nothing else. `scale` goes with
+ * frequencies that are scaled for long contexts (1 without).
+ */
+typedef struct {
+  const uint64_t* turns;      /* device, [dim / 2] */
+  int32_t dim;                /* even, 2 .. 128 */
+  int32_t interleaved;        /* 0 or 1 */
+  float scale;                /* positive and finite, and its inverse too */
+} fp2_rotary_t;
+
+/* Rows that are turned: bf16 [tokens, heads, 128] with the heads side by side
+ * and x_stride elements between tokens (at least heads * 128; a part of a wider
+ * matrix will do), to rows of bf16, or of e4m3 codes e4m3(row / out_scale[head])
+ * as fp2_prefill takes its queries. `out` is x itself (same strides, bf16) or
+ * does not meet it. Pointers are 16-byte aligned, strides multiples of 8 elements
+ * (out_stride of 16 for codes). */
+typedef struct {
+  const void* x;
+  int64_t x_stride;
+  void* out;
+  int64_t out_stride;
+  int32_t heads;              /* 1 .. 8192 */
+  int32_t out_dtype;          /* FP2_BF16 or FP2_FP8_E4M3 */
+  const float* out_scale;     /* device, [heads]; codes only */
+} fp2_rotary_rows_t;
+
+/* Queries, and keys (nullable), of tokens at positions[tokens] (device), turned;
+ * inverse 1 takes a turn back (angles negative, divided by scale). Sums are fp32,
+ * rounded once. */
+fp2_status_t fp2_rotary(const fp2_rotary_t* rotary, int64_t tokens, const int32_t* positions,
+                        int32_t inverse, const fp2_rotary_rows_t* q, const fp2_rotary_rows_t* k,
+                        void* stream);
+
+/* fp2_cache_append with the new keys turned on the way, and the queries of the
+ * same tokens (nullable; num_q_heads heads) turned as fp2_rotary does it. k_new
+ * and v_new are bf16 rows with k_stride and v_stride elements between tokens.
+ * positions (device, [cu_seqlens[batch]]; null: a token's index in its sequence)
+ * are those of the new tokens. Codes are rounded once, from the fp32 of the
+ * turned keys; a block's scale goes by them. Query rows past
+ * cu_seqlens[batch] are not touched. */
+fp2_status_t fp2_cache_append_rotary(const fp2_cache_params_t* params, const fp2_rotary_t* rotary,
+                                     const fp2_rotary_rows_t* q, const void* k_new,
+                                     int64_t k_stride, const void* v_new, int64_t v_stride,
+                                     const int32_t* positions, const int32_t* cu_seqlens,
+                                     const int32_t* cu_seqlens_host, const int32_t* cu_seqlens_k,
+                                     const int32_t* cu_seqlens_k_host, const fp2_kv_cache_t* cache,
+                                     const int32_t* block_table, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Reading, moving, cross attention
+ * ---------------------------------------------------------------------------
+ * The last cu_seqlens tokens of each sequence (all, where they are
+ * cu_seqlens_k) as bf16 rows [cu_seqlens[batch], num_kv_heads, 128]; k_out or
+ * v_out may be null. With `rotary` the keys' turn by positions (as in
+ * fp2_cache_append_rotary; null: indexes) is taken back. Rows past
+ * cu_seqlens[batch] are not touched. */
+fp2_status_t fp2_cache_read(const fp2_cache_params_t* params, const fp2_rotary_t* rotary,
+                            const int32_t* positions, const int32_t* cu_seqlens,
+                            const int32_t* cu_seqlens_host, const int32_t* cu_seqlens_k,
+                            const int32_t* cu_seqlens_k_host, const fp2_kv_cache_t* cache,
+                            const int32_t* block_table, void* k_out, void* v_out, void* stream);
+
+/* All tokens of each sequence to the same places of the pages of target_table
+ * (int32 [batch][target_pages], target_pages >= ceil(max_kv_len / page_size)),
+ * or in place where it is null. With `rotary` key j of head h turns by
+ *   moves[b * batch_stride + h * head_stride + j * token_stride]
+ * positions (device; strides in elements, 0: the same for all), without its
+ * scale; without `rotary` keys are copied as they are, values always are. After
+ * an eviction index minus `kept` puts every key to the position of its new index.
+ * A scale per head stays, and codes are held within +-448, so it should leave
+ * room (a turn makes a value up to sqrt(2) times as large as its pair's larger
+ * one). A scale per block becomes what its turned keys need; codes are rounded
+ * once a call. Pages of target_table must not be pages of the call's sequences
+ * nor appear twice; in place no page may belong to two sequences of the call.
+ * Pages of the source are left as they are. max_seq_len and softmax_scale do
+ * not matter. */
+fp2_status_t fp2_cache_move(const fp2_cache_params_t* params, const fp2_rotary_t* rotary,
+                            const int32_t* moves, int64_t batch_stride, int64_t head_stride,
+                            int64_t token_stride, const int32_t* cu_seqlens_k,
+                            const int32_t* cu_seqlens_k_host, const fp2_kv_cache_t* cache,
+                            const int32_t* block_table, const int32_t* target_table,
+                            int32_t target_pages, void* stream);
+
+/* fp2_cache_attend without the order of tokens: every one of a sequence's
+ * cu_seqlens queries sees all of its cu_seqlens_k keys, more or fewer than the
+ * queries (an encoder's states; a prefix that many requests share). max_seq_len
+ * bounds the queries, up to 1048576, whatever max_kv_len is; window_tokens and
+ * sink_tokens are 0. Queries of a sequence without keys get zeros, and minus
+ * infinity for lse. Else as fp2_cache_attend; the workspace is of
+ * fp2_cache_cross_workspace_bytes. */
+size_t fp2_cache_cross_workspace_bytes(const fp2_cache_params_t* params);
+fp2_status_t fp2_cache_cross(const fp2_cache_params_t* params, const void* q,
+                             const int32_t* cu_seqlens, const int32_t* cu_seqlens_host,
+                             const int32_t* cu_seqlens_k, const int32_t* cu_seqlens_k_host,
+                             const fp2_kv_cache_t* cache, const int32_t* block_table, void* out,
+                             float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Static description of a status code. */
 const char* fp2_status_str(fp2_status_t status);

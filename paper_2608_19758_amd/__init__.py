@@ -51,6 +51,8 @@ EXPORTS = ["fp2_workspace_bytes", "fp2_prefill", "fp2_estimate", "fp2_attend", "
            "fp2_csr_capacity", "fp2_mask_to_csr", "fp2_means_cache_slots", "fp2_prefill_cached",
            "fp2_calibrate", "fp2_time_kernels", "fp2_prefill_noalloc", "fp2_cache_workspace_bytes",
            "fp2_cache_append", "fp2_cache_attend", "fp2_cache_weights", "fp2_cache_evict",
+           "fp2_rotary", "fp2_cache_append_rotary", "fp2_cache_read", "fp2_cache_move",
+           "fp2_cache_cross_workspace_bytes", "fp2_cache_cross",
            "fp2_status_str",
            "fp2_last_error"]
 
@@ -107,6 +109,19 @@ def lib():
         L.fp2_cache_weights.argtypes = [vp] * 11 + [ctypes.c_int64, vp, ctypes.c_size_t, vp]
         L.fp2_cache_evict.restype = ctypes.c_int
         L.fp2_cache_evict.argtypes = [vp] * 6 + [ctypes.c_int32] * 3 + [vp] * 2 + [ctypes.c_int64] + [vp] * 3
+        i32, i64 = ctypes.c_int32, ctypes.c_int64
+        L.fp2_rotary.restype = ctypes.c_int
+        L.fp2_rotary.argtypes = [vp, i64, vp, i32] + [vp] * 3
+        L.fp2_cache_append_rotary.restype = ctypes.c_int
+        L.fp2_cache_append_rotary.argtypes = [vp] * 4 + [i64, vp, i64] + [vp] * 8
+        L.fp2_cache_read.restype = ctypes.c_int
+        L.fp2_cache_read.argtypes = [vp] * 12
+        L.fp2_cache_move.restype = ctypes.c_int
+        L.fp2_cache_move.argtypes = [vp] * 3 + [i64] * 3 + [vp] * 5 + [i32, vp]
+        L.fp2_cache_cross_workspace_bytes.restype = ctypes.c_size_t
+        L.fp2_cache_cross_workspace_bytes.argtypes = [vp]
+        L.fp2_cache_cross.restype = ctypes.c_int
+        L.fp2_cache_cross.argtypes = [vp] * 11 + [ctypes.c_size_t, vp]
         L.fp2_status_str.restype = ctypes.c_char_p
         L.fp2_status_str.argtypes = [ctypes.c_int]
         L.fp2_last_error.restype = ctypes.c_char_p
@@ -496,5 +511,9 @@ def mask_to_csr(p: Params, block_mask, cu_seqlens, *, cu_seqlens_k=None, cu_seql
 
 # the paged cache's operators
 from .cache import (CACHE_WORKSPACE_MAX, CacheParams, KVCache, alloc_cache,  # noqa: E402,F401
-                    alloc_cache_workspace, cache_append, cache_attend, cache_evict, cache_weights,
-                    cache_workspace_bytes, make_cache_params)
+                    alloc_cache_workspace, alloc_cross_workspace, cache_append, cache_attend, cache_cross,
+                    cache_evict, cache_weights, cache_workspace_bytes, cross_workspace_bytes,
+                    make_cache_params)
+# positions: turning queries and keys, and cached tokens
+from .positions import (Rotary, cache_append_rotary, cache_move, cache_read,  # noqa: E402,F401
+                        make_rotary, rotary, rotary_frequencies)

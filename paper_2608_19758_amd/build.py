@@ -14,7 +14,8 @@ LIB = os.path.join(PKG, "libfp2.so")
 SOURCES = ["api.hip", "pool.hip", "estimate.hip", "attend.hip", "schedule.hip", "index.hip",
            "calib.hip", "noalloc.hip",
            "cache_api.hip", "cache_append.hip", "cache_decode.hip", "cache_extend.hip",
-           "cache_weights.hip", "cache_evict.hip"]
+           "cache_weights.hip", "cache_evict.hip",
+           "rotary.hip", "cache_rotary.hip", "cache_move.hip", "cache_cross.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

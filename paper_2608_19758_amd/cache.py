@@ -1,4 +1,4 @@
-"""Paged KV cache: append, attention, weights and eviction (argument marshalling
+"""Paged KV cache: append, attention, cross attention, weights and eviction (argument marshalling
 over the ``fp2_cache_*`` entry points of ``include/fp2.h``, which states their
 semantics and layouts).
 
@@ -130,6 +130,31 @@ class _Args:
                 self.odd = (name, t.device)
         return t.data_ptr()
 
+    def rows(self, name, t, heads, dtypes=_ONE_BF16):
+        """Address and stride (elements between tokens) of rows [tokens, heads, 128] whose heads lie
+        side by side; tokens may lie further apart (a part of a wider matrix)."""
+        if not isinstance(t, torch.Tensor):
+            raise ValueError("%s must be a torch tensor" % name)
+        if t.dtype not in dtypes:
+            raise ValueError("%s must have dtype in %s, got %s" % (name, dtypes, t.dtype))
+        shape = t.shape
+        if len(shape) != 3 or shape[2] != HEAD_DIM or (heads is not None and shape[1] != heads):
+            raise ValueError("%s must be [tokens, %s, %d], got %s"
+                             % (name, "heads" if heads is None else heads, HEAD_DIM, tuple(shape)))
+        stride, head, one = t.stride()
+        if one != 1 or (head != HEAD_DIM and shape[1] > 1):
+            raise ValueError("%s must have its heads side by side" % name)
+        self.place(name, t)
+        return t.data_ptr(), stride if shape[0] > 1 else shape[1] * HEAD_DIM
+
+    def place(self, name, t):
+        """Notes a tensor on another device than the first one's."""
+        dev = t.get_device()
+        if self.dev is None:
+            self.dev = dev
+        if (dev != self.dev or dev < 0) and self.odd is None:
+            self.odd = (name, t.device)
+
     def table(self, batch, name, t, width):
         shape = t.shape if isinstance(t, torch.Tensor) else ()
         if len(shape) != 2 or shape[1] != width or shape[0] < batch:
@@ -242,6 +267,12 @@ def cache_attend(p: CacheParams, q, cache: KVCache, cu_seqlens, cu_seqlens_k, bl
                  lse=None, want_lse=False, workspace=None, cu_seqlens_host=None,
                  cu_seqlens_k_host=None, stream=None):
     """fp2_cache_attend: returns (out bf16 like q, lse fp32 [tokens, num_q_heads] or None)."""
+    return _attention("fp2_cache_attend", alloc_cache_workspace, p, q, cache, cu_seqlens, cu_seqlens_k,
+                      block_table, out, lse, want_lse, workspace, cu_seqlens_host, cu_seqlens_k_host, stream)
+
+
+def _attention(name, alloc, p, q, cache, cu_seqlens, cu_seqlens_k, block_table, out, lse, want_lse, workspace,
+               cu_seqlens_host, cu_seqlens_k_host, stream):
     a, batch, heads = _Args(), p.batch, p.num_q_heads
     row = heads * p.head_dim
     qp = a("q", q, _ONE_BF16, 0, row)
@@ -256,7 +287,7 @@ def cache_attend(p: CacheParams, q, cache: KVCache, cu_seqlens, cu_seqlens_k, bl
         if lse is None and want_lse:
             lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device)
         if workspace is None:
-            workspace = alloc_cache_workspace(p, q.device)
+            workspace = alloc(p, q.device)
     op, lp = a("out", out, _ONE_BF16, size), a("lse", lse, _ONE_F32, rows * heads, optional=True)
     if op < qp + 2 * size and qp < op + 2 * size:
         raise ValueError("out must not overlap q")
@@ -265,9 +296,27 @@ def cache_attend(p: CacheParams, q, cache: KVCache, cu_seqlens, cu_seqlens_k, bl
         if (lp < qp + 2 * size and qp < end) or (lp < op + 2 * size and op < end):
             raise ValueError("lse must not overlap q or out")
     ws = a("workspace", workspace, _BYTES)
-    a.call("fp2_cache_attend", stream, ctypes.byref(p), qp, *lens, ctypes.byref(c), table, op, lp, ws,
+    a.call(name, stream, ctypes.byref(p), qp, *lens, ctypes.byref(c), table, op, lp, ws,
            workspace.numel())
     return out, lse
+
+
+def cross_workspace_bytes(p: CacheParams) -> int:
+    return int(lib().fp2_cache_cross_workspace_bytes(ctypes.byref(p)))
+
+
+def alloc_cross_workspace(p: CacheParams, device="cuda") -> torch.Tensor:
+    return torch.empty(max(1, cross_workspace_bytes(p)), dtype=torch.uint8, device=device)
+
+
+def cache_cross(p: CacheParams, q, cache: KVCache, cu_seqlens, cu_seqlens_k, block_table, *, out=None,
+                lse=None, want_lse=False, workspace=None, cu_seqlens_host=None,
+                cu_seqlens_k_host=None, stream=None):
+    """fp2_cache_cross: every query of a sequence over all of its keys, however many of each.
+    max_seq_len of p bounds the queries and may pass max_kv_len. Returns (out bf16 like q, lse
+    fp32 [queries, num_q_heads] or None)."""
+    return _attention("fp2_cache_cross", alloc_cross_workspace, p, q, cache, cu_seqlens, cu_seqlens_k,
+                      block_table, out, lse, want_lse, workspace, cu_seqlens_host, cu_seqlens_k_host, stream)
 
 
 def cache_weights(p: CacheParams, q, lse, cache: KVCache, cu_seqlens, cu_seqlens_k, block_table, *,

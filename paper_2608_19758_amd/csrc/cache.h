@@ -136,7 +136,7 @@ int64_t cache_weights_partials(const CacheProblem& p);
 hipError_t launch_cache_append(const CacheProblem& p, const uint16_t* k_new, const uint16_t* v_new,
                                hipStream_t s);
 hipError_t launch_cache_decode(const CacheProblem& p, const CachePartials& part, uint16_t* out,
-                               float* lse, hipStream_t s);
+                               float* lse, hipStream_t s, bool cross = false);
 hipError_t launch_cache_extend(const CacheProblem& p, const CachePartials& part, uint16_t* out,
                                float* lse, hipStream_t s);
 hipError_t launch_cache_weights(const CacheProblem& p, const float* lse, const float* in, float* out,

@@ -86,12 +86,24 @@ __device__ __forceinline__ uint32_t odd_value(uint2 v, int e) {
   return ((odd_codes(e < 4 ? v.x : v.y) >> (8 * (e & 3) + 7)) & 1) * 0x7fc00000u;
 }
 
+// What the rows of a sequence without keys come to, heads h0 on: zeros, and minus infinity.
+__device__ __forceinline__ void write_empty(const CacheProblem& p, int b, int h0, int heads, uint16_t* out, float* lse) {
+  const int q0 = ld_uniform(p.cu, b), Lq = ld_uniform(p.cu, b + 1) - q0, n = heads * p.g;
+  if (ld_uniform(p.cuk, b + 1) > ld_uniform(p.cuk, b)) return;
+  for (int i = threadIdx.x; i < Lq * n * 16; i += blockDim.x) {
+    const int64_t at = ((int64_t)q0 + i / 16 / n) * p.hq + h0 * p.g + i / 16 % n;
+    *(uint4*)(out + at * kHeadDim + 8 * (i % 16)) = make_uint4(0, 0, 0, 0);
+    if (lse && i % 16 == 0) lse[at] = -INFINITY;
+  }
+}
+
 // FORM: the cache's type. NT: 16-row tiles of query rows of a wave. RH: waves
 // that share the rows. W: waves (many registers a wave: four, one a SIMD).
 // GROUPED: pages hold a multiple of 16 tokens, so the 16 keys of a group lie one
 // after the other and their address is uniform (scalar); otherwise every key has
 // its own (8 sequences of 64 rows: 99 us, with pages of 24 tokens 108).
-template <int FORM, int NT, int RH, int W, bool GROUPED>
+// CROSS: every row sees all keys of its sequence, as if it stood on the last one.
+template <int FORM, int NT, int RH, int W, bool GROUPED, bool CROSS>
 __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, CachePartials part,
                                                                int shares, uint16_t* __restrict__ out,
                                                                float* __restrict__ lse) {
@@ -104,7 +116,11 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
   const int groups = p.hkv / p.heads, index = blockIdx.x / groups;
   const int units = p.heads * RH, KS = W / units;   // (head, half of the rows): how many waves alternate its tiles
   Share sh;
-  if (!find_share(p, shares, index, sh)) return;
+  if (!find_share(p, shares, index, sh)) {
+    if constexpr (CROSS)   // (otherwise the join's)
+      if (p.splits == 1) write_empty(p, index, blockIdx.x % groups * p.heads, p.heads, out, lse);
+    return;
+  }
 
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -131,7 +147,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
     sh.L = ld_uniform(p.cuk, b + 1) - ld_uniform(p.cuk, b);
   }
   const int q0 = sh.q0, Lq = sh.Lq, L = sh.L;
-  const int first = L - Lq, last = L - 1;      // positions of the first and the last row
+  const int last = L - 1, first = CROSS ? last : L - Lq;      // positions of the first and the last row
   const int rows = Lq * p.g;
   const Tiles tl = tiles_of(p, Lq, L);
   const int lo = max(sh.lo, base) - base, hi = min(sh.hi, base + tl.n) - base;
@@ -145,7 +161,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int r = rb + 16 * nt + c16;
-    pos[nt] = first + r / p.g;
+    pos[nt] = CROSS ? last : first + r / p.g;
     const uint16_t* qrow = p.q + ((int64_t)(q0 + min(r / p.g, Lq - 1)) * p.hq + h * p.g + r % p.g) *
                                      kHeadDim;
 #pragma unroll
@@ -474,6 +490,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
 // 8000 416 instead of 401). A workgroup takes one packed row, groups of 32 lanes
 // the parts in turn, eight of them a step with all their loads in flight; the
 // groups are joined in LDS.
+template <bool CROSS>
 __global__ __launch_bounds__(1024) void combine_kernel(CacheProblem p, CachePartials part,
                                                       int rows_cap, int max_rows,
                                                       uint16_t* __restrict__ out,
@@ -485,7 +502,10 @@ __global__ __launch_bounds__(1024) void combine_kernel(CacheProblem p, CachePart
   const int q0 = ld_uniform(p.cu, b), Lq = ld_uniform(p.cu, b + 1) - q0;
   if (pr >= Lq * p.g) return;
   const int tiles = tiles_of(p, Lq, ld_uniform(p.cuk, b + 1) - ld_uniform(p.cuk, b)).n;
-  if (tiles <= 0) return;
+  if (tiles <= 0) {
+    if (CROSS && pr == 0) write_empty(p, b, h, 1, out, lse);
+    return;
+  }
   // the sequence's parts: slots `s0`, then every second share's (kv_splits:
   // its own shares')
   int parts;
@@ -569,7 +589,7 @@ int rows_cap(const CacheProblem& p) {
 // 64 rows: 101 us with 2, 105 with 4.
 int heads_for(const CacheProblem& p) { return 128 / rows_cap(p); }
 
-template <int FORM, int NT, int RH, int W, bool GROUPED>
+template <int FORM, int NT, int RH, int W, bool GROUPED, bool CROSS>
 hipError_t launch(const CacheProblem& problem, const CachePartials& part, uint16_t* out, float* lse,
                   hipStream_t s) {
   const CacheProblem p = dealt(problem, heads_for(problem));
@@ -581,9 +601,9 @@ hipError_t launch(const CacheProblem& problem, const CachePartials& part, uint16
   // 4096 of 8 sequences 100, and 122 with 1024
   const int threads = joins <= kFewGroups ? 1024 : 256;
   if (!launchable(grid, 64 * W) || (p.splits != 1 && !launchable(joins, threads))) return hipErrorInvalidValue;
-  decode_kernel<FORM, NT, RH, W, GROUPED><<<(unsigned)grid, 64 * W, 0, s>>>(p, part, shares, out, lse);
+  decode_kernel<FORM, NT, RH, W, GROUPED, CROSS><<<(unsigned)grid, 64 * W, 0, s>>>(p, part, shares, out, lse);
   if (p.splits == 1) return hipGetLastError();
-  combine_kernel<<<(unsigned)joins, threads, 0, s>>>(p, part, 16 * NT * RH, max_rows, out, lse);
+  combine_kernel<CROSS><<<(unsigned)joins, threads, 0, s>>>(p, part, 16 * NT * RH, max_rows, out, lse);
   return hipGetLastError();
 }
 
@@ -591,23 +611,23 @@ hipError_t launch(const CacheProblem& problem, const CachePartials& part, uint16
 // of codes. 64 rows need a wave's 512 registers; in bf16 not even those hold
 // them, and two waves share them (145 us, 170 with spilled registers; in codes
 // 108 instead of 101).
-template <int FORM, bool GROUPED>
+template <int FORM, bool GROUPED, bool CROSS>
 hipError_t launch_rows(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse,
                        hipStream_t s) {
   constexpr bool kBf16 = FORM == kCacheBf16;
   const int rows = rows_cap(p);
-  return rows == 16   ? launch<FORM, 1, 1, 8, GROUPED>(p, part, out, lse, s)
-         : rows == 32 ? launch<FORM, 2, 1, kBf16 ? 4 : 8, GROUPED>(p, part, out, lse, s)
-                      : launch<FORM, kBf16 ? 2 : 4, kBf16 ? 2 : 1, 4, GROUPED>(p, part, out, lse, s);
+  return rows == 16   ? launch<FORM, 1, 1, 8, GROUPED, CROSS>(p, part, out, lse, s)
+         : rows == 32 ? launch<FORM, 2, 1, kBf16 ? 4 : 8, GROUPED, CROSS>(p, part, out, lse, s)
+                      : launch<FORM, kBf16 ? 2 : 4, kBf16 ? 2 : 1, 4, GROUPED, CROSS>(p, part, out, lse, s);
 }
 
-template <int FORM>
+template <int FORM, bool CROSS>
 hipError_t launch_pages(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse,
                         hipStream_t s) {
   // scales of blocks imply pages of a multiple of 16 tokens
-  if constexpr (FORM == kCacheBlock) return launch_rows<FORM, true>(p, part, out, lse, s);
-  else if (p.pm.page % 16 == 0) return launch_rows<FORM, true>(p, part, out, lse, s);
-  else return launch_rows<FORM, false>(p, part, out, lse, s);
+  if constexpr (FORM == kCacheBlock) return launch_rows<FORM, true, CROSS>(p, part, out, lse, s);
+  else if (p.pm.page % 16 == 0) return launch_rows<FORM, true, CROSS>(p, part, out, lse, s);
+  else return launch_rows<FORM, false, CROSS>(p, part, out, lse, s);
 }
 
 }  // namespace
@@ -618,11 +638,16 @@ void cache_decode_partials(const CacheProblem& problem, int64_t* slots, int* row
   *rows = rows_cap(p);
 }
 
+template <bool CROSS>
+static hipError_t launch_any(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse, hipStream_t s) {
+  return p.form == kCacheBf16   ? launch_pages<kCacheBf16, CROSS>(p, part, out, lse, s)
+         : p.form == kCacheHead ? launch_pages<kCacheHead, CROSS>(p, part, out, lse, s)
+                                : launch_pages<kCacheBlock, CROSS>(p, part, out, lse, s);
+}
+
 hipError_t launch_cache_decode(const CacheProblem& p, const CachePartials& part, uint16_t* out,
-                               float* lse, hipStream_t s) {
-  return p.form == kCacheBf16   ? launch_pages<kCacheBf16>(p, part, out, lse, s)
-         : p.form == kCacheHead ? launch_pages<kCacheHead>(p, part, out, lse, s)
-                                : launch_pages<kCacheBlock>(p, part, out, lse, s);
+                               float* lse, hipStream_t s, bool cross) {
+  return cross ? launch_any<true>(p, part, out, lse, s) : launch_any<false>(p, part, out, lse, s);
 }
 
 }  // namespace fp2
