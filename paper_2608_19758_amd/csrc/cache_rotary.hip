@@ -1,19 +1,21 @@
 // New tokens' queries, keys and values in one pass: queries and keys turned by
 // their positions, keys and values written into a paged cache in its type.
 //
-// A workgroup takes a run of 64 consecutive tokens of one sequence (128 where a
-// scale stands for as many), works out their turns once in LDS and goes through
-// its heads with them, a wave a head: queries out, keys and values to their
-// slots. With a scale per block of tokens the block lies in one wave, so its
-// largest value is a wave's maximum; 2^e, e = ceil(log2(amax / 448)) of the
-// turned keys, makes x 2^-e exact and a code is rounded once, from fp32. Where a
-// block holds tokens already its scale never falls; if it grows their codes are
-// rounded again.
+// A wave of queries takes eight tokens and several heads, and works its turns out
+// once for them. A wave of keys or values takes 32 tokens of a head; where a scale
+// stands for 64 or 128 tokens two or four waves share the block and its largest
+// value, through LDS. 2^e, e = ceil(log2(amax / 448)) of the turned keys, makes
+// x 2^-e exact, and a code is rounded once, from the fp32 that the wave holds.
+// Where a block holds tokens already its scale never falls; if it grows their
+// codes are rounded again.
 //
 // Bound by memory: 256 bytes a row in, 256 or 128 out.
 //
 // Few new tokens a sequence (a decode step): a wave has one head of a sequence
-// to itself and works its turns out in registers.
+// to itself.
+#include <type_traits>
+
+#include "cache_runs.h"
 #include "rotary_rows.h"
 
 namespace fp2 {
@@ -45,147 +47,208 @@ struct Seq {
   __device__ __forceinline__ int position(const New& x, int t) const { return x.positions ? x.positions[row(t)] : t; }
 };
 
-// Codes of a lane's sixteen values times a power of two.
-__device__ __forceinline__ void shrink16(uint32_t (&w)[4], float by) {
-  float x[16], y[16];
-  unpack16(w, x);
-#pragma unroll
-  for (int e = 0; e < 16; ++e) y[e] = x[e] * by;
-  pack16(x, y, w);
-}
+// Codes of a row times a power of two (at most 1).
 __device__ __forceinline__ void shrink_row(uint8_t* row, int lane, float by) {
   uint4* at = (uint4*)(row + 16 * (lane & 7));
   uint32_t w[4] = {at->x, at->y, at->z, at->w};
-  shrink16(w, by);
+  float x[16];
+  unpack16(w, x);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) x[e] *= by;
+  codes16(x, w);
   *at = make_uint4(w[0], w[1], w[2], w[3]);
 }
 __device__ __forceinline__ float power_down(int from, int to) {   // 2^(from - to), to >= from
   return __uint_as_float((uint32_t)max(127 - (to - from), 0) << 23);
 }
 
-// SB: tokens of a scale (kCacheBlock), else 0.
-template <int FORM, int SB, int PLACE>
-__global__ __launch_bounds__(64 * kWaves) void append_rotary_kernel(CacheProblem p, Rotary r, RotaryRows q, New x,
-                                                                    int chunks, int groups) {
-  constexpr int TOK = SB == 128 ? 128 : 64;      // tokens of a workgroup
-  constexpr int RUN = SB > 32 ? SB : 32;         // tokens whose loads a wave has in flight
-  constexpr int N = RUN / kPass;
-  constexpr int ESZ = FORM == kCacheBf16 ? 2 : 1;
-  __shared__ TurnTable<TOK> table;
-  __shared__ int64_t s_slot[TOK];
-  int64_t at = blockIdx.x;
-  const int group = (int)(at % groups);
-  at /= groups;
-  const int ck = (int)(at % chunks);
-  const Seq s(p, (int)(at / chunks));
-  const int first = (s.P / TOK + ck) * TOK;
-  if (s.n <= 0 || first >= s.L) return;
-  table.fill(r, 64 * kWaves, [&](int i) { return s.position(x, min(max(first + i, s.P), s.L - 1)); });
-  for (int i = threadIdx.x; i < TOK; i += 64 * kWaves) s_slot[i] = slot_of(p.pm, s.b, s.tok0, min(first + i, s.L - 1));
-  __syncthreads();
-
-  const int lane = threadIdx.x & 63, r0 = lane / kLaneRow;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// Queries: heads h0 .. h1 - 1 of eight new tokens, from the i0-th on.
+template <int PLACE>
+__device__ __forceinline__ void turn_queries(const CacheProblem& p, const Rotary& r, const RotaryRows& q, const New& x,
+                                             int b, int64_t i0, int h0, int h1) {
+  constexpr int kAhead = 4;                      // heads whose loads are in flight
+  const Seq s(p, b);
+  if (i0 >= s.n) return;
+  const int lane = threadIdx.x & 63, t = s.P + min((int)i0 + lane / kLaneRow, s.n - 1);
+  const bool there = i0 + lane / kLaneRow < s.n;
   const LaneRow<PLACE> l(lane, r.dim);
-  const int64_t rowb = (int64_t)p.hkv * kHeadDim;
-  const int jobs = 2 * p.hkv + q.heads;
+  const int64_t row = s.row(t);
+  Turns y;
+  l.turns(r, l.freqs(r), s.position(x, t), y);
 #pragma unroll 1
-  for (int j = group * kWaves + w; j < jobs; j += groups * kWaves) {
-    const bool is_q = j >= 2 * p.hkv, is_v = !is_q && j >= p.hkv;
-    const int h = is_q ? j - 2 * p.hkv : is_v ? j - p.hkv : j;
-    const uint16_t* src = (is_q ? q.x : is_v ? x.v : x.k) + h * kHeadDim;
-    const int64_t stride = is_q ? q.x_stride : is_v ? x.v_stride : x.k_stride;
-    uint8_t* pool = (is_v ? p.v : p.k) + h * kHeadDim * ESZ;
-#pragma unroll 1
-    for (int g = 0; g < TOK; g += RUN) {
-      if (first + g >= s.L || first + g + RUN <= s.P) continue;
-      uint32_t raw[N][8];
+  for (int h = h0; h < h1; h += kAhead) {
+    uint32_t w[kAhead][8];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)             // past the end the last head again
+      load_part(l, q.x + row * q.x_stride + min(h + i, h1 - 1) * kHeadDim, w[i]);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (h + i < h1) turn_and_store(l, y, w[i], q, row, h + i, there);
+  }
+}
+
+// 32 new tokens of a head, keys or values, of the block (of 32 PARTS tokens) that is
+// the run-th with new tokens. Every wave of the workgroup takes part.
+template <int FORM, int SB, int PLACE>
+__device__ __forceinline__ void append_step(const CacheProblem& p, const Rotary& r, const New& x, float* s_amax, bool is_v,
+                                            bool on, int b, int h, int w, int part, int64_t run) {
+  constexpr int PARTS = SB > 32 ? SB / 32 : 1;   // waves of a block
+  constexpr int TOK = 32 * PARTS;
+  constexpr int N = 32 / kPass;
+  constexpr int ESZ = FORM == kCacheBf16 ? 2 : 1;
+  const Seq s(p, b);
+  const int64_t block64 = ((int64_t)(s.P / TOK) + run) * TOK;
+  on = on && s.n > 0 && block64 < s.L;
+  const int block = on ? (int)block64 : 0, first = block + 32 * part;
+  const bool mine = on && first < s.L && first + 32 > s.P;     // some of the wave's own tokens are new
+  const int lane = threadIdx.x & 63, r0 = lane / kLaneRow;
+  const LaneRow<PLACE> l(lane, r.dim);
+  const uint16_t* src = (is_v ? x.v : x.k) + h * kHeadDim;
+  const int64_t stride = is_v ? x.v_stride : x.k_stride, rowb = (int64_t)p.hkv * kHeadDim;
+  uint8_t* pool = (is_v ? p.v : p.k) + h * kHeadDim * ESZ;
+  float z[N][16];
+  int64_t slot_l = 0;                            // of token first + lane % 32
+  if (mine) {
+    uint32_t raw[N][8];
+    int pos[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {                // (rows that are not new repeat one that is)
+      const int t = min(max(first + kPass * i + r0, s.P), s.L - 1);
+      load_part(l, src + s.row(t) * stride, raw[i]);
+      pos[i] = is_v ? 0 : s.position(x, t);
+    }
+    slot_l = slot_of(p.pm, s.b, s.tok0, min(first + (lane & 31), s.L - 1));
+    if (is_v) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) unpack16(raw[i], z[i]);
+    } else {
+      const Freqs freqs = l.freqs(r);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int t = first + g + kPass * i + r0;
-        load_part(l, src + s.row(min(max(t, s.P), s.L - 1)) * stride, raw[i]);
+        Turns y;
+        l.turns(r, freqs, pos[i], y);
+        unpack16(raw[i], z[i]);
+        turn16(l, y, z[i]);
       }
-      if (is_q) {
+    }
+  }
+  auto store = [&](int i, auto&& convert) {      // pass i in the cache's type
+    const int t = first + kPass * i + r0;
+    const int64_t slot = __shfl(slot_l, kPass * i + r0, 64);
+    uint32_t c[4 * ESZ];
+    convert(z[i], c);
+    if (t >= s.P && t < s.L) store_part(l, (std::conditional_t<ESZ == 2, uint16_t, uint8_t>*)pool + slot * rowb, c);
+  };
+  if constexpr (FORM == kCacheBf16) {
+    if (!mine) return;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int k = g + kPass * i + r0, t = first + k;
-          Turns y;
-          table.get(k, l.c, y);
-          turn_and_store(l, y, raw[i], q, s.row(t), h, t >= s.P && t < s.L);
-        }
-        continue;
-      }
-      auto values = [&](int i, float (&z)[16]) {   // of pass i, turned
-        unpack16(raw[i], z);
-        if (!is_v) {
-          Turns y;
-          table.get(g + kPass * i + r0, l.c, y);
-          turn16(l, y, z);
-        }
-      };
-      if constexpr (FORM != kCacheBlock) {
-        float scale = 1.f;
-        if constexpr (FORM == kCacheHead) scale = ld_uniform(is_v ? p.v_head : p.k_head, h);
+    for (int i = 0; i < N; ++i) store(i, [](const float (&v)[16], uint32_t (&c)[8]) { pack16(v, c); });
+  } else if constexpr (FORM == kCacheHead) {
+    if (!mine) return;
+    const Divisor d(ld_uniform(is_v ? p.v_head : p.k_head, h));
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int k = g + kPass * i + r0, t = first + k;
-          float z[16];
-          values(i, z);
-          if (t < s.P || t >= s.L) continue;
-          uint8_t* row = pool + s_slot[k] * rowb * ESZ;
-          if constexpr (FORM == kCacheBf16) {
-            uint32_t c[8];
-            pack16(z, c);
-            store_part(l, (uint16_t*)row, c);
-          } else {
-            float u[16];
-            uint32_t c[4];
+    for (int i = 0; i < N; ++i) store(i, [&](const float (&v)[16], uint32_t (&c)[4]) { codes16_by(v, d, c); });
+  } else {
+    constexpr int BLOCKS = SB == 16 ? 2 : 1, PER = N / BLOCKS;   // of a wave, and passes of each
+    float amax[BLOCKS];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) u[e] = z[e] / scale;
-            pack16(z, u, c);
-            store_part(l, row, c);
-          }
-        }
-      } else {
-        constexpr int PER = SB / kPass;              // passes of a block
+    for (int k = 0; k < BLOCKS; ++k) {
+      amax[k] = 0.f;
+      if (mine) {
 #pragma unroll
-        for (int i0 = 0; i0 < N; i0 += PER) {
-          const int kb = g + kPass * i0, tb = first + kb;   // the block's first token
-          if (tb >= s.L || tb + SB <= s.P) continue;
-          uint8_t* sp = (is_v ? p.v_block : p.k_block) + (s_slot[kb] >> p.sb_shift) * p.hkv + h;
-          const int before = tb < s.P ? *sp : 0;     // byte of a block that holds tokens
-          float amax = 0.f;
+        for (int i = PER * k; i < PER * (k + 1); ++i) amax[k] = fmaxf(amax[k], largest16(z[i]));
+        amax[k] = wave_max(amax[k]);
+        if (!(amax[k] < INFINITY)) {             // (rare: infinities do not count)
+          amax[k] = 0.f;
 #pragma unroll
-          for (int i = i0; i < i0 + PER; ++i) {      // (rows outside the new tokens repeat one of them)
-            float z[16];
-            values(i, z);
-            amax = fmaxf(amax, largest16(z));
-          }
-          const int byte = __builtin_amdgcn_readfirstlane(max(scale_byte(wave_max(amax)), before));
-          if (lane == 0) *sp = (uint8_t)byte;
-          const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);   // 2^-e
-          if (tb < s.P && byte > before) {
-            const float by = power_down(before, byte);
-            for (int t = tb + r0; t < min(s.P, tb + SB); t += kPass)
-              shrink_row(pool + s_slot[t - first] * rowb, lane, by);
-          }
-#pragma unroll
-          for (int i = i0; i < i0 + PER; ++i) {
-            const int k = g + kPass * i + r0, t = first + k;
-            float z[16], u[16];
-            uint32_t c[4];
-            // turned once more: kept from above the values would take 16 registers a pass
-#pragma unroll
-            for (int e = 0; e < 8; ++e) raw[i][e] = (uint32_t)pinned((int)raw[i][e]);
-            values(i, z);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) u[e] = z[e] * inv;
-            pack16(z, u, c);
-            if (t >= s.P && t < s.L) store_part(l, pool + s_slot[k] * rowb, c);
-          }
+          for (int i = PER * k; i < PER * (k + 1); ++i) amax[k] = fmaxf(amax[k], largest16_finite(z[i]));
+          amax[k] = wave_max(amax[k]);
         }
       }
     }
+    // bytes of blocks that hold tokens, read before the barrier: behind it the first wave of a block writes its own
+    uint8_t* sp[BLOCKS];
+    int before[BLOCKS];
+#pragma unroll
+    for (int k = 0; k < BLOCKS; ++k) {
+      const int tb = PARTS > 1 ? block : first + SB * k;         // the block's first token
+      sp[k] = nullptr;
+      before[k] = 0;
+      if (!on || tb >= s.L || tb + SB <= s.P) continue;
+      sp[k] = (is_v ? p.v_block : p.k_block) + (slot_of(p.pm, s.b, s.tok0, tb) >> p.sb_shift) * p.hkv + h;
+      if (tb < s.P) before[k] = __builtin_amdgcn_readfirstlane((int)*sp[k]);
+    }
+    if constexpr (PARTS > 1) {
+      if (lane == 0) s_amax[w] = amax[0];
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < PARTS; ++j) amax[0] = fmaxf(amax[0], s_amax[w - part + j]);
+    }
+    if (!on) return;
+#pragma unroll
+    for (int k = 0; k < BLOCKS; ++k) {
+      const int tb = PARTS > 1 ? block : first + SB * k;
+      if (!sp[k]) continue;
+      const int byte = __builtin_amdgcn_readfirstlane(max(scale_byte(amax[k]), before[k]));
+      if (tb < s.P && byte > before[k]) {        // the wave's share of the codes that were there
+        const float by = power_down(before[k], byte);
+        const int from = PARTS > 1 ? first : tb;
+        for (int t = from + r0; t < min(s.P, from + (PARTS > 1 ? 32 : SB)); t += kPass)
+          shrink_row(pool + slot_of(p.pm, s.b, s.tok0, t) * rowb, lane, by);
+      }
+      if (mine) {
+        const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);   // 2^-e
+#pragma unroll
+        for (int i = PER * k; i < PER * (k + 1); ++i) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) z[i][e] *= inv;
+          if (byte < kMaxScaleByte) store(i, [](const float (&v)[16], uint32_t (&c)[4]) { codes16(v, c); });
+          else store(i, [](const float (&v)[16], uint32_t (&c)[4]) { codes16_held(v, c); });
+        }
+      }
+      if (part == 0 && lane == 0) *sp[k] = (uint8_t)byte;
+    }
+  }
+}
+
+// SB: tokens of a scale (kCacheBlock), else 0. Workgroups below `kv` take equal
+// shares of the keys and values, the others of the queries, `heads` heads at a time.
+template <int FORM, int SB, int PLACE>
+__global__ __launch_bounds__(64 * kWaves) void append_rotary_kernel(CacheProblem p, Rotary r, RotaryRows q, New x,
+                                                                    Steps steps, int kv, int heads) {
+  constexpr int PARTS = SB > 32 ? SB / 32 : 1, WIDE = kWaves / PARTS, SHIFT = PARTS == 4 ? 7 : PARTS == 2 ? 6 : 5;
+  __shared__ float s_amax[2][kWaves];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if ((int)blockIdx.x >= kv) {
+    Runs<3, 1> line(p.cu, p.batch);
+    const int groups = (q.heads + heads - 1) / heads;
+    const int64_t items = line.total() * groups, waves = (int64_t)(gridDim.x - kv) * kWaves;
+    const int64_t wave = (int64_t)(blockIdx.x - kv) * kWaves + w, lo = items * wave / waves, hi = items * (wave + 1) / waves;
+    int64_t slot = lo / groups;
+    int g = (int)(lo - slot * groups);
+#pragma unroll 1
+    for (int64_t i = lo; i < hi; ++i) {
+      const int64_t pass = line.seek(slot);
+      turn_queries<PLACE>(p, r, q, x, line.b, pass * kPass, g * heads, min((g + 1) * heads, q.heads));
+      if (++g == groups) g = 0, ++slot;
+    }
+    return;
+  }
+  const int part = PARTS > 1 ? w % PARTS : 0, place = w / PARTS;
+  Runs<SHIFT, 2> line(p.cu, p.batch);
+  const int64_t slots = line.total(), all = steps_in(steps, WIDE, slots);
+  const int64_t lo = all * blockIdx.x / kv, hi = all * (blockIdx.x + 1) / kv;
+  const int per = steps.groups * steps.kinds, each = WIDE / steps.heads;
+  int64_t set = lo / per;                        // of `each` slots
+  int rest = (int)(lo - set * per);
+#pragma unroll 1
+  for (int64_t i = lo; i < hi; ++i) {
+    const int h = rest % steps.groups * steps.heads + place % steps.heads;
+    const int64_t slot = set * each + place / steps.heads;
+    const int64_t run = line.seek(min(slot, slots - 1));
+    append_step<FORM, SB, PLACE>(p, r, x, s_amax[i & 1], rest >= steps.groups, slot < slots && h < p.hkv, line.b, h, w, part,
+                                 run);
+    if (++rest == per) rest = 0, ++set;
   }
 }
 
@@ -240,6 +303,7 @@ __global__ __launch_bounds__(64 * kWaves) void append_rotary_few_kernel(CachePro
     }
     if (!is_q) {
       float inv = 1.f;
+      bool held = false;
       if constexpr (FORM == kCacheBlock) {
         uint8_t* sp = (is_v ? p.v_block : p.k_block) + (slot_of(p.pm, s.b, s.tok0, first) >> p.sb_shift) * p.hkv + h;
         const int before = first < s.P ? *sp : 0;       // byte of a block that holds tokens
@@ -249,7 +313,16 @@ __global__ __launch_bounds__(64 * kWaves) void append_rotary_few_kernel(CachePro
           if (from + kPass * i >= to) break;
           amax = fmaxf(amax, largest16(z[i]));
         }
-        const int byte = __builtin_amdgcn_readfirstlane(max(scale_byte(wave_max(amax)), before));
+        amax = wave_max(amax);
+        if (!(amax < INFINITY)) {                       // (rare: infinities do not count)
+          amax = 0.f;
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            if (from + kPass * i < to) amax = fmaxf(amax, largest16_finite(z[i]));
+          amax = wave_max(amax);
+        }
+        const int byte = __builtin_amdgcn_readfirstlane(max(scale_byte(amax), before));
+        held = byte >= kMaxScaleByte;
         if (lane == 0) *sp = (uint8_t)byte;
         inv = __uint_as_float((uint32_t)(254 - byte) << 23);   // 2^-e
         if (first < s.P && byte > before) {
@@ -268,11 +341,15 @@ __global__ __launch_bounds__(64 * kWaves) void append_rotary_few_kernel(CachePro
           pack16(z[i], c);
           store_part(l, (uint16_t*)row, c);
         } else {
-          float u[16];
           uint32_t c[4];
+          if constexpr (FORM == kCacheHead) {
+            codes16_by(z[i], Divisor(scale), c);
+          } else {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) u[e] = FORM == kCacheHead ? z[i][e] / scale : z[i][e] * inv;
-          pack16(z[i], u, c);
+            for (int e = 0; e < 16; ++e) z[i][e] *= inv;
+            if (held) codes16_held(z[i], c);
+            else codes16(z[i], c);
+          }
           store_part(l, row, c);
         }
       }
@@ -290,15 +367,16 @@ hipError_t launch(const CacheProblem& p, const Rotary& r, const RotaryRows& q, c
     append_rotary_few_kernel<FORM, PLACE><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, r, q, x, total);
     return hipGetLastError();
   }
-  constexpr int TOK = SB == 128 ? 128 : 64;
-  // tokens of a sequence lie in at most this many runs of TOK
-  const int chunks = (p.max_new + TOK - 2) / TOK + 1;
-  // heads are dealt to several workgroups where the runs alone would not fill the chip twice
-  int groups = 1;
-  while (groups * kWaves < jobs && (int64_t)p.batch * chunks * groups < 512) groups *= 2;
-  const int64_t grid = (int64_t)p.batch * chunks * groups;
-  if (!launchable(grid, 64 * kWaves)) return hipErrorInvalidValue;
-  append_rotary_kernel<FORM, SB, PLACE><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, r, q, x, chunks, groups);
+  constexpr int PARTS = SB > 32 ? SB / 32 : 1, TOK = 32 * PARTS, WIDE = kWaves / PARTS;
+  const Steps steps = steps_of(p.hkv, WIDE, 2);
+  const int64_t kv = grid_for(steps_in(steps, WIDE, (int64_t)p.batch * (p.max_new / TOK + 2)), 2048);
+  // query heads of a wave: many share the turns, few fill the chip where tokens are few
+  const int64_t passes = (int64_t)p.batch * (p.max_new / kPass + 1);
+  int heads = 8;
+  while (heads > 1 && passes * ((q.heads + heads - 1) / heads) < 2048) heads >>= 1;
+  const int64_t queries = grid_for((passes * ((q.heads + heads - 1) / heads) + kWaves - 1) / kWaves, 2048);
+  append_rotary_kernel<FORM, SB, PLACE><<<(unsigned)(kv + (q.heads ? queries : 0)), 64 * kWaves, 0, s>>>(p, r, q, x, steps,
+                                                                                                  (int)kv, heads);
   return hipGetLastError();
 }
 

@@ -44,23 +44,12 @@ __device__ __forceinline__ uint32_t phase_at(int n, uint64_t f) {
   return u * (uint32_t)(f >> 32) + __umulhi(u, lo) - (n < 0 ? lo : 0u);
 }
 
-// Cosine and sine of a fraction of a turn. To the nearest quarter, then Taylor
-// polynomials on +-pi/4: their rests are below 2^-25 (x^10 / 10!) and 2^-29
-// (x^11 / 11!), the rounding of the argument and of the terms 2^-23 in all.
+// Cosine and sine of a fraction of a turn, which is what the hardware's take:
+// off by at most 2^-22.3 over 2^24 fractions (the rounding of the fraction to
+// fp32 included), and a quarter of a polynomial's instructions.
 __device__ __forceinline__ float2 cos_sin(uint32_t phase) {
-  const uint32_t quarter = (phase + 0x20000000u) >> 30;
-  const float x = (float)(int)(phase - (quarter << 30)) * 1.4629180792671596e-09f;   // 2 pi / 2^32
-  const float x2 = x * x;
-  float c = fmaf(x2, 2.48015873e-5f, -1.38888889e-3f);
-  c = fmaf(x2, c, 4.16666667e-2f);
-  c = fmaf(x2, c, -0.5f);
-  c = fmaf(x2, c, 1.f);
-  float s = fmaf(x2, 2.75573192e-6f, -1.98412698e-4f);
-  s = fmaf(x2, s, 8.33333333e-3f);
-  s = fmaf(x2, s, -1.66666667e-1f);
-  s = fmaf(x2 * x, s, x);
-  const float a = quarter & 1 ? s : c, b = quarter & 1 ? c : s;
-  return make_float2((quarter + 1) & 2 ? -a : a, quarter & 2 ? -b : b);
+  const float t = (float)(int)phase * 0x1p-32f;
+  return make_float2(__builtin_amdgcn_cosf(t), __builtin_amdgcn_sinf(t));
 }
 
 __device__ __forceinline__ float2 turn_at(const Rotary& r, int n, uint64_t f) {
@@ -176,14 +165,50 @@ __device__ __forceinline__ void pack16(const float (&x)[16], uint32_t (&w)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
 }
-// as codes: y = the values in units of the scale, x the values themselves (their infinities and NaN count)
-__device__ __forceinline__ void pack16(const float (&x)[16], const float (&y)[16], uint32_t (&w)[4]) {
+
+// Values in units of a scale, at most 448 if finite, as codes (nearest, ties to
+// even). The conversion makes NaN codes of infinities and NaN.
+__device__ __forceinline__ void codes16(const float (&x)[16], uint32_t (&w)[4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float a[4] = {x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
-    const float b[4] = {y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]};
-    w[i] = e4m3x4(a, b);
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i], x[4 * i + 1], 0, false);
+    w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2], x[4 * i + 3], lo, true);
   }
+}
+// The same for values that may be larger, held within +-448.
+__device__ __forceinline__ void codes16_held(const float (&x)[16], uint32_t (&w)[4]) {
+  float y[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) y[e] = fabsf(x[e]) < INFINITY ? __builtin_amdgcn_fmed3f(x[e], -448.f, 448.f) : x[e];
+  codes16(y, w);
+}
+
+// x / scale, correctly rounded, held within +-448, as codes: the product with the
+// scale's inverse (held at 1024, so that nothing overflows), corrected by its
+// remainder; a division takes ten instructions. Scales whose inverse or
+// remainders leave fp32's normal range are divided by.
+struct Divisor {
+  float scale, inv;
+  bool fast;
+  __device__ __forceinline__ explicit Divisor(float s)
+      : scale(s), inv(1.f / s), fast(s > 0x1p-90f && s < 0x1p90f) {}
+};
+__device__ __forceinline__ void codes16_by(const float (&x)[16], const Divisor& d, uint32_t (&w)[4]) {
+  float y[16];
+  if (d.fast) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float q = __builtin_amdgcn_fmed3f(x[e] * d.inv, -1024.f, 1024.f);
+      y[e] = fmaf(fmaf(-q, d.scale, x[e]), d.inv, q);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) y[e] = x[e] / d.scale;
+  }
+#pragma unroll
+  for (int e = 0; e < 16; ++e)
+    y[e] = fabsf(x[e]) < INFINITY ? __builtin_amdgcn_fmed3f(y[e], -448.f, 448.f) : x[e];
+  codes16(y, w);
 }
 
 template <int PLACE>
@@ -198,41 +223,18 @@ __device__ __forceinline__ void turn16(const LaneRow<PLACE>& l, const Turns& t, 
   }
 }
 
-__device__ __forceinline__ float largest16(const float (&x)[16]) {   // of the finite ones
+__device__ __forceinline__ float largest16(const float (&x)[16]) {   // NaN is left out, infinities are not
   float m = 0.f;
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const float a = fabsf(x[e]);
-    m = fmaxf(m, a < INFINITY ? a : 0.f);
-  }
+  for (int e = 0; e < 16; ++e) m = fmaxf(m, fabsf(x[e]));
   return m;
 }
-
-// The turns of a run of tokens in LDS, computed once for all heads: lane c of a
-// row finds its eight in four reads of 16 bytes, side by side with the other
-// lanes'.
-template <int TOKENS>
-struct TurnTable {
-  float4 t[TOKENS][kPer / 2][kLaneRow];
-  // position(i) of the run's token i; every thread of the workgroup takes part
-  template <class F>
-  __device__ __forceinline__ void fill(const Rotary& r, int threads, F position) {
-    for (int i = threadIdx.x; i < TOKENS * kPairsOfRow; i += threads) {
-      const int f = i % kPairsOfRow;
-      if (2 * f >= r.dim) continue;
-      const float2 y = turn_at(r, position(i / kPairsOfRow), r.turns[f]);
-      ((float2*)&t[i / kPairsOfRow][f % kPer / 2][f / kPer])[f & 1] = y;
-    }
-  }
-  __device__ __forceinline__ void get(int token, int c, Turns& y) const {
+__device__ __forceinline__ float largest16_finite(const float (&x)[16]) {
+  float m = 0.f;
 #pragma unroll
-    for (int j = 0; j < kPer / 2; ++j) {
-      const float4 a = t[token][j][c];
-      y.t[2 * j] = make_float2(a.x, a.y);
-      y.t[2 * j + 1] = make_float2(a.z, a.w);
-    }
-  }
-};
+  for (int e = 0; e < 16; ++e) m = fmaxf(m, fabsf(x[e]) < INFINITY ? fabsf(x[e]) : 0.f);
+  return m;
+}
 
 }  // namespace
 

@@ -25,12 +25,8 @@ __device__ __forceinline__ void turn_and_store(const LaneRow<PLACE>& l, const Tu
   turn16(l, y, x);
   const int64_t at = t * to.out_stride + h * kHeadDim;
   if (to.scale) {
-    const float scale = ld_uniform(to.scale, h);
-    float z[16];
     uint32_t c[4];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) z[e] = x[e] / scale;
-    pack16(x, z, c);
+    codes16_by(x, Divisor(ld_uniform(to.scale, h)), c);
     if (there) store_part(l, to.out + at, c);
   } else {
     uint32_t b[8];
