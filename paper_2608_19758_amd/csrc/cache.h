@@ -116,7 +116,8 @@ inline bool launchable(int64_t groups, int threads) { return groups * threads < 
 struct CachePartials {
   float* o;                 // [slots, rows, d]
   float* ml;                // [slots, rows, 2] {running maximum (base 2), denominator}
-  int32_t* at;              // few rows, equal shares: [batch, 2] {first share, parts} of a sequence
+  int32_t* at;              // few rows, equal shares: [batch, 2] {first share, parts} of a sequence;
+                            // cross attention of many rows: what each workgroup leaves to join
 };
 
 // At most this many packed rows (new tokens times heads of a group) a sequence

@@ -176,7 +176,8 @@ size_t attend_bytes(const CacheProblem& r, size_t* ml, size_t* at, bool cross = 
   }
   *ml = (size_t)slots * rows * fp2::kHeadDim * sizeof(float);   // a multiple of 256
   *at = *ml + align256((size_t)slots * rows * 2 * sizeof(float));
-  return *at + (few && slots && !r.splits ? align256((size_t)r.batch * 2 * sizeof(int32_t)) : 0);
+  if (!slots || r.splits) return *at;
+  return *at + (few ? align256((size_t)r.batch * 2 * sizeof(int32_t)) : cross ? (size_t)fp2::kCrossCuts * 16 : 0);
 }
 
 size_t weights_bytes(const CacheProblem& r) {

@@ -55,6 +55,7 @@ struct Moves {
 // to.table null: in place, keys only. r.turns null: rows as they are.
 hipError_t launch_cache_move(const CacheProblem& p, const Rotary& r, bool interleaved, const Moves& moves, const PageMap& to,
                              hipStream_t s);
+constexpr int kCrossCuts = 256;      // units that a cross attention cuts, at most (16 bytes each behind its partial outputs)
 hipError_t launch_cache_cross(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse, hipStream_t s);
 void cache_cross_partials(const CacheProblem& p, int64_t* slots, int* rows);
 
