@@ -37,6 +37,12 @@ and KV head in new pages. One kernel serves a forward, by its longest extend: si
 tokens beside a long chunk are faster in a forward of their own. A cache of codes with
 a scale per head is what ``PrefillBackend`` reads, so a prompt may be extended sparsely
 and decoded here.
+
+With ``rotary`` (``make_rotary``) a forward takes queries and keys as the projection gives
+them and turns them on the way in; an eviction with it turns the keys that stay to their
+new indexes. ``read`` gives cached tokens back as bf16 rows, ``move`` takes them to other
+pages or positions, and ``forward_cross`` attends to the states of an encoder (written with
+``append``), or to a prefix that requests share, whatever their length.
 """
 from __future__ import annotations
 
@@ -269,6 +275,24 @@ class CacheConfig:
         return self.params(self.max_batch, self.max_extend_len, self.max_kv_len)
 
 
+def plan_cross(cfg: CacheConfig, query_lens: Sequence[int], state_lens: Sequence[int]) -> ForwardPlan:
+    """Validate one cross attention against the config and build its parameters."""
+    new, kv = [int(x) for x in query_lens], [int(x) for x in state_lens]
+    if len(new) != len(kv):
+        raise ValueError("query_lens and state_lens differ in length")
+    if len(new) > cfg.max_batch:
+        raise ValueError("batch %d > max_batch %d" % (len(new), cfg.max_batch))
+    for b, (n, t) in enumerate(zip(new, kv)):
+        if not 0 <= n <= cfg.max_extend_len:
+            raise ValueError("sequence %d: %d queries outside [0, max_extend_len = %d]" % (b, n, cfg.max_extend_len))
+        if not 0 <= t <= cfg.max_kv_len:
+            raise ValueError("sequence %d: %d states outside [0, max_kv_len = %d]" % (b, t, cfg.max_kv_len))
+    params = dataclasses.replace(cfg, sink_tokens=0, window_tokens=0).params(len(new), max(new, default=0),
+                                                                             max(kv, default=0))
+    cu = [np.concatenate([[0], np.cumsum(x)]).astype(np.int32) for x in (new, kv)]
+    return ForwardPlan(params=params, cu_q=cu[0], cu_k=cu[1], total_tokens=int(cu[0][-1]))
+
+
 @dataclasses.dataclass
 class CacheMetadata:
     plan: ForwardPlan
@@ -276,6 +300,7 @@ class CacheMetadata:
     block_table: object            # device int32 [batch or more, max_pages_per_seq], dense
     replayed: bool = False         # lengths and table are the metadata's own, and may be updated
     rows: Optional[int] = None     # of the tensors of the forwards captured with it, the fewest
+    cross: bool = False            # of a cross attention
 
     @property
     def params(self):
@@ -329,24 +354,35 @@ class CacheBackend:
         """Once per forward, for all layers. replayed: the forward is captured in a graph
         and replayed after update_forward_metadata; its bounds are then the longest of
         these extends and the config's max_kv_len instead of these lengths'."""
+        return self._metadata(plan_forward(self.cfg, extend_lens, prefix_lens), block_table, replayed, False)
+
+    def init_cross_metadata(self, query_lens: Sequence[int], state_lens: Sequence[int], block_table,
+                            replayed: bool = False) -> CacheMetadata:
+        """The same for cross attention: queries, and cached states, of each sequence."""
+        return self._metadata(plan_cross(self.cfg, query_lens, state_lens), block_table, replayed, True)
+
+    def _metadata(self, plan, block_table, replayed, cross):
         import torch
-        plan = plan_forward(self.cfg, extend_lens, prefix_lens)
         if replayed:
-            plan.params = self.cfg.params(plan.params.batch, plan.params.max_seq_len, self.cfg.max_kv_len)
+            kv, new = self.cfg.max_kv_len, plan.params.max_seq_len
+            plan.params = self.cfg.params(plan.params.batch, new, kv)
+            if cross:
+                plan.params.sink_tokens = plan.params.window_tokens = 0
         with fp2.cache.on_stream(self.stream):
             lengths = torch.from_numpy(np.concatenate([plan.cu_q, plan.cu_k])).to(self.device)
             table = _dense_table(block_table, len(plan.cu_q) - 1, self.cfg.max_pages_per_seq)
             if replayed:
                 table = table.clone()
-        return CacheMetadata(plan=plan, lengths=lengths, block_table=table, replayed=replayed)
+        return CacheMetadata(plan=plan, lengths=lengths, block_table=table, replayed=replayed, cross=cross)
 
     def update_forward_metadata(self, meta: CacheMetadata, extend_lens: Sequence[int],
                                 prefix_lens: Optional[Sequence[int]], block_table) -> None:
         """Other lengths and pages for a captured forward (metadata made with
         replayed=True): as many sequences, extends within the first one's bound, and no more new
-        tokens in all than the captured tensors have rows."""
+        tokens in all than the captured tensors have rows. For a cross attention: its queries and
+        states."""
         import torch
-        plan = plan_forward(self.cfg, extend_lens, prefix_lens)
+        plan = (plan_cross if meta.cross else plan_forward)(self.cfg, extend_lens, prefix_lens)
         p = meta.params
         if not meta.replayed:
             raise ValueError("the metadata was not made with replayed=True")
@@ -363,13 +399,11 @@ class CacheBackend:
             meta.block_table[:p.batch].copy_(table[:p.batch])
         meta.plan = plan
 
-    def forward(self, q, k_new, v_new, cache: "fp2.KVCache", meta: CacheMetadata, *, out=None, lse=None,
-                want_lse=False, weights=None):
-        """One layer: k_new and v_new bf16 [new tokens, Hkv, 128] go into the cache, q
-        [new tokens, Hq, 128] attends over it. weights (as from alloc_weights): what the
-        cached tokens received of these queries is added to it, row b for sequence b.
-        Returns (out, lse or None)."""
-        for name, t in (("q", q), ("k_new", k_new), ("v_new", v_new)):
+    def _check_rows(self, meta: CacheMetadata, *named) -> None:
+        """Tensors (name, tensor or None) against the forward's tokens; those of a captured forward bound
+        the later ones."""
+        given = [(n, t) for n, t in named if t is not None]
+        for name, t in given:
             if t.shape[0] < meta.plan.total_tokens:
                 raise ValueError("%s has %d rows, the forward has %d new tokens"
                                  % (name, t.shape[0], meta.plan.total_tokens))
@@ -378,11 +412,31 @@ class CacheBackend:
             with fp2.cache.on_stream(self.stream):
                 captured = torch.cuda.is_current_stream_capturing()
             if captured:     # later lengths are held to these tensors
-                rows = [t.shape[0] for t in (q, k_new, v_new)] + [meta.rows] * (meta.rows is not None)
+                rows = [t.shape[0] for _, t in given] + [meta.rows] * (meta.rows is not None)
                 meta.rows = min(rows)
-        p, lens = meta.params, (meta.cu_q, meta.cu_k, meta.block_table)
-        host = dict(cu_seqlens_host=meta.plan.cu_q, cu_seqlens_k_host=meta.plan.cu_k, stream=self.stream)
-        fp2.cache_append(p, k_new, v_new, cache, *lens, **host)
+
+    def _lengths(self, meta: CacheMetadata, cross: bool = False):
+        if meta.cross != cross:
+            raise ValueError("metadata of a %s" % ("cross attention" if meta.cross else "forward"))
+        return ((meta.cu_q, meta.cu_k, meta.block_table),
+                dict(cu_seqlens_host=meta.plan.cu_q, cu_seqlens_k_host=meta.plan.cu_k, stream=self.stream))
+
+    def forward(self, q, k_new, v_new, cache: "fp2.KVCache", meta: CacheMetadata, *, out=None, lse=None,
+                want_lse=False, weights=None, rotary: Optional["fp2.Rotary"] = None, positions=None):
+        """One layer: k_new and v_new bf16 [new tokens, Hkv, 128] go into the cache, q
+        [new tokens, Hq, 128] attends over it. With rotary both come as the projection gives them (parts of
+        one matrix will do) and are turned by positions (device int32 [new tokens]; None: a token's index in
+        its sequence). weights (as from alloc_weights): what the cached tokens received of these queries is
+        added to it, row b for sequence b. Returns (out, lse or None)."""
+        lens, host = self._lengths(meta)
+        if rotary is None and positions is not None:
+            raise ValueError("positions without rotary")
+        self._check_rows(meta, ("q", q), ("k_new", k_new), ("v_new", v_new), ("positions", positions))
+        p = meta.params
+        if rotary is None:
+            fp2.cache_append(p, k_new, v_new, cache, *lens, **host)
+        else:
+            q = fp2.cache_append_rotary(p, rotary, q, k_new, v_new, cache, *lens, positions=positions, **host)
         out, lse = fp2.cache_attend(p, q, cache, *lens, out=out, lse=lse,
                                     want_lse=want_lse or weights is not None,
                                     workspace=self.workspace, **host)
@@ -391,15 +445,56 @@ class CacheBackend:
                               workspace=self.workspace, **host)
         return out, lse
 
+    def append(self, k_new, v_new, cache: "fp2.KVCache", meta: CacheMetadata) -> None:
+        """One layer: keys and values into the cache without queries (an encoder's states)."""
+        lens, host = self._lengths(meta)
+        self._check_rows(meta, ("k_new", k_new), ("v_new", v_new))
+        fp2.cache_append(meta.params, k_new, v_new, cache, *lens, **host)
+
+    def forward_cross(self, q, cache: "fp2.KVCache", meta: CacheMetadata, *, out=None, lse=None, want_lse=False):
+        """One layer of cross attention (metadata of init_cross_metadata): every query of q [queries, Hq, 128]
+        over all states of its sequence; zeros where there are none. Returns (out, lse or None)."""
+        lens, host = self._lengths(meta, cross=True)
+        self._check_rows(meta, ("q", q))
+        return fp2.cache_cross(meta.params, q, cache, *lens, out=out, lse=lse, want_lse=want_lse,
+                               workspace=self.workspace, **host)
+
+    def read(self, cache: "fp2.KVCache", meta: CacheMetadata, *, rotary: Optional["fp2.Rotary"] = None, positions=None):
+        """The forward's new tokens out of one layer's cache, (keys, values) bf16 [new tokens, Hkv, 128]; with
+        rotary the keys' turn is taken back. A whole sequence is one without prefix_lens."""
+        lens, host = self._lengths(meta)
+        if meta.replayed:     # the rows of a captured read are those of now
+            self._check_rows(meta, ("rows", np.empty((meta.plan.total_tokens, 0))))
+        return fp2.cache_read(meta.params, cache, *lens, rotary=rotary, positions=positions, **host)
+
+    def move(self, cache: "fp2.KVCache", meta: CacheMetadata, target_table=None, *,
+             rotary: Optional["fp2.Rotary"] = None, moves=None) -> None:
+        """One layer: the sequences' tokens to the pages of target_table (int32 [batch, pages]; None: in place),
+        their keys turned by moves (fp2.cache_move) where rotary is given."""
+        lens, host = self._lengths(meta)
+        fp2.cache_move(meta.params, cache, *lens[1:], target_table, rotary=rotary, moves=moves,
+                       cu_seqlens_k_host=host["cu_seqlens_k_host"], stream=self.stream)
+
     def evict(self, cache: "fp2.KVCache", weights, meta: CacheMetadata, target_table, *, budget: int,
-              recent_tokens: int = 0):
+              recent_tokens: int = 0, rotary: Optional["fp2.Rotary"] = None):
         """One layer, after a forward: the sequences of `meta` are cut to `budget` tokens per
-        KV head, in the pages of target_table (int32 [batch, pages]). Returns (the tokens
-        that stay, int32 [batch, Hkv, budget], their weights); the sequences' new lengths
-        are evicted_lens(meta, budget)."""
-        kept, _, w = fp2.cache_evict(meta.params, cache, weights, meta.cu_k, meta.block_table, target_table,
-                                     budget=budget, recent_tokens=recent_tokens,
-                                     cu_seqlens_k_host=meta.plan.cu_k, stream=self.stream)
+        KV head, in the pages of target_table (int32 [batch, pages]). With rotary the keys that stay, which
+        were turned by their indexes, are turned to their new ones (else later forwards need positions that
+        go on from the old ones). Returns (the tokens that stay, int32 [batch, Hkv, budget], their weights);
+        the sequences' new lengths are evicted_lens(meta, budget)."""
+        _, host = self._lengths(meta)
+        p = meta.params
+        kept, cu_k, w = fp2.cache_evict(p, cache, weights, meta.cu_k, meta.block_table, target_table,
+                                        budget=budget, recent_tokens=recent_tokens,
+                                        cu_seqlens_k_host=host["cu_seqlens_k_host"], stream=self.stream)
+        if rotary is not None and p.batch > 0 and p.max_kv_len > 0:
+            import torch
+            stay = min(budget, p.max_kv_len)
+            short = self.cfg.params(p.batch, 0, stay)
+            short.max_pages_per_seq = target_table.shape[1]
+            with fp2.cache.on_stream(self.stream):
+                moves = torch.arange(budget, dtype=torch.int32, device=kept.device) - kept
+            fp2.cache_move(short, cache, cu_k, target_table, rotary=rotary, moves=moves, stream=self.stream)
         return kept, w
 
 

@@ -327,3 +327,20 @@ def test_reference_cross():
     a, b = pos_ref.cross(c, q, [1, 1]), ref.attend(c, q, [1, 1])
     np.testing.assert_allclose(a[0], b[0], rtol=1e-12)
     np.testing.assert_allclose(a[2], b[2], rtol=1e-12)
+
+
+def test_plan_cross():
+    """Queries and states are bounded apart from each other; windows of the config do not count."""
+    from paper_2608_19758_amd import serving
+    cfg = serving.CacheConfig(num_q_heads=8, num_kv_heads=2, page_size=16, max_batch=3, max_extend_len=50, max_kv_len=100,
+                              window_tokens=10, sink_tokens=2)
+    plan = serving.plan_cross(cfg, [50, 0, 7], [0, 100, 3])
+    p = plan.params
+    assert (p.batch, p.max_seq_len, p.max_kv_len, p.window_tokens, p.sink_tokens) == (3, 50, 100, 0, 0)
+    assert plan.cu_q.tolist() == [0, 50, 50, 57] and plan.cu_k.tolist() == [0, 0, 100, 103] and plan.total_tokens == 57
+    assert plan.cu_q.dtype == plan.cu_k.dtype == np.int32
+    for new, kv in (([51], [1]), ([1], [101]), ([-1], [1]), ([1], [-1]), ([1, 1], [1]), ([1] * 4, [1] * 4)):
+        with pytest.raises(ValueError):
+            serving.plan_cross(cfg, new, kv)
+    empty = serving.plan_cross(cfg, [], [])
+    assert empty.params.batch == 0 and empty.total_tokens == 0
