@@ -124,15 +124,12 @@ class _Args:
                                  % (name, n, least, multiple))
         dev = t.get_device()
         if dev != self.dev or dev < 0:
-            if self.dev is None:
-                self.dev = dev
-            if (dev != self.dev or dev < 0) and self.odd is None:
-                self.odd = (name, t.device)
+            self.place(name, t, dev)
         return t.data_ptr()
 
     def rows(self, name, t, heads, dtypes=_ONE_BF16):
-        """Address and stride (elements between tokens) of rows [tokens, heads, 128] whose heads lie
-        side by side; tokens may lie further apart (a part of a wider matrix)."""
+        """Address, stride (elements between tokens), tokens and heads of rows [tokens, heads, 128] whose heads
+        lie side by side; tokens may lie further apart (a part of a wider matrix)."""
         if not isinstance(t, torch.Tensor):
             raise ValueError("%s must be a torch tensor" % name)
         if t.dtype not in dtypes:
@@ -141,15 +138,17 @@ class _Args:
         if len(shape) != 3 or shape[2] != HEAD_DIM or (heads is not None and shape[1] != heads):
             raise ValueError("%s must be [tokens, %s, %d], got %s"
                              % (name, "heads" if heads is None else heads, HEAD_DIM, tuple(shape)))
+        tokens, wide, _ = shape
         stride, head, one = t.stride()
-        if one != 1 or (head != HEAD_DIM and shape[1] > 1):
+        if one != 1 or (head != HEAD_DIM and wide > 1):
             raise ValueError("%s must have its heads side by side" % name)
-        self.place(name, t)
-        return t.data_ptr(), stride if shape[0] > 1 else shape[1] * HEAD_DIM
-
-    def place(self, name, t):
-        """Notes a tensor on another device than the first one's."""
         dev = t.get_device()
+        if dev != self.dev or dev < 0:
+            self.place(name, t, dev)
+        return t.data_ptr(), stride if tokens > 1 else wide * HEAD_DIM, tokens, wide
+
+    def place(self, name, t, dev):
+        """Notes a tensor that is on no CUDA device, or on another one than the first."""
         if self.dev is None:
             self.dev = dev
         if (dev != self.dev or dev < 0) and self.odd is None:

@@ -35,14 +35,22 @@ class _RotaryRows(ctypes.Structure):
                 ("out_scale", ctypes.c_void_p)]
 
 
-@dataclasses.dataclass
+@dataclasses.dataclass(frozen=True)
 class Rotary:
-    """fp2_rotary_t: turns int64 [dim / 2] (the bits of f / (2 pi) * 2^64), pairs (2i, 2i + 1) if
-    interleaved, else (i, i + dim / 2); scale multiplies both parts."""
+    """fp2_rotary_t: turns int64 [dim / 2] on the device (the bits of f / (2 pi) * 2^64), pairs (2i, 2i + 1)
+    if interleaved, else (i, i + dim / 2); scale multiplies both parts. Its tensor is checked here, once."""
     turns: torch.Tensor
     dim: int
     interleaved: bool = False
     scale: float = 1.0
+
+    def __post_init__(self):
+        if not isinstance(self.dim, int) or not 2 <= self.dim <= HEAD_DIM or self.dim % 2:
+            raise ValueError("dim must be even and in [2, %d], got %r" % (HEAD_DIM, self.dim))
+        a = _Args()
+        at = a("turns", self.turns, _ONE_I64, self.dim // 2)
+        object.__setattr__(self, "_args", _RotaryArgs(at, self.dim, bool(self.interleaved), self.scale))
+        object.__setattr__(self, "_dev", self.turns.get_device())
 
 
 def rotary_frequencies(dim: int, base: float = 10000.0, *, scaling: str = "none", factor: float = 1.0,
@@ -117,25 +125,34 @@ def make_rotary(dim: int = HEAD_DIM, *, base: float = 10000.0, interleaved: bool
     return Rotary(torch.from_numpy(signed).to(device), dim, bool(interleaved), amplitude)
 
 
-def _rotary_args(a: _Args, r: Rotary) -> _RotaryArgs:
+def _rotary_args(a: _Args, r: Rotary):
+    """fp2_rotary_t of r, by reference."""
     if not isinstance(r, Rotary):
         raise ValueError("rotary must be a Rotary (make_rotary)")
-    return _RotaryArgs(a("rotary.turns", r.turns, _ONE_I64, r.dim // 2), r.dim, bool(r.interleaved), r.scale)
+    if r._dev != a.dev or r._dev < 0:
+        a.place("rotary.turns", r.turns, r._dev)
+    return ctypes.byref(r._args)
 
 
-def _turned_rows(a: _Args, name, x, heads, out, scale) -> _RotaryRows:
-    at, stride = a.rows(name, x, heads)
-    to, to_stride = a.rows(name + "'s output", out, x.shape[1], _ONE_BF16 if scale is None else _CODES)
-    if out.shape[0] < x.shape[0]:
-        raise ValueError("%s has %d tokens, its output %d" % (name, x.shape[0], out.shape[0]))
-    if x.shape[0] <= 1:     # strides of a single row do not count: its output's may be any, in place the same
-        to_stride = stride
-    s = None if scale is None else a(name + "_scale", scale, _F32, x.shape[1])
-    return _RotaryRows(at, stride, to, to_stride, x.shape[1], BF16 if scale is None else FP8_E4M3, s)
+_CODE_BYTES = torch.uint8
 
 
-def _output_like(x, scale):
-    return torch.empty(x.shape, dtype=torch.bfloat16 if scale is None else torch.uint8, device=x.device)
+def _turned_rows(a: _Args, name, x, heads, out, scale, stream):
+    """fp2_rotary_rows_t of x, its output (made on `stream` where none is given) and its tokens."""
+    at, stride, tokens, wide = a.rows(name, x, heads)
+    if out is None:
+        with on_stream(stream):
+            out = x.new_empty(x.shape) if scale is None else x.new_empty(x.shape, dtype=_CODE_BYTES)
+        to, to_stride = out.data_ptr(), wide * HEAD_DIM
+    else:
+        to, to_stride, there, _ = a.rows(name + "'s output", out, wide, _ONE_BF16 if scale is None else _CODES)
+        if there < tokens:
+            raise ValueError("%s has %d tokens, its output %d" % (name, tokens, there))
+        if tokens <= 1:     # strides of a single row do not count: its output's may be any, in place the same
+            to_stride = stride
+    if scale is None:
+        return _RotaryRows(at, stride, to, to_stride, wide, BF16, None), out, tokens
+    return _RotaryRows(at, stride, to, to_stride, wide, FP8_E4M3, a(name + "_scale", scale, _F32, wide)), out, tokens
 
 
 def rotary(r: Rotary, q, positions, k=None, *, out=None, k_out=None, q_scale=None, inverse: bool = False, stream=None):
@@ -143,22 +160,15 @@ def rotary(r: Rotary, q, positions, k=None, *, out=None, k_out=None, q_scale=Non
     wider matrix; out and k_out may be q and k themselves. With q_scale (fp32 [heads]) the queries come as e4m3
     codes of q / q_scale. inverse takes a turn back. Returns out, or (out, k_out) if k is given."""
     a = _Args()
-    if not isinstance(q, torch.Tensor) or not (k is None or isinstance(k, torch.Tensor)):
-        raise ValueError("q and k must be torch tensors")
-    with on_stream(stream):
-        if out is None:
-            out = _output_like(q, q_scale)
-        if k is not None and k_out is None:
-            k_out = _output_like(k, None)
-    rows = _turned_rows(a, "q", q, None, out, q_scale)
-    krows = None if k is None else _turned_rows(a, "k", k, None, k_out, None)
-    tokens = q.shape[0]
-    if k is not None and k.shape[0] != tokens:
-        raise ValueError("q has %d tokens, k %d" % (tokens, k.shape[0]))
+    rows, out, tokens = _turned_rows(a, "q", q, None, out, q_scale, stream)
+    krows = None
+    if k is not None:
+        krows, k_out, there = _turned_rows(a, "k", k, None, k_out, None, stream)
+        if there != tokens:
+            raise ValueError("q has %d tokens, k %d" % (tokens, there))
+        krows = ctypes.byref(krows)
     pos = a("positions", positions, _ONE_I32, tokens)
-    args = _rotary_args(a, r)
-    a.call("fp2_rotary", stream, ctypes.byref(args), tokens, pos, int(bool(inverse)), ctypes.byref(rows),
-           None if krows is None else ctypes.byref(krows))
+    a.call("fp2_rotary", stream, _rotary_args(a, r), tokens, pos, 1 if inverse else 0, ctypes.byref(rows), krows)
     return out if k is None else (out, k_out)
 
 
@@ -170,23 +180,22 @@ def cache_append_rotary(p: CacheParams, r: Rotary, q, k_new, v_new, cache: KVCac
     num_q_heads, 128] (None: no queries) turned as rotary does it. Returns the queries."""
     a, batch = _Args(), p.batch
     c = a.cache(p, cache)
-    (k, ks), (v, vs) = a.rows("k_new", k_new, p.num_kv_heads), a.rows("v_new", v_new, p.num_kv_heads)
-    tokens = k_new.shape[0]
-    if v_new.shape[0] != tokens or (isinstance(q, torch.Tensor) and q.shape[:1] != (tokens,)):
-        raise ValueError("q, k_new and v_new differ in their tokens")
+    k, ks, tokens, _ = a.rows("k_new", k_new, p.num_kv_heads)
+    v, vs, there, _ = a.rows("v_new", v_new, p.num_kv_heads)
     rows = None
     if q is not None:
-        with on_stream(stream):
-            if out is None and isinstance(q, torch.Tensor):
-                out = _output_like(q, q_scale)
-        rows = _turned_rows(a, "q", q, p.num_q_heads, out, q_scale)
+        rows, out, asked = _turned_rows(a, "q", q, p.num_q_heads, out, q_scale, stream)
+        rows = ctypes.byref(rows)
+        there = there if asked == tokens else asked
+    if there != tokens:
+        raise ValueError("q, k_new and v_new differ in their tokens")
     lens = a.lengths(batch, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host, tokens)
     pos = a("positions", positions, _ONE_I32, tokens, optional=True)
     table = a.table(batch, "block_table", block_table, p.max_pages_per_seq)
     args = _rotary_args(a, r)
     if tokens:
-        a.call("fp2_cache_append_rotary", stream, ctypes.byref(p), ctypes.byref(args),
-               None if rows is None else ctypes.byref(rows), k, ks, v, vs, pos, *lens, ctypes.byref(c), table)
+        a.call("fp2_cache_append_rotary", stream, ctypes.byref(p), args, rows, k, ks, v, vs, pos, *lens, ctypes.byref(c),
+               table)
     return None if q is None else out
 
 
@@ -213,19 +222,23 @@ def cache_read(p: CacheParams, cache: KVCache, cu_seqlens, cu_seqlens_k, block_t
     pos = a("positions", positions, _ONE_I32, rows, optional=True)
     table = a.table(batch, "block_table", block_table, p.max_pages_per_seq)
     args = None if rotary is None else _rotary_args(a, rotary)
-    shape = (rows, p.num_kv_heads, HEAD_DIM)
-    with on_stream(stream):
-        if keys and k_out is None:
-            k_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.k.device)
-        if values and v_out is None:
-            v_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.k.device)
-    k_out, v_out = k_out if keys else None, v_out if values else None
-    size = rows * p.num_kv_heads * HEAD_DIM
-    ko, vo = a("k_out", k_out, _ONE_BF16, size, optional=True), a("v_out", v_out, _ONE_BF16, size, optional=True)
+    size, ko, vo = rows * p.num_kv_heads * HEAD_DIM, None, None
+    if keys and k_out is not None:
+        ko = a("k_out", k_out, _ONE_BF16, size)
+    if values and v_out is not None:
+        vo = a("v_out", v_out, _ONE_BF16, size)
+    if (keys and k_out is None) or (values and v_out is None):
+        shape = (rows, p.num_kv_heads, HEAD_DIM)
+        with on_stream(stream):
+            if keys and k_out is None:
+                k_out = cache.k.new_empty(shape, dtype=torch.bfloat16)
+                ko = k_out.data_ptr()
+            if values and v_out is None:
+                v_out = cache.k.new_empty(shape, dtype=torch.bfloat16)
+                vo = v_out.data_ptr()
     if rows:
-        a.call("fp2_cache_read", stream, ctypes.byref(p), None if args is None else ctypes.byref(args), pos, *lens,
-               ctypes.byref(c), table, ko, vo)
-    return k_out, v_out
+        a.call("fp2_cache_read", stream, ctypes.byref(p), args, pos, *lens, ctypes.byref(c), table, ko, vo)
+    return k_out if keys else None, v_out if values else None
 
 
 def cache_move(p: CacheParams, cache: KVCache, cu_seqlens_k, block_table, target_table=None, *, rotary: Rotary = None,
@@ -253,8 +266,8 @@ def cache_move(p: CacheParams, cache: KVCache, cu_seqlens_k, block_table, target
         if m.dim() != 3 or any(n != 1 and n < w for n, w in zip(m.shape, want)) or m.shape[1] not in (1, want[1]):
             raise ValueError("moves must be int32 [batch] or [%d or 1, %d or 1, %d or 1], got %s"
                              % (*want, tuple(moves.shape)))
-        a.place("moves", m)
+        a.place("moves", m, m.get_device())
         by = m.data_ptr()
         strides = tuple(s if n != 1 else 0 for n, s in zip(m.shape, m.stride()))
-    a.call("fp2_cache_move", stream, ctypes.byref(p), None if args is None else ctypes.byref(args), by, *strides, cuk,
+    a.call("fp2_cache_move", stream, ctypes.byref(p), args, by, *strides, cuk,
            cuk_host, ctypes.byref(c), table, target, pages)

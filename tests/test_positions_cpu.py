@@ -197,9 +197,12 @@ def test_binding_refuses():
                dict(out=q, q_scale=torch.ones(2), positions=at), dict(k=q, k_out=q.float(), positions=at)):
         with pytest.raises(ValueError):
             fp2.rotary(r, q, **kw)
-    for bad in (None, dict(turns=1), fp2.Rotary(r.turns[:63], 128), fp2.Rotary(r.turns.int(), 128)):
+    for bad in (None, dict(turns=1), r.turns):
         with pytest.raises(ValueError):
             fp2.rotary(bad, q, at)
+    for bad in ((r.turns[:63], 128), (r.turns.int(), 128), (r.turns, 127), (r.turns, 130), (torch.zeros(8, dtype=torch.int64)[::2], 8), (None, 128), (r.turns, 2.0)):
+        with pytest.raises(ValueError):
+            fp2.Rotary(*bad)
     with pytest.raises(ValueError, match="CUDA tensor"):      # all else is right
         fp2.rotary(r, q, at)
 
