@@ -39,7 +39,8 @@ constexpr int kRows = 32 * kWaves;
 constexpr int kMaxParts = 32;
 constexpr int kShares = kCrossCuts;  // workgroups that run at a time, one a compute unit
 constexpr int kXcds = 8;         // dies, each with a cache of its own, that workgroups go to in turn
-constexpr int kMinTiles = 4;     // tiles of a part, about the fewest
+constexpr int kMinTiles = 4;     // units of at most as many tiles are not cut
+constexpr int kMinShare = 4;     // length of a share, at least (one unit of 16 tiles: 21 us, with 8 30)
 constexpr int kUnit = 4;         // tiles that a unit's start and end take as long as
 constexpr int kAhead = 5;       // products that operands are read ahead
 constexpr float kTau = 8.0f;
@@ -108,7 +109,7 @@ __device__ __forceinline__ bool find_share(const CacheProblem& p, int cuts, Shar
     units += lane_value(wave_sum_to(u), 63);
   }
   // short units are left whole while there are workgroups for them
-  const int64_t most = min(max(units, total / (kMinTiles + kUnit)), (int64_t)gridDim.x);
+  const int64_t most = min(max(units, total / kMinShare), (int64_t)gridDim.x);
   s.len = max((total + most - 1) / max(most, (int64_t)1), (int64_t)1);
   // neighbours in the line share keys, so they go to one die
   const int shares = (int)((total + s.len - 1) / s.len), each = (shares + kXcds - 1) / kXcds;
@@ -536,7 +537,7 @@ int tiles_of(const CacheProblem& p) { return std::max((p.max_kv + kStep - 1) / k
 // have a share the lengths say.
 int shares_of(const CacheProblem& p) {
   const int64_t units = (int64_t)p.batch * p.hkv * units_of(p), line = units * (tiles_of(p) + kUnit);
-  const int64_t most = std::min<int64_t>(kShares, std::max(units, line / (kMinTiles + kUnit)));
+  const int64_t most = std::min<int64_t>(kShares, std::max(units, line / kMinShare));
   return (int)((most + kXcds - 1) / kXcds * kXcds);
 }
 

@@ -45,7 +45,7 @@ __device__ __forceinline__ void read_heads(const CacheProblem& p, const Rotary& 
   const int lane = threadIdx.x & 63, r0 = lane / kLaneRow;
   const LaneRow<PLACE> l(lane, r.dim);
   int64_t slot[N];
-  Turns y[N];
+  Turns<PLACE> y[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int t = min(max(first + kPass * i + r0, P), L - 1);
@@ -78,13 +78,13 @@ __device__ __forceinline__ void read_heads(const CacheProblem& p, const Rotary& 
 #pragma unroll
           for (int e = 0; e < 8; ++e) c[e] = raw[j][i][e];
         } else {
-          float x[16];
-          unpack16(raw[j][i], x);
+          float x[16];                           // codes are turned in units of their scale
+          if constexpr (TURN) turned16(l, y[i], raw[j][i], x);
+          else unpack16(raw[j][i], x);
           if constexpr (FORM != kCacheBf16) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) x[e] *= by;
           }
-          if constexpr (TURN) turn16(l, y[i], x);
           pack16(x, c);
         }
         if (t >= P && t < L) store_part(l, out + (((int64_t)q0 + t - P) * p.hkv + h + j) * kHeadDim, c);
@@ -186,14 +186,13 @@ __device__ __forceinline__ void move_step(const CacheProblem& p, const Rotary& r
           old[k] = __builtin_amdgcn_readfirstlane(
               (int)p.k_block[(__shfl(from_l, SB * k & 31, 64) >> p.sb_shift) * p.hkv + h]);
       }
-      const Freqs freqs = l.freqs(r);
-      Turns y;
+      const Freqs<PLACE> freqs = l.freqs(r);
+      Turns<PLACE> y;
       if constexpr (TURN == 1) l.turns(r, freqs, m.by[mh], y);
 #pragma unroll
       for (int i = 0; i < N; ++i) {              // codes are turned in units of their scale
-        if constexpr (TURN == 2) l.turns(r, freqs, by[i], y);
-        unpack16(raw[i], x[i]);
-        turn16(l, y, x[i]);
+        if constexpr (TURN == 2) turned16_at(l, r, freqs, by[i], raw[i], x[i]);
+        else turned16(l, y, raw[i], x[i]);
       }
     }
     auto store = [&](int i, const uint32_t (&c)[4 * ESZ]) {

@@ -73,7 +73,7 @@ __device__ __forceinline__ void turn_queries(const CacheProblem& p, const Rotary
   const bool there = i0 + lane / kLaneRow < s.n;
   const LaneRow<PLACE> l(lane, r.dim);
   const int64_t row = s.row(t);
-  Turns y;
+  Turns<PLACE> y;
   l.turns(r, l.freqs(r), s.position(x, t), y);
 #pragma unroll 1
   for (int h = h0; h < h1; h += kAhead) {
@@ -122,13 +122,10 @@ __device__ __forceinline__ void append_step(const CacheProblem& p, const Rotary&
 #pragma unroll
       for (int i = 0; i < N; ++i) unpack16(raw[i], z[i]);
     } else {
-      const Freqs freqs = l.freqs(r);
+      const Freqs<PLACE> freqs = l.freqs(r);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        Turns y;
-        l.turns(r, freqs, pos[i], y);
-        unpack16(raw[i], z[i]);
-        turn16(l, y, z[i]);
+        turned16_at(l, r, freqs, pos[i], raw[i], z[i]);
       }
     }
   }
@@ -272,7 +269,7 @@ __global__ __launch_bounds__(64 * kWaves) void append_rotary_few_kernel(CachePro
   const int64_t rowb = (int64_t)p.hkv * kHeadDim;
   uint8_t* pool = (is_v ? p.v : p.k) + h * kHeadDim * ESZ;
   const LaneRow<PLACE> l(lane, r.dim);
-  const Freqs freqs = l.freqs(r);
+  const Freqs<PLACE> freqs = l.freqs(r);
   const int size = FORM == kCacheBlock && !is_q ? 1 << p.sb_shift : kFew;
   float scale = 1.f;
   if constexpr (FORM == kCacheHead)
@@ -288,15 +285,12 @@ __global__ __launch_bounds__(64 * kWaves) void append_rotary_few_kernel(CachePro
       const int t = min(from + kPass * i + r0, to - 1);
       uint32_t raw[8];
       load_part(l, src + s.row(t) * stride, raw);
-      if (!is_v) {
-        Turns y;
+      if (is_q) {
+        Turns<PLACE> y;
         l.turns(r, freqs, s.position(x, t), y);
-        if (is_q) {
-          turn_and_store(l, y, raw, q, s.row(t), h, from + kPass * i + r0 < to);
-          continue;
-        }
-        unpack16(raw, z[i]);
-        turn16(l, y, z[i]);
+        turn_and_store(l, y, raw, q, s.row(t), h, from + kPass * i + r0 < to);
+      } else if (!is_v) {
+        turned16_at(l, r, freqs, s.position(x, t), raw, z[i]);
       } else {
         unpack16(raw, z[i]);
       }

@@ -12,7 +12,8 @@
 // wave is eight rows. Where the pairs lie:
 //   kPairs   dimensions (2 i, 2 i + 1); a lane's 16 elements are adjacent
 //   kHalves  (i, i + dim / 2), dim a multiple of 16: two runs of eight elements
-//   kOdd     the same for any even dim: element by element
+//   kOdd     the same for any even dim: a lane's 16 elements are adjacent, and
+//            their partners come through LDS
 // Dimensions from dim on stand in pairs too, which are left as they are (not
 // turned by 0: an infinity would make NaN of its neighbour).
 #pragma once
@@ -29,7 +30,9 @@ struct Rotary {
 
 enum PairPlace : int32_t { kPairs = 0, kHalves = 1, kOdd = 2 };
 
-inline PairPlace place_of(int dim, bool interleaved) { return interleaved ? kPairs : dim % 16 ? kOdd : kHalves; }
+inline PairPlace place_of(int dim, bool interleaved) {
+  return interleaved || dim == 2 ? kPairs : dim % 16 ? kOdd : kHalves;
+}
 
 namespace {
 
@@ -57,61 +60,62 @@ __device__ __forceinline__ float2 turn_at(const Rotary& r, int n, uint64_t f) {
   return make_float2(t.x * r.scale, (r.inverse ? -t.y : t.y) * r.scale);
 }
 
-// A lane's eight frequencies and turns.
+// A lane's frequencies and turns: of eight pairs, or (kOdd) of its sixteen elements.
+template <int PLACE>
 struct Freqs {
-  uint64_t f[kPer];
+  uint64_t f[PLACE == kOdd ? 1 : kPer];          // (kOdd: read again where they are needed)
 };
+template <int PLACE>
 struct Turns {
-  float2 t[kPer];
+  float2 t[PLACE == kOdd ? 2 * kPer : kPer];
 };
 
 // What lane c (of the eight) holds of a row. `turned` pairs of its eight: the first ones.
 template <int PLACE>
 struct LaneRow {
   int c, dim;
-  int at[2];        // kPairs, kHalves: first elements of its two runs of eight
+  int at[2];        // first elements of its two runs of eight
   int turned;
   __device__ __forceinline__ LaneRow(int lane, int dim_) : c(lane & 7), dim(dim_) {
     turned = min(max(dim / 2 - kPer * c, 0), kPer);
-    if constexpr (PLACE == kPairs) at[0] = 16 * c, at[1] = 16 * c + 8;
-    else if (turned) at[0] = 8 * c, at[1] = dim / 2 + 8 * c;
-    else at[0] = 16 * c, at[1] = 16 * c + 8;      // dim + 16 (c - dim / 16)
+    if (PLACE == kHalves && turned) at[0] = 8 * c, at[1] = dim / 2 + 8 * c;
+    else at[0] = 16 * c, at[1] = 16 * c + 8;      // (halves: dim + 16 (c - dim / 16))
   }
-  // elements of pair e (kOdd)
-  __device__ __forceinline__ int2 pair(int e) const {
-    const int i = kPer * c + e, h = dim / 2;
-    return i < h ? make_int2(i, i + h) : make_int2(2 * i, 2 * i + 1);
-  }
-  __device__ __forceinline__ Freqs freqs(const Rotary& r) const {
-    Freqs y;
+  __device__ __forceinline__ Freqs<PLACE> freqs(const Rotary& r) const {
+    Freqs<PLACE> y{};
+    if constexpr (PLACE != kOdd) {
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) y.f[e] = e < turned ? r.turns[kPer * c + e] : 0;
+      for (int e = 0; e < kPer; ++e) y.f[e] = e < turned ? r.turns[kPer * c + e] : 0;
+    }
     return y;
   }
-  // The turns of the lane's pairs at position n.
-  __device__ __forceinline__ void turns(const Rotary& r, const Freqs& f, int n, Turns& y) const {
+  // The turns of the lane's pairs, or elements, at position n.
+  __device__ __forceinline__ void turns(const Rotary& r, const Freqs<PLACE>& f, int n, Turns<PLACE>& y) const {
+    if constexpr (PLACE != kOdd) {
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) y.t[e] = turn_at(r, n, f.f[e]);
+      for (int e = 0; e < kPer; ++e) y.t[e] = turn_at(r, n, f.f[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 2 * kPer; ++e) y.t[e] = element_turn(r, n, e);
+    }
+  }
+  // kOdd: element e becomes itself times .x plus its partner times .y: x cos - y sin of the first, y cos + x sin of
+  // the second (past dim anything)
+  __device__ __forceinline__ float2 element_turn(const Rotary& r, int n, int e) const {
+    const int h = dim / 2, j = 16 * c + e;
+    const float2 t = turn_at(r, n, r.turns[j < h ? j : j < dim ? j - h : 0]);
+    return make_float2(t.x, j < h ? -t.y : t.y);
   }
 };
 
 // A lane's part of a row as it comes: 16 bf16 (eight words) or 16 codes (four).
-// kPairs, kOdd: word by word the pairs; kHalves: the first run, then the second.
+// kPairs, kOdd: in the row's order; kHalves: the first run, then the second.
 template <int PLACE, class T>
 __device__ __forceinline__ void load_part(const LaneRow<PLACE>& l, const T* row, uint32_t (&w)[4 * sizeof(T)]) {
-  if constexpr (PLACE == kOdd) {
-#pragma unroll
-    for (int i = 0; i < 4 * (int)sizeof(T); ++i) w[i] = 0;
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      const int2 d = l.pair(e);
-      if constexpr (sizeof(T) == 2) w[e] = (uint32_t)row[d.x] | (uint32_t)row[d.y] << 16;
-      else w[e / 2] |= ((uint32_t)row[d.x] | (uint32_t)row[d.y] << 8) << (16 * (e & 1));
-    }
-  } else if constexpr (sizeof(T) == 2) {
+  if constexpr (sizeof(T) == 2) {
     const uint4 a = *(const uint4*)(row + l.at[0]), b = *(const uint4*)(row + l.at[1]);
     w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
-  } else if constexpr (PLACE == kPairs) {
+  } else if constexpr (PLACE != kHalves) {
     const uint4 a = *(const uint4*)(row + l.at[0]);
     w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
   } else {
@@ -121,22 +125,10 @@ __device__ __forceinline__ void load_part(const LaneRow<PLACE>& l, const T* row,
 }
 template <int PLACE, class T>
 __device__ __forceinline__ void store_part(const LaneRow<PLACE>& l, T* row, const uint32_t (&w)[4 * sizeof(T)]) {
-  if constexpr (PLACE == kOdd) {
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      const int2 d = l.pair(e);
-      if constexpr (sizeof(T) == 2) {
-        row[d.x] = (T)w[e];
-        row[d.y] = (T)(w[e] >> 16);
-      } else {
-        row[d.x] = (T)(w[e / 2] >> (16 * (e & 1)));
-        row[d.y] = (T)(w[e / 2] >> (16 * (e & 1) + 8));
-      }
-    }
-  } else if constexpr (sizeof(T) == 2) {
+  if constexpr (sizeof(T) == 2) {
     *(uint4*)(row + l.at[0]) = make_uint4(w[0], w[1], w[2], w[3]);
     *(uint4*)(row + l.at[1]) = make_uint4(w[4], w[5], w[6], w[7]);
-  } else if constexpr (PLACE == kPairs) {
+  } else if constexpr (PLACE != kHalves) {
     *(uint4*)(row + l.at[0]) = make_uint4(w[0], w[1], w[2], w[3]);
   } else {
     *(uint2*)(row + l.at[0]) = make_uint2(w[0], w[1]);
@@ -211,15 +203,71 @@ __device__ __forceinline__ void codes16_by(const float (&x)[16], const Divisor& 
   codes16(y, w);
 }
 
-template <int PLACE>
-__device__ __forceinline__ void turn16(const LaneRow<PLACE>& l, const Turns& t, float (&v)[16]) {
+// The partners of a lane's sixteen elements, by way of LDS (kOdd): every lane of
+// the wave leaves its part of a row there and reads the elements dim / 2 further
+// or before. Rows lie four words apart from a multiple of the banks.
+template <int N>
+__device__ __forceinline__ void partners16(const LaneRow<kOdd>& l, const uint32_t (&w)[N], float (&v)[16]) {
+  constexpr int kMostWaves = 8, ROW = 8 * N + 4, ESZ = N / 4;   // words of a row, bytes of an element
+  __shared__ __align__(16) uint32_t s_rows[kMostWaves][kPass][ROW];
+  uint32_t* row = s_rows[threadIdx.x >> 6][(threadIdx.x & 63) / kLaneRow];
+  // (one wave's traffic, which LDS takes in order; the fences keep the compiler to it)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) {
-    const int i = PLACE == kHalves ? e : 2 * e, j = PLACE == kHalves ? 8 + e : 2 * e + 1;
-    const float x = v[i], y = v[j];
-    const bool on = PLACE == kHalves ? l.turned > 0 : e < l.turned;
-    v[i] = on ? fmaf(x, t.t[e].x, -(y * t.t[e].y)) : x;
-    v[j] = on ? fmaf(x, t.t[e].y, y * t.t[e].x) : y;
+  for (int i = 0; i < N; i += 4) *(uint4*)(row + N * l.c + i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const int h = l.dim / 2;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int j = 16 * l.c + e, at = j < h ? j + h : j < l.dim ? j - h : j;
+    if constexpr (ESZ == 2) v[e] = __uint_as_float((uint32_t)((const uint16_t*)row)[at] << 16);
+    else v[e] = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t*)row)[at], 0);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// A lane's values, turned. Every lane of the wave takes part.
+template <int PLACE, int N>
+__device__ __forceinline__ void turned16(const LaneRow<PLACE>& l, const Turns<PLACE>& t, const uint32_t (&w)[N], float (&v)[16]) {
+  unpack16(w, v);
+  if constexpr (PLACE == kOdd) {
+    float p[16];
+    partners16(l, w, p);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = 16 * l.c + e < l.dim ? fmaf(v[e], t.t[e].x, p[e] * t.t[e].y) : v[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const int i = PLACE == kHalves ? e : 2 * e, j = PLACE == kHalves ? 8 + e : 2 * e + 1;
+      const float x = v[i], y = v[j];
+      const bool on = PLACE == kHalves ? l.turned > 0 : e < l.turned;
+      v[i] = on ? fmaf(x, t.t[e].x, -(y * t.t[e].y)) : x;
+      v[j] = on ? fmaf(x, t.t[e].y, y * t.t[e].x) : y;
+    }
+  }
+}
+
+// The same at position n, for one row: its turns are not kept (sixteen would not fit beside what is).
+template <int PLACE, int N>
+__device__ __forceinline__ void turned16_at(const LaneRow<PLACE>& l, const Rotary& r, const Freqs<PLACE>& f, int n,
+                                            const uint32_t (&w)[N], float (&v)[16]) {
+  if constexpr (PLACE == kOdd) {
+    float p[16];
+    __builtin_amdgcn_sched_barrier(0);
+    partners16(l, w, p);
+    unpack16(w, v);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float2 t = l.element_turn(r, n, e);
+      v[e] = 16 * l.c + e < l.dim ? fmaf(v[e], t.x, p[e] * t.y) : v[e];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  } else {
+    Turns<PLACE> t;
+    l.turns(r, f, n, t);
+    turned16(l, t, w, v);
   }
 }
 

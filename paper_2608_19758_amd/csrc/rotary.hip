@@ -29,7 +29,7 @@ __global__ __launch_bounds__(64 * kWaves) void rotary_kernel(Rotary r, int64_t t
   const bool there = token < tokens;
   const int64_t t = there ? token : tokens - 1;
   const LaneRow<PLACE> l(lane, r.dim);
-  Turns y;
+  Turns<PLACE> y;
   l.turns(r, l.freqs(r), positions[t], y);
 #pragma unroll 1
   for (int h = h0; h < h1; h += kAhead) {

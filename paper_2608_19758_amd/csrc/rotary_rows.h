@@ -18,11 +18,10 @@ namespace {
 
 // A lane's part of row (token t, head h), turned and stored.
 template <int PLACE>
-__device__ __forceinline__ void turn_and_store(const LaneRow<PLACE>& l, const Turns& y, const uint32_t (&w)[8],
+__device__ __forceinline__ void turn_and_store(const LaneRow<PLACE>& l, const Turns<PLACE>& y, const uint32_t (&w)[8],
                                                const RotaryRows& to, int64_t t, int h, bool there) {
   float x[16];
-  unpack16(w, x);
-  turn16(l, y, x);
+  turned16(l, y, w, x);
   const int64_t at = t * to.out_stride + h * kHeadDim;
   if (to.scale) {
     uint32_t c[4];

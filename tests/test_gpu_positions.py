@@ -12,7 +12,8 @@ from tests.test_gpu_cache import cu_of, dev, on_gpu, params, same
 pytestmark = pytest.mark.gpu
 
 FORMS = ["bf16", "head", 16, 64]
-KINDS = [(128, False), (128, True), (64, False), (96, True), (100, False), (2, False), (2, True), (126, True), (16, False)]
+KINDS = [(128, False), (128, True), (64, False), (96, True), (100, False), (2, False), (2, True), (126, True), (16, False),
+         (126, False), (20, False)]
 
 
 def rotary_of(dim, interleaved, scaling="none", factor=1.0, **kw):
@@ -178,7 +179,7 @@ def run_append(lens, new, form, page, dim=128, interleaved=False, hq=4, hkv=2, a
 
 
 @pytest.mark.parametrize("form", FORMS + [32, 128])
-@pytest.mark.parametrize("dim,interleaved", [(128, False), (128, True), (64, False), (100, False)])
+@pytest.mark.parametrize("dim,interleaved", [(128, False), (128, True), (64, False), (100, False), (20, False), (126, False)])
 def test_append(form, dim, interleaved):
     page = 128 if form == 128 else 64
     run_append([1, 63, 200, 5, 300, 4], [1, 40, 200, 0, 129, 3], form, page, dim, interleaved)
