@@ -102,12 +102,17 @@ struct Share {
   int64_t lo, hi, base, len;
 };
 __device__ __forceinline__ bool find_share(const CacheProblem& p, int cuts, Share& s) {
-  const int lane = threadIdx.x & 63;
-  int64_t total = 0, units = 0, u;
-  for (int b0 = 0; b0 < p.batch; b0 += 64) {
-    total += lane_value(wave_sum_to(line_of(p, cuts, b0 + lane, u)), 63);
-    units += lane_value(wave_sum_to(u), 63);
+  // every lane adds up a run of sequences, the first of which lie as far apart
+  const int lane = threadIdx.x & 63, run = (p.batch + 63) / 64;
+  int64_t own = 0, units = 0, u;
+#pragma unroll 4
+  for (int i = 0; i < run; ++i) {
+    const int b = lane * run + i;
+    own += line_of(p, cuts, b, u);
+    units += u;
   }
+  const int64_t to = wave_sum_to(own), total = lane_value(to, 63);
+  units = lane_value(wave_sum_to(units), 63);
   // short units are left whole while there are workgroups for them
   const int64_t most = min(max(units, total / kMinShare), (int64_t)gridDim.x);
   s.len = max((total + most - 1) / max(most, (int64_t)1), (int64_t)1);
@@ -117,17 +122,20 @@ __device__ __forceinline__ bool find_share(const CacheProblem& p, int cuts, Shar
   if ((int)(blockIdx.x / kXcds) >= each || s.index >= shares) return false;
   s.lo = s.index * s.len;
   s.hi = min(s.lo + s.len, total);
-  s.base = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += 64) {
-    const int64_t own = line_of(p, cuts, b0 + lane, u), to = s.base + wave_sum_to(own);
-    const uint64_t hit = __ballot(to > s.lo);
+  // the lane whose run holds the first, and the sequence of the run
+  const int l = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(to > s.lo)) - 1);
+  s.base = lane_value(to - own, l);
+  s.b = l * run;
+  for (const int end = min(s.b + run, p.batch); run > 1 && s.b < end; s.b += 64) {
+    const int64_t one = s.b + lane < end ? line_of(p, cuts, s.b + lane, u) : 0, upto = s.base + wave_sum_to(one);
+    const uint64_t hit = __ballot(upto > s.lo);
     if (hit) {
-      const int l = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)hit) - 1);
-      s.b = b0 + l;
-      s.base = lane_value(to - own, l);
+      const int k = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)hit) - 1);
+      s.b += k;
+      s.base = lane_value(upto - one, k);
       break;
     }
-    s.base = lane_value(to, 63);
+    s.base = lane_value(upto, 63);
   }
   return true;
 }
@@ -506,25 +514,41 @@ __global__ __launch_bounds__(256) void join_kernel(CacheProblem p, CachePartials
     n = min(parts, q.tiles);
     if (n <= 1 || unit >= q.units) return;
   }
-  const int i0 = unit * (kRows / p.g), rows = min(kRows / p.g, q.n - i0) * p.g;
+  const int first_q = unit * (kRows / p.g), rows = min(kRows / p.g, q.n - first_q) * p.g;
   const int pr = 8 * (blockIdx.x % per) + (threadIdx.x >> 5), d = 4 * (threadIdx.x & 31);
   if (pr >= rows) return;
   auto row = [&](int i) { return (i == 0 ? first : next + (int64_t)step * (i - 1)) * kRows + pr; };
-  float mm = kNoRef;
-  for (int i = 0; i < n; ++i) mm = fmaxf(mm, part.ml[2 * row(i)]);
-  float l = 0.f;
+  // eight parts a step, their loads in flight together (29 queries over 9280 keys, in 33
+  // parts a unit, take 31 us; with the loads of four in flight 37)
+  float mm = kNoRef, l = 0.f;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int i = 0; i < n; ++i) {
-    const int64_t at = row(i);
-    const float2 ml = *(const float2*)(part.ml + 2 * at);
-    const float4 y = *(const float4*)(part.o + at * kHeadDim + d);
-    const float f = fast_exp2(ml.x - mm);
-    l += f * ml.y;
-    a.x += f * y.x, a.y += f * y.y, a.z += f * y.z, a.w += f * y.w;
+#pragma unroll 1
+  for (int i0 = 0; i0 < n; i0 += 8) {
+    float2 ml[8];
+    float4 y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int64_t at = row(min(i0 + j, n - 1));          // past the end the last part again, for nothing
+      ml[j] = *(const float2*)(part.ml + 2 * at);
+      y[j] = *(const float4*)(part.o + at * kHeadDim + d);
+    }
+    float mn = mm;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mn = fmaxf(mn, ml[j].x);
+    const float f = fast_exp2(mm - mn);
+    mm = mn;
+    l *= f;
+    a.x *= f, a.y *= f, a.z *= f, a.w *= f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (i0 + j >= n) break;
+      const float g = fast_exp2(ml[j].x - mm);
+      l += g * ml[j].y;
+      a.x += g * y[j].x, a.y += g * y[j].y, a.z += g * y[j].z, a.w += g * y[j].w;
+    }
   }
   const float inv = (p.form == kCacheHead ? ld_uniform(p.v_head, h) : 1.f) / l;
-  const int64_t at = (int64_t)(q.q0 + i0 + pr / p.g) * p.hq + h * p.g + pr % p.g;
+  const int64_t at = (int64_t)(q.q0 + first_q + pr / p.g) * p.hq + h * p.g + pr % p.g;
   *(uint2*)(out + at * kHeadDim + d) =
       make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
   if (lse && d == 0) lse[at] = (mm + fast_log2(l)) * kLn2f;
