@@ -152,9 +152,9 @@ struct Shared {
 };
 
 // Tiles lo .. hi - 1 of a unit; slot: of the partial results, or -1 where they are all.
-// WIDE: pages hold a multiple of 64 tokens, so a tile lies in one and its address
-// is uniform (scalar).
-template <int FORM, bool WIDE>
+// GROUPED: pages hold a multiple of 8 tokens, so the rows of a tile that a wave
+// stages together lie one after the other and their address is uniform (scalar).
+template <int FORM, bool GROUPED>
 __device__ __forceinline__ void segment(const CacheProblem& p, const CachePartials& part, Shared& sh, int b, int h, int unit,
                                         const Seq& q, int lo, int hi, int64_t slot, uint16_t* __restrict__ out,
                                         float* __restrict__ lse) {
@@ -198,9 +198,10 @@ __device__ __forceinline__ void segment(const CacheProblem& p, const CachePartia
     i32x4_t x[NJ];
     uint32_t scale;
   };
-  // Where a tile lies (WIDE), or this thread's rows of it: the table's entries
-  // as loaded (used a tile later, so that nothing waits for them) and the places
-  // in the pages. Keys past the sequence stand on valid ones.
+  // Where the wave's rows of a tile lie (GROUPED), or this thread's: the table's
+  // entries as loaded (used a tile later, so that nothing waits for them) and the
+  // places in the pages. Keys past the sequence stand on valid ones.
+  constexpr int GROUP = 64 / TPR;                // rows that a wave loads at once
   struct Where {
     int page[NJ], off[NJ];
   };
@@ -210,28 +211,20 @@ __device__ __forceinline__ void segment(const CacheProblem& p, const CachePartia
     const int k0 = kStep * min(i, hi - 1);       // past the end the last tile again
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int t = WIDE ? k0 : min(k0 + r0 + 32 * j, q.L - 1);
+      const int t = GROUPED ? min(k0 + GROUP * w + 32 * j, (q.L - 1) & -GROUP) : min(k0 + r0 + 32 * j, q.L - 1);
       const int pg = p.pm.shift >= 0 ? t >> p.pm.shift : t / p.pm.page;
-      a.page[j] = WIDE ? ld_uniform(table, pg) : table[pg];
+      a.page[j] = GROUPED ? ld_uniform(table, pg) : table[pg];
       a.off[j] = t - pg * p.pm.page;
     }
     return a;
   };
-  const uint32_t roff = (uint32_t)(r0 * rowb + 16 * c);                  // WIDE: this thread's place in a tile
-  const uint32_t soff = (uint32_t)((r0 >> p.sb_shift) * p.hkv);          // and its scale's among the tile's
+  const uint32_t roff = (uint32_t)((GROUPED ? lane / TPR : 0) * rowb + 16 * c);   // this thread's place behind its address
   auto load = [&](const uint8_t* pool, const uint8_t* scales, const Where& a, Regs& x) {
-    if constexpr (WIDE) {
-      const int64_t s0 = (int64_t)a.page[0] * p.pm.page + a.off[0];
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) x.x[j] = *(const i32x4_t*)(pool + (s0 + 32 * j) * rowb + hoff + roff);
-      if constexpr (FORM == kCacheBlock) x.scale = (scales + (s0 >> p.sb_shift) * p.hkv + h)[soff];
-    } else {
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const int64_t s = (int64_t)a.page[j] * p.pm.page + a.off[j];
-        x.x[j] = *(const i32x4_t*)(pool + s * rowb + hoff + 16 * c);
-        if constexpr (FORM == kCacheBlock) x.scale = scales[(s >> p.sb_shift) * p.hkv + h];
-      }
+    for (int j = 0; j < NJ; ++j) {
+      const int64_t s = (int64_t)a.page[j] * p.pm.page + a.off[j];
+      x.x[j] = *(const i32x4_t*)(pool + s * rowb + hoff + roff);
+      if constexpr (FORM == kCacheBlock) x.scale = scales[(s >> p.sb_shift) * p.hkv + h];
     }
   };
   auto widen = [](const Regs& x, i32x4_t (&y)[2]) {   // 16 codes -> 16 bf16
@@ -442,7 +435,7 @@ __device__ __forceinline__ void segment(const CacheProblem& p, const CachePartia
 // Equal shares of the line. A share leaves what it has of a unit that started
 // before it in slot 2 index, of one that goes on behind it in slot 2 index + 1.
 // cuts 0: units are left whole.
-template <int FORM, bool WIDE>
+template <int FORM, bool GROUPED>
 __global__ __launch_bounds__(64 * kWaves, 1) void cross_kernel(CacheProblem p, CachePartials part, int cuts,
                                                                uint16_t* __restrict__ out, float* __restrict__ lse) {
   __shared__ Shared sh;
@@ -466,14 +459,14 @@ __global__ __launch_bounds__(64 * kWaves, 1) void cross_kernel(CacheProblem p, C
     pos = min(start + each, s.hi);
     if (lo >= hi) continue;                      // no tile of it in this share
     const bool whole = lo == 0 && hi == q.tiles;
-    segment<FORM, WIDE>(p, part, sh, s.b, h, unit, q, lo, hi, whole ? -1 : 2 * (int64_t)s.index + (lo == 0), out, lse);
+    segment<FORM, GROUPED>(p, part, sh, s.b, h, unit, q, lo, hi, whole ? -1 : 2 * (int64_t)s.index + (lo == 0), out, lse);
     if (lo == 0 && !whole) cut = Cut{s.b, h, unit, ((int)((start + each - 1) / s.len) - s.index + 1) | s.index << 16};
   }
   if (cuts && threadIdx.x == 0) *(int4*)(part.at + 4 * blockIdx.x) = make_int4(cut.b, cut.h, cut.unit, cut.parts);
 }
 
 // kv_splits: every unit in up to `parts` parts of its own.
-template <int FORM, bool WIDE>
+template <int FORM, bool GROUPED>
 __global__ __launch_bounds__(64 * kWaves, 1) void split_kernel(CacheProblem p, CachePartials part, int units, int parts,
                                                                uint16_t* __restrict__ out, float* __restrict__ lse) {
   __shared__ Shared sh;
@@ -483,7 +476,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void split_kernel(CacheProblem p, C
   const int n = min(parts, q.tiles);
   if (unit >= q.units || sp >= n) return;
   const int lo = (int)((int64_t)q.tiles * sp / n), hi = (int)((int64_t)q.tiles * (sp + 1) / n);
-  segment<FORM, WIDE>(p, part, sh, b, h, unit, q, lo, hi, n > 1 ? ((int64_t)unit * nbh + bh) * parts + sp : -1, out, lse);
+  segment<FORM, GROUPED>(p, part, sh, b, h, unit, q, lo, hi, n > 1 ? ((int64_t)unit * nbh + bh) * parts + sp : -1, out, lse);
 }
 
 // Joins the parts of a unit that was cut: a workgroup takes eight packed rows, 32
@@ -567,26 +560,26 @@ int shares_of(const CacheProblem& p) {
 
 int parts_of(const CacheProblem& p) { return std::min(std::min(p.splits, tiles_of(p)), kMaxParts); }
 
-template <int FORM, bool WIDE>
+template <int FORM, bool GROUPED>
 hipError_t launch(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse, hipStream_t s) {
   if (p.splits == 0) {
     const int grid = shares_of(p);
     const bool cuts = tiles_of(p) > kMinTiles;
-    cross_kernel<FORM, WIDE><<<grid, 64 * kWaves, 0, s>>>(p, part, cuts, out, lse);
+    cross_kernel<FORM, GROUPED><<<grid, 64 * kWaves, 0, s>>>(p, part, cuts, out, lse);
     if (cuts) join_kernel<<<grid * (kRows / 8), 256, 0, s>>>(p, part, 0, 0, out, lse);
     return hipGetLastError();
   }
   const int parts = parts_of(p);
   const int64_t units = (int64_t)p.batch * p.hkv * units_of(p), joins = units * (kRows / 8);
   if (!launchable(units * parts, 64 * kWaves) || (parts > 1 && !launchable(joins, 256))) return hipErrorInvalidValue;
-  split_kernel<FORM, WIDE><<<(unsigned)(units * parts), 64 * kWaves, 0, s>>>(p, part, (int)units_of(p), parts, out, lse);
+  split_kernel<FORM, GROUPED><<<(unsigned)(units * parts), 64 * kWaves, 0, s>>>(p, part, (int)units_of(p), parts, out, lse);
   if (parts > 1) join_kernel<<<(unsigned)joins, 256, 0, s>>>(p, part, (int)units_of(p), parts, out, lse);
   return hipGetLastError();
 }
 
 template <int FORM>
 hipError_t launch_pages(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse, hipStream_t s) {
-  return p.pm.page % kStep == 0 ? launch<FORM, true>(p, part, out, lse, s) : launch<FORM, false>(p, part, out, lse, s);
+  return p.pm.page % 8 == 0 ? launch<FORM, true>(p, part, out, lse, s) : launch<FORM, false>(p, part, out, lse, s);
 }
 
 }  // namespace

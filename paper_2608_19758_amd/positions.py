@@ -141,8 +141,11 @@ def _turned_rows(a: _Args, name, x, heads, out, scale, stream):
     """fp2_rotary_rows_t of x, its output (made on `stream` where none is given) and its tokens."""
     at, stride, tokens, wide = a.rows(name, x, heads)
     if out is None:
-        with on_stream(stream):
-            out = x.new_empty(x.shape) if scale is None else x.new_empty(x.shape, dtype=_CODE_BYTES)
+        if stream is None and scale is None:     # (rows that are dense are contiguous; empty_like is the fastest)
+            out = torch.empty_like(x)
+        else:
+            with on_stream(stream):
+                out = torch.empty(x.shape, dtype=x.dtype if scale is None else _CODE_BYTES, device=x.device)
         to, to_stride = out.data_ptr(), wide * HEAD_DIM
     else:
         to, to_stride, there, _ = a.rows(name + "'s output", out, wide, _ONE_BF16 if scale is None else _CODES)
