@@ -103,6 +103,11 @@ __device__ __forceinline__ void write_empty(const CacheProblem& p, int b, int h0
 // after the other and their address is uniform (scalar); otherwise every key has
 // its own (8 sequences of 64 rows: 99 us, with pages of 24 tokens 108).
 // CROSS: every row sees all keys of its sequence, as if it stood on the last one.
+// Lengths differ most there, so the line of tiles counts what a piece of a sequence
+// costs besides its tiles (its queries, its joined part), in tiles: 8 sequences of
+// 1700 keys, codes, 64 rows 42.3 us without and 32.2 with 8 or 12, 128 of 500 to
+// 3000 keys 192 and 171, one row each of 32 of 300 to 4000 30.4 and 28.0 (bf16
+// 51.2 and 48.8; with 16 51.0).
 template <int FORM, int NT, int RH, int W, bool GROUPED, bool CROSS>
 __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, CachePartials part,
                                                                int shares, uint16_t* __restrict__ out,
@@ -115,8 +120,9 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
   __shared__ float s_ml[W][16][2];
   const int groups = p.hkv / p.heads, index = blockIdx.x / groups;
   const int units = p.heads * RH, KS = W / units;   // (head, half of the rows): how many waves alternate its tiles
+  const int start = CROSS && !p.splits ? (NT * RH == 1 ? 2 : kBf16 ? 4 : NT * RH == 2 ? 8 : 12) : 0;
   Share sh;
-  if (!find_share(p, shares, index, sh)) {
+  if (!find_share(p, shares, index, sh, start)) {
     if constexpr (CROSS)   // (otherwise the join's)
       if (p.splits == 1) write_empty(p, index, blockIdx.x % groups * p.heads, p.heads, out, lse);
     return;
@@ -150,6 +156,7 @@ __global__ __launch_bounds__(64 * W, W / 4) void decode_kernel(CacheProblem p, C
   const int last = L - 1, first = CROSS ? last : L - Lq;      // positions of the first and the last row
   const int rows = Lq * p.g;
   const Tiles tl = tiles_of(p, Lq, L);
+  if (tl.n > 0) base += start;
   const int lo = max(sh.lo, base) - base, hi = min(sh.hi, base + tl.n) - base;
   auto tile_at = [&](int i) { return i < tl.sinks ? i : tl.from + i - tl.sinks; };
   if (lo < hi) {

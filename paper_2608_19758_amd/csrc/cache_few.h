@@ -35,8 +35,9 @@ __device__ __forceinline__ bool sees(const CacheProblem& p, int pos, int key) {
 // The tiles of a call, one sequence after the other, form a line, which is cut
 // into equal shares; a workgroup takes one share of its heads, so that all have
 // the same work whatever the lengths. A share may hold the end of one
-// sequence, whole ones, and the start of another. With kv_splits n >= 1 every
-// sequence is cut into at most n shares of its own instead.
+// sequence, whole ones, and the start of another. Where what a sequence takes
+// besides its tiles counts, `start` places of the line stand before its first one.
+// With kv_splits n >= 1 every sequence is cut into at most n shares of its own instead.
 struct Share {
   int lo, hi;       // tiles of the line
   int b;            // sequence of the first
@@ -75,7 +76,7 @@ __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_am
 
 // Share `index` of the call. Wave-uniform; false where there is none. A call has
 // fewer than 2^31 tiles (the host's check).
-__device__ __forceinline__ bool find_share(const CacheProblem& p, int shares, int index, Share& out) {
+__device__ __forceinline__ bool find_share(const CacheProblem& p, int shares, int index, Share& out, int start = 0) {
   const int lane = threadIdx.x & 63;
   int q0, Lq, L;
   auto tiles_at = [&](int b) {
@@ -85,7 +86,8 @@ __device__ __forceinline__ bool find_share(const CacheProblem& p, int shares, in
       Lq = p.cu[b + 1] - q0;
       L = p.cuk[b + 1] - p.cuk[b];
     }
-    return tiles_of(p, Lq, L).n;
+    const int n = tiles_of(p, Lq, L).n;
+    return n > 0 ? n + start : 0;
   };
   auto take = [&](int l) {
     out.q0 = lane_value(q0, l);

@@ -186,6 +186,15 @@ def test_append(form, dim, interleaved):
     run_append([1, 64, 65, 200, 9, 7], [1, 1, 2, 16, 9, 0], form, page, dim, interleaved, seed=5)
 
 
+@pytest.mark.parametrize("form", FORMS + [32, 128])
+@pytest.mark.parametrize("dim,interleaved", [(128, True), (64, False), (100, False)])
+def test_append_some_tokens(form, dim, interleaved):
+    """As many new tokens as a wave may take alone, in up to three blocks, and one more."""
+    page = 128 if form == 128 else 64
+    run_append([32, 70, 127, 25, 400, 30], [32, 31, 17, 20, 32, 1], form, page, dim, interleaved, seed=6)
+    run_append([41, 33, 150], [32, 33, 22], form, page, dim, interleaved, seed=7)
+
+
 @pytest.mark.parametrize("form", FORMS)
 def test_append_positions_codes_and_plain_rows(form):
     run_append([400, 37], [150, 37], form, 64, at=100000, codes=True, part=False)
