@@ -39,10 +39,11 @@ constexpr int kRows = 32 * kWaves;
 constexpr int kMaxParts = 32;
 constexpr int kShares = kCrossCuts;  // workgroups that run at a time, one a compute unit
 constexpr int kXcds = 8;         // dies, each with a cache of its own, that workgroups go to in turn
-constexpr int kMinTiles = 4;     // units of at most as many tiles are not cut
 constexpr int kMinShare = 4;     // length of a share, at least (one unit of 16 tiles: 21 us, with 8 30)
-constexpr int kUnit = 4;         // tiles that a unit's start and end take as long as
-constexpr int kAhead = 5;       // products that operands are read ahead
+// Tiles that a unit's start and end take as long as. 24 sequences of 100 to 3000 queries over 100 to 9000 keys: 854 us,
+// with 0 1996, with 8 892.
+constexpr int kUnit = 4;
+constexpr int kAhead = 5;        // products that operands are read ahead (600 queries over 4000 keys: 67 us, with 3 71, with 7 68)
 constexpr float kTau = 8.0f;
 constexpr float kNoRef = -1e30f;
 
@@ -550,6 +551,16 @@ __global__ __launch_bounds__(256) void join_kernel(CacheProblem p, CachePartials
 int64_t units_of(const CacheProblem& p) { return ((int64_t)p.max_new * p.g + kRows - 1) / kRows; }
 int tiles_of(const CacheProblem& p) { return std::max((p.max_kv + kStep - 1) / kStep, 1); }
 
+// Whether units are cut. A second piece, and parts to join, cost as long as some eight tiles; and the more
+// workgroups have a unit each, the less there is to gain. Whole and cut: 16 units of 8 tiles 21.9 and 22.9 us,
+// of 16 34 and 26; 64 of 12 29.7 and 31.2, of 24 49 and 38; 128 of 16 38 and 45, of 36 72 and 66; 256 of 24 65 and
+// 68. Of more than fit at once the lengths differ, and a workgroup has as many units as the next: 320 of 12 62 and 68,
+// 768 109 and 107.
+bool cut(const CacheProblem& p) {
+  const int64_t units = (int64_t)p.batch * p.hkv * units_of(p);
+  return tiles_of(p) > (units <= kShares ? 8 + units / 16 : 12);
+}
+
 // Workgroups of the equal shares, whole dies' worth: as many as the call's bounds allow. Which of them
 // have a share the lengths say.
 int shares_of(const CacheProblem& p) {
@@ -564,7 +575,7 @@ template <int FORM, bool GROUPED>
 hipError_t launch(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse, hipStream_t s) {
   if (p.splits == 0) {
     const int grid = shares_of(p);
-    const bool cuts = tiles_of(p) > kMinTiles;
+    const bool cuts = cut(p);
     cross_kernel<FORM, GROUPED><<<grid, 64 * kWaves, 0, s>>>(p, part, cuts, out, lse);
     if (cuts) join_kernel<<<grid * (kRows / 8), 256, 0, s>>>(p, part, 0, 0, out, lse);
     return hipGetLastError();
@@ -586,7 +597,7 @@ hipError_t launch_pages(const CacheProblem& p, const CachePartials& part, uint16
 
 void cache_cross_partials(const CacheProblem& p, int64_t* slots, int* rows) {
   *rows = kRows;
-  if (p.splits == 0) *slots = tiles_of(p) > kMinTiles ? 2 * (int64_t)shares_of(p) : 0;
+  if (p.splits == 0) *slots = cut(p) ? 2 * (int64_t)shares_of(p) : 0;
   else *slots = parts_of(p) > 1 ? (int64_t)p.batch * p.hkv * units_of(p) * parts_of(p) : 0;
 }
 

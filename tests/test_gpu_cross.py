@@ -59,6 +59,24 @@ def test_many_queries(form, g):
     run_cross(c, 2 * g, [70, 300, 0, 9, 1, 33, 64])
 
 
+@pytest.mark.parametrize("form,page", [("bf16", 128), ("head", 128), (16, 128), (128, 128), ("bf16", 24), ("head", 5)])
+@pytest.mark.parametrize("g", [1, 4, 8])
+def test_cut_sequences(form, page, g):
+    """Keys so long that sequences are cut, short and empty ones between them."""
+    c = ref.Cache([1, 0, 1700, 65, 0, 300, 1601, 5, 0], 2, form, page, seed=12)
+    run_cross(c, 2 * g, [70, 3, 300, 0, 9, 1, 33, 64, 0])
+    run_cross(c, 2 * g, [1, 3, 8, 0, 7, 1, 5, 8, 0])
+
+
+@pytest.mark.parametrize("new", [[1] * 150, [3, 0, 1] * 50, [70, 0, 40] * 50])
+def test_many_sequences_cut(new):
+    """More sequences than a wave has lanes, some longer than those that are left whole."""
+    lens = [(37 * b) % 190 for b in range(150)]
+    lens[3], lens[64], lens[149] = 1900, 1750, 2000
+    c = ref.Cache(lens, 1, 64, 64, seed=13)
+    run_cross(c, 2, new)
+
+
 @pytest.mark.parametrize("form,page", [("bf16", 1), ("bf16", 24), ("head", 5), ("head", 48), ("bf16", 4096),
                                        (16, 48), (32, 96), (64, 192)])
 def test_pages(form, page):
