@@ -235,6 +235,8 @@ fp2_status_t check_rotary(const fp2_rotary_t* r) {
   if (!r) return fail(FP2_EINVAL, "rotary is null");
   if (r->dim < 2 || r->dim > fp2::kHeadDim || r->dim % 2)
     return fail(FP2_EINVAL, "rotary: dim %d is not even and in [2, 128]", r->dim);
+  if (r->interleaved != 0 && r->interleaved != 1)
+    return fail(FP2_EINVAL, "rotary: interleaved %d is not 0 or 1", r->interleaved);
   if (!r->turns) return fail(FP2_EINVAL, "rotary: turns is null");
   if (!aligned(r->turns, 8)) return fail(FP2_EINVAL, "rotary: turns must be 8-byte aligned");
   if (!(r->scale > 0.f) || !isfinite(r->scale) || !isfinite(1.f / r->scale))

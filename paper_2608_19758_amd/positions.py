@@ -35,7 +35,7 @@ class _RotaryRows(ctypes.Structure):
                 ("out_scale", ctypes.c_void_p)]
 
 
-@dataclasses.dataclass(frozen=True)
+@dataclasses.dataclass(frozen=True, eq=False)
 class Rotary:
     """fp2_rotary_t: turns int64 [dim / 2] on the device (the bits of f / (2 pi) * 2^64), pairs (2i, 2i + 1)
     if interleaved, else (i, i + dim / 2); scale multiplies both parts. Its tensor is checked here, once."""
@@ -51,6 +51,9 @@ class Rotary:
         at = a("turns", self.turns, _ONE_I64, self.dim // 2)
         object.__setattr__(self, "_args", _RotaryArgs(at, self.dim, bool(self.interleaved), self.scale))
         object.__setattr__(self, "_dev", self.turns.get_device())
+
+    def __reduce__(self):     # a copy has a tensor of its own, and its address
+        return Rotary, (self.turns, self.dim, self.interleaved, self.scale)
 
 
 def rotary_frequencies(dim: int, base: float = 10000.0, *, scaling: str = "none", factor: float = 1.0,
@@ -158,6 +161,16 @@ def _turned_rows(a: _Args, name, x, heads, out, scale, stream):
     return _RotaryRows(at, stride, to, to_stride, wide, FP8_E4M3, a(name + "_scale", scale, _F32, wide)), out, tokens
 
 
+def _meet(a, b, tokens):
+    """Whether rows (address, stride and width in bytes) that are written meet others: those of one stride may
+    lie between each other's (parts of one matrix)."""
+    (x, xs, xw), (y, ys, yw) = a, b
+    if tokens == 0 or x >= y + (tokens - 1) * ys + yw or y >= x + (tokens - 1) * xs + xw:
+        return False
+    off = (y - x) % xs if xs == ys and xs > 0 else 0
+    return off < xw or off + yw > xs
+
+
 def rotary(r: Rotary, q, positions, k=None, *, out=None, k_out=None, q_scale=None, inverse: bool = False, stream=None):
     """fp2_rotary: q (and k) bf16 [tokens, heads, 128] turned by positions int32 [tokens]. Rows may be parts of a
     wider matrix; out and k_out may be q and k themselves. With q_scale (fp32 [heads]) the queries come as e4m3
@@ -187,7 +200,15 @@ def cache_append_rotary(p: CacheParams, r: Rotary, q, k_new, v_new, cache: KVCac
     v, vs, there, _ = a.rows("v_new", v_new, p.num_kv_heads)
     rows = None
     if q is not None:
+        given = out is not None
         rows, out, asked = _turned_rows(a, "q", q, p.num_q_heads, out, q_scale, stream)
+        if given and cu_seqlens_host is None and asked == tokens == there:   # (with it the call itself looks)
+            e, wide = 2 if q_scale is None else 1, p.num_q_heads * HEAD_DIM
+            o, x = (rows.out, e * rows.out_stride, e * wide), (rows.x, 2 * rows.x_stride, 2 * wide)
+            width = 2 * p.num_kv_heads * HEAD_DIM
+            if (o != x and _meet(o, x, tokens)) or _meet(o, (k, 2 * ks, width), tokens) or \
+                    _meet(o, (v, 2 * vs, width), tokens):
+                raise ValueError("q's output must not overlap k_new, v_new or other rows of q")
         rows = ctypes.byref(rows)
         there = there if asked == tokens else asked
     if there != tokens:

@@ -1,7 +1,10 @@
 """Rotary positions, reading back, moving and cross attention without a GPU: refusals before any
 launch, frequencies, and the reference that the GPU tests use."""
+import copy
 import ctypes
+import dataclasses
 import math
+import pickle
 
 import numpy as np
 import pytest
@@ -245,6 +248,38 @@ def test_cache_binding_refuses():
                lambda: fp2.cache_move(p, cache, *lens[1:], target, **ok)):
         with pytest.raises(ValueError, match="CUDA tensor"):
             go()
+
+
+def test_interleaved_is_0_or_1():
+    for op in ("rotary", "append", "read", "move"):
+        for bad in (2, -1):
+            assert call(op, base(), rotary=turns(interleaved=bad)) == fp2.EINVAL
+            assert "interleaved" in fp2.last_error()
+
+
+def test_rotary_copies():
+    """A copy's arguments are those of its own tensor."""
+    r = cpu_rotary(64, interleaved=True, scale=1.5)
+    for c in (copy.deepcopy(r), pickle.loads(pickle.dumps(r)), copy.copy(r), dataclasses.replace(r)):
+        assert c._args.turns == c.turns.data_ptr() and torch.equal(c.turns, r.turns)
+        assert (c.dim, c.interleaved, c.scale, c._args.dim, c._args.interleaved) == (64, True, 1.5, 64, 1)
+    c = copy.deepcopy(r)
+    assert c.turns.data_ptr() != r.turns.data_ptr() and c != r and r == r and len({r, c}) == 2
+
+
+def test_append_output_overlap():
+    """Queries out onto other rows of the call, without lengths on the host; parts of one matrix may be turned in place."""
+    p, cache, lens, _ = cpu_call()
+    r, m = cpu_rotary(), torch.zeros((6, 8, 128), dtype=torch.bfloat16)
+    q, k, v = m[:5, :4], m[:5, 4:6], m[:5, 6:]
+    for out in (m[:5, 1:5], m[:5, 4:8], m[1:, :4], m[1:, 2:6], m.view(-1, 4, 128)[:5]):
+        with pytest.raises(ValueError, match="overlap"):
+            fp2.cache_append_rotary(p, r, q, k, v, cache, *lens, out=out)
+    for scale, codes in ((None, None), (torch.ones(4), m.view(torch.uint8).view(-1, 4, 128))):
+        with pytest.raises(ValueError, match="CUDA tensor" if scale is None else "overlap"):
+            fp2.cache_append_rotary(p, r, q, k, v, cache, *lens, out=q if scale is None else codes, q_scale=scale)
+    with pytest.raises(ValueError, match="CUDA tensor"):
+        fp2.cache_append_rotary(p, r, m[:5, :4], m[:5, 6:], m[:5, 6:], cache, *lens, out=m[:5, :4].clone())
 
 
 # ---- frequencies
