@@ -23,10 +23,11 @@ namespace fp2 {
 namespace {
 
 constexpr int kWaves = 8;
-// New tokens of a sequence that a wave takes alone. 256 sequences of 32 tokens: 49
-// us, dealt out as many 132; 64 tokens in a wave: 26 us instead of 31 for 64
-// sequences, 13 instead of 9 for one.
-constexpr int kFew = 32;
+// New tokens of a sequence that a wave takes alone, at most: with registers for 16,
+// or for 32 (256 sequences of 32 tokens: 55 us, dealt out as many 132; one token of
+// 256: 15 and 19). 64 tokens in a wave: 26 us instead of 31 for 64 sequences, 13
+// instead of 9 for one.
+constexpr int kFew = 16, kSome = 32;
 
 struct New {
   const uint16_t* k;
@@ -252,13 +253,90 @@ __global__ __launch_bounds__(64 * kWaves) void append_rotary_kernel(CacheProblem
   }
 }
 
-// At most kFew new tokens a sequence. They lie in at most three blocks, one after
-// the other; the codes that a block held are read only if its scale grows.
+// One new token a sequence: a wave takes eight heads of its queries, keys or values.
+// The codes that a block held are read only if its scale grows.
 template <int FORM, int PLACE>
+__global__ __launch_bounds__(64 * kWaves) void append_rotary_one_kernel(CacheProblem p, Rotary r, RotaryRows q, New x,
+                                                                        int64_t total) {
+  typedef std::conditional_t<FORM == kCacheBf16, uint16_t, uint8_t> elem_t;
+  const int64_t at = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (at >= total) return;
+  const int kv = (p.hkv + kPass - 1) / kPass, jobs = 2 * kv + (q.heads + kPass - 1) / kPass, j = (int)(at % jobs);
+  const Seq s(p, (int)(at / jobs));
+  if (s.n <= 0) return;
+  const bool is_q = j >= 2 * kv, is_v = !is_q && j >= kv;
+  const int h0 = kPass * (is_q ? j - 2 * kv : is_v ? j - kv : j), heads = is_q ? q.heads : p.hkv;
+  const int lane = threadIdx.x & 63, r0 = lane / kLaneRow, h = min(h0 + r0, heads - 1), t = s.L - 1;
+  const bool there = h0 + r0 < heads;
+  const LaneRow<PLACE> l(lane, r.dim);
+  const int64_t row = s.row(t);
+  uint32_t raw[8];
+  load_part(l, (is_q ? q.x + row * q.x_stride : is_v ? x.v + row * x.v_stride : x.k + row * x.k_stride) + h * kHeadDim, raw);
+  float z[16];
+  if (is_v) unpack16(raw, z);
+  else turned16_at(l, r, l.freqs(r), s.position(x, t), raw, z);
+  uint32_t c[4], w[8];
+  if (is_q) {
+    const int64_t to = row * q.out_stride + h * kHeadDim;
+    if (q.scale) {
+      codes16_by(z, Divisor(q.scale[h]), c);
+      if (there) store_part(l, q.out + to, c);
+    } else {
+      pack16(z, w);
+      if (there) store_part(l, (uint16_t*)q.out + to, w);
+    }
+    return;
+  }
+  elem_t* pool = (elem_t*)(is_v ? p.v : p.k);
+  const int64_t slot = slot_of(p.pm, s.b, s.tok0, t);
+  elem_t* to = pool + (slot * p.hkv + h) * kHeadDim;
+  if constexpr (FORM == kCacheBf16) {
+    pack16(z, w);
+    if (there) store_part(l, to, w);
+  } else if constexpr (FORM == kCacheHead) {
+    codes16_by(z, Divisor((is_v ? p.v_head : p.k_head)[h]), c);
+    if (there) store_part(l, to, c);
+  } else {
+    const int first = t & -(1 << p.sb_shift);
+    uint8_t* sp = (is_v ? p.v_block : p.k_block) + (slot >> p.sb_shift) * p.hkv + h;
+    const int before = first < t ? *sp : 0;              // byte of a block that holds tokens
+    auto largest = [&](float m) {                        // of a row
+#pragma unroll
+      for (int o = 1; o < kLaneRow; o *= 2) m = fmaxf(m, __shfl_xor(m, o, 64));
+      return m;
+    };
+    float amax = largest(largest16(z));
+    if (__any(!(amax < INFINITY))) {                     // (rare: infinities do not count)
+      const float finite = largest(largest16_finite(z));
+      amax = amax < INFINITY ? amax : finite;
+    }
+    const int byte = max(scale_byte(amax), before);
+    const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);   // 2^-e
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z[e] *= inv;
+    if (__any(byte >= kMaxScaleByte)) codes16_held(z, c);
+    else codes16(z, c);
+    if (there) store_part(l, to, c);
+    if (there && l.c == 0) *sp = (uint8_t)byte;
+    // the whole wave takes the heads whose scales grew, one after the other
+    for (uint64_t grew = __ballot(there && l.c == 0 && first < t && byte > before); grew; grew &= grew - 1) {
+      const int from = __ffsll((unsigned long long)grew) - 1;
+      const float by = power_down(__builtin_amdgcn_readlane(before, from), __builtin_amdgcn_readlane(byte, from));
+      elem_t* head = pool + (h0 + from / kLaneRow) * kHeadDim;
+#pragma unroll 4
+      for (int u = first + r0; u < t; u += kPass)
+        shrink_row(head + slot_of(p.pm, s.b, s.tok0, u) * p.hkv * kHeadDim, lane, by);
+    }
+  }
+}
+
+// At most MOST new tokens a sequence: a wave takes a head. They lie in at most three
+// blocks, one after the other; the codes that a block held are read only if its scale grows.
+template <int FORM, int PLACE, int MOST>
 __global__ __launch_bounds__(64 * kWaves) void append_rotary_few_kernel(CacheProblem p, Rotary r, RotaryRows q, New x,
                                                                         int64_t total) {
   constexpr int ESZ = FORM == kCacheBf16 ? 2 : 1;
-  constexpr int N = kFew / kPass;
+  constexpr int N = MOST / kPass;
   const int64_t at = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (at >= total) return;
   const int jobs = 2 * p.hkv + q.heads, j = (int)(at % jobs);
@@ -273,14 +351,14 @@ __global__ __launch_bounds__(64 * kWaves) void append_rotary_few_kernel(CachePro
   uint8_t* pool = (is_v ? p.v : p.k) + h * kHeadDim * ESZ;
   const LaneRow<PLACE> l(lane, r.dim);
   const Freqs<PLACE> freqs = l.freqs(r);
-  const int size = FORM == kCacheBlock && !is_q ? 1 << p.sb_shift : kFew;
+  const int size = FORM == kCacheBlock && !is_q ? 1 << p.sb_shift : MOST;
   float scale = 1.f;
   if constexpr (FORM == kCacheHead)
     if (!is_q) scale = ld_uniform(is_v ? p.v_head : p.k_head, h);
 #pragma unroll 1
   for (int from = s.P; from < s.L;) {
     // the new tokens from .. to - 1 of a block
-    const int first = FORM == kCacheBlock && !is_q ? from & -size : from, to = min(min(first + size, s.L), from + kFew);
+    const int first = FORM == kCacheBlock && !is_q ? from & -size : from, to = min(min(first + size, s.L), from + MOST);
     float z[N][16];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -357,12 +435,18 @@ __global__ __launch_bounds__(64 * kWaves) void append_rotary_few_kernel(CachePro
 
 template <int FORM, int SB, int PLACE>
 hipError_t launch(const CacheProblem& p, const Rotary& r, const RotaryRows& q, const New& x, hipStream_t s) {
-  const int jobs = 2 * p.hkv + q.heads;
-  if (p.max_new <= kFew) {
+  if (p.max_new <= kSome) {
+    const bool one = p.max_new == 1;
+    const int each = one ? kPass : 1, jobs = 2 * ((p.hkv + each - 1) / each) + (q.heads + each - 1) / each;
     const int64_t total = (int64_t)p.batch * jobs, grid = (total + kWaves - 1) / kWaves;
     if (!launchable(grid, 64 * kWaves)) return hipErrorInvalidValue;
-    append_rotary_few_kernel<FORM, PLACE><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, r, q, x, total);
-    return hipGetLastError();
+    auto go = [&](auto kernel) {
+      kernel<<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, r, q, x, total);
+      return hipGetLastError();
+    };
+    return one                 ? go(append_rotary_one_kernel<FORM, PLACE>)
+           : p.max_new <= kFew ? go(append_rotary_few_kernel<FORM, PLACE, kFew>)
+                               : go(append_rotary_few_kernel<FORM, PLACE, kSome>);
   }
   constexpr int PARTS = SB > 32 ? SB / 32 : 1, TOK = 32 * PARTS, WIDE = kWaves / PARTS;
   const Steps steps = steps_of(p.hkv, WIDE, 2);

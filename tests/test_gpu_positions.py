@@ -195,6 +195,48 @@ def test_append_some_tokens(form, dim, interleaved):
     run_append([41, 33, 150], [32, 33, 22], form, page, dim, interleaved, seed=7)
 
 
+@pytest.mark.parametrize("form", FORMS + [32, 128])
+@pytest.mark.parametrize("dim,interleaved", [(128, True), (128, False), (64, False), (100, False), (2, False)])
+def test_append_one_token(form, dim, interleaved):
+    """A decode step: blocks that the token starts, blocks whose scale it raises and others, idle sequences."""
+    page = 128 if form == 128 else 64
+    lens, new = [1, 16, 17, 64, 65, 200, 128, 9, 30, 127], [1, 1, 1, 1, 1, 1, 1, 0, 1, 1]
+    run_append(lens, new, form, page, dim, interleaved, seed=8)
+    run_append(lens, new, form, page, dim, interleaved, hq=36, hkv=9, seed=9, codes=True, part=False, spread=2.0)
+    run_append(lens, new, form, page, dim, interleaved, hq=8, hkv=8, seed=10, at=70000, spread=0.1)
+
+
+@pytest.mark.parametrize("sb", [16, 64])
+def test_append_one_token_after_the_other(sb):
+    """40 steps of one token: each block's codes have been rounded to its scale at most once for each growth, and
+    infinities and NaN of a head stay with their pairs and move no scale."""
+    r, f, _ = rotary_of(128, False)
+    heads, n, start = 3, 40, 50
+    c = ref.Cache([start + n], heads, sb, 64, seed=14)
+    k, v = rows(n, heads, 15), rows(n, heads, 16)
+    k *= torch.linspace(0.25, 4.0, n)[:, None, None].bfloat16()
+    k[5, 0, 3], k[6, 1, 70], k[7, 2, 0] = float("inf"), float("nan"), float("-inf")
+    one, many = on_gpu(c), on_gpu(c)
+    was, roundings = one.k_scale.cpu(), 2
+    for i in range(n):
+        cuk = cu_of([start + i + 1])
+        fp2.cache_append_rotary(params(c, heads, [1]), r, None, dev(k[i:i + 1]), dev(v[i:i + 1]), one, dev(cu_of([1])), dev(cuk),
+                                dev(c.table))
+        now = one.k_scale.cpu()
+        roundings, was = roundings + (now != was).numpy(), now
+    fp2.cache_append_rotary(params(c, heads, [n]), r, None, dev(k), dev(v), many, dev(cu_of([n])), dev(cu_of(c.lens)), dev(c.table))
+    same(one.k_scale, many.k_scale.cpu(), "k scales")
+    same(one.v_scale, many.v_scale.cpu(), "v scales")
+    at = c.slots(0, np.arange(start, start + n))
+    scale = many.k_scale.cpu().numpy()[at // sb].astype(np.float64)
+    a, b = (ref.VALUES[x.k.cpu().numpy()[at]] * 2.0 ** (scale - 127)[..., None] for x in (one, many))
+    assert np.array_equal(np.isnan(a), np.isnan(b)) and np.isnan(a).sum() == 6
+    # both round once, and each growth what is there once more, by at most half a step: 2^-4 of it, or 2^-10 scales
+    x, y = np.nan_to_num(a), np.nan_to_num(b)
+    bound = roundings[at // sb][..., None] * (np.abs(y) * 2.0 ** -4 + 2.0 ** -10 * 2.0 ** (scale - 127)[..., None])
+    assert (np.abs(x - y) <= bound).all()
+
+
 @pytest.mark.parametrize("form", FORMS)
 def test_append_positions_codes_and_plain_rows(form):
     run_append([400, 37], [150, 37], form, 64, at=100000, codes=True, part=False)
