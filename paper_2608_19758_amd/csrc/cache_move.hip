@@ -14,7 +14,10 @@
 // codes and scales. All that is read of a block is read before it is written, so
 // the pages may be the same (in place).
 //
-// Bound by memory: 128 or 256 bytes a row in, and 256 (reading) or as many out.
+// Bound by memory: 128 or 256 bytes a row in, and 256 (reading) or as many out. 408K
+// tokens of 8 heads, scales of 64, read and turned back: 481 us (4.9 TB/s); 229K
+// moved to other pages, scales of 64: 171 (4.3 TB/s: rows of 1 KB at places of their
+// own); 1000 tokens of every head's own 10, 2001 read 6.8.
 #include <algorithm>
 #include <type_traits>
 
@@ -284,9 +287,11 @@ hipError_t launch_read(const CacheProblem& p, const Rotary& r, const int32_t* po
   // the most runs that the bounds allow
   const int64_t runs = (int64_t)p.batch * ((p.max_new >> kReadShift) + 2);
   const int kinds = (k_out != nullptr) + (v_out != nullptr);
-  // heads of a wave: many share the turns, few fill the chip where tokens are few
+  // heads of a wave: many share the turns, few fill the chip where tokens are few (8 heads: 2000 tokens 8.5 us with
+  // one a wave, 12.7 with eight; 20000 25.7 with four, 27.5 with eight, 45.8 with one; 200000 261 with eight, 441)
   int heads = std::min(8, p.hkv);
   while (heads > 1 && runs * kinds * ((p.hkv + heads - 1) / heads) < 4096) heads >>= 1;
+  // (200000 tokens: with 2048 workgroups at most 272 us)
   const int64_t grid = grid_for((runs * kinds * ((p.hkv + heads - 1) / heads) + kWaves - 1) / kWaves, 8192);
   read_kernel<FORM, PLACE, TURN><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, r, positions, k_out, v_out, heads);
   return hipGetLastError();
@@ -296,6 +301,7 @@ template <int FORM, int SB, int PLACE, int TURN>
 hipError_t launch_move(const CacheProblem& p, const Rotary& r, const Moves& m, const PageMap& to, hipStream_t s) {
   constexpr int PARTS = SB > 32 ? SB / 32 : 1, TOK = 32 * PARTS, WIDE = kWaves / PARTS;
   const Steps steps = steps_of(p.hkv, WIDE, to.table ? 2 : 1);
+  // (200000 tokens: 189 us, with 8192 workgroups at most 199)
   const int64_t grid = grid_for(steps_in(steps, WIDE, (int64_t)p.batch * (p.max_kv / TOK + 1)), 2048);
   move_tokens_kernel<FORM, SB, PLACE, TURN><<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, r, m, to, steps);
   return hipGetLastError();

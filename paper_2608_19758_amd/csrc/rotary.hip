@@ -3,8 +3,10 @@
 //
 // A wave takes eight tokens, eight lanes a row, works out its turns once (in
 // registers) and goes through `run` heads with them, four heads' loads in
-// flight. Bound by memory: 256 bytes a row in, 256 or 128 out; the turns are 2
-// multiplications and some 20 other instructions each, shared by the heads.
+// flight. Bound by memory: 256 bytes a row in, 256 or 128 out; a turn is some 35
+// instructions, shared by the heads. 16384 tokens of 32 heads, to codes, and of
+// eight of keys: 53 us (5.0 TB/s); 8 tokens 4.5, a launch and three loads that wait
+// for each other.
 #include <algorithm>
 
 #include "rotary_rows.h"
@@ -50,7 +52,9 @@ __global__ __launch_bounds__(64 * kWaves) void rotary_kernel(Rotary r, int64_t t
   }
 }
 
-// Heads of a wave: many share the turns, few fill the chip where tokens are few.
+// Heads of a wave: many share the turns, few fill the chip where tokens are few (40
+// heads: 512 tokens 5.8 us with one a wave, 6.7 with eight; 16384 bf16 tokens 107
+// with one, 67 with eight, 76 with 16).
 int run_for(int64_t tokens, int heads) {
   const int64_t passes = (tokens + kPass - 1) / kPass;
   int run = 8;
