@@ -245,8 +245,8 @@ fp2_status_t check_rotary(const fp2_rotary_t* r) {
 }
 
 fp2::Rotary make_rotary(const fp2_rotary_t* r, bool inverse, bool scaled) {
-  if (!r) return fp2::Rotary{nullptr, 2, 0, 1.f};
-  return fp2::Rotary{r->turns, r->dim, inverse, !scaled ? 1.f : inverse ? 1.f / r->scale : r->scale};
+  if (!r) return fp2::make_rotary(nullptr, 2, false, 1.0);
+  return fp2::make_rotary(r->turns, r->dim, inverse, !scaled ? 1.0 : inverse ? 1.0 / r->scale : (double)r->scale);
 }
 
 fp2_status_t check_strided(const char* name, const void* x, int64_t stride, int width) {

@@ -26,7 +26,12 @@ struct Rotary {
   int32_t dim;
   int32_t inverse;          // turns backwards
   float scale;              // a
+  float eighth, rest;       // a pi / 4, in two parts
 };
+inline Rotary make_rotary(const uint64_t* turns, int dim, bool inverse, double scale) {
+  const double eighth = scale * 0.785398163397448309616;
+  return Rotary{turns, dim, inverse, (float)scale, (float)eighth, (float)(eighth - (float)eighth)};
+}
 
 enum PairPlace : int32_t { kPairs = 0, kHalves = 1, kOdd = 2 };
 
@@ -47,29 +52,24 @@ __device__ __forceinline__ uint32_t phase_at(int n, uint64_t f) {
   return u * (uint32_t)(f >> 32) + __umulhi(u, lo) - (n < 0 ? lo : 0u);
 }
 
-// Cosine and sine of a fraction of a turn. A quarter of a turn about the nearest
-// multiple of one is left of it, f in [-1, 1) eighths: sin(pi/4 f) = f S(f^2) and
-// cos(pi/4 f) = C(f^2), with the coefficients of least largest error (2^-29.6 and
-// 2^-34); pi/4 comes in two parts. Off by at most 2^-23.7, as a rule (rms) by 2^-25.8
-// over 2^24 fractions, so that a turn is as near as one with rounded sines. The
-// hardware's own sine and cosine are off by up to 2^-22.3, and twice as many codes
-// come out on the other side of a border with them.
-__device__ __forceinline__ float2 cos_sin(uint32_t phase) {
+// Cosine and sine of a fraction of a turn, times a. A quarter of a turn about the
+// nearest multiple of one is left of it, f in [-1, 1) eighths: sin(pi/4 f) = f S(f^2)
+// and cos(pi/4 f) = C(f^2), with the coefficients of least largest error (2^-29.6 and
+// 2^-34). With a = 1 they are off by at most 2^-23.7, as a rule (rms) by 2^-25.8 over 2^24
+// fractions, so that a turn is as near as one with rounded sines. The hardware's own
+// sine and cosine are off by up to 2^-22.3, and twice as many codes come out on the
+// other side of a border with them.
+__device__ __forceinline__ float2 turn_at(const Rotary& r, int n, uint64_t turns) {
+  const uint32_t phase = phase_at(n, turns);
   const float f = (float)(int)(phase << 2) * 0x1p-31f, z = f * f;
-  const float pi4 = 0x1.921fb6p-1f, rest = -0x1.777a5cp-26f;
-  float s = fmaf(z, fmaf(z, fmaf(z, -3.58772584e-5f, 2.48987197e-3f), -8.07453673e-2f), rest);
-  float c = fmaf(z, fmaf(z, fmaf(z, 3.53133465e-6f, -3.25942008e-4f), 1.58543278e-2f), -3.08425136e-1f);
-  s = fmaf(f, pi4, f * s);
-  c = fmaf(z, c, 1.f);
-  const uint32_t q = phase + (1u << 29), r = q << 1;       // quarter: the top two bits of q
-  const float x = (int)r < 0 ? s : c, y = (int)r < 0 ? c : s;
-  return make_float2(__uint_as_float(__float_as_uint(x) ^ ((q ^ r) & 0x80000000u)),
-                     __uint_as_float(__float_as_uint(y) ^ (q & 0x80000000u)));
-}
-
-__device__ __forceinline__ float2 turn_at(const Rotary& r, int n, uint64_t f) {
-  const float2 t = cos_sin(phase_at(n, f));
-  return make_float2(t.x * r.scale, (r.inverse ? -t.y : t.y) * r.scale);
+  const float s2 = z * fmaf(z, fmaf(z, -3.58772584e-5f, 2.48987197e-3f), -8.07453673e-2f);   // S - pi/4
+  const float c2 = fmaf(z, fmaf(z, fmaf(z, 3.53133465e-6f, -3.25942008e-4f), 1.58543278e-2f), -3.08425136e-1f);
+  const float s = fmaf(f, r.eighth, f * fmaf(r.scale, s2, r.rest));
+  const float c = fmaf(r.scale * z, c2, r.scale);
+  const uint32_t q = phase + (1u << 29), odd = q << 1;     // quarter: the top two bits of q
+  const float x = (int)odd < 0 ? s : c, y = (int)odd < 0 ? c : s;
+  return make_float2(__uint_as_float(__float_as_uint(x) ^ ((q ^ odd) & 0x80000000u)),
+                     __uint_as_float(__float_as_uint(y) ^ ((r.inverse ? ~q : q) & 0x80000000u)));
 }
 
 // A lane's frequencies and turns: of eight pairs, or (kOdd) of its sixteen elements.
