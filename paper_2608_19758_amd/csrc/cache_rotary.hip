@@ -12,10 +12,10 @@
 // Bound by memory: 256 bytes a row in, 256 or 128 out. 32768 tokens of 32 and 8
 // heads, scales of 64: 165 us (4.4 TB/s).
 //
-// Few new tokens a sequence: a wave has one head of a sequence to itself, or, of a
-// single token, eight heads. One token of 32 sequences, scales of 16: 4.9 us, which
+// Few new tokens a sequence: a wave has one head of a sequence to itself, or, of up to
+// four tokens, several heads. One token of 32 sequences, scales of 16: 4.9 us, which
 // are a launch, the lengths, the page, the block's scale, one after the other; of
-// 1024 sequences 9.6.
+// 1024 sequences 9.7 (with a head a wave 49), four of 256 9.7 (17).
 #include <type_traits>
 
 #include "cache_runs.h"
@@ -26,8 +26,8 @@ namespace fp2 {
 namespace {
 
 constexpr int kWaves = 8;
-// New tokens of a sequence that a wave takes alone, at most: with registers for 16,
-// or for 32 (256 sequences of 32 tokens: 55 us, dealt out as many 132; 256 of 16: 24
+// New tokens of a sequence that a wave takes alone, at most: eight rows, or with
+// registers for 16 tokens, or for 32 (64 sequences of 8: 6.9 us, with those for 16 7.2; 256 sequences of 32 tokens: 55 us, dealt out as many 132; 256 of 16: 24
 // with registers for 16, 29 with those for 32). 64 tokens in a wave: 26 us instead of
 // 31 for 64 sequences, 13 instead of 9 for one.
 constexpr int kFew = 16, kSome = 32;
@@ -256,21 +256,24 @@ __global__ __launch_bounds__(64 * kWaves) void append_rotary_kernel(CacheProblem
   }
 }
 
-// One new token a sequence: a wave takes eight heads of its queries, keys or values.
-// The codes that a block held are read only if its scale grows.
-template <int FORM, int PLACE>
-__global__ __launch_bounds__(64 * kWaves) void append_rotary_one_kernel(CacheProblem p, Rotary r, RotaryRows q, New x,
-                                                                        int64_t total) {
+// At most T (1, 2, 4, 8) new tokens a sequence: a wave takes all of them and 8 / T
+// heads of its queries, keys or values. They lie in at most two blocks; the codes that
+// the first one held are read only if its scale grows.
+template <int FORM, int PLACE, int T>
+__global__ __launch_bounds__(64 * kWaves) void append_rotary_rows_kernel(CacheProblem p, Rotary r, RotaryRows q, New x,
+                                                                         int64_t total) {
   typedef std::conditional_t<FORM == kCacheBf16, uint16_t, uint8_t> elem_t;
+  constexpr int HEADS = kPass / T;
   const int64_t at = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (at >= total) return;
-  const int kv = (p.hkv + kPass - 1) / kPass, jobs = 2 * kv + (q.heads + kPass - 1) / kPass, j = (int)(at % jobs);
+  const int kv = (p.hkv + HEADS - 1) / HEADS, jobs = 2 * kv + (q.heads + HEADS - 1) / HEADS, j = (int)(at % jobs);
   const Seq s(p, (int)(at / jobs));
   if (s.n <= 0) return;
   const bool is_q = j >= 2 * kv, is_v = !is_q && j >= kv;
-  const int h0 = kPass * (is_q ? j - 2 * kv : is_v ? j - kv : j), heads = is_q ? q.heads : p.hkv;
-  const int lane = threadIdx.x & 63, r0 = lane / kLaneRow, h = min(h0 + r0, heads - 1), t = s.L - 1;
-  const bool there = h0 + r0 < heads;
+  const int h0 = HEADS * (is_q ? j - 2 * kv : is_v ? j - kv : j), heads = is_q ? q.heads : p.hkv;
+  const int lane = threadIdx.x & 63, r0 = lane / kLaneRow, i = r0 % T;   // rows of a head lie side by side
+  const int h = min(h0 + r0 / T, heads - 1), t = min(s.P + i, s.L - 1);
+  const bool there = h0 + r0 / T < heads && i < s.n;
   const LaneRow<PLACE> l(lane, r.dim);
   const int64_t row = s.row(t);
   uint32_t raw[8];
@@ -302,16 +305,20 @@ __global__ __launch_bounds__(64 * kWaves) void append_rotary_one_kernel(CachePro
   } else {
     const int first = t & -(1 << p.sb_shift);
     uint8_t* sp = (is_v ? p.v_block : p.k_block) + (slot >> p.sb_shift) * p.hkv + h;
-    const int before = first < t ? *sp : 0;              // byte of a block that holds tokens
-    auto largest = [&](float m) {                        // of a row
-#pragma unroll
-      for (int o = 1; o < kLaneRow; o *= 2) m = fmaxf(m, __shfl_xor(m, o, 64));
+    const int before = first < s.P ? *sp : 0;            // byte of a block that holds tokens
+    auto over = [](float m, int from, int to) {          // the largest of lanes that differ in these bits
+      for (int o = from; o < to; o *= 2) m = fmaxf(m, __shfl_xor(m, o, 64));
       return m;
     };
-    float amax = largest(largest16(z));
+    float amax = over(largest16(z), 1, kLaneRow);        // of the row
     if (__any(!(amax < INFINITY))) {                     // (rare: infinities do not count)
-      const float finite = largest(largest16_finite(z));
+      const float finite = over(largest16_finite(z), 1, kLaneRow);
       amax = amax < INFINITY ? amax : finite;
+    }
+    if constexpr (T > 1) {                               // of the row's block
+      const bool one = first <= s.P;
+      const float a = over(one ? amax : 0.f, kLaneRow, kLaneRow * T), b = over(one ? 0.f : amax, kLaneRow, kLaneRow * T);
+      amax = one ? a : b;
     }
     const int byte = max(scale_byte(amax), before);
     const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);   // 2^-e
@@ -320,14 +327,15 @@ __global__ __launch_bounds__(64 * kWaves) void append_rotary_one_kernel(CachePro
     if (__any(byte >= kMaxScaleByte)) codes16_held(z, c);
     else codes16(z, c);
     if (there) store_part(l, to, c);
-    if (there && l.c == 0) *sp = (uint8_t)byte;
-    // the whole wave takes the heads whose scales grew, one after the other
-    for (uint64_t grew = __ballot(there && l.c == 0 && first < t && byte > before); grew; grew &= grew - 1) {
+    if (there && l.c == 0 && t == max(first, s.P)) *sp = (uint8_t)byte;
+    // the whole wave takes the heads whose first block's scale grew, one after the other
+    const int held = s.P & -(1 << p.sb_shift);
+    for (uint64_t grew = __ballot(there && l.c == 0 && i == 0 && first < s.P && byte > before); grew; grew &= grew - 1) {
       const int from = __ffsll((unsigned long long)grew) - 1;
       const float by = power_down(__builtin_amdgcn_readlane(before, from), __builtin_amdgcn_readlane(byte, from));
-      elem_t* head = pool + (h0 + from / kLaneRow) * kHeadDim;
+      elem_t* head = pool + (h0 + from / (kLaneRow * T)) * kHeadDim;
 #pragma unroll 4
-      for (int u = first + r0; u < t; u += kPass)
+      for (int u = held + r0; u < s.P; u += kPass)
         shrink_row(head + slot_of(p.pm, s.b, s.tok0, u) * p.hkv * kHeadDim, lane, by);
     }
   }
@@ -439,15 +447,18 @@ __global__ __launch_bounds__(64 * kWaves) void append_rotary_few_kernel(CachePro
 template <int FORM, int SB, int PLACE>
 hipError_t launch(const CacheProblem& p, const Rotary& r, const RotaryRows& q, const New& x, hipStream_t s) {
   if (p.max_new <= kSome) {
-    const bool one = p.max_new == 1;
-    const int each = one ? kPass : 1, jobs = 2 * ((p.hkv + each - 1) / each) + (q.heads + each - 1) / each;
-    const int64_t total = (int64_t)p.batch * jobs, grid = (total + kWaves - 1) / kWaves;
+    const int each = p.max_new == 1 ? 8 : p.max_new == 2 ? 4 : p.max_new <= 4 ? 2 : 1;   // heads of a wave
+    const int64_t total = (int64_t)p.batch * (2 * ((p.hkv + each - 1) / each) + (q.heads + each - 1) / each);
+    const int64_t grid = (total + kWaves - 1) / kWaves;
     if (!launchable(grid, 64 * kWaves)) return hipErrorInvalidValue;
     auto go = [&](auto kernel) {
       kernel<<<(unsigned)grid, 64 * kWaves, 0, s>>>(p, r, q, x, total);
       return hipGetLastError();
     };
-    return one                 ? go(append_rotary_one_kernel<FORM, PLACE>)
+    return each == 8           ? go(append_rotary_rows_kernel<FORM, PLACE, 1>)
+           : each == 4         ? go(append_rotary_rows_kernel<FORM, PLACE, 2>)
+           : each == 2         ? go(append_rotary_rows_kernel<FORM, PLACE, 4>)
+           : p.max_new <= 8    ? go(append_rotary_rows_kernel<FORM, PLACE, 8>)
            : p.max_new <= kFew ? go(append_rotary_few_kernel<FORM, PLACE, kFew>)
                                : go(append_rotary_few_kernel<FORM, PLACE, kSome>);
   }

@@ -206,6 +206,18 @@ def test_append_one_token(form, dim, interleaved):
     run_append(lens, new, form, page, dim, interleaved, hq=8, hkv=8, seed=10, at=70000, spread=0.1)
 
 
+@pytest.mark.parametrize("form", FORMS + [32, 128])
+@pytest.mark.parametrize("most", [2, 3, 4, 5, 8])
+def test_append_drafted_tokens(form, most):
+    """Up to two, four and eight new tokens: in one block, in two, behind codes that are held and not."""
+    page = 128 if form == 128 else 64
+    new = [most, most, 1, most, most - 1, 0, most, most, 2, most]
+    lens = [most, 16 + most, 17, 64 + most // 2, 130, 20, 128, 66, 2, 48 + most - 1]
+    for dim, interleaved in ((128, False), (96, True), (100, False)):
+        run_append(lens, new, form, page, dim, interleaved, hq=12, hkv=3, seed=20 + most)
+        run_append(lens, new, form, page, dim, interleaved, hq=8, hkv=8, seed=30 + most, codes=True, part=False, spread=2.5)
+
+
 @pytest.mark.parametrize("sb", [16, 64])
 def test_append_one_token_after_the_other(sb):
     """40 steps of one token: each block's codes have been rounded to its scale at most once for each growth, and

@@ -180,7 +180,7 @@ def test_cross_workspace_is_bounded(hkv, hq):
 def test_launches_past_the_limit():
     """2^32 threads or more are refused before any launch."""
     big = dict(batch=65536, num_kv_heads=1024, num_q_heads=1024, max_kv_len=4096)
-    assert call("append", base(**big, max_seq_len=2), q=None, ks=1 << 17, vs=1 << 17) == fp2.EUNSUPPORTED
+    assert call("append", base(**big, max_seq_len=9), q=None, ks=1 << 17, vs=1 << 17) == fp2.EUNSUPPORTED
     assert call("cross", base(batch=65536, num_kv_heads=1024, num_q_heads=1024, max_seq_len=4096, max_kv_len=64, kv_splits=1)) == fp2.EUNSUPPORTED
 
 
