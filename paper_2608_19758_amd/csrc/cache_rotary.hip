@@ -27,9 +27,9 @@ namespace {
 
 constexpr int kWaves = 8;
 // New tokens of a sequence that a wave takes alone, at most: eight rows, or with
-// registers for 16 tokens, or for 32 (64 sequences of 8: 6.9 us, with those for 16 7.2; 256 sequences of 32 tokens: 55 us, dealt out as many 132; 256 of 16: 24
-// with registers for 16, 29 with those for 32). 64 tokens in a wave: 26 us instead of
-// 31 for 64 sequences, 13 instead of 9 for one.
+// registers for 16 tokens, or for 32 (64 sequences of 8: 6.9 us, with those for 16
+// 7.2; 256 of 16: 24, with those for 32 29; 256 of 32: 55, dealt out as many 132).
+// 64 tokens in a wave: 26 us instead of 31 for 64 sequences, 13 instead of 9 for one.
 constexpr int kFew = 16, kSome = 32;
 
 struct New {
