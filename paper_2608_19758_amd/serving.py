@@ -40,7 +40,8 @@ and decoded here.
 
 With ``rotary`` (``make_rotary``) a forward takes queries and keys as the projection gives
 them and turns them on the way in; an eviction with it turns the keys that stay to their
-new indexes. ``read`` gives cached tokens back as bf16 rows, ``move`` takes them to other
+new indexes. ``read`` gives cached tokens back as bf16 rows (whole sequences too, however
+many chunks they came in: ``init_read_metadata``), ``move`` takes them to other
 pages or positions, and ``forward_cross`` attends to the states of an encoder (written with
 ``append``), or to a prefix that requests share, whatever their length.
 """
@@ -293,6 +294,16 @@ def plan_cross(cfg: CacheConfig, query_lens: Sequence[int], state_lens: Sequence
     return ForwardPlan(params=params, cu_q=cu[0], cu_k=cu[1], total_tokens=int(cu[0][-1]))
 
 
+def plan_read(cfg: CacheConfig, read_lens: Sequence[int],
+              prefix_lens: Optional[Sequence[int]] = None) -> ForwardPlan:
+    """Validate one reading back: the last read_lens tokens of sequences, each behind prefix_lens others. Unlike
+    a forward's new tokens they are bounded by max_kv_len alone."""
+    for b, n in enumerate(read_lens):
+        if int(n) > cfg.max_kv_len:
+            raise ValueError("sequence %d: %d tokens > max_kv_len %d" % (b, n, cfg.max_kv_len))
+    return plan_forward(dataclasses.replace(cfg, max_extend_len=cfg.max_kv_len), read_lens, prefix_lens)
+
+
 @dataclasses.dataclass
 class CacheMetadata:
     plan: ForwardPlan
@@ -301,6 +312,7 @@ class CacheMetadata:
     replayed: bool = False         # lengths and table are the metadata's own, and may be updated
     rows: Optional[int] = None     # of the tensors of the forwards captured with it, the fewest
     cross: bool = False            # of a cross attention
+    read: bool = False             # of tokens to read back, which no forward appends
 
     @property
     def params(self):
@@ -354,14 +366,20 @@ class CacheBackend:
         """Once per forward, for all layers. replayed: the forward is captured in a graph
         and replayed after update_forward_metadata; its bounds are then the longest of
         these extends and the config's max_kv_len instead of these lengths'."""
-        return self._metadata(plan_forward(self.cfg, extend_lens, prefix_lens), block_table, replayed, False)
+        return self._metadata(plan_forward(self.cfg, extend_lens, prefix_lens), block_table, replayed)
 
     def init_cross_metadata(self, query_lens: Sequence[int], state_lens: Sequence[int], block_table,
                             replayed: bool = False) -> CacheMetadata:
         """The same for cross attention: queries, and cached states, of each sequence."""
-        return self._metadata(plan_cross(self.cfg, query_lens, state_lens), block_table, replayed, True)
+        return self._metadata(plan_cross(self.cfg, query_lens, state_lens), block_table, replayed, cross=True)
 
-    def _metadata(self, plan, block_table, replayed, cross):
+    def init_read_metadata(self, read_lens: Sequence[int], prefix_lens: Optional[Sequence[int]], block_table,
+                           replayed: bool = False) -> CacheMetadata:
+        """The same for reading back (or moving): the last read_lens tokens of each sequence, up to max_kv_len;
+        without prefix_lens whole sequences."""
+        return self._metadata(plan_read(self.cfg, read_lens, prefix_lens), block_table, replayed, read=True)
+
+    def _metadata(self, plan, block_table, replayed, cross=False, read=False):
         import torch
         if replayed:
             kv, new = self.cfg.max_kv_len, plan.params.max_seq_len
@@ -373,16 +391,17 @@ class CacheBackend:
             table = _dense_table(block_table, len(plan.cu_q) - 1, self.cfg.max_pages_per_seq)
             if replayed:
                 table = table.clone()
-        return CacheMetadata(plan=plan, lengths=lengths, block_table=table, replayed=replayed, cross=cross)
+        return CacheMetadata(plan=plan, lengths=lengths, block_table=table, replayed=replayed, cross=cross,
+                             read=read)
 
     def update_forward_metadata(self, meta: CacheMetadata, extend_lens: Sequence[int],
                                 prefix_lens: Optional[Sequence[int]], block_table) -> None:
         """Other lengths and pages for a captured forward (metadata made with
         replayed=True): as many sequences, extends within the first one's bound, and no more new
         tokens in all than the captured tensors have rows. For a cross attention: its queries and
-        states."""
+        states; for a read: its tokens and those before them."""
         import torch
-        plan = (plan_cross if meta.cross else plan_forward)(self.cfg, extend_lens, prefix_lens)
+        plan = (plan_cross if meta.cross else plan_read if meta.read else plan_forward)(self.cfg, extend_lens, prefix_lens)
         p = meta.params
         if not meta.replayed:
             raise ValueError("the metadata was not made with replayed=True")
@@ -415,9 +434,9 @@ class CacheBackend:
                 rows = [t.shape[0] for _, t in given] + [meta.rows] * (meta.rows is not None)
                 meta.rows = min(rows)
 
-    def _lengths(self, meta: CacheMetadata, cross: bool = False):
-        if meta.cross != cross:
-            raise ValueError("metadata of a %s" % ("cross attention" if meta.cross else "forward"))
+    def _lengths(self, meta: CacheMetadata, cross: bool = False, appends: bool = False):
+        if meta.cross != cross or (meta.read and appends):
+            raise ValueError("metadata of a %s" % ("cross attention" if meta.cross else "read" if meta.read else "forward"))
         return ((meta.cu_q, meta.cu_k, meta.block_table),
                 dict(cu_seqlens_host=meta.plan.cu_q, cu_seqlens_k_host=meta.plan.cu_k, stream=self.stream))
 
@@ -428,7 +447,7 @@ class CacheBackend:
         one matrix will do) and are turned by positions (device int32 [new tokens]; None: a token's index in
         its sequence). weights (as from alloc_weights): what the cached tokens received of these queries is
         added to it, row b for sequence b. Returns (out, lse or None)."""
-        lens, host = self._lengths(meta)
+        lens, host = self._lengths(meta, appends=True)
         if rotary is None and positions is not None:
             raise ValueError("positions without rotary")
         self._check_rows(meta, ("q", q), ("k_new", k_new), ("v_new", v_new), ("positions", positions))
@@ -447,7 +466,7 @@ class CacheBackend:
 
     def append(self, k_new, v_new, cache: "fp2.KVCache", meta: CacheMetadata) -> None:
         """One layer: keys and values into the cache without queries (an encoder's states)."""
-        lens, host = self._lengths(meta)
+        lens, host = self._lengths(meta, appends=True)
         self._check_rows(meta, ("k_new", k_new), ("v_new", v_new))
         fp2.cache_append(meta.params, k_new, v_new, cache, *lens, **host)
 
@@ -460,8 +479,9 @@ class CacheBackend:
                                workspace=self.workspace, **host)
 
     def read(self, cache: "fp2.KVCache", meta: CacheMetadata, *, rotary: Optional["fp2.Rotary"] = None, positions=None):
-        """The forward's new tokens out of one layer's cache, (keys, values) bf16 [new tokens, Hkv, 128]; with
-        rotary the keys' turn is taken back. A whole sequence is one without prefix_lens."""
+        """The tokens of init_read_metadata (or a forward's new ones) out of one layer's cache, (keys, values) bf16
+        [tokens, Hkv, 128]; with rotary the keys' turn by positions (device int32 [tokens]; None: indexes) is
+        taken back."""
         lens, host = self._lengths(meta)
         if meta.replayed:     # the rows of a captured read are those of now
             self._check_rows(meta, ("rows", np.empty((meta.plan.total_tokens, 0))))

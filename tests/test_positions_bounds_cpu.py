@@ -1,0 +1,48 @@
+"""Bounds of the cache backend's positions, reading back and cross attention without a GPU."""
+import numpy as np
+import pytest
+
+from paper_2608_19758_amd import serving
+
+
+def config(**kw):
+    d = dict(num_q_heads=8, num_kv_heads=2, page_size=16, max_batch=3, max_extend_len=50, max_kv_len=1000)
+    d.update(kw)
+    return serving.CacheConfig(**d)
+
+
+# ---- reading back
+
+def test_plan_read():
+    """Whole sequences, longer than a forward's chunk, and the last tokens of others."""
+    cfg = config()
+    plan = serving.plan_read(cfg, [1000, 0, 51])
+    p = plan.params
+    assert (p.batch, p.max_seq_len, p.max_kv_len) == (3, 1000, 1000)
+    assert plan.cu_q.tolist() == plan.cu_k.tolist() == [0, 1000, 1000, 1051] and plan.total_tokens == 1051
+    assert plan.cu_q.dtype == plan.cu_k.dtype == np.int32
+    plan = serving.plan_read(cfg, [60, 3], [900, 0])
+    assert plan.cu_q.tolist() == [0, 60, 63] and plan.cu_k.tolist() == [0, 960, 963]
+    assert (plan.params.max_seq_len, plan.params.max_kv_len) == (60, 960)
+    assert serving.plan_read(cfg, []).total_tokens == 0
+    for lens, pre in (([1001], None), ([1000], [1]), ([-1], None), ([1], [-1]), ([1], [1, 1]), ([1] * 4, None)):
+        with pytest.raises(ValueError):
+            serving.plan_read(cfg, lens, pre)
+    with pytest.raises(ValueError, match="max_kv_len"):
+        serving.plan_read(cfg, [1001])
+    with pytest.raises(ValueError, match="max_extend_len"):       # a forward's chunk is as long as it was
+        serving.plan_forward(cfg, [51])
+
+
+def test_metadata_of_a_read_is_no_forwards():
+    be = serving.CacheBackend(config(), device="cpu")
+    with pytest.raises(ValueError, match="block_table"):          # the lengths are right
+        be.init_read_metadata([1000, 0, 51], None, None)
+    with pytest.raises(ValueError, match="max_kv_len"):
+        be.init_read_metadata([1001], None, None)
+    meta = serving.CacheMetadata(serving.plan_read(be.cfg, [1000]), None, None, read=True)
+    for go in (lambda: be.forward(None, None, None, None, meta), lambda: be.append(None, None, None, meta)):
+        with pytest.raises(ValueError, match="metadata of a read"):
+            go()
+    with pytest.raises(ValueError, match="metadata of a read"):
+        be.forward_cross(None, None, meta)
