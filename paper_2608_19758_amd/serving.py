@@ -43,7 +43,8 @@ them and turns them on the way in; an eviction with it turns the keys that stay 
 new indexes. ``read`` gives cached tokens back as bf16 rows (whole sequences too, however
 many chunks they came in: ``init_read_metadata``), ``move`` takes them to other
 pages or positions, and ``forward_cross`` attends to the states of an encoder (written with
-``append``), or to a prefix that requests share, whatever their length.
+``append``), or to a prefix that requests share, whatever their length; more queries than
+``max_extend_len``, or than there are states, are allowed for by ``max_query_len``.
 """
 from __future__ import annotations
 
@@ -259,6 +260,7 @@ class CacheConfig:
     sink_tokens: int = 0           # first tokens that stay visible and are never evicted
     window_tokens: int = 0         # 0: every earlier token is visible
     softmax_scale: float = 0.0     # <= 0: 1/sqrt(128)
+    max_query_len: int = 0         # queries of one sequence in a cross attention, whatever max_kv_len; 0: max_extend_len
 
     @property
     def max_pages_per_seq(self) -> int:
@@ -283,9 +285,10 @@ def plan_cross(cfg: CacheConfig, query_lens: Sequence[int], state_lens: Sequence
         raise ValueError("query_lens and state_lens differ in length")
     if len(new) > cfg.max_batch:
         raise ValueError("batch %d > max_batch %d" % (len(new), cfg.max_batch))
+    most, name = (cfg.max_query_len, "max_query_len") if cfg.max_query_len else (cfg.max_extend_len, "max_extend_len")
     for b, (n, t) in enumerate(zip(new, kv)):
-        if not 0 <= n <= cfg.max_extend_len:
-            raise ValueError("sequence %d: %d queries outside [0, max_extend_len = %d]" % (b, n, cfg.max_extend_len))
+        if not 0 <= n <= most:
+            raise ValueError("sequence %d: %d queries outside [0, %s = %d]" % (b, n, name, most))
         if not 0 <= t <= cfg.max_kv_len:
             raise ValueError("sequence %d: %d states outside [0, max_kv_len = %d]" % (b, t, cfg.max_kv_len))
     params = dataclasses.replace(cfg, sink_tokens=0, window_tokens=0).params(len(new), max(new, default=0),
@@ -346,6 +349,10 @@ class CacheBackend:
         idle = cfg.params(cfg.max_batch, 0, cfg.max_kv_len)
         if fp2.lib().fp2_cache_append(ctypes.byref(idle), *[None] * 9):
             raise ValueError("configuration rejected by the library: " + fp2.last_error())
+        # nor has one without sequences, which checks the bound of the queries
+        none = dataclasses.replace(cfg, sink_tokens=0, window_tokens=0).params(0, cfg.max_query_len, cfg.max_kv_len)
+        if fp2.lib().fp2_cache_cross(ctypes.byref(none), *[None] * 10, 0, None):
+            raise ValueError("max_query_len rejected by the library: " + fp2.last_error())
         with fp2.cache.on_stream(stream):
             self.workspace = torch.empty(fp2.CACHE_WORKSPACE_MAX, dtype=torch.uint8, device=self.device)
 
@@ -370,7 +377,7 @@ class CacheBackend:
 
     def init_cross_metadata(self, query_lens: Sequence[int], state_lens: Sequence[int], block_table,
                             replayed: bool = False) -> CacheMetadata:
-        """The same for cross attention: queries, and cached states, of each sequence."""
+        """The same for cross attention: queries (up to max_query_len), and cached states, of each sequence."""
         return self._metadata(plan_cross(self.cfg, query_lens, state_lens), block_table, replayed, cross=True)
 
     def init_read_metadata(self, read_lens: Sequence[int], prefix_lens: Optional[Sequence[int]], block_table,

@@ -85,3 +85,42 @@ def test_captured_read_of_whole_sequences():
     for part in ([901, 0, 0], [900, 300, 1], [1, 1]):
         with pytest.raises(ValueError):
             be.update_forward_metadata(meta, part, None, table)
+
+
+@pytest.mark.parametrize("form", ["bf16", "head", 32])
+def test_cross_of_more_queries_than_states(form):
+    """A cache of short states under queries of many more: eager, and captured and replayed."""
+    cfg = config(form, max_extend_len=128, max_kv_len=128, max_query_len=1500)
+    be, eager = serving.CacheBackend(cfg), serving.CacheBackend(cfg)
+    (table,), pages = tables(cfg, 1, 13)
+    g = torch.Generator().manual_seed(13)
+    cache = be.alloc_cache(pages, *scales(form))
+    states = [77, 0, 128]
+    _, k, v = rows(g, sum(states))
+    be.append(k, v, cache, be.init_forward_metadata(states, None, table))
+    for new in ([1500, 3, 129], [2, 0, 1]):
+        q = rows(g, sum(new))[0]
+        out, lse = be.forward_cross(q, cache, be.init_cross_metadata(new, states, table), want_lse=True)
+        torch.cuda.synchronize()
+        o, tol, z, ztol = pos_ref.cross(view(cfg, states, cache, table, form), q.cpu(), new)
+        close(out, o, tol, "out")
+        close(lse, z, ztol, "lse")
+    new = [400, 300, 200]
+    meta = be.init_cross_metadata(new, states, table, replayed=True)
+    q, out = rows(g, sum(new))[0], torch.zeros((sum(new), HQ, 128), dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        be.forward_cross(q, cache, meta, out=out)
+    for order, now in (([0, 1, 2], new), ([2, 0, 1], [400, 200, 300]), ([1, 2, 0], [1, 400, 0]), ([0, 1, 2], new)):
+        tab, kv = table[order], [states[i] for i in order]
+        be.update_forward_metadata(meta, now, kv, tab)
+        graph.replay()
+        spoil()
+        want, _ = eager.forward_cross(q, cache, eager.init_cross_metadata(now, kv, tab, replayed=True))
+        torch.cuda.synchronize()
+        assert torch.equal(out[:sum(now)], want[:sum(now)])
+    with pytest.raises(ValueError):
+        be.update_forward_metadata(meta, [401, 0, 0], states, table)
+    with pytest.raises(ValueError, match="max_query_len"):
+        be.init_cross_metadata([1501], [77], table)

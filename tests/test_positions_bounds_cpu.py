@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+import paper_2608_19758_amd as fp2
 from paper_2608_19758_amd import serving
 
 
@@ -46,3 +47,37 @@ def test_metadata_of_a_read_is_no_forwards():
             go()
     with pytest.raises(ValueError, match="metadata of a read"):
         be.forward_cross(None, None, meta)
+
+
+# ---- cross attention
+
+def test_plan_cross_of_more_queries_than_states():
+    cfg = config(max_kv_len=100, max_query_len=5000)
+    plan = serving.plan_cross(cfg, [5000, 1, 0], [100, 0, 3])
+    p = plan.params
+    assert (p.batch, p.max_seq_len, p.max_kv_len) == (3, 5000, 100)
+    assert plan.cu_q.tolist() == [0, 5000, 5001, 5001] and plan.cu_k.tolist() == [0, 100, 100, 103]
+    for cfg, new in ((cfg, 5001), (config(max_query_len=20), 21), (config(), 51)):
+        with pytest.raises(ValueError, match="%d queries" % new):
+            serving.plan_cross(cfg, [new], [100])
+    with pytest.raises(ValueError, match="max_extend_len"):       # what is appended keeps its own bound
+        serving.plan_forward(config(max_query_len=5000), [51])
+
+
+@pytest.mark.parametrize("n", [-1, (1 << 20) + 1])
+def test_query_bounds_refused(n):
+    with pytest.raises(ValueError, match="max_seq_len"):
+        serving.CacheBackend(config(max_query_len=n), device="cpu")
+
+
+def test_workspace_fits_every_cross_attention():
+    rng = np.random.default_rng(1)
+    for kw in (dict(), dict(num_q_heads=64, num_kv_heads=8, max_batch=16), dict(num_kv_heads=8), dict(num_kv_heads=1)):
+        cfg = config(max_kv_len=70000, max_query_len=1 << 20, **kw)
+        be = serving.CacheBackend(cfg, device="cpu")
+        for _ in range(200):
+            b = int(rng.integers(1, cfg.max_batch + 1))
+            new = np.exp(rng.uniform(0, np.log(cfg.max_query_len), b)).astype(int)
+            kv = np.exp(rng.uniform(0, np.log(cfg.max_kv_len), b)).astype(int)
+            plan = serving.plan_cross(cfg, new.tolist(), kv.tolist())
+            assert fp2.cross_workspace_bytes(plan.params) <= be.workspace.numel()
