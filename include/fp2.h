@@ -640,8 +640,8 @@ fp2_status_t fp2_cache_append_rotary(const fp2_cache_params_t* params, const fp2
  * The last cu_seqlens tokens of each sequence (all, where they are
  * cu_seqlens_k) as bf16 rows [cu_seqlens[batch], num_kv_heads, 128]; k_out or
  * v_out may be null. With `rotary` the keys' turn by positions (as in
- * fp2_cache_append_rotary; null: indexes) is taken back. Rows past
- * cu_seqlens[batch] are not touched. */
+ * fp2_cache_append_rotary; null: indexes) is taken back. Outputs must not overlap
+ * each other or positions. Rows past cu_seqlens[batch] are not touched. */
 fp2_status_t fp2_cache_read(const fp2_cache_params_t* params, const fp2_rotary_t* rotary,
                             const int32_t* positions, const int32_t* cu_seqlens,
                             const int32_t* cu_seqlens_host, const int32_t* cu_seqlens_k,

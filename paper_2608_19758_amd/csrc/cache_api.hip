@@ -496,9 +496,12 @@ fp2_status_t fp2_cache_read(const fp2_cache_params_t* params, const fp2_rotary_t
   if (!k_out && !v_out) return fail(FP2_EINVAL, "k_out and v_out are null");
   if ((st = check_cache(params, cache, block_table, v_out != nullptr))) return st;
   if (!aligned(k_out, 16) || !aligned(v_out, 16)) return fail(FP2_EINVAL, "k_out and v_out must be 16-byte aligned");
-  if (cu_seqlens_host && k_out && v_out) {
-    const int64_t n = 2ll * cu_seqlens_host[params->batch] * params->num_kv_heads * fp2::kHeadDim;
-    if (overlap((const char*)k_out, n, (const char*)v_out, n)) return fail(FP2_EINVAL, "k_out overlaps v_out");
+  if (cu_seqlens_host) {   // then the rows that are written are known
+    const int64_t rows = cu_seqlens_host[params->batch], n = 2 * rows * params->num_kv_heads * fp2::kHeadDim;
+    const char *ko = (const char*)k_out, *vo = (const char*)v_out, *pos = (const char*)positions;
+    if (ko && vo && overlap(ko, n, vo, n)) return fail(FP2_EINVAL, "k_out overlaps v_out");
+    if (pos && ((ko && overlap(ko, n, pos, 4 * rows)) || (vo && overlap(vo, n, pos, 4 * rows))))
+      return fail(FP2_EINVAL, "an output overlaps positions");
   }
   const CacheProblem r = make_problem(params, nullptr, cu_seqlens, cu_seqlens_k, cache, block_table);
   return hip_status(fp2::launch_cache_read(r, make_rotary(rotary, true, true), rotary && rotary->interleaved, positions,

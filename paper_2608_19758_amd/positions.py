@@ -171,6 +171,11 @@ def _meet(a, b, tokens):
     return off < xw or off + yw > xs
 
 
+def _share(x, n, y, m):
+    """Whether n bytes at x share memory with m bytes at y."""
+    return x < y + m and y < x + n
+
+
 def rotary(r: Rotary, q, positions, k=None, *, out=None, k_out=None, q_scale=None, inverse: bool = False, stream=None):
     """fp2_rotary: q (and k) bf16 [tokens, heads, 128] turned by positions int32 [tokens]. Rows may be parts of a
     wider matrix; out and k_out may be q and k themselves. With q_scale (fp32 [heads]) the queries come as e4m3
@@ -251,6 +256,11 @@ def cache_read(p: CacheParams, cache: KVCache, cu_seqlens, cu_seqlens_k, block_t
         ko = a("k_out", k_out, _ONE_BF16, size)
     if values and v_out is not None:
         vo = a("v_out", v_out, _ONE_BF16, size)
+    if cu_seqlens_host is None:     # (with it the call itself looks)
+        if ko is not None and vo is not None and _share(ko, 2 * size, vo, 2 * size):
+            raise ValueError("k_out must not overlap v_out")
+        if pos is not None and any(o is not None and _share(o, 2 * size, pos, 4 * rows) for o in (ko, vo)):
+            raise ValueError("k_out and v_out must not overlap positions")
     if (keys and k_out is None) or (values and v_out is None):
         shape = (rows, p.num_kv_heads, HEAD_DIM)
         with on_stream(stream):

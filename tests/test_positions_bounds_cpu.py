@@ -1,9 +1,12 @@
 """Bounds of the cache backend's positions, reading back and cross attention without a GPU."""
 import numpy as np
 import pytest
+import torch
 
 import paper_2608_19758_amd as fp2
 from paper_2608_19758_amd import serving
+from tests.test_cache_cpu import FAKE, base
+from tests.test_positions_cpu import FAR, call, cpu_call, cpu_rotary
 
 
 def config(**kw):
@@ -81,3 +84,35 @@ def test_workspace_fits_every_cross_attention():
             kv = np.exp(rng.uniform(0, np.log(cfg.max_kv_len), b)).astype(int)
             plan = serving.plan_cross(cfg, new.tolist(), kv.tolist())
             assert fp2.cross_workspace_bytes(plan.params) <= be.workspace.numel()
+
+
+# ---- outputs of a read that meet other tensors of the call
+
+ROWS = FAKE + 64 * FAR
+
+
+@pytest.mark.parametrize("over", [
+    dict(positions=ROWS, k_out=ROWS), dict(positions=ROWS, v_out=ROWS), dict(positions=ROWS + 4 * 2048 - 4, k_out=ROWS),
+    dict(positions=ROWS + 4 * 2048 - 4, v_out=ROWS, k_out=None), dict(positions=ROWS + 12, k_out=ROWS + 16)])
+def test_read_over_its_positions(over):
+    """8 heads: rows of 2048 bytes, four of them."""
+    assert call("read", base(), cuh=[0, 2, 4], **over) == fp2.EINVAL
+    assert "positions" in fp2.last_error()
+
+
+def test_read_binding_refuses_outputs_that_meet():
+    """Without lengths on the host, as with them."""
+    p, cache, lens, host = cpu_call()
+    r = cpu_rotary()
+    m = torch.zeros((12, 2, 128), dtype=torch.bfloat16)
+    at = m.view(-1)[:10].view(torch.int32)
+    far = torch.zeros((5, 2, 128), dtype=torch.bfloat16)
+    for kw in (dict(k_out=m[:5], v_out=m[4:9]), dict(k_out=m[2:7], v_out=m[:5]), dict(k_out=m[:5], v_out=m[:5]),
+               dict(k_out=m[:5], values=False, rotary=r, positions=at), dict(v_out=m[:5], k_out=far, rotary=r, positions=at)):
+        with pytest.raises(ValueError, match="overlap"):
+            fp2.cache_read(p, cache, *lens, **kw)
+    # outputs side by side are right: what is refused is the device
+    with pytest.raises(ValueError, match="CUDA tensor"):
+        fp2.cache_read(p, cache, *lens, k_out=m[:5], v_out=m[5:10])
+    with pytest.raises(ValueError, match="CUDA tensor"):
+        fp2.cache_read(p, cache, *lens, k_out=m[1:6], v_out=m[6:11], rotary=r, positions=at[:5])
