@@ -199,7 +199,7 @@ def cache_append_rotary(p: CacheParams, r: Rotary, q, k_new, v_new, cache: KVCac
     """fp2_cache_append_rotary: k_new and v_new bf16 [new tokens, num_kv_heads, 128] into the cache's pages, the
     keys turned by positions (int32 [new tokens]; None: their indexes in the sequence), and q [new tokens,
     num_q_heads, 128] (None: no queries) turned as rotary does it. Returns the queries."""
-    a, batch = _Args(), p.batch
+    a, batch, met = _Args(), p.batch, None
     c = a.cache(p, cache)
     k, ks, tokens, _ = a.rows("k_new", k_new, p.num_kv_heads)
     v, vs, there, _ = a.rows("v_new", v_new, p.num_kv_heads)
@@ -214,12 +214,15 @@ def cache_append_rotary(p: CacheParams, r: Rotary, q, k_new, v_new, cache: KVCac
             if (o != x and _meet(o, x, tokens)) or _meet(o, (k, 2 * ks, width), tokens) or \
                     _meet(o, (v, 2 * vs, width), tokens):
                 raise ValueError("q's output must not overlap k_new, v_new or other rows of q")
+            met = o
         rows = ctypes.byref(rows)
         there = there if asked == tokens else asked
     if there != tokens:
         raise ValueError("q, k_new and v_new differ in their tokens")
     lens = a.lengths(batch, cu_seqlens, cu_seqlens_k, cu_seqlens_host, cu_seqlens_k_host, tokens)
     pos = a("positions", positions, _ONE_I32, tokens, optional=True)
+    if met and pos is not None and _meet(met, (pos, 4, 4), tokens):
+        raise ValueError("q's output must not overlap positions")
     table = a.table(batch, "block_table", block_table, p.max_pages_per_seq)
     args = _rotary_args(a, r)
     if tokens:

@@ -116,3 +116,19 @@ def test_read_binding_refuses_outputs_that_meet():
         fp2.cache_read(p, cache, *lens, k_out=m[:5], v_out=m[5:10])
     with pytest.raises(ValueError, match="CUDA tensor"):
         fp2.cache_read(p, cache, *lens, k_out=m[1:6], v_out=m[6:11], rotary=r, positions=at[:5])
+
+
+def test_append_binding_refuses_queries_over_positions():
+    """Without lengths on the host, as with them."""
+    p, cache, lens, host = cpu_call()
+    r, m = cpu_rotary(), torch.zeros((6, 8, 128), dtype=torch.bfloat16)
+    q, k, v = m[:5, :4], m[:5, 4:6], m[:5, 6:]
+    out = torch.zeros((12, 4, 128), dtype=torch.bfloat16)
+    ints = out.view(-1).view(torch.int32)
+    codes = dict(out=out.view(torch.uint8).view(-1, 4, 128)[:5], q_scale=torch.ones(4))
+    # rows of 256 integers' bytes, and of 128 where they are codes
+    for kw, at in ((dict(out=out[:5]), 0), (dict(out=out[:5]), 700), (dict(out=out[:5]), 5 * 256 - 1), (codes, 0), (codes, 5 * 128 - 1)):
+        with pytest.raises(ValueError, match="positions"):
+            fp2.cache_append_rotary(p, r, q, k, v, cache, *lens, positions=ints[at:at + 5], **kw)
+    with pytest.raises(ValueError, match="CUDA tensor"):          # beside them: right
+        fp2.cache_append_rotary(p, r, q, k, v, cache, *lens, positions=ints[5 * 256:][:5], out=out[:5])
