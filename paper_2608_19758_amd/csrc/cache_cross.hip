@@ -595,7 +595,9 @@ hipError_t launch(const CacheProblem& p, const CachePartials& part, uint16_t* ou
 
 template <int FORM>
 hipError_t launch_pages(const CacheProblem& p, const CachePartials& part, uint16_t* out, float* lse, hipStream_t s) {
-  return p.pm.page % 8 == 0 ? launch<FORM, true>(p, part, out, lse, s) : launch<FORM, false>(p, part, out, lse, s);
+  // scales of blocks imply pages of a multiple of 16 tokens
+  if constexpr (FORM == kCacheBlock) return launch<FORM, true>(p, part, out, lse, s);
+  else return p.pm.page % 8 == 0 ? launch<FORM, true>(p, part, out, lse, s) : launch<FORM, false>(p, part, out, lse, s);
 }
 
 }  // namespace

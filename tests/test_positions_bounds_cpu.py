@@ -132,3 +132,14 @@ def test_append_binding_refuses_queries_over_positions():
             fp2.cache_append_rotary(p, r, q, k, v, cache, *lens, positions=ints[at:at + 5], **kw)
     with pytest.raises(ValueError, match="CUDA tensor"):          # beside them: right
         fp2.cache_append_rotary(p, r, q, k, v, cache, *lens, positions=ints[5 * 256:][:5], out=out[:5])
+
+
+def test_no_cross_kernels_that_no_call_reaches():
+    """Scales of blocks of 16 tokens and more imply pages of a multiple of 8."""
+    from paper_2608_19758_amd import build
+    with open(build.LIB, "rb") as f:
+        names = f.read()
+    for kernel in (b"cross_kernel", b"split_kernel"):
+        for form, grouped in ((0, 0), (0, 1), (1, 0), (1, 1), (2, 1)):
+            assert kernel + b"ILi%dELb%dE" % (form, grouped) in names
+        assert kernel + b"ILi2ELb0E" not in names
