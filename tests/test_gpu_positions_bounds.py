@@ -10,6 +10,7 @@ from tests import cache_ref as ref
 from tests import positions_ref as pos_ref
 from tests.test_gpu_cache import close, cu_of, dev
 from tests.test_gpu_cache_serving import HKV, HQ, config, rows, scales, tables
+from tests.test_gpu_positions import run_move
 from tests.test_gpu_positions_serving import spoil, view
 
 pytestmark = pytest.mark.gpu
@@ -124,3 +125,17 @@ def test_cross_of_more_queries_than_states(form):
         be.update_forward_metadata(meta, [401, 0, 0], states, table)
     with pytest.raises(ValueError, match="max_query_len"):
         be.init_cross_metadata([1501], [77], table)
+
+
+# ---- more sequences than a wave has lanes, each block by itself
+
+@pytest.mark.parametrize("form,page", [("bf16", 16), ("head", 24), (16, 48), (32, 32), (64, 64), (128, 128)])
+@pytest.mark.parametrize("kind", ["copy", "one", "each"])
+def test_move_of_many_sequences(form, page, kind):
+    """200 sequences, a quarter of them empty: every row, block and scale against the definition."""
+    g = np.random.default_rng(30)
+    lens = [int(n) for n in g.integers(0, 60, 200) * (g.random(200) < 0.75)]
+    lens[150] = 300
+    run_move(form, page, kind, lens=lens)
+    if kind != "copy":
+        run_move(form, page, kind, lens=lens, in_place=True)
