@@ -9,7 +9,7 @@ from paper_2608_19758_amd import serving
 from tests import cache_ref as ref
 from tests import positions_ref as pos_ref
 from tests.test_gpu_cache import close, cu_of, dev
-from tests.test_gpu_cache_serving import HKV, HQ, config, rows, scales, tables
+from tests.test_gpu_cache_serving import HKV, HQ, config, equal, rows, scales, tables
 from tests.test_gpu_positions import run_move
 from tests.test_gpu_positions_serving import spoil, view
 
@@ -139,3 +139,139 @@ def test_move_of_many_sequences(form, page, kind):
     run_move(form, page, kind, lens=lens)
     if kind != "copy":
         run_move(form, page, kind, lens=lens, in_place=True)
+
+
+# ---- calls whose workgroups take several shares of the work: bit for bit what calls of a few sequences give,
+# in which each workgroup has one at most (the tests above and beside this file hold those to the definition)
+
+MOST = 400      # tokens of a sequence, at most
+
+
+def pools(form, lens, hkv, page, seed):
+    """A cache of random rows, and its table of shuffled pages."""
+    g = torch.Generator("cuda").manual_seed(seed)
+    width = -(-MOST // page)
+    need = [-(-n // page) for n in lens]
+    order = np.random.default_rng(seed).permutation(sum(need)).astype(np.int32)
+    table = np.full((len(lens), width), 2 ** 30, np.int32)
+    for b, (n, at) in enumerate(zip(need, np.cumsum([0] + need))):
+        table[b, :n] = order[at:at + n]
+    slots = sum(need) * page
+    x = [torch.randn((slots, hkv, 128), device="cuda", generator=g) for _ in "kv"]
+    if form == "bf16":
+        return fp2.KVCache(*(t.bfloat16() for t in x)), table
+    codes = [(t * 100).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8) for t in x]
+    if form == "head":
+        return fp2.KVCache(*codes, *(torch.rand(hkv, device="cuda", generator=g) * 0.01 + 0.005 for _ in "kv")), table
+    return fp2.KVCache(*codes, *(torch.randint(110, 130, (slots // form, hkv), dtype=torch.uint8, device="cuda", generator=g)
+                                 for _ in "kv")), table
+
+
+def copy_of(c):
+    return fp2.KVCache(*(None if x is None else x.clone() for x in (c.k, c.v, c.k_scale, c.v_scale)))
+
+
+def lengths_of(n, most, long, seed):
+    """Most of them up to `most`, one in ten empty, one in thirty up to `long`."""
+    g = np.random.default_rng(seed)
+    a = g.integers(1, most + 1, n)
+    a[g.random(n) < 0.1] = 0
+    far = g.random(n) < 1 / 30
+    a[far] = g.integers(most, long + 1, far.sum())
+    a[n // 2] = long
+    return [int(x) for x in a]
+
+
+def call_of(form, lens, new, hq, hkv, page, width):
+    return fp2.make_cache_params(batch=len(lens), num_q_heads=hq, num_kv_heads=hkv, max_seq_len=new, max_kv_len=MOST,
+                                 page_size=page, max_pages_per_seq=width, dtype="bf16" if form == "bf16" else "fp8",
+                                 scale_tokens=form if isinstance(form, int) else 0)
+
+
+LARGE = [("bf16", 16), ("head", 16), (16, 16), (32, 32), (64, 64), (128, 128)]
+
+
+@pytest.mark.parametrize("form,page", LARGE)
+def test_large_append(form, page):
+    """3000 sequences of 8 heads: 7000 runs of tokens and more, in 2048 workgroups of keys and values; 20000 runs of
+    eight queries of 8 heads in 16384 waves."""
+    hq, hkv, n = 16, 8, 3000
+    new = lengths_of(n, 36, 300, 40)
+    lens = [a + int(b) for a, b in zip(new, np.random.default_rng(41).integers(0, 90, n))]
+    cache, table = pools(form, lens, hkv, page, 42)
+    few, r, total = copy_of(cache), fp2.make_rotary(96), sum(new)
+    assert sum(m // 8 + 1 for m in new) * 2 > 16384
+    g = torch.Generator("cuda").manual_seed(43)
+    q, k, v = (torch.randn((total, h, 128), device="cuda", generator=g).bfloat16() for h in (hq, hkv, hkv))
+    cu, cuk, tab = cu_of(new), cu_of(lens), dev(table)
+    print("large append %s, %d tokens" % (form, total), flush=True)
+    out = fp2.cache_append_rotary(call_of(form, lens, 300, hq, hkv, page, table.shape[1]), r, q, k, v, cache, dev(cu),
+                                  dev(cuk), tab)
+    for b in range(0, n, 50):
+        part = slice(b, min(b + 50, n))
+        rows_ = slice(int(cu[b]), int(cu[part.stop]))
+        if rows_.start == rows_.stop:
+            continue
+        got = fp2.cache_append_rotary(call_of(form, lens[part], 300, hq, hkv, page, table.shape[1]), r, q[rows_], k[rows_],
+                                      v[rows_], few, dev(cu_of(new[part])), dev(cu_of(lens[part])), tab[part].contiguous())
+        assert torch.equal(out[rows_], got)
+    torch.cuda.synchronize()
+    equal(cache, few)
+
+
+@pytest.mark.parametrize("form,page", [("bf16", 16), ("head", 16), (16, 16), (64, 64)])
+def test_large_read(form, page):
+    """14000 sequences: 70000 runs of 16 tokens' keys or values in 65536 waves."""
+    hkv, n = 2, 14000
+    lens = lengths_of(n, 16, 300, 50)
+    new = [max(m - int(x), 0) for m, x in zip(lens, np.random.default_rng(51).integers(0, 9, n))]
+    cache, table = pools(form, lens, hkv, page, 52)
+    r, total = fp2.make_rotary(128, interleaved=True), sum(new)
+    assert (total // 16 + 2 * n) * 2 > 65536
+    cu, cuk, tab = cu_of(new), cu_of(lens), dev(table)
+    print("large read %s, %d tokens" % (form, total), flush=True)
+    k, v = fp2.cache_read(call_of(form, lens, 300, hkv, hkv, page, table.shape[1]), cache, dev(cu), dev(cuk), tab, rotary=r,
+                          rows=total)
+    for b in range(0, n, 1000):
+        part = slice(b, min(b + 1000, n))
+        rows_ = slice(int(cu[b]), int(cu[part.stop]))
+        wk, wv = fp2.cache_read(call_of(form, lens[part], 300, hkv, hkv, page, table.shape[1]), cache, dev(cu_of(new[part])),
+                                dev(cu_of(lens[part])), tab[part].contiguous(), rotary=r, rows=rows_.stop - rows_.start)
+        assert torch.equal(k[rows_], wk) and torch.equal(v[rows_], wv)
+    # values by themselves: a number times a power of two is exact, times a head's scale rounded to fp32 and then bf16
+    at = np.concatenate([np.arange(m - x, m) for m, x in zip(lens, new)])
+    slots = dev(table[np.repeat(np.arange(n), new), at // page].astype(np.int64) * page + at % page)
+    want = cache.v[slots]
+    if form != "bf16":
+        want = want.view(torch.float8_e4m3fn).float()
+        want = want * (cache.v_scale if form == "head" else (cache.v_scale[slots // form].int() << 23).view(torch.float32))[..., None]
+    torch.cuda.synchronize()
+    assert torch.equal(v, want.bfloat16())
+
+
+@pytest.mark.parametrize("form,page", LARGE)
+@pytest.mark.parametrize("in_place", [True, False])
+def test_large_move(form, page, in_place):
+    """6000 sequences of 8 heads, at least as many runs of tokens, in 2048 workgroups; with a number of positions for
+    each sequence, and for each head and token."""
+    hkv, n = 8, 6000
+    lens = lengths_of(n, 40, 300, 60)
+    cache, table = pools(form, lens, hkv, page, 61)
+    to = None
+    if not in_place:       # a pool twice as large, the targets in its second half
+        grow = lambda x: None if x is None else x if x.dim() == 1 else torch.cat([x, torch.zeros_like(x)])      # noqa: E731
+        half = cache.k.shape[0] // page
+        cache = fp2.KVCache(*(grow(x) for x in (cache.k, cache.v, cache.k_scale, cache.v_scale)))
+        to = dev(np.where(table == 2 ** 30, table, table + half).astype(np.int32))
+    few, r, cuk, tab = copy_of(cache), fp2.make_rotary(128), cu_of(lens), dev(table)
+    g = torch.Generator("cuda").manual_seed(62)
+    for moves in (torch.randint(-9000, 9000, (n,), dtype=torch.int32, device="cuda", generator=g),
+                  torch.randint(-9000, 9000, (n, hkv, MOST), dtype=torch.int32, device="cuda", generator=g)):
+        print("large move %s, %d tokens, moves %s" % (form, sum(lens), tuple(moves.shape)), flush=True)
+        fp2.cache_move(call_of(form, lens, 0, hkv, hkv, page, table.shape[1]), cache, dev(cuk), tab, to, rotary=r, moves=moves)
+        for b in range(0, n, 80):
+            part = slice(b, min(b + 80, n))
+            fp2.cache_move(call_of(form, lens[part], 0, hkv, hkv, page, table.shape[1]), few, dev(cu_of(lens[part])),
+                           tab[part].contiguous(), None if to is None else to[part].contiguous(), rotary=r, moves=moves[part])
+        torch.cuda.synchronize()
+        equal(cache, few)
