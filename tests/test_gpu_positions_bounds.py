@@ -275,3 +275,36 @@ def test_large_move(form, page, in_place):
                            tab[part].contiguous(), None if to is None else to[part].contiguous(), rotary=r, moves=moves[part])
         torch.cuda.synchronize()
         equal(cache, few)
+
+
+# ---- queries turned in place on the way into the cache, and as codes on into the sparse prefill
+
+@pytest.mark.parametrize("new", [[1] * 5, [2, 0, 1, 2, 1], [4, 3, 0, 1, 4], [8, 1, 0, 5, 7], [16, 9, 0, 1, 12],
+                                 [32, 17, 0, 3, 20], [40, 33, 0, 1, 250]])
+@pytest.mark.parametrize("dim,interleaved", [(128, False), (64, True), (100, False)])
+def test_append_turns_queries_in_place(new, dim, interleaved):
+    """As to rows of their own: dense queries, and those of a wider matrix, whose other columns stay."""
+    hq, hkv, page = 8, 2, 16
+    lens = [n + 13 * b for b, n in enumerate(new)]
+    total, r = sum(new), fp2.make_rotary(dim, interleaved=interleaved)
+    g = torch.Generator().manual_seed(70)
+    m = torch.randn((total + 2, hq + 2 * hkv, 128), generator=g).bfloat16().cuda()
+    parts = lambda x: (x[:total, :hq], x[:total, hq:hq + hkv], x[:total, hq + hkv:])        # noqa: E731
+    cache, table = pools(16, lens, hkv, page, 71)
+    p = fp2.make_cache_params(batch=5, num_q_heads=hq, num_kv_heads=hkv, max_seq_len=max(new), max_kv_len=max(lens),
+                              page_size=page, max_pages_per_seq=table.shape[1], dtype="fp8", scale_tokens=16)
+    args = dev(cu_of(new)), dev(cu_of(lens)), dev(table)
+    print("in place, new %s dim %d" % (new, dim), flush=True)
+    first, second, third = cache, copy_of(cache), copy_of(cache)
+    before = m.clone()
+    want = fp2.cache_append_rotary(p, r, *parts(m), first, *args)
+    assert torch.equal(m, before)
+    q, k, v = parts(m)
+    dense = q.contiguous()
+    assert fp2.cache_append_rotary(p, r, dense, k, v, second, *args, out=dense) is dense
+    assert torch.equal(dense, want)
+    assert fp2.cache_append_rotary(p, r, q, k, v, third, *args, out=q, cu_seqlens_host=cu_of(new)) is q
+    torch.cuda.synchronize()
+    assert torch.equal(q, want) and torch.equal(m[:, hq:], before[:, hq:]) and torch.equal(m[total:], before[total:])
+    equal(first, second)
+    equal(first, third)
