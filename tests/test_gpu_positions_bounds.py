@@ -9,7 +9,7 @@ from paper_2608_19758_amd import serving
 from tests import cache_ref as ref
 from tests import positions_ref as pos_ref
 from tests.test_gpu_cache import close, cu_of, dev
-from tests.test_gpu_cache_serving import HKV, HQ, config, equal, rows, scales, tables
+from tests.test_gpu_cache_serving import HKV, HQ, PAGE, config, equal, rows, scales, tables
 from tests.test_gpu_positions import run_move
 from tests.test_gpu_positions_serving import spoil, view
 
@@ -308,3 +308,32 @@ def test_append_turns_queries_in_place(new, dim, interleaved):
     assert torch.equal(q, want) and torch.equal(m[:, hq:], before[:, hq:]) and torch.equal(m[total:], before[total:])
     equal(first, second)
     equal(first, third)
+
+
+def test_codes_of_turned_queries_into_the_sparse_prefill():
+    """A prompt whose keys an append turns into a cache with a scale per head, its queries turned to codes, all
+    blocks kept: against dense attention over what cache and codes hold. The bar is that of the sparse kernels'
+    parity tests in codes, 6e-2."""
+    n, cfg = 500, config("head")
+    sparse = serving.PrefillBackend(serving.BackendConfig(
+        num_q_heads=HQ, num_kv_heads=HKV, page_size=PAGE, max_batch=1, max_extend_len=600, max_kv_len=1024,
+        dtype="fp8", window_blocks=8))
+    be = serving.CacheBackend(cfg)
+    (table,), pages = tables(cfg, 1, 14)
+    g = torch.Generator().manual_seed(14)
+    q, k, v = rows(g, n)
+    r, freq = fp2.make_rotary(128), fp2.rotary_frequencies(128)[0]
+    cache, scale = be.alloc_cache(pages, *scales("head")), torch.full((HQ,), 0.0125, device="cuda")
+    meta = be.init_forward_metadata([n], None, table)
+    codes = fp2.cache_append_rotary(meta.params, r, q, k, v, cache, meta.cu_q, meta.cu_k, meta.block_table, q_scale=scale)
+    alone = fp2.rotary(r, q, torch.arange(n, dtype=torch.int32, device="cuda"), q_scale=scale)
+    out, _ = sparse.forward_extend(codes, cache.k, cache.v, sparse.init_forward_metadata([n], None, table), q_scale=scale,
+                                   k_scale=cache.k_scale, v_scale=cache.v_scale)
+    torch.cuda.synchronize()
+    assert torch.equal(codes, alone)
+    by = float(np.float32(0.0125))
+    want, err = pos_ref.turn(q.double().cpu().numpy(), np.repeat(np.arange(n)[:, None], HQ, 1), freq, False)
+    pos_ref.check_codes(codes, want / by, err / by + np.abs(want / by) * pos_ref.U, "codes")
+    turned = torch.from_numpy(ref.VALUES[codes.cpu().numpy()] * by)
+    o = ref.attend(view(cfg, [n], cache, table, "head"), turned, [n])[0]
+    assert np.abs(out.double().cpu().numpy() - o).max() <= 6e-2
