@@ -517,8 +517,8 @@ __global__ __launch_bounds__(256) void join_kernel(CacheProblem p, CachePartials
   const int pr = 8 * (blockIdx.x % per) + (threadIdx.x >> 5), d = 4 * (threadIdx.x & 31);
   if (pr >= rows) return;
   auto row = [&](int i) { return (i == 0 ? first : next + (int64_t)step * (i - 1)) * kRows + pr; };
-  // eight parts a step, their loads in flight together (29 queries over 9280 keys, in 33
-  // parts a unit, take 31 us; with the loads of four in flight 37)
+  // eight parts a step, their loads in flight together (29 queries over 9280 keys, in 30 or 31
+  // parts a unit, take 31.6 us; with the loads of four in flight 33.1)
   float mm = kNoRef, l = 0.f;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1

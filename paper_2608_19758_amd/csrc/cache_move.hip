@@ -2,8 +2,8 @@
 // positions. Eight lanes a row, a wave a head at a time; the waves beside it take
 // the other heads of the same tokens, so memory is read in long runs.
 //
-// Reading: a wave takes 16 tokens and several heads, two heads' loads ahead, and
-// works out what it turns keys back by once for them.
+// Reading: a wave takes 16 tokens and several heads, the loads of two (bf16) or four
+// (codes) of them at once, and works out what it turns keys back by once for them.
 //
 // Moving: a wave takes 32 tokens of a head. Keys of codes with a scale per head
 // keep the scale (a turn is linear: the codes' numbers are turned and rounded
@@ -14,10 +14,12 @@
 // codes and scales. All that is read of a block is read before it is written, so
 // the pages may be the same (in place).
 //
-// Bound by memory: 128 or 256 bytes a row in, and 256 (reading) or as many out. 408K
-// tokens of 8 heads, scales of 64, read and turned back: 481 us (4.9 TB/s); 229K
-// moved to other pages, scales of 64: 171 (4.3 TB/s: rows of 1 KB at places of their
-// own); 1000 tokens of every head's own 10, 2001 read 6.8.
+// Bound by memory: 128 or 256 bytes a row in, and 256 (reading) or as many out. 398K
+// tokens of 8 heads, scales of 64, read and turned back: 481 us (5.1 TB/s); 186K
+// moved to other pages, scales of 64: 171 (4.4 TB/s: rows of 1 KB at places of their
+// own); 1000 tokens of every head's own 10, 2001 read 6.8. With a number of positions
+// for each head and token a row has 64 turns of its own, and the vector ALUs are busy
+// 75% of the time: the same 186K 220 us (a scale a head 239, bf16 319 as with one number).
 #include <algorithm>
 #include <type_traits>
 

@@ -11,7 +11,7 @@ namespace {
 // line of slots. Lengths are known on the device only, and a grid by their bounds
 // would be mostly empty where they are ragged (an empty workgroup takes 1.7 ns),
 // so a bounded grid deals the line to its workgroups in equal shares, each in one piece
-// (every n-th step instead: 222 us for the move of 229K tokens that takes 177). Sequence b
+// (every n-th step instead: 222 us for the move of 186K tokens that takes 177). Sequence b
 // has the slots from cu[b] / 2^SHIFT + EXTRA b on: EXTRA more than its tokens fill,
 // for the runs that its ends cut; a few slots have no tokens.
 template <int SHIFT, int EXTRA>
