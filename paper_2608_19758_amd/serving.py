@@ -301,10 +301,11 @@ def plan_read(cfg: CacheConfig, read_lens: Sequence[int],
               prefix_lens: Optional[Sequence[int]] = None) -> ForwardPlan:
     """Validate one reading back: the last read_lens tokens of sequences, each behind prefix_lens others. Unlike
     a forward's new tokens they are bounded by max_kv_len alone."""
-    for b, n in enumerate(read_lens):
-        if int(n) > cfg.max_kv_len:
+    lens = [int(x) for x in read_lens]
+    for b, n in enumerate(lens):
+        if n > cfg.max_kv_len:
             raise ValueError("sequence %d: %d tokens > max_kv_len %d" % (b, n, cfg.max_kv_len))
-    return plan_forward(dataclasses.replace(cfg, max_extend_len=cfg.max_kv_len), read_lens, prefix_lens)
+    return plan_forward(dataclasses.replace(cfg, max_extend_len=cfg.max_kv_len), lens, prefix_lens)
 
 
 @dataclasses.dataclass

@@ -29,6 +29,7 @@ def test_plan_read():
     assert plan.cu_q.tolist() == [0, 60, 63] and plan.cu_k.tolist() == [0, 960, 963]
     assert (plan.params.max_seq_len, plan.params.max_kv_len) == (60, 960)
     assert serving.plan_read(cfg, []).total_tokens == 0
+    assert serving.plan_read(cfg, (n for n in (60, 3))).total_tokens == 63
     for lens, pre in (([1001], None), ([1000], [1]), ([-1], None), ([1], [-1]), ([1], [1, 1]), ([1] * 4, None)):
         with pytest.raises(ValueError):
             serving.plan_read(cfg, lens, pre)
